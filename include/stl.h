@@ -95,7 +95,10 @@ enum {
                                2048 <= m <= 4194304 (else UNSUPPORTED) */
     STL_FLAG_VARIANT_MASK = 0xff,
     STL_FLAG_GELU = 0x100,  /* C <- gelu(C) (exact erf form) applied in fp32 before the final rounding */
-    STL_FLAG_B_TRANSPOSED = 0x200   /* stl_aa_*: the second operand is stored transposed, (nbatch*n) x k */
+    STL_FLAG_B_TRANSPOSED = 0x200,  /* stl_aa_*: the second operand is stored transposed, (nbatch*n) x k */
+    STL_FLAG_POST_NORM = 0x400,     /* stl_residual_norm_*: the block's output is normalised before the residual sum */
+    STL_FLAG_PRE_NORM = 0x800,      /* stl_residual_norm_*: the sum is normalised for the next block */
+    STL_FLAG_CENTER = 0x1000        /* stl_residual_norm_*: both norms subtract the mean (layer norm); without it root mean square */
 };
 
 /* Bytes of device scratch `ws` needed by op (STL_OP_*) with `flags`; 0 on invalid problem. */
@@ -289,6 +292,44 @@ stl_status_t stl_ragged_backward(const stl_problem_t *prob, int64_t rows, const 
                                  const void *Xhat_saved, const void *Yhat_saved, void *dX, float *dWhat,
                                  float *dE_X, float *dD, float *dfold, int accumulate, void *ws,
                                  size_t ws_bytes, void *stream);
+
+/*
+ * The step between two blocks of a residual network, around the layers above:
+ *     u    = norm(H) w_post + b_post   (STL_FLAG_POST_NORM; u = H without)
+ *     Xout = skip X + scale g (.) u
+ *     Z    = norm(Xout) w_pre + b_pre  (STL_FLAG_PRE_NORM; no Z without)
+ * norm(v) = v / sqrt(mean(v^2) + eps) over a row, with v - mean(v) for v under STL_FLAG_CENTER.  Row i of the matrices takes row
+ * i / rows_per_gate of the gate: one gate for all rows (rows_per_gate >= rows), one per image, one per row (1).
+ * X, H, Xout, Z: rows x n; gate: ceil(rows / rows_per_gate) x n or NULL (ones); w_post, b_post, w_pre, b_pre: n, or NULL (ones, zeros;
+ * those of a norm that the flags leave out are not read).  Storage dtype; a row is summed and normalised in fp32, each output rounded
+ * once, Z from the sum before it is rounded.  Xout may be X.
+ * 0 <= rows <= STL_MAX_DIM (no rows: nothing is done and the pointers of matrices may be NULL), any n from 1 to STL_RESIDUAL_WIDEST
+ * (UNSUPPORTED above), rows_per_gate >= 1, eps > 0.
+ */
+typedef struct {
+    int64_t rows, n, rows_per_gate;
+    float skip, scale, eps;
+    int32_t dtype;     /* stl_dtype_t */
+} stl_residual_t;
+#define STL_RESIDUAL_WIDEST 32768
+stl_status_t stl_residual_norm_forward(const stl_residual_t *prob, const void *X, const void *H, const void *gate, const void *w_post,
+                                       const void *b_post, const void *w_pre, const void *b_pre, void *Xout, void *Z, int flags, void *stream);
+/*
+ * Backward of <dXout, Xout> + <dZ, Z>, with x^ = norm(Xout), t = dZ w_pre, r = 1 / sqrt(...) of the row:
+ *     d  = dXout + r (t - [mean t] - x^ mean(t x^)),   dX = skip d,   du = scale g (.) d,   dgate = scale sum u (.) d
+ *     dH = r_h (th - [mean th] - h^ mean(th h^)), th = du w_post (dH = du without STL_FLAG_POST_NORM)
+ *     dw_post = sum du h^,  db_post = sum du,  dw_pre = sum dZ x^,  db_pre = sum dZ         (sums over rows; [mean] under STL_FLAG_CENTER)
+ * Xout: as the forward call wrote it (read with STL_FLAG_PRE_NORM only).  H, gate and the weights: as in the forward call.
+ * dXout, dZ: storage dtype, either may be NULL (zeros).  dX, dH: storage dtype; dgate (the gate's shape), dw_post, db_post, dw_pre, db_pre:
+ * fp32; any may be NULL.  The gradient of what the flags or a missing gate leave out: INVALID_ARG.  dX may be dXout.
+ * accumulate: 0 overwrites the fp32 gradients, 1 adds into them (no rows: zeros, or nothing).  The same bits from run to run.
+ * ws / ws_bytes: at least stl_residual_norm_workspace_bytes(prob, flags).
+ */
+size_t stl_residual_norm_workspace_bytes(const stl_residual_t *prob, int flags);
+stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *Xout, const void *H, const void *gate, const void *w_post,
+                                        const void *b_post, const void *w_pre, const void *dXout, const void *dZ, void *dX, void *dH, float *dgate,
+                                        float *dw_post, float *db_post, float *dw_pre, float *db_pre, int accumulate, void *ws, size_t ws_bytes,
+                                        int flags, void *stream);
 
 /* Static text for a status code. */
 const char *stl_status_string(stl_status_t status);

@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     stl_aa_backward, stl_aa_forward, stl_aa_workspace_bytes, stl_backward, stl_decode, stl_encode_activation, stl_encode_weight, stl_encode_weight_backward, stl_forward, stl_forward_static, STL_STATIC_SCRATCH_BYTES, stl_last_error,
     stl_mlp_forward, stl_mlp_workspace_bytes, stl_plane_elems, stl_plane_matmul, stl_ragged_backward, stl_ragged_forward, stl_ragged_workspace_bytes, stl_recode, stl_status_string, stl_version,
     stl_workspace_bytes,
+    STL_MAX_DIM, STL_FLAG_CENTER, STL_FLAG_POST_NORM, STL_FLAG_PRE_NORM, ResidualProblem, stl_residual_norm_backward, stl_residual_norm_forward,
+    stl_residual_norm_workspace_bytes,
 )

@@ -18,6 +18,7 @@ STL_OP_ENCODE_WEIGHT, STL_OP_FORWARD, STL_OP_BACKWARD, STL_OP_ENCODE_WEIGHT_BACK
 STL_FLAG_AUTO, STL_FLAG_UNFUSED, STL_FLAG_EPILOGUE, STL_FLAG_FUSED, STL_FLAG_PIPELINED = 0, 1, 2, 3, 4
 STL_FLAG_GELU = 0x100
 STL_FLAG_B_TRANSPOSED = 0x200
+STL_FLAG_POST_NORM, STL_FLAG_PRE_NORM, STL_FLAG_CENTER = 0x400, 0x800, 0x1000
 
 # every symbol include/stl.h declares
 SYMBOLS = (
@@ -25,6 +26,7 @@ SYMBOLS = (
     "stl_plane_matmul", "stl_decode", "stl_mlp_workspace_bytes", "stl_mlp_forward", "stl_recode",
     "stl_aa_workspace_bytes", "stl_aa_forward", "stl_aa_backward",
     "stl_ragged_workspace_bytes", "stl_ragged_forward", "stl_ragged_backward",
+    "stl_residual_norm_workspace_bytes", "stl_residual_norm_forward", "stl_residual_norm_backward",
     "stl_status_string", "stl_last_error", "stl_version",
 )
 
@@ -51,6 +53,27 @@ class Problem:
 
     def c(self) -> _CProblem:
         return _CProblem(self.m, self.k, self.n, self.t, self.r, self.dtype)
+
+
+class _CResidual(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("rows_per_gate", ctypes.c_int64), ("skip", ctypes.c_float),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class ResidualProblem:
+    """Sizes and constants of stl_residual_norm_*; rows_per_gate None: all rows share the gate."""
+    rows: int
+    n: int
+    rows_per_gate: int | None = None
+    skip: float = 1.0
+    scale: float = 1.0
+    eps: float = 1e-6
+    dtype: int = STL_BF16
+
+    def c(self) -> _CResidual:
+        per = self.rows_per_gate if self.rows_per_gate is not None else max(self.rows, 1)
+        return _CResidual(self.rows, self.n, per, self.skip, self.scale, self.eps, self.dtype)
 
 
 _lib = None
@@ -95,7 +118,12 @@ def _load():
     lib.stl_ragged_workspace_bytes.argtypes = [pp, ctypes.c_int64, ctypes.c_int]
     lib.stl_ragged_forward.argtypes = [pp, ctypes.c_int64] + [_P] * 9 + [ctypes.c_size_t, _P]
     lib.stl_ragged_backward.argtypes = [pp, ctypes.c_int64] + [_P] * 13 + [ctypes.c_int, _P, ctypes.c_size_t, _P]
-    for name in ("stl_ragged_forward", "stl_ragged_backward", "stl_aa_forward", "stl_aa_backward", "stl_encode_weight", "stl_forward", "stl_backward", "stl_encode_activation", "stl_plane_matmul",
+    rp = ctypes.POINTER(_CResidual)
+    lib.stl_residual_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.stl_residual_norm_workspace_bytes.argtypes = [rp, ctypes.c_int]
+    lib.stl_residual_norm_forward.argtypes = [rp] + [_P] * 9 + [ctypes.c_int, _P]
+    lib.stl_residual_norm_backward.argtypes = [rp] + [_P] * 15 + [ctypes.c_int, _P, ctypes.c_size_t, ctypes.c_int, _P]
+    for name in ("stl_residual_norm_forward", "stl_residual_norm_backward", "stl_ragged_forward", "stl_ragged_backward", "stl_aa_forward", "stl_aa_backward", "stl_encode_weight", "stl_forward", "stl_backward", "stl_encode_activation", "stl_plane_matmul",
                  "stl_decode", "stl_mlp_forward", "stl_recode", "stl_encode_weight_backward"):
         getattr(lib, name).restype = ctypes.c_int
     lib.stl_status_string.restype = ctypes.c_char_p
@@ -150,6 +178,7 @@ def stl_version() -> str:
 
 
 STL_PLANE_GROUP = 64
+STL_MAX_DIM = 16776960
 
 
 def stl_plane_elems(R: int, Cc: int, r: int) -> int:
@@ -253,3 +282,20 @@ def stl_ragged_backward(prob: Problem, rows: int, X, What, E_X, D, fold, dC, Xha
     _check(_load().stl_ragged_backward(ctypes.byref(prob.c()), rows, _ptr(X), _ptr(What), _ptr(E_X), _ptr(D), _ptr(fold),
                                        _ptr(dC), _ptr(Xhat_saved), _ptr(Yhat_saved), _ptr(dX), _ptr(dWhat), _ptr(dE_X),
                                        _ptr(dD), _ptr(dfold), accumulate, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def stl_residual_norm_workspace_bytes(prob: ResidualProblem, flags: int) -> int:
+    return int(_load().stl_residual_norm_workspace_bytes(ctypes.byref(prob.c()), flags))
+
+
+def stl_residual_norm_forward(prob: ResidualProblem, X, H, gate, w_post, b_post, w_pre, b_pre, Xout, Z, flags: int = STL_FLAG_PRE_NORM,
+                              stream=None) -> None:
+    _check(_load().stl_residual_norm_forward(ctypes.byref(prob.c()), _ptr(X), _ptr(H), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre),
+                                             _ptr(b_pre), _ptr(Xout), _ptr(Z), flags, _stream(stream)))
+
+
+def stl_residual_norm_backward(prob: ResidualProblem, Xout, H, gate, w_post, b_post, w_pre, dXout, dZ, dX, dH, dgate, dw_post, db_post, dw_pre,
+                               db_pre, accumulate: int = 0, ws=None, ws_bytes: int = 0, flags: int = STL_FLAG_PRE_NORM, stream=None) -> None:
+    _check(_load().stl_residual_norm_backward(ctypes.byref(prob.c()), _ptr(Xout), _ptr(H), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre),
+                                              _ptr(dXout), _ptr(dZ), _ptr(dX), _ptr(dH), _ptr(dgate), _ptr(dw_post), _ptr(db_post),
+                                              _ptr(dw_pre), _ptr(db_pre), accumulate, _ptr(ws), ws_bytes, flags, _stream(stream)))

@@ -21,12 +21,12 @@ FLAGS = [
 
 
 def sources():
-    return sorted(CSRC.glob("*.hip"))
+    return sorted(CSRC.glob("*.hip")) + sorted((CSRC / "lm").glob("*.hip"))
 
 
 def build(force: bool = True, verbose: bool = False) -> Path:
     OBJ_DIR.mkdir(exist_ok=True)
-    headers = list(CSRC.glob("*.h")) + [HERE.parent / "include" / "stl.h"]
+    headers = list(CSRC.glob("**/*.h")) + [HERE.parent / "include" / "stl.h"]
     newest_hdr = max(h.stat().st_mtime for h in headers)
 
     def compile_one(src: Path):

@@ -10,7 +10,7 @@
 
 namespace {
 
-thread_local char g_err[512] = "";
+thread_local char g_err[stl::kErrorText] = "";
 
 stl_status_t fail(stl_status_t st, const char *fmt, ...)
 {
@@ -455,6 +455,8 @@ stl_status_t static_scratch_base(char **out)
 }
 
 }  // namespace
+
+char *stl::error_text() { return g_err; }
 
 extern "C" {
 

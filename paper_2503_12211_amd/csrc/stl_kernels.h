@@ -22,6 +22,10 @@ inline hipError_t allow_lds(const void *kern, int bytes, int most, std::atomic<u
     return e;
 }
 
+// the calling thread's error text behind stl_last_error(), kErrorText bytes (stl_api.hip)
+constexpr int kErrorText = 512;
+char *error_text();
+
 // dtype: 0 = fp32 storage, 1 = bf16 storage (matches stl_dtype_t)
 // pg: rows per group of the plane tensor's layout (see plane_row_base); 0 = plane-major (one group of all rows)
 constexpr int kPlaneGroup = 64;   // group size of the activation-side plane tensors

@@ -1,0 +1,54 @@
+"""CPU-side checks of the residual step's and the vocabulary loss's entry points: what is refused, before any launch."""
+import pytest
+
+import paper_2503_12211_amd as stl
+
+FAKE = 0x1000  # a non-null "device pointer"; never dereferenced because validation fails first
+
+
+def refused(status, fn, *args):
+    with pytest.raises(stl.StlError) as e:
+        fn(*args, stream=0)
+    assert e.value.status == status
+    assert stl.stl_last_error()
+
+
+@pytest.mark.parametrize("kw,status", [(dict(rows=-1), 1), (dict(n=0), 1), (dict(rows_per_gate=0), 1), (dict(eps=0.0), 1), (dict(eps=float("nan")), 1),
+                                       (dict(rows=stl.STL_MAX_DIM + 1), 1), (dict(n=32769), 2), (dict(dtype=5), 2)])
+def test_residual_problems_that_are_refused(kw, status):
+    prob = stl.ResidualProblem(**{**dict(rows=16, n=64), **kw})
+    flags = stl.STL_FLAG_PRE_NORM
+    assert stl.stl_residual_norm_workspace_bytes(prob, flags) == 0
+    refused(status, stl.stl_residual_norm_forward, prob, FAKE, FAKE, None, None, None, None, None, FAKE, FAKE, flags)
+    refused(status, stl.stl_residual_norm_backward, prob, FAKE, FAKE, None, None, None, None, FAKE, FAKE, FAKE, FAKE, None, None, None, None, None, 0, FAKE,
+            1 << 40, flags)
+
+
+def test_residual_arguments_that_are_refused():
+    prob = stl.ResidualProblem(16, 64)
+    pre, post = stl.STL_FLAG_PRE_NORM, stl.STL_FLAG_POST_NORM
+    fwd, bwd = stl.stl_residual_norm_forward, stl.stl_residual_norm_backward
+    need = stl.stl_residual_norm_workspace_bytes(prob, pre)
+    assert need > 0
+    refused(2, fwd, prob, FAKE, FAKE, None, None, None, None, None, FAKE, FAKE, pre | stl.STL_FLAG_GELU)
+    for hole in ((None, FAKE, FAKE, FAKE), (FAKE, None, FAKE, FAKE), (FAKE, FAKE, None, FAKE), (FAKE, FAKE, FAKE, None)):
+        refused(1, fwd, prob, hole[0], hole[1], None, None, None, None, None, hole[2], hole[3], pre)
+    refused(1, fwd, prob, FAKE + 8, FAKE, None, None, None, None, None, FAKE, FAKE, pre)
+
+    def grads(**kw):
+        a = dict(Xout=FAKE, H=FAKE, gate=FAKE, w_post=None, b_post=None, w_pre=None, dXout=FAKE, dZ=FAKE, dX=FAKE, dH=FAKE, dgate=None, dw_post=None,
+                 db_post=None, dw_pre=None, db_pre=None, accumulate=0, ws=FAKE, ws_bytes=need, flags=pre | post)
+        a.update(kw)
+        return (prob, *a.values())
+
+    refused(1, bwd, *grads(accumulate=2))
+    refused(1, bwd, *grads(gate=None, dgate=FAKE))
+    refused(1, bwd, *grads(flags=pre, dw_post=FAKE))
+    refused(1, bwd, *grads(flags=post, db_pre=FAKE))
+    refused(1, bwd, *grads(Xout=None))
+    refused(1, bwd, *grads(H=None))
+    refused(1, bwd, *grads(dZ=FAKE + 4))
+    refused(3, bwd, *grads(ws=None))
+    refused(3, bwd, *grads(ws_bytes=need - 1))
+    refused(1, bwd, *grads(ws=FAKE + 8))
+    refused(2, bwd, *grads(flags=0x1))
