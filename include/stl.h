@@ -331,6 +331,44 @@ stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *
                                         float *dw_post, float *db_post, float *dw_pre, float *db_pre, int accumulate, void *ws, size_t ws_bytes,
                                         int flags, void *stream);
 
+/*
+ * Loss over a vocabulary from hidden states, without the logits z = X W^T in memory.  Up to two terms for every row t:
+ *     label_loss[t] = log sum_v exp z_tv - z_t,label[t]                                     (label not NULL)
+ *     top_loss[t]   = sum_j q_j (log q_j - log softmax(z_t / tau)[top_id[t][j]])           (ntop > 0)
+ * the second being distillation from a teacher's `ntop` largest logits: q = softmax over j of top_logit[t][j] / tau.  A label outside
+ * 0 .. vocab-1 (such as -100) is none; so is an entry with an id outside, or a logit of minus infinity, and a row may have none.  A row
+ * without a term has that loss 0 and no gradient from it; where it has neither its X is not looked at (whatever it holds) and costs no products.
+ * An id may stand in a row more than once: it is one entry with the sum of its shares.
+ * X: rows x d, W: vocab x d (storage dtype).  label: rows; top_id, top_logit: rows x ntop.  label_loss, top_loss: rows fp32 (out) or NULL.
+ * Sums are fp32; bf16 logits are fp32 sums of exact products, fp32 logits fp32 products.
+ * 0 <= rows <= STL_MAX_DIM (0: pointers of what has rows may be NULL), 1 <= d <= STL_VOCAB_WIDEST, 1 <= vocab <= STL_VOCAB_MOST,
+ * 0 <= ntop <= STL_VOCAB_MOST_TOP, 0.25 <= temperature <= 16 (not read without a teacher).  At least one term.
+ * ws / ws_bytes: at least stl_vocab_loss_workspace_bytes(prob, STL_OP_FORWARD or STL_OP_BACKWARD); rows are taken in chunks, so that it is
+ * bounded by a few GB however many there are.
+ */
+typedef struct {
+    int64_t rows, d, vocab, ntop;
+    float temperature;
+    int32_t dtype;     /* stl_dtype_t */
+} stl_vocab_t;
+#define STL_VOCAB_WIDEST 1048576
+#define STL_VOCAB_MOST 4194304
+#define STL_VOCAB_MOST_TOP 1024
+size_t stl_vocab_loss_workspace_bytes(const stl_vocab_t *prob, int op);
+stl_status_t stl_vocab_loss_forward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
+                                    const float *top_logit, float *label_loss, float *top_loss, void *ws, size_t ws_bytes, void *stream);
+/*
+ * Backward of sum_t dlabel[t] label_loss[t] + dtop[t] top_loss[t], and the losses themselves where they are asked for (a training step whose
+ * row weights are known needs this call alone: the logits are formed once):
+ *     dz_tv = dlabel[t] (softmax(z_t)[v] - [v = label[t]]) + dtop[t] / tau (softmax(z_t / tau)[v] - sum_{j: top_id[t][j] = v} q_j)
+ *     dX = dz W,   dW = dz^T X.
+ * dlabel, dtop: rows fp32; NULL stands for zeros (one of them at least).  dX: rows x d, dW: vocab x d (out, storage dtype), either may be NULL
+ * (not both).  bf16: dz is rounded to bf16 once for the two products, dX and dW once.  The same bits from run to run.
+ */
+stl_status_t stl_vocab_loss_backward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
+                                     const float *top_logit, const float *dlabel, const float *dtop, float *label_loss, float *top_loss, void *dX,
+                                     void *dW, void *ws, size_t ws_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *stl_status_string(stl_status_t status);
 /* Text of the last error raised on the calling thread ("" if none).  Thread-local storage. */

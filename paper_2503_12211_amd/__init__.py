@@ -11,5 +11,5 @@ from .binding import (  # noqa: F401
     stl_mlp_forward, stl_mlp_workspace_bytes, stl_plane_elems, stl_plane_matmul, stl_ragged_backward, stl_ragged_forward, stl_ragged_workspace_bytes, stl_recode, stl_status_string, stl_version,
     stl_workspace_bytes,
     STL_MAX_DIM, STL_FLAG_CENTER, STL_FLAG_POST_NORM, STL_FLAG_PRE_NORM, ResidualProblem, stl_residual_norm_backward, stl_residual_norm_forward,
-    stl_residual_norm_workspace_bytes,
+    stl_residual_norm_workspace_bytes, VocabProblem, stl_vocab_loss_backward, stl_vocab_loss_forward, stl_vocab_loss_workspace_bytes,
 )

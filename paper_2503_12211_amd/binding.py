@@ -27,6 +27,7 @@ SYMBOLS = (
     "stl_aa_workspace_bytes", "stl_aa_forward", "stl_aa_backward",
     "stl_ragged_workspace_bytes", "stl_ragged_forward", "stl_ragged_backward",
     "stl_residual_norm_workspace_bytes", "stl_residual_norm_forward", "stl_residual_norm_backward",
+    "stl_vocab_loss_workspace_bytes", "stl_vocab_loss_forward", "stl_vocab_loss_backward",
     "stl_status_string", "stl_last_error", "stl_version",
 )
 
@@ -76,6 +77,25 @@ class ResidualProblem:
         return _CResidual(self.rows, self.n, per, self.skip, self.scale, self.eps, self.dtype)
 
 
+class _CVocab(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ntop", ctypes.c_int64),
+                ("temperature", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class VocabProblem:
+    """Sizes of stl_vocab_loss_*; ntop 0: no teacher."""
+    rows: int
+    d: int
+    vocab: int
+    ntop: int = 0
+    temperature: float = 1.0
+    dtype: int = STL_BF16
+
+    def c(self) -> _CVocab:
+        return _CVocab(self.rows, self.d, self.vocab, self.ntop, self.temperature, self.dtype)
+
+
 _lib = None
 _P = ctypes.c_void_p
 
@@ -123,7 +143,12 @@ def _load():
     lib.stl_residual_norm_workspace_bytes.argtypes = [rp, ctypes.c_int]
     lib.stl_residual_norm_forward.argtypes = [rp] + [_P] * 9 + [ctypes.c_int, _P]
     lib.stl_residual_norm_backward.argtypes = [rp] + [_P] * 15 + [ctypes.c_int, _P, ctypes.c_size_t, ctypes.c_int, _P]
-    for name in ("stl_residual_norm_forward", "stl_residual_norm_backward", "stl_ragged_forward", "stl_ragged_backward", "stl_aa_forward", "stl_aa_backward", "stl_encode_weight", "stl_forward", "stl_backward", "stl_encode_activation", "stl_plane_matmul",
+    vp = ctypes.POINTER(_CVocab)
+    lib.stl_vocab_loss_workspace_bytes.restype = ctypes.c_size_t
+    lib.stl_vocab_loss_workspace_bytes.argtypes = [vp, ctypes.c_int]
+    lib.stl_vocab_loss_forward.argtypes = [vp] + [_P] * 8 + [ctypes.c_size_t, _P]
+    lib.stl_vocab_loss_backward.argtypes = [vp] + [_P] * 12 + [ctypes.c_size_t, _P]
+    for name in ("stl_vocab_loss_forward", "stl_vocab_loss_backward", "stl_residual_norm_forward", "stl_residual_norm_backward", "stl_ragged_forward", "stl_ragged_backward", "stl_aa_forward", "stl_aa_backward", "stl_encode_weight", "stl_forward", "stl_backward", "stl_encode_activation", "stl_plane_matmul",
                  "stl_decode", "stl_mlp_forward", "stl_recode", "stl_encode_weight_backward"):
         getattr(lib, name).restype = ctypes.c_int
     lib.stl_status_string.restype = ctypes.c_char_p
@@ -299,3 +324,18 @@ def stl_residual_norm_backward(prob: ResidualProblem, Xout, H, gate, w_post, b_p
     _check(_load().stl_residual_norm_backward(ctypes.byref(prob.c()), _ptr(Xout), _ptr(H), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre),
                                               _ptr(dXout), _ptr(dZ), _ptr(dX), _ptr(dH), _ptr(dgate), _ptr(dw_post), _ptr(db_post),
                                               _ptr(dw_pre), _ptr(db_pre), accumulate, _ptr(ws), ws_bytes, flags, _stream(stream)))
+
+
+def stl_vocab_loss_workspace_bytes(prob: VocabProblem, op: int) -> int:
+    return int(_load().stl_vocab_loss_workspace_bytes(ctypes.byref(prob.c()), op))
+
+
+def stl_vocab_loss_forward(prob: VocabProblem, X, W, label, top_id, top_logit, label_loss, top_loss, ws=None, ws_bytes: int = 0, stream=None) -> None:
+    _check(_load().stl_vocab_loss_forward(ctypes.byref(prob.c()), _ptr(X), _ptr(W), _ptr(label), _ptr(top_id), _ptr(top_logit), _ptr(label_loss),
+                                          _ptr(top_loss), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def stl_vocab_loss_backward(prob: VocabProblem, X, W, label, top_id, top_logit, dlabel, dtop, label_loss, top_loss, dX, dW, ws=None, ws_bytes: int = 0,
+                            stream=None) -> None:
+    _check(_load().stl_vocab_loss_backward(ctypes.byref(prob.c()), _ptr(X), _ptr(W), _ptr(label), _ptr(top_id), _ptr(top_logit), _ptr(dlabel), _ptr(dtop),
+                                           _ptr(label_loss), _ptr(top_loss), _ptr(dX), _ptr(dW), _ptr(ws), ws_bytes, _stream(stream)))

@@ -58,6 +58,44 @@ stl_status_t check_residual(const stl_residual_t *p, int flags, stl::lm::Residua
     return STL_OK;
 }
 
+static_assert(STL_VOCAB_MOST_TOP == stl::lm::kMostTop, "documented count");
+
+stl_status_t check_vocab(const stl_vocab_t *p, stl::lm::VocabArgs *a)
+{
+    if (!p) return fail(STL_ERR_INVALID_ARG, "problem descriptor is NULL");
+    if (p->dtype != STL_F32 && p->dtype != STL_BF16) return fail(STL_ERR_UNSUPPORTED, "unknown dtype %d", p->dtype);
+    if (p->rows < 0 || p->d < 1 || p->vocab < 1 || p->ntop < 0)
+        return fail(STL_ERR_INVALID_ARG, "rows=%lld d=%lld vocab=%lld ntop=%lld: rows and ntop may be 0, the others are positive", (long long)p->rows,
+                    (long long)p->d, (long long)p->vocab, (long long)p->ntop);
+    if (p->rows > STL_MAX_DIM || p->d > STL_VOCAB_WIDEST || p->vocab > STL_VOCAB_MOST || p->ntop > STL_VOCAB_MOST_TOP)
+        return fail(STL_ERR_INVALID_ARG, "more than %d rows, d=%d, vocab=%d or ntop=%d", STL_MAX_DIM, STL_VOCAB_WIDEST, STL_VOCAB_MOST, STL_VOCAB_MOST_TOP);
+    if (p->ntop > 0 && !(p->temperature >= stl::lm::kLowestTau && p->temperature <= stl::lm::kHighestTau))
+        return fail(STL_ERR_INVALID_ARG, "temperature %g outside [%g, %g]", (double)p->temperature, (double)stl::lm::kLowestTau, (double)stl::lm::kHighestTau);
+    *a = stl::lm::VocabArgs{};
+    a->rows = (int)p->rows, a->d = (int)p->d, a->vocab = (int)p->vocab, a->ntop = (int)p->ntop;
+    a->tau = p->ntop > 0 ? p->temperature : 1.f;
+    a->bf16 = p->dtype == STL_BF16;
+    return STL_OK;
+}
+
+// what the forward and the backward call have in common
+stl_status_t vocab_inputs(const char *fn, const stl_vocab_t *p, stl::lm::VocabArgs *a, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
+                          const float *top_logit, const float *label_loss, const float *top_loss)
+{
+    const stl_status_t st = check_vocab(p, a);
+    if (st != STL_OK) return st;
+    if (any_misaligned(X, W, label, top_id, top_logit, label_loss, top_loss)) return fail(STL_ERR_INVALID_ARG, "%s: a pointer is not 16-byte aligned", fn);
+    if (a->rows > 0) {
+        if (!X || !W) return fail(STL_ERR_INVALID_ARG, "%s: NULL pointer", fn);
+        if (!label && a->ntop == 0) return fail(STL_ERR_INVALID_ARG, "%s: neither labels nor a teacher", fn);
+        if (a->ntop > 0 && (!top_id || !top_logit)) return fail(STL_ERR_INVALID_ARG, "%s: ntop=%d without top_id or top_logit", fn, a->ntop);
+    }
+    if ((label_loss && !label && a->rows > 0) || (top_loss && a->ntop == 0)) return fail(STL_ERR_INVALID_ARG, "%s: the loss of a term that is not there", fn);
+    a->X = X, a->W = W, a->label = label;
+    if (a->ntop > 0) a->top_id = top_id, a->top_logit = top_logit;
+    return STL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -104,7 +142,7 @@ stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *
         // sums over no rows; there is no row of a gate either
         float *outs[4] = {dw_post, db_post, dw_pre, db_pre};
         for (float *o : outs)
-            if (o && !accumulate) LM_HIP(stl::lm::launch_zero(o, (size_t)a.n * sizeof(float), s), "residual_norm_backward/no rows");
+            if (o && !accumulate) LM_HIP(stl::lm::launch_zero_elements(false, o, (size_t)a.n, s), "residual_norm_backward/no rows");
         return STL_OK;
     }
     if ((a.pre && !Xout) || (!H && (a.post || dgate))) return fail(STL_ERR_INVALID_ARG, "residual_norm_backward: NULL pointer");
@@ -115,6 +153,53 @@ stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *
     if (a.pre) a.w_pre = w_pre;
     const stl::lm::ResidualGrads g{dXout, a.pre ? dZ : nullptr, dX, dH, dgate, dw_post, db_post, dw_pre, db_pre, accumulate};
     LM_HIP(stl::lm::launch_residual_backward(prob->dtype, a, g, ws, s), "residual_norm_backward");
+    return STL_OK;
+}
+
+size_t stl_vocab_loss_workspace_bytes(const stl_vocab_t *prob, int op)
+{
+    stl::lm::VocabArgs a;
+    if (check_vocab(prob, &a) != STL_OK) return 0;
+    if (op != STL_OP_FORWARD && op != STL_OP_BACKWARD) {
+        fail(STL_ERR_INVALID_ARG, "vocab_loss_workspace_bytes: op is STL_OP_FORWARD or STL_OP_BACKWARD");
+        return 0;
+    }
+    return stl::lm::vocab_workspace_bytes(a, op == STL_OP_BACKWARD);
+}
+
+stl_status_t stl_vocab_loss_forward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
+                                    const float *top_logit, float *label_loss, float *top_loss, void *ws, size_t ws_bytes, void *stream)
+{
+    stl::lm::VocabArgs a;
+    stl_status_t st = vocab_inputs("vocab_loss_forward", prob, &a, X, W, label, top_id, top_logit, label_loss, top_loss);
+    if (st != STL_OK || a.rows == 0) return st;
+    if (!label_loss && !top_loss) return fail(STL_ERR_INVALID_ARG, "vocab_loss_forward: no output");
+    st = check_workspace("vocab_loss_forward", ws, ws_bytes, stl::lm::vocab_workspace_bytes(a, false));
+    if (st != STL_OK) return st;
+    LM_HIP(stl::lm::launch_vocab_loss(a, nullptr, label_loss, top_loss, ws, (hipStream_t)stream), "vocab_loss_forward");
+    return STL_OK;
+}
+
+stl_status_t stl_vocab_loss_backward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
+                                     const float *top_logit, const float *dlabel, const float *dtop, float *label_loss, float *top_loss, void *dX,
+                                     void *dW, void *ws, size_t ws_bytes, void *stream)
+{
+    stl::lm::VocabArgs a;
+    stl_status_t st = vocab_inputs("vocab_loss_backward", prob, &a, X, W, label, top_id, top_logit, label_loss, top_loss);
+    if (st != STL_OK) return st;
+    if (any_misaligned(dlabel, dtop, dX, dW)) return fail(STL_ERR_INVALID_ARG, "vocab_loss_backward: a pointer is not 16-byte aligned");
+    hipStream_t s = (hipStream_t)stream;
+    if (a.rows == 0) {
+        // a sum over no rows
+        if (dW) LM_HIP(stl::lm::launch_zero_elements(a.bf16, dW, (size_t)a.vocab * a.d, s), "vocab_loss_backward/no rows");
+        return STL_OK;
+    }
+    if (!dX && !dW) return fail(STL_ERR_INVALID_ARG, "vocab_loss_backward: neither dX nor dW");
+    if (!(dlabel && label) && !(dtop && a.ntop > 0)) return fail(STL_ERR_INVALID_ARG, "vocab_loss_backward: no upstream gradient of a term that is there");
+    st = check_workspace("vocab_loss_backward", ws, ws_bytes, stl::lm::vocab_workspace_bytes(a, true));
+    if (st != STL_OK) return st;
+    const stl::lm::VocabGrads g{dlabel, dtop, dX, dW};
+    LM_HIP(stl::lm::launch_vocab_loss(a, &g, label_loss, top_loss, ws, s), "vocab_loss_backward");
     return STL_OK;
 }
 

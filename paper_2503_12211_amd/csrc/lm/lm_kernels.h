@@ -5,8 +5,8 @@
 namespace stl {
 namespace lm {
 
-// fills with zero bits (a kernel: memset nodes in a captured graph are avoided); bytes a multiple of 4, p aligned to 4
-hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);
+// n zeros (a kernel: memset nodes in a captured graph are avoided)
+hipError_t launch_zero_elements(bool bf16, void *p, size_t n, hipStream_t s);
 
 // ---- residual step (lm_residual.h) -------------------------------------------------------------------------------------------
 struct ResidualArgs {
@@ -26,6 +26,60 @@ constexpr int kResidualWidest = 32768;       // a row is held in the registers o
 size_t residual_workspace_bytes(int rows, int n, int per_gate);
 hipError_t launch_residual_forward(int dtype, const ResidualArgs &a, void *Xout, void *Z, hipStream_t s);
 hipError_t launch_residual_backward(int dtype, const ResidualArgs &a, const ResidualGrads &g, void *ws, hipStream_t s);
+
+// ---- vocabulary loss (lm_vocab.hip, lm_vocab_rows.hip) -----------------------------------------------------------------------
+struct VocabArgs {
+    int rows, d, vocab, ntop;
+    float tau;
+    bool bf16;
+    const void *X, *W;
+    const int64_t *label, *top_id;           // NULL: no such term
+    const float *top_logit;
+};
+struct VocabGrads {
+    const float *dlabel, *dtop;              // rows; upstream gradients of the two losses
+    void *dX, *dW;                           // storage type, either may be NULL
+};
+constexpr int kMostTop = 1024;
+// A logit between its product and its gradient is held (bf16 storage) in 16 bits: as one of kSteps even steps from its group's maximum down to its
+// minimum, 65535 for what is below every share that fp32 can hold (minus infinity among it).  A group of 64 normal logits spreads over five
+// deviations: at a deviation of 2 a step is 1.5e-4, that is an error of exp(z) of 4e-5 (root mean square), a fortieth of the rounding of the gradient
+// to bf16 that follows (as bf16 exponentials they would add that rounding once more).  In terms of z / tau it is 1 / tau of that.
+constexpr float kSteps = 65534.f, kLowestTau = 0.25f, kHighestTau = 16.f;
+size_t vocab_workspace_bytes(const VocabArgs &a, bool grads);
+// label_loss, top_loss: rows fp32 or NULL; g NULL: losses alone
+hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, void *ws, hipStream_t s);
+
+// The rows that have a label or a teacher, in order: list[0 .. count), and count itself, on the device; list has room for `rows`.
+struct RowList {
+    int *list, *count;
+};
+hipError_t launch_select_rows(const VocabArgs &a, RowList rl, hipStream_t s);
+// rows first .. first + cap of the list, side by side with ld elements each (zeros behind a row's end and behind the list's); bf16 storage may be
+// packed (d no multiple of what the products need)
+hipError_t launch_gather_rows(bool bf16, const void *X, RowList rl, int first, int cap, int d, int ld, void *out, hipStream_t s);
+// rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)
+hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
+
+// Logits of one chunk of listed rows on their way to the gradient (storage fp32: the logits themselves).  bf16: what the product leaves for
+// every listed row and group of 64 columns: the largest logit m, sums of exp(z - m) and exp((z - m) / tau), and with gradients the logits as 16-bit
+// steps below m and the size of a step.
+struct VocabChunk {
+    int first, cap;                          // listed rows first .. first + cap (those that exist)
+    void *codes;                             // cap x ld: 16 bits (bf16 storage) or fp32 logits; the gradient is written in their place
+    size_t ld;
+    float *group_max, *group_sum, *group_sum_tau, *group_step;      // cap x groups (bf16 storage); group_sum_tau only where tau is not 1 and both terms are there
+    int groups;
+    const void *Xc;                          // the listed rows, ldx elements each
+    int ldx;
+};
+hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
+// dX rows of the list from `parts` sums of cap x ld each
+hipError_t launch_finish_dx(bool bf16, const float *part, int parts, size_t stride, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s);
+// zeros for the rows that are not listed: their rows of dX and their losses (each may be NULL)
+hipError_t launch_zero_others(const VocabArgs &a, void *dX, float *label_loss, float *top_loss, hipStream_t s);
+// out[i][j] = sum over parts of part[p][i][j], rows of ld in the parts and of d in `out`
+hipError_t launch_finish_dw(bool bf16, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s);
 
 }  // namespace lm
 }  // namespace stl

@@ -4,16 +4,19 @@
 namespace stl {
 namespace lm {
 
-__global__ __launch_bounds__(256) void zero_kernel(uint32_t *p, size_t words)
+template <typename T>
+__global__ __launch_bounds__(256) void zero_kernel(T *p, size_t n)
 {
-    for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) p[i] = 0u;
+    for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
 }
 
-hipError_t launch_zero(void *p, size_t bytes, hipStream_t s)
+hipError_t launch_zero_elements(bool bf16, void *p, size_t n, hipStream_t s)
 {
-    const size_t words = bytes / 4, blocks = (words + 255) / 256;
-    if (words == 0) return hipSuccess;
-    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, (uint32_t *)p, words);
+    const size_t blocks = (n + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048));
+    if (n == 0) return hipSuccess;
+    if (bf16) hipLaunchKernelGGL(zero_kernel<bf16_t>, grid, dim3(256), 0, s, (bf16_t *)p, n);
+    else hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(256), 0, s, (float *)p, n);
     return hipGetLastError();
 }
 

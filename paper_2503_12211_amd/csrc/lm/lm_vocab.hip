@@ -1,0 +1,469 @@
+// Vocabulary loss: the matrix products of bf16 storage on the matrix cores, and the order of launches for both storage types.
+//
+// Rows with a term are listed on the device and taken in chunks; the logits of a chunk are never in memory as such.  bf16 storage:
+//   1. logits product  X W^T: every wavefront turns its 64 columns of a row into their maximum and the sum of their exponentials, and (for
+//      gradients) writes the logits as 16-bit steps below that maximum;
+//   2. a pass over the rows gives the losses and writes the bf16 gradient dz over the steps (lm_vocab_rows.hip);
+//   3. dX = dz W, contraction over the vocabulary, split where there are few blocks;  4. dW = dz^T X, contraction over the rows.
+// Three products of 2 T V d operations, where forming the logits twice would take four; what bounds them is the matrix cores (lm_gemm.h).
+// fp32 storage: the same steps on the fp32 products of ../stl_gemm_generic.hip, the chunk's logits in fp32.
+#include "lm_gemm.h"
+#include "lm_kernels.h"
+#include "lm_device.h"
+
+namespace stl {
+namespace lm {
+
+// ---- logits ------------------------------------------------------------------------------------------------------------------------
+struct LogitsOut {
+    float *group_max, *group_sum, *group_sum_tau, *group_step;
+    int groups;
+    uint16_t *codes;
+    long ld;
+    float inv_tau;       // temperature of the first sum (1 with labels), and
+    float inv_tau2;      // of the second
+    float deepest;       // below a group's maximum by this much, no share is left in fp32
+};
+
+// rows: count - first listed rows of the chunk (at most cap), a device value
+template <int BM, int WAVES_M, int WAVES_N, int NS, bool CODES, bool TWO>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_logits_kernel(const Operands o, const int *count, int first, int cap, int vocab, const LogitsOut out)
+{
+    using namespace pipe;
+    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, false, false> R;
+    static_assert(R::WN == 64, "a wavefront's columns are one group");
+    extern __shared__ __align__(16) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char *slab = smem + NS * R::STAGE_BYTES + wave * R::SLAB;
+    const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
+    int rows = *count - first;
+    if (rows > cap) rows = cap;
+    if (rows <= 0) return;
+    const int tiles_m = (rows + BM - 1) / BM, tiles_n = (vocab + 255) / 256, total = tiles_m * tiles_n, nks = o.Kl / BKS;
+    R ring;
+    ring.init(wave, lane);
+    auto start_block = [&](int v) {
+        int bi, bj;
+        block_at(v, tiles_m, tiles_n, bi, bj);
+        ring.start(o, nks, bi * BM, bj * 256, smem_lds, wave, lane);
+    };
+    const int step = block_step(), end = end_block(total);
+    int v = first_block(total);
+    if (v < end) start_block(v);
+    for (; v < end; v += step) {
+        int bi, bj;
+        block_at(v, tiles_m, tiles_n, bi, bj);
+        ring.block(
+            nks, smem, smem_lds, wave, lane,
+            [&]() {
+                if (v + step < end) start_block(v + step);
+            },
+            [&](typename R::Tile &w) {
+                int el = lane;                               // opaque: what follows from it is not kept over the products
+                asm volatile("" : "+v"(el));
+                const int row0 = bi * BM + wave / WAVES_N * R::WM, col0 = bj * 256 + wave % WAVES_N * 64, quad = el >> 4, rl = el & 15;
+                const int col = col0 + 4 * quad;             // the lane's columns: col + 16 b + e
+                const bool whole = col0 + 64 <= vocab;
+                if (col0 >= vocab && (!CODES || col0 >= out.ld)) return;
+                const int group = col0 / 64;
+                const float scale = out.inv_tau * 1.44269504088896340736f, scale2 = out.inv_tau2 * 1.44269504088896340736f;
+                constexpr int PA = 2;                        // fragment rows that the slab holds: 16 rows of 128 bytes each
+                static_for<0, R::FM / PA>([&](auto pass_c) {
+                    constexpr int a0 = decltype(pass_c)::value * PA;
+                    static_for<0, PA>([&](auto a_c) {
+                        constexpr int a = a0 + decltype(a_c)::value;
+                        float m = -INFINITY, least = INFINITY;
+                        if (!whole) {
+#pragma unroll
+                            for (int b = 0; b < R::FN; ++b)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const bool in = col + 16 * b + e < vocab;
+                                    if constexpr (CODES) least = fminf(least, in ? w.acc[a][b][e] : least);
+                                    w.acc[a][b][e] = in ? w.acc[a][b][e] : -INFINITY;
+                                }
+                        } else if constexpr (CODES) {
+#pragma unroll
+                            for (int b = 0; b < R::FN; ++b)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) least = fminf(least, w.acc[a][b][e]);
+                        }
+#pragma unroll
+                        for (int b = 0; b < R::FN; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) m = fmaxf(m, w.acc[a][b][e]);
+                        m = fmaxf(m, __shfl_xor(m, 16));
+                        m = fmaxf(m, __shfl_xor(m, 32));
+                        // a group of nothing but minus infinities: exp(-inf - 0), not exp(-inf + inf)
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        float s = 0.f, s2 = 0.f;
+#pragma unroll
+                        for (int b = 0; b < R::FN; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float below = w.acc[a][b][e] - ref;
+                                s += __builtin_amdgcn_exp2f(below * scale);
+                                if constexpr (TWO) s2 += __builtin_amdgcn_exp2f(below * scale2);
+                            }
+                        s += __shfl_xor(s, 16);
+                        s += __shfl_xor(s, 32);
+                        if constexpr (TWO) {
+                            s2 += __shfl_xor(s2, 16);
+                            s2 += __shfl_xor(s2, 32);
+                        }
+                        float per_step = 0.f, steps = 0.f;
+                        if constexpr (CODES) {
+                            least = fminf(least, __shfl_xor(least, 16));
+                            least = fminf(least, __shfl_xor(least, 32));
+                            // (the order of the bounds makes any spread that is not a number a finite one)
+                            const float spread = fminf(fmaxf(ref - least, 1e-3f), out.deepest);
+                            per_step = spread * (1.f / kSteps);
+                            steps = kSteps / spread;
+                        }
+                        const size_t at = (size_t)(row0 + 16 * a + rl) * out.groups + group;
+                        if (quad == 0 && row0 + 16 * a + rl < rows && group < out.groups) {
+                            out.group_max[at] = m;
+                            out.group_sum[at] = s;
+                            if constexpr (TWO) out.group_sum_tau[at] = s2;
+                            if constexpr (CODES) out.group_step[at] = per_step;
+                        }
+                        if constexpr (CODES) {
+                            char *rowp = slab + (16 * (a - a0) + rl) * 128;
+                            const int swz = (rl >> 1) & 7;
+#pragma unroll
+                            for (int b = 0; b < R::FN; ++b) {
+                                uint32_t c[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    c[e] = (uint32_t)fminf((ref - w.acc[a][b][e]) * steps + 0.5f, 65535.f);
+                                }
+                                *reinterpret_cast<u32x2_t *>(rowp + (((2 * b + (quad >> 1)) ^ swz) << 4) + (quad & 1) * 8) =
+                                    u32x2_t{c[0] | c[1] << 16, c[2] | c[3] << 16};
+                            }
+                        }
+                    });
+                    if constexpr (CODES) {
+                        // rows leave as whole 128-byte lines; a wavefront's LDS operations execute in order
+                        asm volatile("" ::: "memory");
+                        const int rr = el >> 3, rc = el & 7;
+#pragma unroll
+                        for (int i = 0; i < PA * 2; ++i) {
+                            const int row = i * 8 + rr, gi = row0 + a0 * 16 + row;
+                            const u32x4_t piece = *reinterpret_cast<const u32x4_t *>(slab + row * 128 + ((rc ^ ((row >> 1) & 7)) << 4));
+                            if (gi < rows && col0 + rc * 8 < out.ld) *reinterpret_cast<u32x4_t *>(out.codes + (size_t)gi * out.ld + col0 + rc * 8) = piece;
+                        }
+                        asm volatile("" ::: "memory");
+                    }
+                });
+            });
+    }
+}
+
+// ---- dX and dW -----------------------------------------------------------------------------------------------------------------------
+// dX parts: part s, rows x ldx = dz (columns of split s) W.  The contraction over the vocabulary is cut into `splits` runs of whole stages.
+template <int BM, int WAVES_M, int WAVES_N, int NS>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, const int *count, int first, int cap, int d, int splits, float *part,
+                                                                      size_t stride, int ldx)
+{
+    using namespace pipe;
+    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
+    extern __shared__ __align__(16) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char *slab = smem + NS * R::STAGE_BYTES + wave * R::SLAB;
+    const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
+    int rows = *count - first;
+    if (rows > cap) rows = cap;
+    if (rows <= 0) return;
+    const int tiles_m = (rows + BM - 1) / BM, tiles_n = (d + 255) / 256, per = tiles_m * tiles_n, total = per * splits, stages = (o.Kl + BKS - 1) / BKS;
+    R ring;
+    ring.init(wave, lane);
+    auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
+    auto start_block = [&](int v) {
+        const int sp = v / per, s0 = begin_of(sp), s1 = begin_of(sp + 1);
+        int bi, bj;
+        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+        Operands mine = o;
+        mine.A += (long)s0 * BKS;
+        mine.B += (long)s0 * BKS * o.ldb;
+        mine.Kl = (o.Kl < s1 * BKS ? o.Kl : s1 * BKS) - s0 * BKS;
+        ring.start(mine, s1 - s0, bi * BM, bj * 256, smem_lds, wave, lane);
+    };
+    const int step = block_step(), end = end_block(total);
+    int v = first_block(total);
+    if (v < end) start_block(v);
+    for (; v < end; v += step) {
+        const int sp = v / per;
+        int bi, bj;
+        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+        ring.block(
+            begin_of(sp + 1) - begin_of(sp), smem, smem_lds, wave, lane,
+            [&]() {
+                if (v + step < end) start_block(v + step);
+            },
+            [&](typename R::Tile &w) {
+                int el = lane;
+                asm volatile("" : "+v"(el));
+                w.template store<float, false, false>(slab, part + sp * stride, bi * BM + wave / WAVES_N * R::WM, bj * 256 + wave % WAVES_N * R::WN, rows, ldx, 0,
+                                                      1 << 30, 1, el);
+            });
+    }
+}
+
+// dW = dz^T X over the listed rows of a chunk: straight to dW (bf16), or to parts in fp32, added to what is there behind the first chunk.
+template <typename TO, bool ACC>
+__global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *count, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo)
+{
+    using namespace pipe;
+    typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
+    extern __shared__ __align__(16) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char *slab = smem + 4 * R::STAGE_BYTES + wave * R::SLAB;
+    const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
+    int rows = *count - first;
+    if (rows > cap) rows = cap;
+    if (rows <= 0) {
+        if (ACC) return;                                     // nothing to add
+        rows = 0;
+    }
+    const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, per = tiles_m * tiles_n, total = per * splits, stages = (rows + BKS - 1) / BKS;
+    R ring;
+    ring.init(wave, lane);
+    auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
+    auto start_block = [&](int v) {
+        const int sp = v / per, s0 = begin_of(sp);
+        int bi, bj;
+        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+        Operands mine = o;
+        mine.A += (long)s0 * BKS * o.lda;
+        mine.B += (long)s0 * BKS * o.ldb;
+        ring.start(mine, begin_of(sp + 1) - s0, bi * 256, bj * 256, smem_lds, wave, lane);
+    };
+    const int step = block_step(), end = end_block(total);
+    int v = first_block(total);
+    if (v < end) start_block(v);
+    for (; v < end; v += step) {
+        const int sp = v / per;
+        int bi, bj;
+        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+        ring.block(
+            begin_of(sp + 1) - begin_of(sp), smem, smem_lds, wave, lane,
+            [&]() {
+                if (v + step < end) start_block(v + step);
+            },
+            [&](typename R::Tile &w) {
+                int el = lane;
+                asm volatile("" : "+v"(el));
+                w.template store<TO, ACC, false>(slab, out + sp * stride, bi * 256 + wave / 4 * R::WM, bj * 256 + wave % 4 * R::WN, vocab, ldo, 0, 1 << 30, 1, el);
+            });
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------------------
+template <class K, class... Args>
+static hipError_t launch_ring(K kern, std::atomic<uint64_t> &granted, int lds, int threads, long blocks, hipStream_t s, Args... args)
+{
+    if (const hipError_t e = allow_lds(reinterpret_cast<const void *>(kern), lds, lds, granted); e != hipSuccess) return e;
+    if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kern, dim3(pipe::list_grid(blocks, pipe::cu_count())), dim3(threads), lds, s, args...);
+    return hipGetLastError();
+}
+
+template <int BM, int WAVES_M, int WAVES_N, int NS, bool CODES, bool TWO>
+static hipError_t launch_logits_as(const Operands &o, const int *count, int first, int cap, int vocab, const LogitsOut &out, hipStream_t s)
+{
+    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, false, false> R;
+    static std::atomic<uint64_t> granted{0};                 // of this instantiation
+    return launch_ring(vocab_logits_kernel<BM, WAVES_M, WAVES_N, NS, CODES, TWO>, granted, R::LDS_BYTES, R::THREADS,
+                       (long)((cap + BM - 1) / BM) * ((vocab + 255) / 256), s, o, count, first, cap, vocab, out);
+}
+template <int BM, int WAVES_M, int WAVES_N, int NS>
+static hipError_t launch_logits(const Operands &o, const int *count, int first, int cap, int vocab, const LogitsOut &out, bool two, hipStream_t s)
+{
+    if (out.codes)
+        return two ? launch_logits_as<BM, WAVES_M, WAVES_N, NS, true, true>(o, count, first, cap, vocab, out, s)
+                   : launch_logits_as<BM, WAVES_M, WAVES_N, NS, true, false>(o, count, first, cap, vocab, out, s);
+    return two ? launch_logits_as<BM, WAVES_M, WAVES_N, NS, false, true>(o, count, first, cap, vocab, out, s)
+               : launch_logits_as<BM, WAVES_M, WAVES_N, NS, false, false>(o, count, first, cap, vocab, out, s);
+}
+
+template <int BM, int WAVES_M, int WAVES_N, int NS>
+static hipError_t launch_dx(const Operands &o, const int *count, int first, int cap, int d, int splits, float *part, size_t stride, int ldx, hipStream_t s)
+{
+    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
+    static std::atomic<uint64_t> granted{0};
+    return launch_ring(vocab_dx_kernel<BM, WAVES_M, WAVES_N, NS>, granted, R::LDS_BYTES, R::THREADS, (long)((cap + BM - 1) / BM) * ((d + 255) / 256) * splits, s, o,
+                       count, first, cap, d, splits, part, stride, ldx);
+}
+
+template <typename TO, bool ACC>
+static hipError_t launch_dw(const Operands &o, const int *count, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
+{
+    typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
+    static std::atomic<uint64_t> granted{0};
+    return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, (long)((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o, count, first, cap,
+                       vocab, splits, out, stride, ldo);
+}
+
+// ---- the whole of a call -----------------------------------------------------------------------------------------------------------------
+namespace {
+
+inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline long round_up(long x, long to) { return (x + to - 1) / to * to; }
+
+// How a call is cut, and where things lie in the workspace.
+struct Plan {
+    int cap;                 // listed rows of a chunk
+    int chunks;
+    int rows_held;           // rows that Xc has
+    int ldx;                 // elements of a row of Xc (and of a packed W)
+    bool pack_w;             // W's rows are copied to ldx elements each
+    size_t ldz;              // elements of a row of the logits' codes / of the gradient in the logits
+    int groups;
+    bool small;              // blocks of 64 rows
+    int dx_splits, dw_splits;
+    bool dw_parts;           // dW through fp32 parts
+    size_t list, count, xc, wp, gmax, gsum, gsum2, gstep, codes, dx_part, dx_stride, dw_part, dw_stride, total;
+};
+
+Plan plan_of(const VocabArgs &a, bool grads)
+{
+    Plan p{};
+    const int cus = 256;     // of an MI355X; the workspace has to be the same on a machine without one
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round256(bytes);
+        return here;
+    };
+    p.list = take((size_t)a.rows * sizeof(int));
+    p.count = take(sizeof(int));
+    if (a.bf16) {
+        // 4.3 GB of codes at most, and as many rows as fill the chip several times over
+        long cap = ((long)1 << 31) / a.vocab / 256 * 256;
+        cap = cap > 8192 ? 8192 : cap < 256 ? 256 : cap;
+        p.cap = (int)(a.rows < cap ? a.rows : cap);
+        p.chunks = (a.rows + p.cap - 1) / p.cap;
+        p.rows_held = (int)round_up(p.cap, 256);
+        p.ldx = (int)round_up(a.d, pipe::BKS);
+        p.pack_w = p.ldx != a.d;
+        p.groups = (a.vocab + 63) / 64;
+        p.ldz = (size_t)p.groups * 64;
+        p.small = p.cap <= 64;
+        p.xc = take((size_t)p.rows_held * p.ldx * 2);
+        if (p.pack_w) p.wp = take((size_t)a.vocab * p.ldx * 2);
+        p.gmax = take((size_t)p.cap * p.groups * sizeof(float));
+        p.gsum = take((size_t)p.cap * p.groups * sizeof(float));
+        if (a.ntop && a.tau != 1.f) p.gsum2 = take((size_t)p.cap * p.groups * sizeof(float));
+        if (grads) {
+            p.gstep = take((size_t)p.cap * p.groups * sizeof(float));
+            p.codes = take((size_t)p.rows_held * p.ldz * 2);
+            const int stages = (a.vocab + pipe::BKS - 1) / pipe::BKS, row_blocks = (p.cap + (p.small ? 63 : 255)) / (p.small ? 64 : 256);
+            const long dx_blocks = (long)row_blocks * ((a.d + 255) / 256);
+            // parts as even rounds over the CUs, of at least 16 stages each
+            p.dx_splits = (int)(dx_blocks >= cus ? 1 : cus / dx_blocks);
+            if (p.dx_splits > stages / 16) p.dx_splits = stages / 16 > 0 ? stages / 16 : 1;
+            p.dx_stride = (size_t)p.cap * p.ldx;
+            p.dx_part = take(p.dx_stride * p.dx_splits * sizeof(float));
+            const long dw_blocks = (long)((a.vocab + 255) / 256) * ((a.d + 255) / 256);
+            const int row_stages = (p.cap + pipe::BKS - 1) / pipe::BKS;
+            p.dw_splits = (int)(dw_blocks >= cus ? 1 : cus / dw_blocks);
+            if (p.dw_splits > row_stages / 8) p.dw_splits = row_stages / 8 > 0 ? row_stages / 8 : 1;
+            p.dw_parts = p.chunks > 1 || p.dw_splits > 1 || a.d % 8 != 0;
+            p.dw_stride = (size_t)a.vocab * p.ldx;
+            if (p.dw_parts) p.dw_part = take(p.dw_stride * p.dw_splits * sizeof(float));
+        }
+    } else {
+        long cap = ((long)1 << 28) / a.vocab;                // 1 GiB of logits
+        cap = cap < 64 ? 64 : cap;
+        p.cap = (int)(a.rows < cap ? a.rows : cap);
+        p.chunks = (a.rows + p.cap - 1) / p.cap;
+        p.ldx = a.d;
+        p.ldz = a.vocab;
+        p.xc = take((size_t)p.cap * a.d * 4);
+        p.codes = take((size_t)p.cap * p.ldz * 4);
+        if (grads) p.dx_part = take((size_t)p.cap * a.d * 4);
+    }
+    p.total = at;
+    return p;
+}
+
+#define LM_TRY(call)                                   \
+    do {                                               \
+        const hipError_t e_ = (call);                  \
+        if (e_ != hipSuccess) return e_;               \
+    } while (0)
+
+hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, const Plan &p, char *base, const RowList &rl, hipStream_t s)
+{
+    bf16_t *xc = (bf16_t *)(base + p.xc), *codes = g ? (bf16_t *)(base + p.codes) : nullptr;
+    const bf16_t *W = (const bf16_t *)a.W;
+    if (p.pack_w) {
+        LM_TRY(launch_pad_rows(a.W, a.vocab, a.d, p.ldx, base + p.wp, s));
+        W = (const bf16_t *)(base + p.wp);
+    }
+    const bool two = p.gsum2 != 0 && a.label;
+    const float inv_tau = 1.f / a.tau;
+    for (int ch = 0; ch < p.chunks; ++ch) {
+        const int first = ch * p.cap;
+        LM_TRY(launch_gather_rows(true, a.X, rl, first, p.rows_held, a.d, p.ldx, xc, s));
+        const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
+        const LogitsOut lo{(float *)(base + p.gmax), (float *)(base + p.gsum), two ? (float *)(base + p.gsum2) : nullptr,
+                           (float *)(base + p.gstep), p.groups, codes, (long)p.ldz, a.label ? 1.f : inv_tau, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f)};
+        LM_TRY((p.small ? launch_logits<64, 1, 4, 7>(logits, rl.count, first, p.cap, a.vocab, lo, two, s)
+                        : launch_logits<256, 2, 4, 4>(logits, rl.count, first, p.cap, a.vocab, lo, two, s)));
+        const VocabChunk c{first, p.cap, codes, p.ldz, lo.group_max, lo.group_sum, lo.group_sum_tau, lo.group_step, p.groups, xc, p.ldx};
+        LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
+        if (g && g->dX) {
+            const Operands o{codes, W, (long)p.ldz, p.ldx, p.rows_held, p.ldx, a.vocab};
+            float *part = (float *)(base + p.dx_part);
+            LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.dx_splits, part, p.dx_stride, p.ldx, s)
+                            : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.dx_splits, part, p.dx_stride, p.ldx, s)));
+            LM_TRY(launch_finish_dx(true, part, p.dx_splits, p.dx_stride, p.ldx, rl, first, p.cap, a.d, g->dX, s));
+        }
+        if (g && g->dW) {
+            const Operands o{codes, xc, (long)p.ldz, p.ldx, (int)p.ldz, p.ldx, 0};
+            float *part = (float *)(base + p.dw_part);
+            if (!p.dw_parts) LM_TRY((launch_dw<bf16_t, false>(o, rl.count, first, p.cap, a.vocab, 1, (bf16_t *)g->dW, 0, a.d, s)));
+            else if (ch == 0) LM_TRY((launch_dw<float, false>(o, rl.count, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+            else LM_TRY((launch_dw<float, true>(o, rl.count, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+        }
+    }
+    if (g && g->dW && p.dw_parts)
+        LM_TRY(launch_finish_dw(true, (const float *)(base + p.dw_part), p.dw_splits, p.dw_stride, p.ldx, a.vocab, a.d, g->dW, s));
+    return hipSuccess;
+}
+
+hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, const Plan &p, char *base, const RowList &rl, hipStream_t s)
+{
+    float *xc = (float *)(base + p.xc), *z = (float *)(base + p.codes), *dx = (float *)(base + p.dx_part);
+    for (int ch = 0; ch < p.chunks; ++ch) {
+        const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
+        LM_TRY(launch_gather_rows(false, a.X, rl, first, cap, a.d, a.d, xc, s));
+        LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.vocab, a.d, 1, false, false, false, false}, xc, a.W, z, s));
+        const VocabChunk c{first, cap, z, p.ldz, nullptr, nullptr, nullptr, nullptr, 0, xc, a.d};
+        LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
+        if (g && g->dX) {
+            LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.d, a.vocab, 1, false, true, false, false}, z, a.W, dx, s));
+            LM_TRY(launch_finish_dx(false, dx, 1, 0, a.d, rl, first, cap, a.d, g->dX, s));
+        }
+        if (g && g->dW) LM_TRY(launch_plane_gemm(0, GemmDesc{a.vocab, a.d, cap, 1, true, true, true, ch > 0}, z, xc, g->dW, s));
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t vocab_workspace_bytes(const VocabArgs &a, bool grads) { return a.rows == 0 ? 0 : plan_of(a, grads).total; }
+
+hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, void *ws, hipStream_t s)
+{
+    const Plan p = plan_of(a, g != nullptr);
+    char *base = (char *)ws;
+    const RowList rl{(int *)(base + p.list), (int *)(base + p.count)};
+    LM_TRY(launch_select_rows(a, rl, s));
+    LM_TRY(launch_zero_others(a, g ? g->dX : nullptr, label_loss, top_loss, s));
+    return a.bf16 ? loss_bf16(a, g, label_loss, top_loss, p, base, rl, s) : loss_f32(a, g, label_loss, top_loss, p, base, rl, s);
+}
+
+}  // namespace lm
+}  // namespace stl

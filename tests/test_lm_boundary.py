@@ -52,3 +52,47 @@ def test_residual_arguments_that_are_refused():
     refused(3, bwd, *grads(ws_bytes=need - 1))
     refused(1, bwd, *grads(ws=FAKE + 8))
     refused(2, bwd, *grads(flags=0x1))
+
+
+@pytest.mark.parametrize("kw,status", [(dict(rows=-1), 1), (dict(d=0), 1), (dict(vocab=0), 1), (dict(ntop=-1), 1), (dict(ntop=1025), 1), (dict(d=1048577), 1),
+                                       (dict(vocab=4194305), 1), (dict(rows=stl.STL_MAX_DIM + 1), 1), (dict(dtype=9), 2), (dict(ntop=4, temperature=0.2), 1),
+                                       (dict(ntop=4, temperature=17.0), 1), (dict(ntop=4, temperature=float("nan")), 1)])
+def test_vocabulary_problems_that_are_refused(kw, status):
+    prob = stl.VocabProblem(**{**dict(rows=16, d=64, vocab=100), **kw})
+    assert stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_BACKWARD) == 0
+    refused(status, stl.stl_vocab_loss_forward, prob, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, 1 << 50)
+    refused(status, stl.stl_vocab_loss_backward, prob, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, None, FAKE, FAKE, FAKE, 1 << 50)
+
+
+def test_vocabulary_arguments_that_are_refused():
+    prob, taught = stl.VocabProblem(16, 64, 100), stl.VocabProblem(16, 64, 100, 4)
+    fwd, bwd = stl.stl_vocab_loss_forward, stl.stl_vocab_loss_backward
+    need, need_b = (stl.stl_vocab_loss_workspace_bytes(prob, op) for op in (stl.STL_OP_FORWARD, stl.STL_OP_BACKWARD))
+    assert 0 < need < need_b
+    assert stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_ENCODE_WEIGHT) == 0
+
+    def f(prob=prob, **kw):
+        a = dict(X=FAKE, W=FAKE, label=FAKE, top_id=None, top_logit=None, label_loss=FAKE, top_loss=None, ws=FAKE, ws_bytes=need)
+        a.update(kw)
+        return (prob, *a.values())
+
+    for kw in (dict(X=None), dict(W=None), dict(label=None, label_loss=None), dict(label=None), dict(label_loss=None), dict(top_loss=FAKE), dict(W=FAKE + 2),
+               dict(label=FAKE + 8), dict(prob=taught, top_logit=FAKE), dict(prob=taught, top_id=FAKE), dict(ws=FAKE + 4, ws_bytes=1 << 40)):
+        refused(1, fwd, *f(**kw))
+    refused(3, fwd, *f(ws=None))
+    refused(3, fwd, *f(ws_bytes=need - 1))
+
+    def b(prob=prob, **kw):
+        a = dict(X=FAKE, W=FAKE, label=FAKE, top_id=None, top_logit=None, dlabel=FAKE, dtop=None, label_loss=None, top_loss=None, dX=FAKE, dW=FAKE, ws=FAKE,
+                 ws_bytes=need_b)
+        a.update(kw)
+        return (prob, *a.values())
+
+    for kw in (dict(dX=None, dW=None), dict(dlabel=None), dict(dlabel=None, dtop=FAKE), dict(dX=FAKE + 8), dict(dlabel=FAKE + 4), dict(X=None)):
+        refused(1, bwd, *b(**kw))
+    refused(3, bwd, *b(ws_bytes=need_b - 1))
+
+
+def test_vocabulary_workspace_is_bounded_in_the_rows():
+    sizes = [stl.stl_vocab_loss_workspace_bytes(stl.VocabProblem(rows, 4096, 131072), stl.STL_OP_BACKWARD) for rows in (8192, 16384, 1 << 20)]
+    assert sizes[0] < 4 << 30 and sizes[2] - sizes[1] < 8 << 20 and sizes[2] < 6 << 30
