@@ -5,29 +5,34 @@
 namespace stl {
 namespace lm {
 
-// Sum over the 64 lanes of a wavefront, in every lane: four DPP adds leave each row of 16 lanes with its sum, the four rows are added from
-// scalar registers.
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v)
+// Sum (maximum) over the 64 lanes of a wavefront: four DPP steps leave each row of 16 lanes with its own in every lane, two more take rows 0 and 2, then
+// row 1, into the rows above; the last lane has it all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float v, float old)
 {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(old), (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
 }
-__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
-__device__ __forceinline__ float wave_sum(float v)
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); }
+__device__ __forceinline__ float wave_sum_last(float v)          // in lane 63
 {
-    v += dpp<0xb1>(v);       // quad_perm 1 0 3 2
-    v += dpp<0x4e>(v);       // quad_perm 2 3 0 1
-    v += dpp<0x141>(v);      // row_half_mirror
-    v += dpp<0x140>(v);      // row_mirror
-    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+    v += dpp<0xb1, 0xf>(v, 0.f);       // quad_perm 1 0 3 2
+    v += dpp<0x4e, 0xf>(v, 0.f);       // quad_perm 2 3 0 1
+    v += dpp<0x141, 0xf>(v, 0.f);      // row_half_mirror
+    v += dpp<0x140, 0xf>(v, 0.f);      // row_mirror
+    v += dpp<0x142, 0xa>(v, 0.f);      // row_bcast 15
+    v += dpp<0x143, 0xc>(v, 0.f);      // row_bcast 31
+    return v;
 }
+__device__ __forceinline__ float wave_sum(float v) { return last_lane(wave_sum_last(v)); }
 __device__ __forceinline__ float wave_max(float v)
 {
-    v = fmaxf(v, dpp<0xb1>(v));
-    v = fmaxf(v, dpp<0x4e>(v));
-    v = fmaxf(v, dpp<0x141>(v));
-    v = fmaxf(v, dpp<0x140>(v));
-    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+    v = fmaxf(v, dpp<0xb1, 0xf>(v, v));
+    v = fmaxf(v, dpp<0x4e, 0xf>(v, v));
+    v = fmaxf(v, dpp<0x141, 0xf>(v, v));
+    v = fmaxf(v, dpp<0x140, 0xf>(v, v));
+    v = fmaxf(v, dpp<0x142, 0xa>(v, v));
+    v = fmaxf(v, dpp<0x143, 0xc>(v, v));
+    return last_lane(v);
 }
 
 // Eight consecutive elements of a row, held as loaded; `left` of them (or fewer) are in the row, the others read as `fill` bits.  Rows start at
@@ -52,6 +57,8 @@ template <> struct Chunk<bf16_t> {
         }
     }
     __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); }
+    // an opaque value from here on: what is computed from it is not kept over the turns of a loop
+    __device__ __forceinline__ void opaque() { asm volatile("" : "+v"(v)); }
     static __device__ __forceinline__ void store(bf16_t *p, int left, const float *f)
     {
         const u32x4_t w = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
@@ -80,6 +87,7 @@ template <> struct Chunk<float> {
         }
     }
     __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+    __device__ __forceinline__ void opaque() {}
     static __device__ __forceinline__ void store(float *p, int left, const float *f)
     {
         if (left >= 8) {

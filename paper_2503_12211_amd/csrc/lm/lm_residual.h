@@ -22,13 +22,16 @@ constexpr int kSums = 5;
 template <int TPR, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float *red, int &half, int waves)
 {
+    if constexpr (TPR == 64) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
-    if constexpr (TPR > 64) {
+        for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
+    } else {
         constexpr int WPR = TPR / 64;
         const int wave = (int)threadIdx.x >> 6;
         float *mine = red + half * waves * kSums;
-        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = wave_sum_last(v[k]);
+        if ((threadIdx.x & 63) == 63) {
 #pragma unroll
             for (int k = 0; k < K; ++k) mine[wave * kSums + k] = v[k];
         }
@@ -45,10 +48,13 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float *red, int &half, i
     }
 }
 
+// fp32 storage takes a mean twice, the second time of the centred row (its sum comes with the squares'): the rounding of the first would otherwise be
+// the whole of an element that is close to the mean.
 template <typename T, int TPR, int NV, bool CENTER>
 __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_forward_kernel(const ResidualArgs a, void *Xout_, void *Z_)
 {
     constexpr int THREADS = TPR < 512 ? 512 : TPR, RL = THREADS / TPR, WAVES = THREADS / 64;
+    constexpr bool TWICE = CENTER && sizeof(T) == 4;
     __shared__ float red[2 * WAVES * kSums];
     int half = 0;
     const int t = (int)threadIdx.x % TPR, n = a.n;
@@ -112,16 +118,16 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_forward_kernel
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[c][e] = e < left[c] ? v[c][e] - mean : 0.f;
             }
-            float s[CENTER ? 2 : 1] = {};
+            float s[TWICE ? 2 : 1] = {};
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     s[0] = fmaf(v[c][e], v[c][e], s[0]);
-                    if constexpr (CENTER) s[1] += v[c][e];
+                    if constexpr (TWICE) s[1] += v[c][e];
                 }
             row_sums<TPR>(s, red, half, WAVES);
-            if constexpr (CENTER) {
+            if constexpr (TWICE) {
                 const float rest = s[1] * inv_n;
 #pragma unroll
                 for (int c = 0; c < NV; ++c)
@@ -154,23 +160,27 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_forward_kernel
     }
 }
 
-// A mean is taken twice, the second time of the centred row (its sum comes with the squares'): the rounding of the first would otherwise be
-// the whole of an element that is close to the mean.
-//
-// Gradients.  The rows are dealt in items: item i holds `chunk` rows (or what is left) of group i / pieces, all of which share a row of the gate, so
-// that the gate's sum over an item is one partial; the weights' and offsets' sums run over all items of a workgroup.  Partials are added
-// in a fixed order by residual_sums_kernel: results are the same from run to run.
+// Gradients.  The rows are dealt in items: item i holds `chunk` rows (or what is left) of group i / pieces, all of which share a row of the gate;
+// the weights' and offsets' sums run over all items of a workgroup.  Partials are added in a fixed order by residual_sums_kernel: results are the same
+// from run to run.
 //   d = dXout + r (t - [mean t] - x^ mean(t x^)),  t = dZ w_pre,  x^ = norm(Xout);   du = scale g d;   dH likewise from th = du w_post.
+// What bounds it beside memory is the vector unit (some 30 operations an element and row on two wavefronts a SIMD), so what a column's gate and
+// weights multiply is multiplied once an item: with A = sum h^ d and B = sum d over an item's rows,
+//   dgate = scale (w_post A + b_post B),   dw_post = scale sum over items g A,   db_post = scale sum over items g B.
+// Where every row has its own gate (gate_rows), A and B are summed with it and the row's gate gradient is written as it is found.
 struct ResidualItems {
     int groups, pieces, chunk, per;          // per: rows of a group
-    bool gate_rows;                          // every row has its own row of the gate: its gradient is written as it is found
+    bool gate_rows;
     float *gate_part, *vec_part;             // groups x pieces x n;  workgroups x 4 x n (dw_pre, db_pre, dw_post, db_post)
 };
+// (workgroups of 256 threads, two a CU: 94 us for 8192 x 4096 bf16 instead of 88)
+constexpr int kBackThreads = 512;
 
 template <typename T, int TPR, int NV, bool CENTER, bool OFFSETS>
-__global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kernel(const ResidualArgs a, const ResidualGrads o, const ResidualItems it)
+__global__ __launch_bounds__(TPR < kBackThreads ? kBackThreads : TPR) void residual_backward_kernel(const ResidualArgs a, const ResidualGrads o, const ResidualItems it)
 {
-    constexpr int THREADS = TPR < 512 ? 512 : TPR, RL = THREADS / TPR, WAVES = THREADS / 64;
+    constexpr int THREADS = TPR < kBackThreads ? kBackThreads : TPR, RL = THREADS / TPR, WAVES = THREADS / 64;
+    constexpr bool TWICE = CENTER && sizeof(T) == 4;
     __shared__ float red[2 * WAVES * kSums];
     __shared__ f32x4_t fold[RL > 1 ? THREADS * 2 : 1];
     int half = 0;
@@ -180,22 +190,22 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
     T *dX = (T *)o.dX, *dH = (T *)o.dH;
     const bool need_h = a.post || o.dgate;
     int col[NV], left[NV];
-    Chunk<T> wo[NV], bo[NV], wp[NV], g[NV];
-    float s_wp[NV][8], s_wo[NV][8], s_g[NV][8], s_bp[OFFSETS ? NV : 1][8], s_bo[OFFSETS ? NV : 1][8];
+    Chunk<T> wo[NV], wp[NV], g[NV];
+    float s_wp[NV][8], s_wo[NV][8], s_a[NV][8];              // sums over rows: dZ x^, g A over items, A
+    float s_bp[OFFSETS ? NV : 1][8], s_bo[OFFSETS ? NV : 1][8], s_b[OFFSETS ? NV : 1][8];
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         col[c] = (c * TPR + t) * 8;
         left[c] = n - col[c];
-        wo[c].fill(1.f), bo[c].fill(0.f), wp[c].fill(1.f), g[c].fill(1.f);
+        wo[c].fill(1.f), wp[c].fill(1.f), g[c].fill(1.f);
         if (left[c] > 0) {
             if (a.w_post) wo[c].load((const T *)a.w_post + col[c], left[c]);
-            if (a.b_post) bo[c].load((const T *)a.b_post + col[c], left[c]);
             if (a.w_pre) wp[c].load((const T *)a.w_pre + col[c], left[c]);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s_wp[c][e] = s_wo[c][e] = s_g[c][e] = 0.f;
-            if constexpr (OFFSETS) s_bp[c][e] = s_bo[c][e] = 0.f;
+            s_wp[c][e] = s_wo[c][e] = s_a[c][e] = 0.f;
+            if constexpr (OFFSETS) s_bp[c][e] = s_bo[c][e] = s_b[c][e] = 0.f;
         }
     }
     // a sum over the rows of the workgroup's row lanes, written as the row `dst` of a partial
@@ -219,17 +229,9 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
             }
         }
     };
-    const int items = it.groups * it.pieces;
-    for (int i = (int)blockIdx.x; i < items; i += (int)gridDim.x) {
-        const int group = i / it.pieces, r0 = group * it.per + (i - group * it.pieces) * it.chunk;
-        int r1 = r0 + it.chunk;
-        if (r1 > (group + 1) * it.per) r1 = (group + 1) * it.per;
-        if (r1 > a.rows) r1 = a.rows;
-        if (gate && !it.gate_rows) {
-#pragma unroll
-            for (int c = 0; c < NV; ++c)
-                if (left[c] > 0) g[c].load(gate + (size_t)group * n + col[c], left[c]);
-        }
+    // the rows r0 + lane_row, + RL, ... below r1; GATES: each with its own row of the gate
+    auto rows = [&](const int r0, const int r1, auto gates_c) {
+        constexpr bool GATES = decltype(gates_c)::value;
         Chunk<T> xr[NV], hr[NV], dr[NV], zr[NV];
         auto fetch = [&](int r) {
 #pragma unroll
@@ -249,19 +251,22 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
         int row = r0 + lane_row;
         fetch(row);
         for (int first = r0; first < r1; first += RL, row += RL) {
-            float x[NV][8], h[NV][8], d[NV][8], tz[NV][8], z[NV][8];
-            if (gate && it.gate_rows && row < r1) {
+            float x[NV][8], h[NV][8], tz[NV][8];
+            Chunk<T> d_now[NV], z_now[NV];
+            if (GATES && row < r1) {
 #pragma unroll
                 for (int c = 0; c < NV; ++c)
                     if (left[c] > 0) g[c].load(gate + (size_t)row * n + col[c], left[c]);
             }
 #pragma unroll
-            for (int c = 0; c < NV; ++c)
+            for (int c = 0; c < NV; ++c) {
+                d_now[c] = dr[c], z_now[c] = zr[c];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[c][e] = xr[c].get(e), h[c][e] = hr[c].get(e), d[c][e] = dr[c].get(e), z[c][e] = zr[c].get(e);
-                    tz[c][e] = z[c][e] * wp[c].get(e);
+                    x[c][e] = xr[c].get(e), h[c][e] = hr[c].get(e);
+                    tz[c][e] = zr[c].get(e) * wp[c].get(e);
                 }
+            }
             fetch(row + RL);
             float mean_t = 0.f;
             if constexpr (CENTER) {
@@ -281,7 +286,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
                         h[c][e] = e < left[c] ? h[c][e] - mh : 0.f;
                     }
             }
-            float s[CENTER ? 5 : 3] = {};
+            float s[TWICE ? 5 : 3] = {};
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
@@ -289,10 +294,10 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
                     s[0] = fmaf(x[c][e], x[c][e], s[0]);
                     s[1] = fmaf(h[c][e], h[c][e], s[1]);
                     s[2] = fmaf(tz[c][e], x[c][e], s[2]);
-                    if constexpr (CENTER) s[3] += x[c][e], s[4] += h[c][e];
+                    if constexpr (TWICE) s[3] += x[c][e], s[4] += h[c][e];
                 }
             row_sums<TPR>(s, red, half, WAVES);
-            if constexpr (CENTER) {
+            if constexpr (TWICE) {
                 const float rest_x = s[3] * inv_n, rest_h = a.post ? s[4] * inv_n : 0.f;
 #pragma unroll
                 for (int c = 0; c < NV; ++c)
@@ -305,48 +310,56 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
                 s[1] = fmaf(-rest_h, s[4], s[1]);
                 s[2] = fmaf(-rest_x * (float)n, mean_t, s[2]);
             }
-            const float rx = rsqrtf(s[0] * inv_n + a.eps), rh = a.post ? rsqrtf(s[1] * inv_n + a.eps) : 1.f, cx = rx * rx * s[2] * inv_n;
-            float q[2] = {0.f, 0.f};
+            const float rx = a.pre ? rsqrtf(s[0] * inv_n + a.eps) : 0.f, rh = a.post ? rsqrtf(s[1] * inv_n + a.eps) : 1.f, cx = -rx * rx * s[2] * inv_n;
+            float q[2] = {0.f, 0.f}, d[NV][8];
 #pragma unroll
-            for (int c = 0; c < NV; ++c)
+            for (int c = 0; c < NV; ++c) {
+                z_now[c].opaque();
+                d_now[c].opaque();
+                float gate_grad[GATES ? 8 : 1];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float sg = a.scale * g[c].get(e), hh = h[c][e] * rh;
-                    if (a.pre) d[c][e] = fmaf(rx, tz[c][e] - mean_t - x[c][e] * cx, d[c][e]);
+                    const float z = z_now[c].get(e), xh = x[c][e] * rx, hh = h[c][e] * rh, ge = g[c].get(e);
+                    d[c][e] = fmaf(rx, CENTER ? tz[c][e] - mean_t : tz[c][e], fmaf(xh, cx, d_now[c].get(e)));
                     if (CENTER && e >= left[c]) d[c][e] = 0.f;
-                    s_wp[c][e] = fmaf(z[c][e], x[c][e] * rx, s_wp[c][e]);
-                    const float du = sg * d[c][e], u = fmaf(hh, wo[c].get(e), bo[c].get(e));
-                    s_wo[c][e] = fmaf(du, hh, s_wo[c][e]);
-                    if constexpr (OFFSETS) s_bp[c][e] += z[c][e], s_bo[c][e] += du;
-                    // the gate's gradient of the row is kept where x was
-                    x[c][e] = a.scale * u * d[c][e];
-                    s_g[c][e] += x[c][e];
+                    s_wp[c][e] = fmaf(z, xh, s_wp[c][e]);
+                    const float du = ge * d[c][e];
+                    s_a[c][e] = fmaf(hh, GATES ? du : d[c][e], s_a[c][e]);
+                    if constexpr (OFFSETS) s_bp[c][e] += z, s_b[c][e] += GATES ? du : d[c][e];
+                    if constexpr (GATES) gate_grad[e] = hh * wo[c].get(e) * d[c][e];
                     tz[c][e] = du * wo[c].get(e);
-                    q[0] += tz[c][e];
+                    if constexpr (CENTER) q[0] += tz[c][e];
                     q[1] = fmaf(tz[c][e], h[c][e], q[1]);
                 }
+                if constexpr (GATES) {
+                    if (o.dgate && row < r1 && left[c] > 0) {
+                        const size_t at = (size_t)row * n + col[c];
+                        Chunk<T> bo;
+                        Chunk<float> old;
+                        bo.fill(0.f), old.fill(0.f);
+                        if (a.b_post) bo.load((const T *)a.b_post + col[c], left[c]);
+                        if (o.accumulate) old.load(o.dgate + at, left[c]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) gate_grad[e] = fmaf(a.scale, fmaf(bo.get(e), d[c][e], gate_grad[e]), old.get(e));
+                        Chunk<float>::store(o.dgate + at, left[c], gate_grad);
+                    }
+                }
+            }
+            float out = a.scale, mean_th = 0.f, ch = 0.f;
             if (a.post) {
                 row_sums<TPR>(q, red, half, WAVES);
-                const float mean_th = CENTER ? q[0] * inv_n : 0.f, ch = rh * rh * q[1] * inv_n;
-#pragma unroll
-                for (int c = 0; c < NV; ++c)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) tz[c][e] = rh * (tz[c][e] - mean_th - h[c][e] * ch);
+                mean_th = CENTER ? q[0] * inv_n : 0.f, ch = -rh * rh * q[1] * inv_n;
+                out *= rh;
             }
             if (row < r1) {
 #pragma unroll
                 for (int c = 0; c < NV; ++c) {
                     if (left[c] <= 0) continue;
                     const size_t at = (size_t)row * n + col[c];
-                    if (dH) Chunk<T>::store(dH + at, left[c], tz[c]);
-                    if (o.dgate && it.gate_rows) {
-                        if (o.accumulate) {
-                            Chunk<float> old;
-                            old.load(o.dgate + at, left[c]);
+                    if (dH) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) x[c][e] += old.get(e);
-                        }
-                        Chunk<float>::store(o.dgate + at, left[c], x[c]);
+                        for (int e = 0; e < 8; ++e) tz[c][e] = out * fmaf(h[c][e], ch, CENTER ? tz[c][e] - mean_th : tz[c][e]);
+                        Chunk<T>::store(dH + at, left[c], tz[c]);
                     }
                     if (dX) {
 #pragma unroll
@@ -356,14 +369,54 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void residual_backward_kerne
                 }
             }
         }
-        if (o.dgate && !it.gate_rows) {
-            flush(s_g, it.gate_part + (size_t)i * n);
+    };
+    const int items = it.groups * it.pieces;
+    for (int i = (int)blockIdx.x; i < items; i += (int)gridDim.x) {
+        const int group = i / it.pieces, r0 = group * it.per + (i - group * it.pieces) * it.chunk;
+        int r1 = r0 + it.chunk;
+        if (r1 > (group + 1) * it.per) r1 = (group + 1) * it.per;
+        if (r1 > a.rows) r1 = a.rows;
+        if (it.gate_rows) {
+            rows(r0, r1, std::true_type{});
+        } else {
+            if (gate) {
 #pragma unroll
-            for (int c = 0; c < NV; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s_g[c][e] = 0.f;
+                for (int c = 0; c < NV; ++c)
+                    if (left[c] > 0) g[c].load(gate + (size_t)group * n + col[c], left[c]);
+            }
+            rows(r0, r1, std::false_type{});
         }
+        // the item's sums: into the workgroup's, and the gate's partial
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            Chunk<T> bo;
+            bo.fill(0.f);
+            if (OFFSETS && a.b_post && left[c] > 0) bo.load((const T *)a.b_post + col[c], left[c]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float mul = it.gate_rows ? 1.f : g[c].get(e);
+                s_wo[c][e] = fmaf(mul, s_a[c][e], s_wo[c][e]);
+                s_a[c][e] = a.scale * s_a[c][e] * wo[c].get(e);
+                if constexpr (OFFSETS) {
+                    s_bo[c][e] = fmaf(mul, s_b[c][e], s_bo[c][e]);
+                    s_a[c][e] = fmaf(a.scale * s_b[c][e], bo.get(e), s_a[c][e]);
+                    s_b[c][e] = 0.f;
+                }
+            }
+        }
+        if (o.dgate && !it.gate_rows) flush(s_a, it.gate_part + (size_t)i * n);
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s_a[c][e] = 0.f;
     }
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s_wo[c][e] *= a.scale;
+            if constexpr (OFFSETS) s_bo[c][e] *= a.scale;
+        }
     float *mine = it.vec_part + (size_t)blockIdx.x * 4 * n;
     if (o.dw_pre) flush(s_wp, mine);
     if (o.dw_post) flush(s_wo, mine + 2 * (size_t)n);
@@ -407,12 +460,12 @@ template <typename T>
 hipError_t residual_backward(const ResidualArgs &a, const ResidualGrads &g, const ResidualItems &it, int grid, hipStream_t s)
 {
     return residual_shape(a.n, [&](auto tpr_c, auto nv_c) {
-        constexpr int TPR = decltype(tpr_c)::value, NV = decltype(nv_c)::value, THREADS = TPR < 512 ? 512 : TPR;
+        constexpr int TPR = decltype(tpr_c)::value, NV = decltype(nv_c)::value, THREADS = TPR < kBackThreads ? kBackThreads : TPR;
         auto run = [&](auto kern) {
             hipLaunchKernelGGL(kern, dim3(grid), dim3(THREADS), 0, s, a, g, it);
             return hipGetLastError();
         };
-        const bool offsets = g.db_pre || g.db_post;
+        const bool offsets = g.db_pre || g.db_post || a.b_post;
         if (a.center) return offsets ? run(residual_backward_kernel<T, TPR, NV, true, true>) : run(residual_backward_kernel<T, TPR, NV, true, false>);
         return offsets ? run(residual_backward_kernel<T, TPR, NV, false, true>) : run(residual_backward_kernel<T, TPR, NV, false, false>);
     });

@@ -185,18 +185,22 @@ inline float rsqrtf(float x) { return 1.0f / sqrtf(x); }
 #define __builtin_amdgcn_rcpf(x) (1.0f / (x))
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
 inline float __shfl_xor(float v, int m) { return emu::from_lane(v, [&](int l) { return l ^ m; }); }
+inline int __shfl_up(int v, int n) { return emu::from_lane(v, [&](int l) { return l < n ? l : l - n; }); }
 inline int __builtin_amdgcn_readlane_emu(int v, int from) { return emu::from_lane(v, [&](int) { return from; }); }
 #define __builtin_amdgcn_readlane(v, l) __builtin_amdgcn_readlane_emu(v, l)
-inline int emu_dpp(int v, int ctrl)
+inline int emu_dpp(int old, int v, int ctrl, int rows)
 {
-    return emu::from_lane(v, [&](int l) {
+    const int got = emu::from_lane(v, [&](int l) {
         if (ctrl < 0x100) return (l & ~3) | (ctrl >> (2 * (l & 3)) & 3);      // quad_perm
         if (ctrl == 0x141) return (l & ~7) | (7 - (l & 7));                   // row_half_mirror
         if (ctrl == 0x140) return (l & ~15) | (15 - (l & 15));                // row_mirror
+        if (ctrl == 0x142) return l < 16 ? l : (l & ~15) - 1;                 // row_bcast 15
+        if (ctrl == 0x143) return l < 32 ? l : 31;                            // row_bcast 31
         emu::die("a DPP control that is not known here");
     });
+    return rows >> (emu::lane() / 16) & 1 ? got : old;
 }
-#define __builtin_amdgcn_update_dpp(old, v, ctrl, rows, banks, bound) emu_dpp(v, ctrl)
+#define __builtin_amdgcn_update_dpp(old, v, ctrl, rows, banks, bound) emu_dpp(old, v, ctrl, rows)
 typedef __bf16 emu_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float emu_f32x4 __attribute__((ext_vector_type(4)));
 typedef float emu_f32x16 __attribute__((ext_vector_type(16)));
