@@ -51,13 +51,15 @@ size_t vocab_workspace_bytes(const VocabArgs &a, bool grads);
 hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, void *ws, hipStream_t s);
 
 // The rows that have a label or a teacher, in order: list[0 .. count), and count itself, on the device; list has room for `rows`.
+// scale: a factor for the gradient in the logits of bf16 storage, and its reciprocal (dz_scale in lm_vocab_rows.hip).
 struct RowList {
     int *list, *count;
+    float *scale;
 };
-hipError_t launch_select_rows(const VocabArgs &a, RowList rl, hipStream_t s);
-// rows first .. first + cap of the list, side by side with ld elements each (zeros behind a row's end and behind the list's); bf16 storage may be
-// packed (d no multiple of what the products need)
-hipError_t launch_gather_rows(bool bf16, const void *X, RowList rl, int first, int cap, int d, int ld, void *out, hipStream_t s);
+hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s);
+// rows first .. first + cap of the list of X, side by side with ld elements each (zeros behind a row's end and behind the list's).  With the
+// first chunk also: zeros for the rows that are not listed, in dX and the losses (each may be NULL).
+hipError_t launch_arrange_rows(const VocabArgs &a, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss, hipStream_t s);
 // rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
 
@@ -74,12 +76,27 @@ struct VocabChunk {
     int ldx;
 };
 hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
-// dX rows of the list from `parts` sums of cap x ld each
-hipError_t launch_finish_dx(bool bf16, const float *part, int parts, size_t stride, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s);
-// zeros for the rows that are not listed: their rows of dX and their losses (each may be NULL)
-hipError_t launch_zero_others(const VocabArgs &a, void *dX, float *label_loss, float *top_loss, hipStream_t s);
-// out[i][j] = sum over parts of part[p][i][j], rows of ld in the parts and of d in `out`
-hipError_t launch_finish_dw(bool bf16, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s);
+// How the contraction of dX over the vocabulary is cut, on the device, where the rows of the chunk are known: in as many runs of whole stages (16 at
+// least) as give every CU of an MI355X a block.  Part s of `rows` rows lies s * rows * ld floats on.
+struct Splits {
+    int block_rows, tiles_n, stages;
+    __host__ __device__ int of(int rows) const
+    {
+        const int tiles = (rows + block_rows - 1) / block_rows * tiles_n, most = stages / 16 > 0 ? stages / 16 : 1, n = tiles >= 256 ? 1 : 256 / (tiles > 0 ? tiles : 1);
+        return n < most ? n : most;
+    }
+    // rows of all parts together, at most, for up to `cap` rows
+    __host__ long rows(int cap) const
+    {
+        const long full = (long)256 / tiles_n * block_rows, all = (long)cap * (stages / 16 > 0 ? stages / 16 : 1);
+        const long some = full < all ? full : all;
+        return some > cap ? some : cap;
+    }
+};
+// dX rows of the list from the parts
+hipError_t launch_finish_dx(bool bf16, const float *part, Splits sp, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s);
+// out[i][j] = sum over parts of part[p][i][j], rows of ld in the parts and of d in `out`, and 1 / scale
+hipError_t launch_finish_dw(bool bf16, RowList rl, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s);
 
 }  // namespace lm
 }  // namespace stl

@@ -160,10 +160,9 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_logits_kernel(con
 }
 
 // ---- dX and dW -----------------------------------------------------------------------------------------------------------------------
-// dX parts: part s, rows x ldx = dz (columns of split s) W.  The contraction over the vocabulary is cut into `splits` runs of whole stages.
+// dX parts: part s, rows x ldx = dz (columns of split s) W.
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, const int *count, int first, int cap, int d, int splits, float *part,
-                                                                      size_t stride, int ldx)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, const int *count, int first, int cap, int d, Splits sps, float *part, int ldx)
 {
     using namespace pipe;
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
@@ -174,7 +173,8 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
     int rows = *count - first;
     if (rows > cap) rows = cap;
     if (rows <= 0) return;
-    const int tiles_m = (rows + BM - 1) / BM, tiles_n = (d + 255) / 256, per = tiles_m * tiles_n, total = per * splits, stages = (o.Kl + BKS - 1) / BKS;
+    const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
+    const size_t stride = (size_t)rows * ldx;
     R ring;
     ring.init(wave, lane);
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
@@ -211,7 +211,8 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
 
 // dW = dz^T X over the listed rows of a chunk: straight to dW (bf16), or to parts in fp32, added to what is there behind the first chunk.
 template <typename TO, bool ACC>
-__global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *count, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo)
+__global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *count, const float *scale, int first, int cap, int vocab, int splits, TO *out,
+                                                       size_t stride, int ldo)
 {
     using namespace pipe;
     typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
@@ -253,6 +254,12 @@ __global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *co
             [&](typename R::Tile &w) {
                 int el = lane;
                 asm volatile("" : "+v"(el));
+                if constexpr (sizeof(TO) == 2) {
+                    const float factor = scale[1];
+                    static_for<0, R::FM>([&](auto a_c) {
+                        static_for<0, R::FN>([&](auto b_c) { w.acc[decltype(a_c)::value][decltype(b_c)::value] *= factor; });
+                    });
+                }
                 w.template store<TO, ACC, false>(slab, out + sp * stride, bi * 256 + wave / 4 * R::WM, bj * 256 + wave % 4 * R::WN, vocab, ldo, 0, 1 << 30, 1, el);
             });
     }
@@ -287,21 +294,20 @@ static hipError_t launch_logits(const Operands &o, const int *count, int first, 
 }
 
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-static hipError_t launch_dx(const Operands &o, const int *count, int first, int cap, int d, int splits, float *part, size_t stride, int ldx, hipStream_t s)
+static hipError_t launch_dx(const Operands &o, const int *count, int first, int cap, int d, const Splits &sp, float *part, int ldx, hipStream_t s)
 {
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
     static std::atomic<uint64_t> granted{0};
-    return launch_ring(vocab_dx_kernel<BM, WAVES_M, WAVES_N, NS>, granted, R::LDS_BYTES, R::THREADS, (long)((cap + BM - 1) / BM) * ((d + 255) / 256) * splits, s, o,
-                       count, first, cap, d, splits, part, stride, ldx);
+    return launch_ring(vocab_dx_kernel<BM, WAVES_M, WAVES_N, NS>, granted, R::LDS_BYTES, R::THREADS, pipe::cu_count(), s, o, count, first, cap, d, sp, part, ldx);
 }
 
 template <typename TO, bool ACC>
-static hipError_t launch_dw(const Operands &o, const int *count, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
+static hipError_t launch_dw(const Operands &o, const RowList &rl, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
 {
     typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
     static std::atomic<uint64_t> granted{0};
-    return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, (long)((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o, count, first, cap,
-                       vocab, splits, out, stride, ldo);
+    return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, (long)((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o,
+                       (const int *)rl.count, (const float *)rl.scale, first, cap, vocab, splits, out, stride, ldo);
 }
 
 // ---- the whole of a call -----------------------------------------------------------------------------------------------------------------
@@ -320,9 +326,10 @@ struct Plan {
     size_t ldz;              // elements of a row of the logits' codes / of the gradient in the logits
     int groups;
     bool small;              // blocks of 64 rows
-    int dx_splits, dw_splits;
+    Splits dx;
+    int dw_splits;
     bool dw_parts;           // dW through fp32 parts
-    size_t list, count, xc, wp, gmax, gsum, gsum2, gstep, codes, dx_part, dx_stride, dw_part, dw_stride, total;
+    size_t list, count, scale, xc, wp, gmax, gsum, gsum2, gstep, codes, dx_part, dw_part, dw_stride, total;
 };
 
 Plan plan_of(const VocabArgs &a, bool grads)
@@ -337,6 +344,7 @@ Plan plan_of(const VocabArgs &a, bool grads)
     };
     p.list = take((size_t)a.rows * sizeof(int));
     p.count = take(sizeof(int));
+    p.scale = take(2 * sizeof(float));
     if (a.bf16) {
         // 4.3 GB of codes at most, and as many rows as fill the chip several times over
         long cap = ((long)1 << 31) / a.vocab / 256 * 256;
@@ -357,13 +365,8 @@ Plan plan_of(const VocabArgs &a, bool grads)
         if (grads) {
             p.gstep = take((size_t)p.cap * p.groups * sizeof(float));
             p.codes = take((size_t)p.rows_held * p.ldz * 2);
-            const int stages = (a.vocab + pipe::BKS - 1) / pipe::BKS, row_blocks = (p.cap + (p.small ? 63 : 255)) / (p.small ? 64 : 256);
-            const long dx_blocks = (long)row_blocks * ((a.d + 255) / 256);
-            // parts as even rounds over the CUs, of at least 16 stages each
-            p.dx_splits = (int)(dx_blocks >= cus ? 1 : cus / dx_blocks);
-            if (p.dx_splits > stages / 16) p.dx_splits = stages / 16 > 0 ? stages / 16 : 1;
-            p.dx_stride = (size_t)p.cap * p.ldx;
-            p.dx_part = take(p.dx_stride * p.dx_splits * sizeof(float));
+            p.dx = Splits{p.small ? 64 : 256, (a.d + 255) / 256, (a.vocab + pipe::BKS - 1) / pipe::BKS};
+            p.dx_part = take((size_t)p.dx.rows(p.cap) * p.ldx * sizeof(float));
             const long dw_blocks = (long)((a.vocab + 255) / 256) * ((a.d + 255) / 256);
             const int row_stages = (p.cap + pipe::BKS - 1) / pipe::BKS;
             p.dw_splits = (int)(dw_blocks >= cus ? 1 : cus / dw_blocks);
@@ -405,7 +408,7 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
     const float inv_tau = 1.f / a.tau;
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap;
-        LM_TRY(launch_gather_rows(true, a.X, rl, first, p.rows_held, a.d, p.ldx, xc, s));
+        LM_TRY(launch_arrange_rows(a, rl, first, p.rows_held, p.ldx, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
         const LogitsOut lo{(float *)(base + p.gmax), (float *)(base + p.gsum), two ? (float *)(base + p.gsum2) : nullptr,
                            (float *)(base + p.gstep), p.groups, codes, (long)p.ldz, a.label ? 1.f : inv_tau, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f)};
@@ -416,20 +419,20 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
         if (g && g->dX) {
             const Operands o{codes, W, (long)p.ldz, p.ldx, p.rows_held, p.ldx, a.vocab};
             float *part = (float *)(base + p.dx_part);
-            LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.dx_splits, part, p.dx_stride, p.ldx, s)
-                            : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.dx_splits, part, p.dx_stride, p.ldx, s)));
-            LM_TRY(launch_finish_dx(true, part, p.dx_splits, p.dx_stride, p.ldx, rl, first, p.cap, a.d, g->dX, s));
+            LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.dx, part, p.ldx, s)
+                            : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.dx, part, p.ldx, s)));
+            LM_TRY(launch_finish_dx(true, part, p.dx, p.ldx, rl, first, p.cap, a.d, g->dX, s));
         }
         if (g && g->dW) {
             const Operands o{codes, xc, (long)p.ldz, p.ldx, (int)p.ldz, p.ldx, 0};
             float *part = (float *)(base + p.dw_part);
-            if (!p.dw_parts) LM_TRY((launch_dw<bf16_t, false>(o, rl.count, first, p.cap, a.vocab, 1, (bf16_t *)g->dW, 0, a.d, s)));
-            else if (ch == 0) LM_TRY((launch_dw<float, false>(o, rl.count, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
-            else LM_TRY((launch_dw<float, true>(o, rl.count, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+            if (!p.dw_parts) LM_TRY((launch_dw<bf16_t, false>(o, rl, first, p.cap, a.vocab, 1, (bf16_t *)g->dW, 0, a.d, s)));
+            else if (ch == 0) LM_TRY((launch_dw<float, false>(o, rl, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+            else LM_TRY((launch_dw<float, true>(o, rl, first, p.cap, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
         }
     }
     if (g && g->dW && p.dw_parts)
-        LM_TRY(launch_finish_dw(true, (const float *)(base + p.dw_part), p.dw_splits, p.dw_stride, p.ldx, a.vocab, a.d, g->dW, s));
+        LM_TRY(launch_finish_dw(true, rl, (const float *)(base + p.dw_part), p.dw_splits, p.dw_stride, p.ldx, a.vocab, a.d, g->dW, s));
     return hipSuccess;
 }
 
@@ -438,13 +441,13 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
     float *xc = (float *)(base + p.xc), *z = (float *)(base + p.codes), *dx = (float *)(base + p.dx_part);
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
-        LM_TRY(launch_gather_rows(false, a.X, rl, first, cap, a.d, a.d, xc, s));
+        LM_TRY(launch_arrange_rows(a, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.vocab, a.d, 1, false, false, false, false}, xc, a.W, z, s));
         const VocabChunk c{first, cap, z, p.ldz, nullptr, nullptr, nullptr, nullptr, 0, xc, a.d};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.d, a.vocab, 1, false, true, false, false}, z, a.W, dx, s));
-            LM_TRY(launch_finish_dx(false, dx, 1, 0, a.d, rl, first, cap, a.d, g->dX, s));
+            LM_TRY(launch_finish_dx(false, dx, Splits{}, a.d, rl, first, cap, a.d, g->dX, s));
         }
         if (g && g->dW) LM_TRY(launch_plane_gemm(0, GemmDesc{a.vocab, a.d, cap, 1, true, true, true, ch > 0}, z, xc, g->dW, s));
     }
@@ -459,9 +462,8 @@ hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *lab
 {
     const Plan p = plan_of(a, g != nullptr);
     char *base = (char *)ws;
-    const RowList rl{(int *)(base + p.list), (int *)(base + p.count)};
-    LM_TRY(launch_select_rows(a, rl, s));
-    LM_TRY(launch_zero_others(a, g ? g->dX : nullptr, label_loss, top_loss, s));
+    const RowList rl{(int *)(base + p.list), (int *)(base + p.count), (float *)(base + p.scale)};
+    LM_TRY(launch_select_rows(a, g, rl, s));
     return a.bf16 ? loss_bf16(a, g, label_loss, top_loss, p, base, rl, s) : loss_f32(a, g, label_loss, top_loss, p, base, rl, s);
 }
 

@@ -29,66 +29,115 @@ struct Terms {
 };
 static Terms terms_of(const VocabArgs &a) { return Terms{a.label, a.top_id, a.top_logit, a.vocab, a.ntop}; }
 
-// One workgroup: every thread counts a run of neighbouring rows, the counts are added up over the workgroup, and every thread lists its rows.
-__global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, int *list, int *count)
+// dz_scale.  The gradient in the logits is rounded to bf16 on its way into the products.  What it is made of is at most the row's weight, w = |dlabel| +
+// |dtop| / tau, and its largest entries (a label's, -(1 - p) dlabel) are close below; so all rows are multiplied by the factor that takes the
+// largest w to 1.97 times a power of two, where bf16's steps are finest relative to what they hold, and the products' sums by its reciprocal: the
+// rounding of a label's entry falls from up to 2.3e-3 (root mean square, just above a power of two) to 1.15e-3.  A power of two of no
+// matter: the factor lies in (0.98, 1.97].
+__device__ __forceinline__ float dz_scale(float w)
 {
-    __shared__ int sums[1024];
-    const int per = (rows + 1023) / 1024, r0 = (int)threadIdx.x * per, r1 = r0 + per < rows ? r0 + per : rows;
-    int n = 0;
-    for (int r = r0; r < r1; ++r) n += t.any(r);
-    sums[threadIdx.x] = n;
-    __syncthreads();
-    for (int step = 1; step < 1024; step *= 2) {
-        const int v = (int)threadIdx.x >= step ? sums[threadIdx.x - step] : 0;
-        __syncthreads();
-        sums[threadIdx.x] += v;
-        __syncthreads();
-    }
-    int at = sums[threadIdx.x] - n;
-    for (int r = r0; r < r1; ++r)
-        if (t.any(r)) list[at++] = r;
-    if (threadIdx.x == 1023) *count = sums[1023];
+    const uint32_t bits = __float_as_uint(w);
+    const uint32_t e = bits >> 23;
+    if (e == 0 || e >= 254) return 1.f;                      // zero, smaller than is normal, or not finite
+    return 1.96875f / __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
 }
 
-hipError_t launch_select_rows(const VocabArgs &a, RowList rl, hipStream_t s)
+// One workgroup: every thread counts a run of neighbouring rows, the counts are added up over the workgroup, and every thread lists its rows.
+__global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, const float *dlabel, const float *dtop, float inv_tau, int *list, int *count,
+                                                           float *scale)
 {
-    hipLaunchKernelGGL(select_rows_kernel, dim3(1), dim3(1024), 0, s, terms_of(a), a.rows, rl.list, rl.count);
+    __shared__ int sums[16];
+    __shared__ float tops[16];
+    const int per = (rows + 1023) / 1024, r0 = (int)threadIdx.x * per, r1 = r0 + per < rows ? r0 + per : rows, lane = (int)threadIdx.x & 63;
+    int n = 0;
+    float top = 0.f;
+    for (int r = r0; r < r1; ++r) {
+        const bool l = t.labelled(r), q = t.taught(r);
+        n += l || q;
+        top = fmaxf(top, (l && dlabel ? fabsf(dlabel[r]) : 0.f) + (q && dtop ? fabsf(dtop[r]) * inv_tau : 0.f));
+    }
+    int upto = n;                                            // over the lanes up to this one
+    for (int step = 1; step < 64; step *= 2) {
+        const int v = __shfl_up(upto, step);
+        if (lane >= step) upto += v;
+    }
+    top = wave_max(top);
+    if (lane == 63) {
+        sums[threadIdx.x >> 6] = upto;
+        tops[threadIdx.x >> 6] = top;
+    }
+    __syncthreads();
+    int at = upto - n, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < (int)threadIdx.x >> 6) at += sums[w];
+        all += sums[w];
+        top = fmaxf(top, tops[w]);
+    }
+    for (int r = r0; r < r1; ++r)
+        if (t.any(r)) list[at++] = r;
+    if (threadIdx.x == 0) {
+        *count = all;
+        scale[0] = dz_scale(top);
+        scale[1] = 1.f / scale[0];
+    }
+}
+
+hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s)
+{
+    hipLaunchKernelGGL(select_rows_kernel, dim3(1), dim3(1024), 0, s, terms_of(a), a.rows, g ? g->dlabel : nullptr, g ? g->dtop : nullptr, 1.f / a.tau, rl.list,
+                       rl.count, rl.scale);
     return hipGetLastError();
 }
 
 // ---- rows side by side ---------------------------------------------------------------------------------------------------------------
-// a workgroup a row: the row list[first + b] (or, without a list, first + b) of `in`, zeros where there is none and behind its end
+// row `from` of `in` (none: zeros) to row `to` of `out`, zeros behind its end, by a workgroup of 256
 template <typename T>
-__global__ __launch_bounds__(256) void copy_rows_kernel(const T *in, const int *list, const int *count, int first, int d, int ld, T *out)
+__device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, size_t to, int ld)
 {
-    const int r = first + (int)blockIdx.x;
-    const int row = !list ? r : r < *count ? list[r] : -1;
-    T *o = out + (size_t)blockIdx.x * ld;
     for (int c = (int)threadIdx.x * 8; c < ld; c += 2048) {
         Chunk<T> v;
         v.fill(0.f);
-        if (row >= 0 && c < d) v.load(in + (size_t)row * d + c, d - c);
+        if (from >= 0 && c < d) v.load(in + (size_t)from * d + c, d - c);
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = v.get(e);
-        Chunk<T>::store(o + c, ld - c, f);
+        Chunk<T>::store(out + to * ld + c, ld - c, f);
     }
 }
 
-hipError_t launch_gather_rows(bool bf16, const void *X, RowList rl, int first, int cap, int d, int ld, void *out, hipStream_t s)
+// a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed
+template <typename T>
+__global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, const T *X, const int *list, const int *count, int first, int cap, int d, int ld, T *out,
+                                                           int zeros, T *dX, float *label_loss, float *top_loss)
 {
+    const int b = (int)blockIdx.x;
+    if (b < cap) copy_row(X, first + b < *count ? list[first + b] : -1L, d, out, b, ld);
+    if (b < zeros && !t.any(b)) {
+        if (threadIdx.x == 0) {
+            if (label_loss) label_loss[b] = 0.f;
+            if (top_loss) top_loss[b] = 0.f;
+        }
+        if (dX) copy_row(X, -1L, d, dX, b, d);
+    }
+}
+
+hipError_t launch_arrange_rows(const VocabArgs &a, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss, hipStream_t s)
+{
+    const int zeros = first == 0 ? a.rows : 0;
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, (const T *)X, (const int *)rl.list, (const int *)rl.count, first, d, ld, (T *)out);
+        hipLaunchKernelGGL(kern, dim3(cap > zeros ? cap : zeros), dim3(256), 0, s, terms_of(a), (const T *)a.X, (const int *)rl.list, (const int *)rl.count, first,
+                           cap, a.d, ld, (T *)out, zeros, (T *)dX, label_loss, top_loss);
         return hipGetLastError();
     };
-    return bf16 ? run(copy_rows_kernel<bf16_t>, (bf16_t *)nullptr) : run(copy_rows_kernel<float>, (float *)nullptr);
+    return a.bf16 ? run(arrange_rows_kernel<bf16_t>, (bf16_t *)nullptr) : run(arrange_rows_kernel<float>, (float *)nullptr);
 }
+
+__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t *in, int d, bf16_t *out, int ld) { copy_row(in, blockIdx.x, d, out, blockIdx.x, ld); }
 
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s)
 {
-    hipLaunchKernelGGL(copy_rows_kernel<bf16_t>, dim3(rows), dim3(256), 0, s, (const bf16_t *)in, (const int *)nullptr, (const int *)nullptr, 0, d, ld,
-                       (bf16_t *)out);
+    hipLaunchKernelGGL(pad_rows_kernel, dim3(rows), dim3(256), 0, s, (const bf16_t *)in, d, (bf16_t *)out, ld);
     return hipGetLastError();
 }
 
@@ -128,7 +177,7 @@ __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp
 // What bounds it: reading and writing the row, 4 bytes a logit (bf16) or 8.
 template <typename T, bool GRADS>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const VocabGrads g, const T *W, int d, float tau, const int *list, const int *count,
-                                                                 VocabChunk c, float *label_loss, float *top_loss)
+                                                                 const float *scale, VocabChunk c, float *label_loss, float *top_loss)
 {
     constexpr bool BF16 = sizeof(T) == 2;
     __shared__ float red[kRowWaves];
@@ -201,19 +250,32 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
     // the logits of the label and the teacher's entries
     if constexpr (BF16) {
         const bf16_t *x = (const bf16_t *)c.Xc + (size_t)r * c.ldx;
-        for (int j = wave; j <= ntop; j += kRowWaves) {
-            if (ids[j] < 0) continue;
-            const bf16_t *w = (const bf16_t *)W + (size_t)ids[j] * d;
-            float dot = 0.f;
-            for (int e0 = lane * 8; e0 < d; e0 += 512) {
-                Chunk<bf16_t> a, b;
-                a.load(x + e0, d - e0);
-                b.load(w + e0, d - e0);
+        // four entries of a wavefront at a time: the loads of four rows of W in flight (an entry that is none reads the first row)
+        constexpr int AT_ONCE = 4;
+        for (int j0 = wave * AT_ONCE; j0 <= ntop; j0 += kRowWaves * AT_ONCE) {
+            const bf16_t *w[AT_ONCE];
+            float dot[AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot = fmaf(a.get(e), b.get(e), dot);
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int id = j0 + k <= ntop ? ids[j0 + k] : -1;
+                w[k] = (const bf16_t *)W + (size_t)(id < 0 ? 0 : id) * d;
+                dot[k] = 0.f;
             }
-            dot = wave_sum(dot);
-            if (lane == 0) z[j] = dot;
+            for (int e0 = lane * 8; e0 < d; e0 += 512) {
+                Chunk<bf16_t> a, b[AT_ONCE];
+                a.load(x + e0, d - e0);
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) b[k].load(w[k] + e0, d - e0);
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot[k] = fmaf(a.get(e), b[k].get(e), dot[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const float sum = wave_sum(dot[k]);
+                if (lane == 0 && j0 + k <= ntop) z[j0 + k] = sum;
+            }
         }
     } else {
         for (int j = tid; j <= ntop; j += kRowThreads)
@@ -242,7 +304,8 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
         top_loss[row] = 0.f;
     }
     if constexpr (GRADS) {
-        const float cl = labelled && g.dlabel ? g.dlabel[row] : 0.f, ct = taught && g.dtop ? g.dtop[row] * inv_tau : 0.f;
+        const float factor = BF16 ? *scale : 1.f;
+        const float cl = labelled && g.dlabel ? g.dlabel[row] * factor : 0.f, ct = taught && g.dtop ? g.dtop[row] * inv_tau * factor : 0.f;
         if constexpr (BF16) {
             // chunks of eight logits lie in one group of 64
             const float *gstep = c.group_step + (size_t)r * c.groups;
@@ -293,7 +356,7 @@ hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl
         // with gradients of bf16 storage also the rows up to a whole stage of the products' contraction
         const int rows = a.bf16 && g ? (c.cap + 31) / 32 * 32 : c.cap;
         hipLaunchKernelGGL(kern, dim3(rows), dim3(kRowThreads), 0, s, terms_of(a), g ? *g : none, (const T *)a.W, a.d, a.tau, (const int *)rl.list,
-                           (const int *)rl.count, c, label_loss, top_loss);
+                           (const int *)rl.count, (const float *)rl.scale, c, label_loss, top_loss);
         return hipGetLastError();
     };
     if (a.bf16) return g ? run(vocab_rows_kernel<bf16_t, true>, (bf16_t *)nullptr) : run(vocab_rows_kernel<bf16_t, false>, (bf16_t *)nullptr);
@@ -301,74 +364,62 @@ hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl
 }
 
 // ---- the gradients' last stage ---------------------------------------------------------------------------------------------------------
-// a workgroup a row of the chunk: the sum of its parts, rounded once, to where the row came from
+// a row of `out`: the sum of its parts times `factor`, rounded once, by a workgroup of 256
 template <typename T>
-__global__ __launch_bounds__(256) void finish_rows_kernel(const float *part, int parts, size_t stride, int ld, const int *list, const int *count, int first,
-                                                          int d, T *out)
+__device__ __forceinline__ void finish_row(const float *part, int parts, size_t stride, int d, float factor, T *out)
 {
-    const size_t r = blockIdx.x + (size_t)blockIdx.y * 32768;
-    if (list && first + (int)r >= *count) return;
-    const size_t row = list ? (size_t)list[first + r] : r;
     for (int c = (int)threadIdx.x * 8; c < d; c += 2048) {
         float f[8] = {};
         for (int p = 0; p < parts; ++p) {
             Chunk<float> v;
-            v.load(part + p * stride + r * ld + c, d - c);
+            v.load(part + p * stride + c, d - c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] += v.get(e);
         }
-        Chunk<T>::store(out + row * d + c, d - c, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= factor;
+        Chunk<T>::store(out + c, d - c, f);
     }
 }
 
-hipError_t launch_finish_dx(bool bf16, const float *part, int parts, size_t stride, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s)
+// a workgroup a row of the chunk, to where the row came from
+template <typename T>
+__global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, Splits sp, int ld, const int *list, const int *count, const float *scale, int first,
+                                                        int cap, int d, T *dX)
+{
+    int rows = *count - first;
+    if (rows > cap) rows = cap;
+    const int r = (int)blockIdx.x;
+    if (r >= rows) return;
+    const bool bf16 = sizeof(T) == 2;
+    finish_row(part + (size_t)r * ld, bf16 ? sp.of(rows) : 1, (size_t)rows * ld, d, bf16 ? scale[1] : 1.f, dX + (size_t)list[first + r] * d);
+}
+
+hipError_t launch_finish_dx(bool bf16, const float *part, Splits sp, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s)
 {
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, parts, stride, ld, (const int *)rl.list, (const int *)rl.count, first, d, (T *)dX);
+        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, sp, ld, (const int *)rl.list, (const int *)rl.count, (const float *)rl.scale, first, cap, d, (T *)dX);
         return hipGetLastError();
     };
-    return bf16 ? run(finish_rows_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_rows_kernel<float>, (float *)nullptr);
+    return bf16 ? run(finish_dx_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_dx_kernel<float>, (float *)nullptr);
 }
 
-hipError_t launch_finish_dw(bool bf16, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s)
+template <typename T>
+__global__ __launch_bounds__(256) void finish_dw_kernel(const float *part, int parts, size_t stride, int ld, int d, const float *scale, T *dW)
+{
+    const size_t r = blockIdx.x;
+    finish_row(part + r * ld, parts, stride, d, scale[1], dW + r * d);
+}
+
+hipError_t launch_finish_dw(bool bf16, RowList rl, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s)
 {
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        // 32768 rows of workgroups at a time
-        for (size_t at = 0; at < rows; at += 32768) {
-            const size_t now = rows - at < 32768 ? rows - at : 32768;
-            hipLaunchKernelGGL(kern, dim3((unsigned)now), dim3(256), 0, s, part + at * ld, parts, stride, ld, (const int *)nullptr, (const int *)nullptr, 0, d,
-                               (T *)dW + at * d);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        return hipSuccess;
+        hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(256), 0, s, part, parts, stride, ld, d, (const float *)rl.scale, (T *)dW);
+        return hipGetLastError();
     };
-    return bf16 ? run(finish_rows_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_rows_kernel<float>, (float *)nullptr);
-}
-
-// zeros in dX's rows without a term, and in their losses' places
-template <typename T>
-__global__ __launch_bounds__(256) void zero_others_kernel(Terms t, int d, T *out, float *label_loss, float *top_loss)
-{
-    const int row = (int)blockIdx.x;
-    if (t.any(row)) return;
-    if (threadIdx.x == 0) {
-        if (label_loss) label_loss[row] = 0.f;
-        if (top_loss) top_loss[row] = 0.f;
-    }
-    if (out) {
-        const float f[8] = {};
-        for (int c = (int)threadIdx.x * 8; c < d; c += 2048) Chunk<T>::store(out + (size_t)row * d + c, d - c, f);
-    }
-}
-
-hipError_t launch_zero_others(const VocabArgs &a, void *dX, float *label_loss, float *top_loss, hipStream_t s)
-{
-    if (a.bf16) hipLaunchKernelGGL(zero_others_kernel<bf16_t>, dim3(a.rows), dim3(256), 0, s, terms_of(a), a.d, (bf16_t *)dX, label_loss, top_loss);
-    else hipLaunchKernelGGL(zero_others_kernel<float>, dim3(a.rows), dim3(256), 0, s, terms_of(a), a.d, (float *)dX, label_loss, top_loss);
-    return hipGetLastError();
+    return bf16 ? run(finish_dw_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_dw_kernel<float>, (float *)nullptr);
 }
 
 }  // namespace lm
