@@ -2,6 +2,8 @@
 #pragma once
 #include "../stl_kernels.h"
 
+#include <type_traits>
+
 namespace stl {
 namespace lm {
 
@@ -26,6 +28,19 @@ constexpr int kResidualWidest = 32768;       // a row is held in the registers o
 size_t residual_workspace_bytes(int rows, int n, int per_gate);
 hipError_t launch_residual_forward(int dtype, const ResidualArgs &a, void *Xout, void *Z, hipStream_t s);
 hipError_t launch_residual_backward(int dtype, const ResidualArgs &a, const ResidualGrads &g, void *ws, hipStream_t s);
+
+// ---- fp32 products (lm_f32.hip) ------------------------------------------------------------------------------------------------
+// Out (I x J) (+)= A B over L, dense rows: A stored [i][l] (a_along) or [l][i], B stored [j][l] (b_along) or [l][j]
+struct GemmF32 {
+    int I, J, L;
+    const float *A;
+    bool a_along;
+    const float *B;
+    bool b_along;
+    float *Out;
+    bool accumulate;         // of [l][i] and [l][j] only
+};
+hipError_t launch_gemm_f32(const GemmF32 &g, hipStream_t s);
 
 // ---- vocabulary loss (lm_vocab.hip, lm_vocab_rows.hip) -----------------------------------------------------------------------
 struct VocabArgs {

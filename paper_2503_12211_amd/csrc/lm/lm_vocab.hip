@@ -6,7 +6,7 @@
 //   2. a pass over the rows gives the losses and writes the bf16 gradient dz over the steps (lm_vocab_rows.hip);
 //   3. dX = dz W, contraction over the vocabulary, split where there are few blocks;  4. dW = dz^T X, contraction over the rows.
 // Three products of 2 T V d operations, where forming the logits twice would take four; what bounds them is the matrix cores (lm_gemm.h).
-// fp32 storage: the same steps on the fp32 products of ../stl_gemm_generic.hip, the chunk's logits in fp32.
+// fp32 storage: the same steps on the fp32 products of lm_f32.hip, the chunk's logits in fp32.
 #include "lm_gemm.h"
 #include "lm_kernels.h"
 #include "lm_device.h"
@@ -439,17 +439,18 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
 hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, const Plan &p, char *base, const RowList &rl, hipStream_t s)
 {
     float *xc = (float *)(base + p.xc), *z = (float *)(base + p.codes), *dx = (float *)(base + p.dx_part);
+    const float *W = (const float *)a.W;
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
         LM_TRY(launch_arrange_rows(a, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
-        LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.vocab, a.d, 1, false, false, false, false}, xc, a.W, z, s));
+        LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false}, s));
         const VocabChunk c{first, cap, z, p.ldz, nullptr, nullptr, nullptr, nullptr, 0, xc, a.d};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
-            LM_TRY(launch_plane_gemm(0, GemmDesc{cap, a.d, a.vocab, 1, false, true, false, false}, z, a.W, dx, s));
+            LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false}, s));
             LM_TRY(launch_finish_dx(false, dx, Splits{}, a.d, rl, first, cap, a.d, g->dX, s));
         }
-        if (g && g->dW) LM_TRY(launch_plane_gemm(0, GemmDesc{a.vocab, a.d, cap, 1, true, true, true, ch > 0}, z, xc, g->dW, s));
+        if (g && g->dW) LM_TRY(launch_gemm_f32({a.vocab, a.d, cap, z, false, xc, false, (float *)g->dW, ch > 0}, s));
     }
     return hipSuccess;
 }

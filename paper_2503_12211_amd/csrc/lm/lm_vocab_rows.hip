@@ -51,9 +51,11 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, co
     const int per = (rows + 1023) / 1024, r0 = (int)threadIdx.x * per, r1 = r0 + per < rows ? r0 + per : rows, lane = (int)threadIdx.x & 63;
     int n = 0;
     float top = 0.f;
+    uint32_t has = 0;                                        // of the first 32 rows
     for (int r = r0; r < r1; ++r) {
         const bool l = t.labelled(r), q = t.taught(r);
         n += l || q;
+        if (r - r0 < 32) has |= (uint32_t)(l || q) << (r - r0);
         top = fmaxf(top, (l && dlabel ? fabsf(dlabel[r]) : 0.f) + (q && dtop ? fabsf(dtop[r]) * inv_tau : 0.f));
     }
     int upto = n;                                            // over the lanes up to this one
@@ -74,7 +76,7 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, co
         top = fmaxf(top, tops[w]);
     }
     for (int r = r0; r < r1; ++r)
-        if (t.any(r)) list[at++] = r;
+        if (r - r0 < 32 ? has >> (r - r0) & 1 : t.any(r)) list[at++] = r;
     if (threadIdx.x == 0) {
         *count = all;
         scale[0] = dz_scale(top);
@@ -250,9 +252,25 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
     // the logits of the label and the teacher's entries
     if constexpr (BF16) {
         const bf16_t *x = (const bf16_t *)c.Xc + (size_t)r * c.ldx;
+        if (!t.top_id) {
+            // a label alone: its product is shared by the workgroup
+            float dot = 0.f;
+            if (labelled) {
+                const bf16_t *w = (const bf16_t *)W + (size_t)ids[0] * d;
+                for (int e0 = tid * 8; e0 < d; e0 += kRowThreads * 8) {
+                    Chunk<bf16_t> a, b;
+                    a.load(x + e0, d - e0);
+                    b.load(w + e0, d - e0);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = fmaf(a.get(e), b.get(e), dot);
+                }
+            }
+            dot = block_sum(dot, red);
+            if (tid == 0) z[0] = dot;
+        }
         // four entries of a wavefront at a time: the loads of four rows of W in flight (an entry that is none reads the first row)
         constexpr int AT_ONCE = 4;
-        for (int j0 = wave * AT_ONCE; j0 <= ntop; j0 += kRowWaves * AT_ONCE) {
+        for (int j0 = t.top_id ? wave * AT_ONCE : 1; j0 <= ntop; j0 += kRowWaves * AT_ONCE) {
             const bf16_t *w[AT_ONCE];
             float dot[AT_ONCE];
 #pragma unroll
