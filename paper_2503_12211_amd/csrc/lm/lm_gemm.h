@@ -34,7 +34,7 @@ struct Ring {
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 16, FN = WN / 16;
     static constexpr int OPER_BYTES = BM * pipe::BKS * 2, STAGE_BYTES = (BM + BN) * pipe::BKS * 2;
     static constexpr int D = (BM + BN) / 16 / NW;          // DMA instructions per wavefront and stage
-    static constexpr int SLAB = 4096, LDS_BYTES = NS * STAGE_BYTES + NW * SLAB;
+    static constexpr int SLAB = 4096, SLABS_AT = NS * STAGE_BYTES, LDS_BYTES = SLABS_AT + NW * SLAB;
     static_assert(LDS_BYTES <= 160 * 1024 && NS >= 3, "LDS");
     typedef pipe::WaveTile<FM, FN> Tile;
     pipe::Frag<A_T, BM> fa;

@@ -74,7 +74,10 @@ struct RowList {
 hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s);
 // rows first .. first + cap of the list of X, side by side with ld elements each (zeros behind a row's end and behind the list's).  With the
 // first chunk also: zeros for the rows that are not listed, in dX and the losses (each may be NULL).
-hipError_t launch_arrange_rows(const VocabArgs &a, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss, hipStream_t s);
+// Up to kFewRows rows are listed by every workgroup of this launch for itself, and by the first of them for the launches that follow.
+constexpr int kFewRows = 256;
+hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss,
+                               hipStream_t s);
 // rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
 

@@ -26,15 +26,16 @@ struct LogitsOut {
 };
 
 // rows: count - first listed rows of the chunk (at most cap), a device value
-template <int BM, int WAVES_M, int WAVES_N, int NS, bool CODES, bool TWO>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_logits_kernel(const Operands o, const int *count, int first, int cap, int vocab, const LogitsOut out)
+template <bool CODES, bool TWO>
+__global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, const int *count, int first, int cap, int vocab, const LogitsOut out)
 {
     using namespace pipe;
-    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, false, false> R;
+    typedef Ring<256, 256, 2, 4, 4, false, false, false> R;
+    constexpr int BM = R::BM, WAVES_N = R::WAVES_N;
     static_assert(R::WN == 64, "a wavefront's columns are one group");
     extern __shared__ __align__(16) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    char *slab = smem + NS * R::STAGE_BYTES + wave * R::SLAB;
+    char *slab = smem + R::SLABS_AT + wave * R::SLAB;
     const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
     int rows = *count - first;
     if (rows > cap) rows = cap;
@@ -159,6 +160,99 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_logits_kernel(con
     }
 }
 
+// Few rows (at most 16 FM listed ones of the chunk): reading W once is the work, and how it is read decides.  Memory gives 512 MB in rows of 8 KB, of which
+// a visit takes 64 (128, 256, 512, 1024) bytes side by side, at 4.1 (4.3, 4.7, 5.3, 6.0) TB/s, a plain loop 6.2; the LDS-DMA rings ask for 64 or 128.  So
+// a workgroup has one group of 64 columns, that is 64 rows of W, and takes 1 KB (512 elements of the contraction) of each at a time, a wavefront's
+// instruction a row: through registers, on the way while the stage before is multiplied, into LDS (two workgroups a CU: one multiplies while the
+// other waits).  Each of the four wavefronts multiplies a quarter of a stage, X coming straight from L2 into fragments, and their sums meet in LDS,
+// where a lane then has a column.  16 rows x 4096, vocabulary 65536 (537 MB): 97 us (5.5 TB/s), 128 in blocks of the LDS-DMA ring.
+// LDS: row stride 1 KB, 16-byte chunk c of row r at c ^ (r & 15): the 16 rows of a fragment fall on all banks.
+template <int FM, bool CODES, bool TWO>
+__global__ __launch_bounds__(256, 2) void vocab_logits_few_kernel(const Operands o, const int *count, int first, int cap, int vocab, const LogitsOut out)
+{
+    constexpr int NW = 4, ROWS = 16 * FM, STAGE = 512, STEPS = STAGE / 32 / NW;      // a wavefront's steps of 32 elements in a stage
+    __shared__ __align__(16) char tile[64 * 1024];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, kq = lane >> 4, col0 = (int)blockIdx.x * 64;
+    int rows = *count - first;
+    if (rows > cap) rows = cap;
+    if (rows <= 0) return;
+    const int stages = (o.Kl + STAGE - 1) / STAGE;
+    u32x4_t rb[16], ra[STEPS][FM];
+    f32x4_t acc[FM][4];
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[f][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    auto fetch = [&](int s) {
+        const int l0 = s * STAGE;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = col0 + 4 * i + wave, l = l0 + 8 * lane;          // rows behind the last feed columns that are masked below
+            rb[i] = l < o.Kl ? *reinterpret_cast<const u32x4_t *>(o.B + (long)(row < vocab ? row : vocab - 1) * o.ldb + l) : u32x4_t{0u, 0u, 0u, 0u};
+        }
+    };
+    fetch(0);
+    for (int s = 0; s < stages; ++s) {
+        // (X's fragments come from L2 while W's rows go into LDS)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) {
+                const int l = s * STAGE + (STEPS * wave + k) * 32 + 8 * kq;
+                ra[k][f] = l < o.Kl ? *reinterpret_cast<const u32x4_t *>(o.A + (long)(16 * f + n16) * o.lda + l) : u32x4_t{0u, 0u, 0u, 0u};
+            }
+        if (s > 0) __syncthreads();                          // all have read the stage before
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = 4 * i + wave;
+            *reinterpret_cast<u32x4_t *>(tile + row * 1024 + ((lane ^ (row & 15)) << 4)) = rb[i];
+        }
+        __syncthreads();
+        if (s + 1 < stages) fetch(s + 1);
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            const int chunk = 4 * (STEPS * wave + k) + kq;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const bf16x8_t b = *reinterpret_cast<const bf16x8_t *>(tile + (16 * c + n16) * 1024 + ((chunk ^ n16) << 4));
+#pragma unroll
+                for (int f = 0; f < FM; ++f) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ra[k][f]), b, acc[f][c], 0, 0, 0);
+            }
+        }
+    }
+    // accumulator e of fragment (f, c): row 16 f + 4 kq + e, column 16 c + n16
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(tile);           // [wavefront][row][64]
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[(wave * ROWS + 16 * f + 4 * kq + e) * 64 + 16 * c + n16] = acc[f][c][e];
+    __syncthreads();
+    const float scale = out.inv_tau * 1.44269504088896340736f, scale2 = out.inv_tau2 * 1.44269504088896340736f;
+    const bool in = col0 + lane < vocab;
+    for (int r = wave; r < ROWS && r < rows; r += NW) {
+        float z = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) z += sums[(w * ROWS + r) * 64 + lane];
+        z = in ? z : -INFINITY;
+        const float m = wave_max(z), ref = m == -INFINITY ? 0.f : m, below = z - ref;
+        const float s = wave_sum(__builtin_amdgcn_exp2f(below * scale));
+        float s2 = 0.f, spread = 0.f;
+        if constexpr (TWO) s2 = wave_sum(__builtin_amdgcn_exp2f(below * scale2));
+        if constexpr (CODES) spread = fminf(fmaxf(wave_max(in ? -below : 0.f), 1e-3f), out.deepest);
+        if (lane == 0) {
+            const size_t at = (size_t)r * out.groups + blockIdx.x;
+            out.group_max[at] = m;
+            out.group_sum[at] = s;
+            if constexpr (TWO) out.group_sum_tau[at] = s2;
+            if constexpr (CODES) out.group_step[at] = spread * (1.f / kSteps);
+        }
+        if constexpr (CODES) out.codes[(size_t)r * out.ld + col0 + lane] = (uint16_t)(uint32_t)fminf(-below * (kSteps / spread) + 0.5f, 65535.f);
+    }
+}
+
 // ---- dX and dW -----------------------------------------------------------------------------------------------------------------------
 // dX parts: part s, rows x ldx = dz (columns of split s) W.
 template <int BM, int WAVES_M, int WAVES_N, int NS>
@@ -275,22 +369,26 @@ static hipError_t launch_ring(K kern, std::atomic<uint64_t> &granted, int lds, i
     return hipGetLastError();
 }
 
-template <int BM, int WAVES_M, int WAVES_N, int NS, bool CODES, bool TWO>
+template <bool CODES, bool TWO>
 static hipError_t launch_logits_as(const Operands &o, const int *count, int first, int cap, int vocab, const LogitsOut &out, hipStream_t s)
 {
-    typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, false, false> R;
+    // Up to 32 rows are few: whole calls at 4096 x 65536, us, there / in blocks of 256 rows: 16 rows 109 / 149, 32 rows 116 / 149; 64 rows 166 / 149, for
+    // whose fragments and sums there are not enough registers.
+    auto few = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(out.groups), dim3(256), 0, s, o, count, first, cap, vocab, out);
+        return hipGetLastError();
+    };
+    if (cap <= 16) return few(vocab_logits_few_kernel<1, CODES, TWO>);
+    if (cap <= 32) return few(vocab_logits_few_kernel<2, CODES, TWO>);
+    typedef Ring<256, 256, 2, 4, 4, false, false, false> R;
     static std::atomic<uint64_t> granted{0};                 // of this instantiation
-    return launch_ring(vocab_logits_kernel<BM, WAVES_M, WAVES_N, NS, CODES, TWO>, granted, R::LDS_BYTES, R::THREADS,
-                       (long)((cap + BM - 1) / BM) * ((vocab + 255) / 256), s, o, count, first, cap, vocab, out);
+    return launch_ring(vocab_logits_kernel<CODES, TWO>, granted, R::LDS_BYTES, R::THREADS, (long)((cap + 255) / 256) * ((vocab + 255) / 256), s, o, count, first, cap,
+                       vocab, out);
 }
-template <int BM, int WAVES_M, int WAVES_N, int NS>
 static hipError_t launch_logits(const Operands &o, const int *count, int first, int cap, int vocab, const LogitsOut &out, bool two, hipStream_t s)
 {
-    if (out.codes)
-        return two ? launch_logits_as<BM, WAVES_M, WAVES_N, NS, true, true>(o, count, first, cap, vocab, out, s)
-                   : launch_logits_as<BM, WAVES_M, WAVES_N, NS, true, false>(o, count, first, cap, vocab, out, s);
-    return two ? launch_logits_as<BM, WAVES_M, WAVES_N, NS, false, true>(o, count, first, cap, vocab, out, s)
-               : launch_logits_as<BM, WAVES_M, WAVES_N, NS, false, false>(o, count, first, cap, vocab, out, s);
+    if (out.codes) return two ? launch_logits_as<true, true>(o, count, first, cap, vocab, out, s) : launch_logits_as<true, false>(o, count, first, cap, vocab, out, s);
+    return two ? launch_logits_as<false, true>(o, count, first, cap, vocab, out, s) : launch_logits_as<false, false>(o, count, first, cap, vocab, out, s);
 }
 
 template <int BM, int WAVES_M, int WAVES_N, int NS>
@@ -351,12 +449,12 @@ Plan plan_of(const VocabArgs &a, bool grads)
         cap = cap > 8192 ? 8192 : cap < 256 ? 256 : cap;
         p.cap = (int)(a.rows < cap ? a.rows : cap);
         p.chunks = (a.rows + p.cap - 1) / p.cap;
-        p.rows_held = (int)round_up(p.cap, 256);
-        p.ldx = (int)round_up(a.d, pipe::BKS);
+        p.small = p.cap <= 64;
+        p.rows_held = (int)round_up(p.cap, p.small ? 64 : 256);
+        p.ldx = (int)round_up(a.d, pipe::BKS);                 // whole stages of the products
         p.pack_w = p.ldx != a.d;
         p.groups = (a.vocab + 63) / 64;
         p.ldz = (size_t)p.groups * 64;
-        p.small = p.cap <= 64;
         p.xc = take((size_t)p.rows_held * p.ldx * 2);
         if (p.pack_w) p.wp = take((size_t)a.vocab * p.ldx * 2);
         p.gmax = take((size_t)p.cap * p.groups * sizeof(float));
@@ -408,12 +506,11 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
     const float inv_tau = 1.f / a.tau;
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap;
-        LM_TRY(launch_arrange_rows(a, rl, first, p.rows_held, p.ldx, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
+        LM_TRY(launch_arrange_rows(a, g, rl, first, p.rows_held, p.ldx, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
         const LogitsOut lo{(float *)(base + p.gmax), (float *)(base + p.gsum), two ? (float *)(base + p.gsum2) : nullptr,
                            (float *)(base + p.gstep), p.groups, codes, (long)p.ldz, a.label ? 1.f : inv_tau, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f)};
-        LM_TRY((p.small ? launch_logits<64, 1, 4, 7>(logits, rl.count, first, p.cap, a.vocab, lo, two, s)
-                        : launch_logits<256, 2, 4, 4>(logits, rl.count, first, p.cap, a.vocab, lo, two, s)));
+        LM_TRY(launch_logits(logits, rl.count, first, p.cap, a.vocab, lo, two, s));
         const VocabChunk c{first, p.cap, codes, p.ldz, lo.group_max, lo.group_sum, lo.group_sum_tau, lo.group_step, p.groups, xc, p.ldx};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
@@ -442,7 +539,7 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
     const float *W = (const float *)a.W;
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
-        LM_TRY(launch_arrange_rows(a, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
+        LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false}, s));
         const VocabChunk c{first, cap, z, p.ldz, nullptr, nullptr, nullptr, nullptr, 0, xc, a.d};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
@@ -464,7 +561,7 @@ hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *lab
     const Plan p = plan_of(a, g != nullptr);
     char *base = (char *)ws;
     const RowList rl{(int *)(base + p.list), (int *)(base + p.count), (float *)(base + p.scale)};
-    LM_TRY(launch_select_rows(a, g, rl, s));
+    if (a.rows > kFewRows) LM_TRY(launch_select_rows(a, g, rl, s));
     return a.bf16 ? loss_bf16(a, g, label_loss, top_loss, p, base, rl, s) : loss_f32(a, g, label_loss, top_loss, p, base, rl, s);
 }
 

@@ -42,23 +42,24 @@ __device__ __forceinline__ float dz_scale(float w)
     return 1.96875f / __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
 }
 
-// One workgroup: every thread counts a run of neighbouring rows, the counts are added up over the workgroup, and every thread lists its rows.
-__global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, const float *dlabel, const float *dtop, float inv_tau, int *list, int *count,
-                                                           float *scale)
-{
-    __shared__ int sums[16];
-    __shared__ float tops[16];
-    const int per = (rows + 1023) / 1024, r0 = (int)threadIdx.x * per, r1 = r0 + per < rows ? r0 + per : rows, lane = (int)threadIdx.x & 63;
-    int n = 0;
-    float top = 0.f;
-    uint32_t has = 0;                                        // of the first 32 rows
-    for (int r = r0; r < r1; ++r) {
-        const bool l = t.labelled(r), q = t.taught(r);
-        n += l || q;
-        if (r - r0 < 32) has |= (uint32_t)(l || q) << (r - r0);
-        top = fmaxf(top, (l && dlabel ? fabsf(dlabel[r]) : 0.f) + (q && dtop ? fabsf(dtop[r]) * inv_tau : 0.f));
+struct Weights {
+    const float *dlabel, *dtop;
+    float inv_tau;
+    __device__ __forceinline__ float of(int r, bool labelled, bool taught) const
+    {
+        return (labelled && dlabel ? fabsf(dlabel[r]) : 0.f) + (taught && dtop ? fabsf(dtop[r]) * inv_tau : 0.f);
     }
-    int upto = n;                                            // over the lanes up to this one
+};
+static Weights weights_of(const VocabArgs &a, const VocabGrads *g) { return Weights{g ? g->dlabel : nullptr, g ? g->dtop : nullptr, 1.f / a.tau}; }
+
+// Over the THREADS of a workgroup: `n` of this one and the threads before it, and of all; the largest `top`.
+template <int THREADS>
+__device__ __forceinline__ int scan_rows(int n, int &all, float &top)
+{
+    __shared__ int sums[THREADS / 64];
+    __shared__ float tops[THREADS / 64];
+    const int lane = (int)threadIdx.x & 63;
+    int upto = n;
     for (int step = 1; step < 64; step *= 2) {
         const int v = __shfl_up(upto, step);
         if (lane >= step) upto += v;
@@ -69,12 +70,29 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, co
         tops[threadIdx.x >> 6] = top;
     }
     __syncthreads();
-    int at = upto - n, all = 0;
-    for (int w = 0; w < 16; ++w) {
-        if (w < (int)threadIdx.x >> 6) at += sums[w];
+    all = 0;
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < (int)threadIdx.x >> 6) upto += sums[w];
         all += sums[w];
         top = fmaxf(top, tops[w]);
     }
+    return upto;
+}
+
+// One workgroup: every thread counts a run of neighbouring rows, the counts are added up over the workgroup, and every thread lists its rows.
+__global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, Weights w, int *list, int *count, float *scale)
+{
+    const int per = (rows + 1023) / 1024, r0 = (int)threadIdx.x * per, r1 = r0 + per < rows ? r0 + per : rows;
+    int n = 0, all;
+    float top = 0.f;
+    uint32_t has = 0;                                        // of the first 32 rows
+    for (int r = r0; r < r1; ++r) {
+        const bool l = t.labelled(r), q = t.taught(r);
+        n += l || q;
+        if (r - r0 < 32) has |= (uint32_t)(l || q) << (r - r0);
+        top = fmaxf(top, w.of(r, l, q));
+    }
+    int at = scan_rows<1024>(n, all, top) - n;
     for (int r = r0; r < r1; ++r)
         if (r - r0 < 32 ? has >> (r - r0) & 1 : t.any(r)) list[at++] = r;
     if (threadIdx.x == 0) {
@@ -86,8 +104,7 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(Terms t, int rows, co
 
 hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s)
 {
-    hipLaunchKernelGGL(select_rows_kernel, dim3(1), dim3(1024), 0, s, terms_of(a), a.rows, g ? g->dlabel : nullptr, g ? g->dtop : nullptr, 1.f / a.tau, rl.list,
-                       rl.count, rl.scale);
+    hipLaunchKernelGGL(select_rows_kernel, dim3(1), dim3(1024), 0, s, terms_of(a), a.rows, weights_of(a, g), rl.list, rl.count, rl.scale);
     return hipGetLastError();
 }
 
@@ -107,13 +124,38 @@ __device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, 
     }
 }
 
-// a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed
-template <typename T>
-__global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, const T *X, const int *list, const int *count, int first, int cap, int d, int ld, T *out,
-                                                           int zeros, T *dX, float *label_loss, float *top_loss)
+// a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed.  FEW: there is no list
+// yet; a thread has a row, and every workgroup lists them.
+template <typename T, bool FEW>
+__global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, Weights w, const T *X, int *list, int *count, float *scale, int first, int cap, int d,
+                                                           int ld, T *out, int zeros, T *dX, float *label_loss, float *top_loss)
 {
     const int b = (int)blockIdx.x;
-    if (b < cap) copy_row(X, first + b < *count ? list[first + b] : -1L, d, out, b, ld);
+    long from = -1;
+    if constexpr (FEW) {
+        __shared__ int mine;
+        const int r = (int)threadIdx.x;
+        const bool l = r < rows && t.labelled(r), q = r < rows && t.taught(r);
+        int all;
+        float top = r < rows ? w.of(r, l, q) : 0.f;
+        const int at = scan_rows<256>(l || q, all, top) - 1;
+        if (r == 0) mine = -1;
+        __syncthreads();
+        if ((l || q) && at == b) mine = r;
+        if (b == 0) {
+            if (l || q) list[at] = r;
+            if (r == 0) {
+                *count = all;
+                scale[0] = dz_scale(top);
+                scale[1] = 1.f / scale[0];
+            }
+        }
+        __syncthreads();
+        from = mine;
+    } else {
+        if (b < cap && first + b < *count) from = list[first + b];
+    }
+    if (b < cap) copy_row(X, from, d, out, b, ld);
     if (b < zeros && !t.any(b)) {
         if (threadIdx.x == 0) {
             if (label_loss) label_loss[b] = 0.f;
@@ -123,16 +165,19 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, const T *X, 
     }
 }
 
-hipError_t launch_arrange_rows(const VocabArgs &a, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss, hipStream_t s)
+hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss,
+                               hipStream_t s)
 {
     const int zeros = first == 0 ? a.rows : 0;
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3(cap > zeros ? cap : zeros), dim3(256), 0, s, terms_of(a), (const T *)a.X, (const int *)rl.list, (const int *)rl.count, first,
-                           cap, a.d, ld, (T *)out, zeros, (T *)dX, label_loss, top_loss);
+        hipLaunchKernelGGL(kern, dim3(cap > zeros ? cap : zeros), dim3(256), 0, s, terms_of(a), a.rows, weights_of(a, g), (const T *)a.X, rl.list, rl.count, rl.scale,
+                           first, cap, a.d, ld, (T *)out, zeros, (T *)dX, label_loss, top_loss);
         return hipGetLastError();
     };
-    return a.bf16 ? run(arrange_rows_kernel<bf16_t>, (bf16_t *)nullptr) : run(arrange_rows_kernel<float>, (float *)nullptr);
+    const bool few = a.rows <= kFewRows;
+    if (a.bf16) return few ? run(arrange_rows_kernel<bf16_t, true>, (bf16_t *)nullptr) : run(arrange_rows_kernel<bf16_t, false>, (bf16_t *)nullptr);
+    return few ? run(arrange_rows_kernel<float, true>, (float *)nullptr) : run(arrange_rows_kernel<float, false>, (float *)nullptr);
 }
 
 __global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t *in, int d, bf16_t *out, int ld) { copy_row(in, blockIdx.x, d, out, blockIdx.x, ld); }
