@@ -124,5 +124,56 @@ struct Ring {
     }
 };
 
+// A workgroup's way through its share of a list of blocks: every step-th from v on, below end.  place(v, o, stages, i0, j0) says what block v is;
+// epilogue(accumulators, v, i0, j0).
+template <class R, class P, class E>
+__device__ __forceinline__ void walk(R, int v, int end, int step, const Operands &o, const char *smem, uint32_t smem_lds, int wave, int lane, P &&place, E &&epilogue)
+{
+    R ring;
+    ring.init(wave, lane);
+    auto start = [&](int u) {
+        Operands mine = o;
+        int stages, i0, j0;
+        place(u, mine, stages, i0, j0);
+        ring.start(mine, stages, i0, j0, smem_lds, wave, lane);
+    };
+    if (v < end) start(v);
+    for (; v < end; v += step) {
+        Operands mine = o;
+        int stages, i0, j0;
+        place(v, mine, stages, i0, j0);
+        ring.block(
+            stages, smem, smem_lds, wave, lane,
+            [&]() {
+                if (v + step < end) start(v + step);
+            },
+            [&](typename R::Tile &w) { epilogue(w, v, i0, j0); });
+    }
+}
+
+// The same over the blocks of 256 x 256 of a whole list, in which those of a last round that would leave half of the workgroups idle are cut into two halves
+// of 128 rows, one for each of twice as many workgroups (Half); a half that begins behind the last of the output's `rows` rows is none.  777 rows, 1024, vocabulary 50001: 784 blocks on 256 CUs, HALF_US.
+template <class Full, class Half, class P, class E>
+__device__ __forceinline__ void walk_list(int total, int rows, const Operands &o, const char *smem, uint32_t smem_lds, int wave, int lane, P &&place, E &&epilogue)
+{
+    const int first = pipe::first_block(total), end = pipe::end_block(total), step = pipe::block_step(), whole = pipe::whole_end(total), rest = end - whole;
+    if (2 * rest > step) {
+        walk(Full{}, first, end, step, o, smem, smem_lds, wave, lane, place, epilogue);
+        return;
+    }
+    walk(Full{}, first, whole, step, o, smem, smem_lds, wave, lane, place, epilogue);
+    // (its ring lies in that of the whole blocks, which all wavefronts have left, and ends below their slabs)
+    const int u = (int)(blockIdx.x >> 3);
+    if (u >= 2 * rest) return;
+    auto half = [&](int h, Operands &mine, int &stages, int &i0, int &j0) {
+        place(whole + h / 2, mine, stages, i0, j0);
+        i0 += (h & 1) * 128;
+    };
+    Operands mine = o;
+    int stages, i0, j0;
+    half(u, mine, stages, i0, j0);
+    if (i0 < rows) walk(Half{}, u, u + 1, 1, o, smem, smem_lds, wave, lane, half, [&](typename Half::Tile &w, int h, int r, int c) { epilogue(w, whole + h / 2, r, c); });
+}
+
 }  // namespace lm
 }  // namespace stl

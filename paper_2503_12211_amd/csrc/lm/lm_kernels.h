@@ -95,19 +95,26 @@ struct VocabChunk {
 };
 hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
 // How the contraction of dX over the vocabulary is cut, on the device, where the rows of the chunk are known: in as many runs of whole stages (16 at
-// least) as give every CU of an MI355X a block.  Part s of `rows` rows lies s * rows * ld floats on.
+// least) as take the least time, us: rounds of blocks over the CUs of an MI355X, of 0.53 a stage and 5 beside, and 0.12 a block and run for writing its
+// fp32 part and adding it up.  Part s of `rows` rows lies s * rows * ld floats on.
 struct Splits {
     int block_rows, tiles_n, stages;
+    static constexpr int kMost = 16, kBlocks = 1024;         // runs, and blocks of all runs where there is more than one
     __host__ __device__ int of(int rows) const
     {
-        const int tiles = (rows + block_rows - 1) / block_rows * tiles_n, most = stages / 16 > 0 ? stages / 16 : 1, n = tiles >= 256 ? 1 : 256 / (tiles > 0 ? tiles : 1);
-        return n < most ? n : most;
+        const int tiles = (rows + block_rows - 1) / block_rows * tiles_n;
+        int best = 1;
+        float least = 0.f;
+        for (int s = 1; s == 1 || (s <= kMost && s * tiles <= kBlocks && 16 * s <= stages); ++s) {
+            const float us = (float)((s * tiles + 255) / 256) * (0.53f * (float)stages / (float)s + 5.f) + 0.12f * (float)(s * tiles);
+            if (s == 1 || us < least) least = us, best = s;
+        }
+        return best;
     }
     // rows of all parts together, at most, for up to `cap` rows
     __host__ long rows(int cap) const
     {
-        const long full = (long)256 / tiles_n * block_rows, all = (long)cap * (stages / 16 > 0 ? stages / 16 : 1);
-        const long some = full < all ? full : all;
+        const long full = (long)kBlocks / tiles_n * block_rows, all = (long)cap * kMost, some = full < all ? full : all;
         return some > cap ? some : cap;
     }
 };

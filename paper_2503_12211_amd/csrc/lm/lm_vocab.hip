@@ -25,58 +25,52 @@ struct LogitsOut {
     float deepest;       // below a group's maximum by this much, no share is left in fp32
 };
 
-// rows: count - first listed rows of the chunk (at most cap), a device value
+typedef Ring<256, 256, 2, 4, 4, false, false, false> LogitsFull;
+typedef Ring<128, 256, 2, 4, 5, false, false, false> LogitsHalf;
+static_assert(LogitsFull::WN == 64 && LogitsHalf::WN == 64, "a wavefront's columns are one group");
+static_assert(LogitsHalf::SLABS_AT <= LogitsFull::SLABS_AT && LogitsHalf::LDS_BYTES <= LogitsFull::LDS_BYTES, "LDS of walk_list");
+
+// listed rows of the chunk: count - first, a device value, at most cap
 template <bool CODES, bool TWO>
 __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, const int *count, int first, int cap, int vocab, const LogitsOut out)
 {
     using namespace pipe;
-    typedef Ring<256, 256, 2, 4, 4, false, false, false> R;
-    constexpr int BM = R::BM, WAVES_N = R::WAVES_N;
-    static_assert(R::WN == 64, "a wavefront's columns are one group");
     extern __shared__ __align__(16) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    char *slab = smem + R::SLABS_AT + wave * R::SLAB;
     const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
     int rows = *count - first;
     if (rows > cap) rows = cap;
     if (rows <= 0) return;
-    const int tiles_m = (rows + BM - 1) / BM, tiles_n = (vocab + 255) / 256, total = tiles_m * tiles_n, nks = o.Kl / BKS;
-    R ring;
-    ring.init(wave, lane);
-    auto start_block = [&](int v) {
-        int bi, bj;
-        block_at(v, tiles_m, tiles_n, bi, bj);
-        ring.start(o, nks, bi * BM, bj * 256, smem_lds, wave, lane);
-    };
-    const int step = block_step(), end = end_block(total);
-    int v = first_block(total);
-    if (v < end) start_block(v);
-    for (; v < end; v += step) {
-        int bi, bj;
-        block_at(v, tiles_m, tiles_n, bi, bj);
-        ring.block(
-            nks, smem, smem_lds, wave, lane,
-            [&]() {
-                if (v + step < end) start_block(v + step);
-            },
-            [&](typename R::Tile &w) {
+    const int tiles_m = (rows + 255) / 256, tiles_n = (vocab + 255) / 256, nks = o.Kl / BKS;
+    walk_list<LogitsFull, LogitsHalf>(
+        tiles_m * tiles_n, rows, o, smem, smem_lds, wave, lane,
+        [&](int v, Operands &, int &stages, int &i0, int &j0) {
+            int bi, bj;
+            block_at(v, tiles_m, tiles_n, bi, bj);
+            stages = nks;
+            i0 = bi * 256;
+            j0 = bj * 256;
+        },
+        [&](auto &w, int, int i0, int j0) {
+                constexpr int FM = sizeof(w.acc) / sizeof(w.acc[0]), FN = 4, WM = 16 * FM;
+                char *slab = smem + (FM == LogitsFull::FM ? LogitsFull::SLABS_AT : LogitsHalf::SLABS_AT) + wave * LogitsFull::SLAB;
                 int el = lane;                               // opaque: what follows from it is not kept over the products
                 asm volatile("" : "+v"(el));
-                const int row0 = bi * BM + wave / WAVES_N * R::WM, col0 = bj * 256 + wave % WAVES_N * 64, quad = el >> 4, rl = el & 15;
+                const int row0 = i0 + wave / 4 * WM, col0 = j0 + wave % 4 * 64, quad = el >> 4, rl = el & 15;
                 const int col = col0 + 4 * quad;             // the lane's columns: col + 16 b + e
                 const bool whole = col0 + 64 <= vocab;
                 if (col0 >= vocab && (!CODES || col0 >= out.ld)) return;
                 const int group = col0 / 64;
                 const float scale = out.inv_tau * 1.44269504088896340736f, scale2 = out.inv_tau2 * 1.44269504088896340736f;
                 constexpr int PA = 2;                        // fragment rows that the slab holds: 16 rows of 128 bytes each
-                static_for<0, R::FM / PA>([&](auto pass_c) {
+                static_for<0, FM / PA>([&](auto pass_c) {
                     constexpr int a0 = decltype(pass_c)::value * PA;
                     static_for<0, PA>([&](auto a_c) {
                         constexpr int a = a0 + decltype(a_c)::value;
                         float m = -INFINITY, least = INFINITY;
                         if (!whole) {
 #pragma unroll
-                            for (int b = 0; b < R::FN; ++b)
+                            for (int b = 0; b < FN; ++b)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const bool in = col + 16 * b + e < vocab;
@@ -85,12 +79,12 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
                                 }
                         } else if constexpr (CODES) {
 #pragma unroll
-                            for (int b = 0; b < R::FN; ++b)
+                            for (int b = 0; b < FN; ++b)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) least = fminf(least, w.acc[a][b][e]);
                         }
 #pragma unroll
-                        for (int b = 0; b < R::FN; ++b)
+                        for (int b = 0; b < FN; ++b)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) m = fmaxf(m, w.acc[a][b][e]);
                         m = fmaxf(m, __shfl_xor(m, 16));
@@ -99,7 +93,7 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
                         const float ref = m == -INFINITY ? 0.f : m;
                         float s = 0.f, s2 = 0.f;
 #pragma unroll
-                        for (int b = 0; b < R::FN; ++b)
+                        for (int b = 0; b < FN; ++b)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float below = w.acc[a][b][e] - ref;
@@ -132,7 +126,7 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
                             char *rowp = slab + (16 * (a - a0) + rl) * 128;
                             const int swz = (rl >> 1) & 7;
 #pragma unroll
-                            for (int b = 0; b < R::FN; ++b) {
+                            for (int b = 0; b < FN; ++b) {
                                 uint32_t c[4];
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
@@ -156,8 +150,7 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
                         asm volatile("" ::: "memory");
                     }
                 });
-            });
-    }
+        });
 }
 
 // Few rows (at most 16 FM listed ones of the chunk): reading W once is the work, and how it is read decides.  Memory gives 512 MB in rows of 8 KB, of which
@@ -269,50 +262,39 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
     if (rows <= 0) return;
     const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
     const size_t stride = (size_t)rows * ldx;
-    R ring;
-    ring.init(wave, lane);
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
-    auto start_block = [&](int v) {
-        const int sp = v / per, s0 = begin_of(sp), s1 = begin_of(sp + 1);
-        int bi, bj;
-        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
-        Operands mine = o;
-        mine.A += (long)s0 * BKS;
-        mine.B += (long)s0 * BKS * o.ldb;
-        mine.Kl = (o.Kl < s1 * BKS ? o.Kl : s1 * BKS) - s0 * BKS;
-        ring.start(mine, s1 - s0, bi * BM, bj * 256, smem_lds, wave, lane);
-    };
-    const int step = block_step(), end = end_block(total);
-    int v = first_block(total);
-    if (v < end) start_block(v);
-    for (; v < end; v += step) {
-        const int sp = v / per;
-        int bi, bj;
-        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
-        ring.block(
-            begin_of(sp + 1) - begin_of(sp), smem, smem_lds, wave, lane,
-            [&]() {
-                if (v + step < end) start_block(v + step);
-            },
-            [&](typename R::Tile &w) {
-                int el = lane;
-                asm volatile("" : "+v"(el));
-                w.template store<float, false, false>(slab, part + sp * stride, bi * BM + wave / WAVES_N * R::WM, bj * 256 + wave % WAVES_N * R::WN, rows, ldx, 0,
-                                                      1 << 30, 1, el);
-            });
-    }
+    walk(R{}, first_block(total), end_block(total), block_step(), o, smem, smem_lds, wave, lane,
+         [&](int v, Operands &mine, int &n, int &i0, int &j0) {
+             const int sp = v / per, s0 = begin_of(sp), s1 = begin_of(sp + 1);
+             int bi, bj;
+             block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+             mine.A += (long)s0 * BKS;
+             mine.B += (long)s0 * BKS * o.ldb;
+             mine.Kl = (o.Kl < s1 * BKS ? o.Kl : s1 * BKS) - s0 * BKS;
+             n = s1 - s0;
+             i0 = bi * BM;
+             j0 = bj * 256;
+         },
+         [&](typename R::Tile &w, int v, int i0, int j0) {
+             int el = lane;
+             asm volatile("" : "+v"(el));
+             w.template store<float, false, false>(slab, part + v / per * stride, i0 + wave / R::WAVES_N * R::WM, j0 + wave % R::WAVES_N * R::WN, rows, ldx, 0, 1 << 30, 1,
+                                                   el);
+         });
 }
 
 // dW = dz^T X over the listed rows of a chunk: straight to dW (bf16), or to parts in fp32, added to what is there behind the first chunk.
+typedef Ring<256, 256, 2, 4, 4, true, true, false> DwFull;
+typedef Ring<128, 256, 2, 4, 5, true, true, false> DwHalf;
+static_assert(DwHalf::SLABS_AT <= DwFull::SLABS_AT && DwHalf::LDS_BYTES <= DwFull::LDS_BYTES, "LDS of walk_list");
+
 template <typename TO, bool ACC>
-__global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *count, const float *scale, int first, int cap, int vocab, int splits, TO *out,
+__global__ __launch_bounds__(512) void vocab_dw_kernel(const Operands o, const int *count, const float *scale, int first, int cap, int vocab, int splits, TO *out,
                                                        size_t stride, int ldo)
 {
     using namespace pipe;
-    typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
     extern __shared__ __align__(16) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    char *slab = smem + 4 * R::STAGE_BYTES + wave * R::SLAB;
     const uint32_t smem_lds = (uint32_t)(uintptr_t)STL_LDS(smem);
     int rows = *count - first;
     if (rows > cap) rows = cap;
@@ -320,43 +302,33 @@ __global__ __launch_bounds__(512) void vocab_dw_kernel(Operands o, const int *co
         if (ACC) return;                                     // nothing to add
         rows = 0;
     }
-    const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, per = tiles_m * tiles_n, total = per * splits, stages = (rows + BKS - 1) / BKS;
-    R ring;
-    ring.init(wave, lane);
+    const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, per = tiles_m * tiles_n, stages = (rows + BKS - 1) / BKS;
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
-    auto start_block = [&](int v) {
-        const int sp = v / per, s0 = begin_of(sp);
-        int bi, bj;
-        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
-        Operands mine = o;
-        mine.A += (long)s0 * BKS * o.lda;
-        mine.B += (long)s0 * BKS * o.ldb;
-        ring.start(mine, begin_of(sp + 1) - s0, bi * 256, bj * 256, smem_lds, wave, lane);
-    };
-    const int step = block_step(), end = end_block(total);
-    int v = first_block(total);
-    if (v < end) start_block(v);
-    for (; v < end; v += step) {
-        const int sp = v / per;
-        int bi, bj;
-        block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
-        ring.block(
-            begin_of(sp + 1) - begin_of(sp), smem, smem_lds, wave, lane,
-            [&]() {
-                if (v + step < end) start_block(v + step);
-            },
-            [&](typename R::Tile &w) {
-                int el = lane;
-                asm volatile("" : "+v"(el));
-                if constexpr (sizeof(TO) == 2) {
-                    const float factor = scale[1];
-                    static_for<0, R::FM>([&](auto a_c) {
-                        static_for<0, R::FN>([&](auto b_c) { w.acc[decltype(a_c)::value][decltype(b_c)::value] *= factor; });
-                    });
-                }
-                w.template store<TO, ACC, false>(slab, out + sp * stride, bi * 256 + wave / 4 * R::WM, bj * 256 + wave % 4 * R::WN, vocab, ldo, 0, 1 << 30, 1, el);
-            });
-    }
+    walk_list<DwFull, DwHalf>(
+        per * splits, vocab, o, smem, smem_lds, wave, lane,
+        [&](int v, Operands &mine, int &n, int &i0, int &j0) {
+            const int sp = v / per, s0 = begin_of(sp);
+            int bi, bj;
+            block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+            mine.A += (long)s0 * BKS * o.lda;
+            mine.B += (long)s0 * BKS * o.ldb;
+            n = begin_of(sp + 1) - s0;
+            i0 = bi * 256;
+            j0 = bj * 256;
+        },
+        [&](auto &w, int v, int i0, int j0) {
+            constexpr int FM = sizeof(w.acc) / sizeof(w.acc[0]);
+            char *slab = smem + (FM == DwFull::FM ? DwFull::SLABS_AT : DwHalf::SLABS_AT) + wave * DwFull::SLAB;
+            int el = lane;
+            asm volatile("" : "+v"(el));
+            if constexpr (sizeof(TO) == 2) {
+                const float factor = scale[1];
+                static_for<0, FM>([&](auto a_c) {
+                    static_for<0, 4>([&](auto b_c) { w.acc[decltype(a_c)::value][decltype(b_c)::value] *= factor; });
+                });
+            }
+            w.template store<TO, ACC, false>(slab, out + v / per * stride, i0 + wave / 4 * 16 * FM, j0 + wave % 4 * 64, vocab, ldo, 0, 1 << 30, 1, el);
+        });
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------------
@@ -380,9 +352,9 @@ static hipError_t launch_logits_as(const Operands &o, const int *count, int firs
     };
     if (cap <= 16) return few(vocab_logits_few_kernel<1, CODES, TWO>);
     if (cap <= 32) return few(vocab_logits_few_kernel<2, CODES, TWO>);
-    typedef Ring<256, 256, 2, 4, 4, false, false, false> R;
+    typedef LogitsFull R;
     static std::atomic<uint64_t> granted{0};                 // of this instantiation
-    return launch_ring(vocab_logits_kernel<CODES, TWO>, granted, R::LDS_BYTES, R::THREADS, (long)((cap + 255) / 256) * ((vocab + 255) / 256), s, o, count, first, cap,
+    return launch_ring(vocab_logits_kernel<CODES, TWO>, granted, R::LDS_BYTES, R::THREADS, 2L * ((cap + 255) / 256) * ((vocab + 255) / 256), s, o, count, first, cap,
                        vocab, out);
 }
 static hipError_t launch_logits(const Operands &o, const int *count, int first, int cap, int vocab, const LogitsOut &out, bool two, hipStream_t s)
@@ -402,9 +374,9 @@ static hipError_t launch_dx(const Operands &o, const int *count, int first, int 
 template <typename TO, bool ACC>
 static hipError_t launch_dw(const Operands &o, const RowList &rl, int first, int cap, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
 {
-    typedef Ring<256, 256, 2, 4, 4, true, true, false> R;
+    typedef DwFull R;
     static std::atomic<uint64_t> granted{0};
-    return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, (long)((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o,
+    return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, 2L * ((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o,
                        (const int *)rl.count, (const float *)rl.scale, first, cap, vocab, splits, out, stride, ldo);
 }
 
