@@ -56,11 +56,11 @@ struct VocabGrads {
     void *dX, *dW;                           // storage type, either may be NULL
 };
 constexpr int kMostTop = 1024;
-// A logit between its product and its gradient is held (bf16 storage) in 16 bits: as one of kSteps even steps from its group's maximum down to its
+// A logit between its product and its gradient is held (bf16 storage) in 16 bits: as one of 65534 even steps from its group's maximum down to its
 // minimum, 65535 for what is below every share that fp32 can hold (minus infinity among it).  A group of 64 normal logits spreads over five
 // deviations: at a deviation of 2 a step is 1.5e-4, that is an error of exp(z) of 4e-5 (root mean square), a fortieth of the rounding of the gradient
 // to bf16 that follows (as bf16 exponentials they would add that rounding once more).  In terms of z / tau it is 1 / tau of that.
-constexpr float kSteps = 65534.f, kLowestTau = 0.25f, kHighestTau = 16.f;
+constexpr float kSteps = 65535.f, kLowestTau = 0.25f, kHighestTau = 16.f;
 size_t vocab_workspace_bytes(const VocabArgs &a, bool grads);
 // label_loss, top_loss: rows fp32 or NULL; g NULL: losses alone
 hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, void *ws, hipStream_t s);
@@ -82,13 +82,17 @@ hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList 
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
 
 // Logits of one chunk of listed rows on their way to the gradient (storage fp32: the logits themselves).  bf16: what the product leaves for
-// every listed row and group of 64 columns: the largest logit m, sums of exp(z - m) and exp((z - m) / tau), and with gradients the logits as 16-bit
-// steps below m and the size of a step.
+// every listed row and group of 64 columns, with y = z log2(e) / t, t = 1 where there are labels and tau otherwise: the largest y, m, the sums of
+// 2^(y - m) and of 2^((y - m) / tau), and with gradients y as 16-bit steps below m and the size of a step.
+struct alignas(16) GroupSums {
+    float m, sum, sum_tau, step;
+};
 struct VocabChunk {
     int first, cap;                          // listed rows first .. first + cap (those that exist)
     void *codes;                             // cap x ld: 16 bits (bf16 storage) or fp32 logits; the gradient is written in their place
     size_t ld;
-    float *group_max, *group_sum, *group_sum_tau, *group_step;      // cap x groups (bf16 storage); group_sum_tau only where tau is not 1 and both terms are there
+    const GroupSums *sums;                   // cap x groups (bf16 storage)
+    bool two;                                // they have the second sum: both terms are there and tau is not 1
     int groups;
     const void *Xc;                          // the listed rows, ldx elements each
     int ldx;

@@ -16,19 +16,115 @@ namespace lm {
 
 // ---- logits ------------------------------------------------------------------------------------------------------------------------
 struct LogitsOut {
-    float *group_max, *group_sum, *group_sum_tau, *group_step;
+    GroupSums *sums;
     int groups;
     uint16_t *codes;
     long ld;
-    float inv_tau;       // temperature of the first sum (1 with labels), and
-    float inv_tau2;      // of the second
-    float deepest;       // below a group's maximum by this much, no share is left in fp32
+    float scale;         // log2(e) over the temperature of the first sum: y = scale z
+    float ratio;         // the first temperature over the second
+    float deepest;       // below a group's maximum by this much in y, no share is left in fp32
 };
+
+// From a group's largest y and its spread to its smallest: what a step is, and what takes y to [0, 1] for the conversion to 16 bits, in which 1
+// is 65535.  The smallest y comes to lie on 65534.  (The order of the bounds makes any spread that is not a number a finite one.)
+struct Steps {
+    float size, mul, add;
+    __device__ __forceinline__ Steps(float ref, float spread, float deepest)
+    {
+        const float whole = fminf(fmaxf(spread, 1e-3f), deepest) * (kSteps / (kSteps - 1.f));
+        size = whole * (1.f / kSteps);
+        mul = -__builtin_amdgcn_rcpf(whole);                 // (an error of 1e-7 of it is 0.007 steps at the far end)
+        add = -ref * mul;
+    }
+};
+__device__ __forceinline__ uint32_t codes_of(float y0, float y1, const Steps &st)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(fmaf(y0, st.mul, st.add), fmaf(y1, st.mul, st.add)));
+}
 
 typedef Ring<256, 256, 2, 4, 4, false, false, false> LogitsFull;
 typedef Ring<128, 256, 2, 4, 5, false, false, false> LogitsHalf;
 static_assert(LogitsFull::WN == 64 && LogitsHalf::WN == 64, "a wavefront's columns are one group");
 static_assert(LogitsHalf::SLABS_AT <= LogitsFull::SLABS_AT && LogitsHalf::LDS_BYTES <= LogitsFull::LDS_BYTES, "LDS of walk_list");
+
+// What a wavefront makes of its 16 FM x 64 products: the group's sums for every row, and the codes.  WHOLE: all columns are in the vocabulary.
+// A lane has the columns col0 + 16 b + 4 (lane / 16) + e of the rows row0 + 16 a + lane % 16.
+template <int FM, bool CODES, bool TWO, bool WHOLE>
+__device__ __forceinline__ void logits_out(pipe::acc4_t (&acc)[FM][4], int row0, int col0, int rows, int vocab, char *slab, int lane, const LogitsOut &out)
+{
+    // no contraction of y's product with what follows it: the losses have the same bits with and without gradients
+#pragma clang fp contract(off)
+    using pipe::static_for;
+    constexpr int PA = 2;                                    // fragment rows that the slab holds: 16 rows of 128 bytes each
+    int el = lane;                                           // opaque: what follows from it is not kept over the products
+    asm volatile("" : "+v"(el));
+    const int quad = el >> 4, rl = el & 15, col = col0 + 4 * quad, group = col0 / 64;
+    static_for<0, FM / PA>([&](auto pass_c) {
+        constexpr int a0 = decltype(pass_c)::value * PA;
+        static_for<0, PA>([&](auto a_c) {
+            constexpr int a = a0 + decltype(a_c)::value;
+            // (scaled first: of products the compiler knows that they are in canonical form, into which it has to bring every operand of a maximum
+            // that may not be)
+            float y[16], m = -INFINITY, least = INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                y[i] = acc[a][i / 4][i % 4] * out.scale;
+                if constexpr (!WHOLE) {
+                    const bool in = col + 16 * (i / 4) + i % 4 < vocab;
+                    if constexpr (CODES) least = fminf(least, in ? y[i] : INFINITY);
+                    y[i] = in ? y[i] : -INFINITY;
+                } else if constexpr (CODES) {
+                    least = fminf(least, y[i]);
+                }
+                m = fmaxf(m, y[i]);
+            }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            if constexpr (CODES) {
+                least = fminf(least, __shfl_xor(least, 16));
+                least = fminf(least, __shfl_xor(least, 32));
+            }
+            // a group of nothing but minus infinities: 2^(-inf - 0), not 2^(-inf + inf)
+            const float ref = m == -INFINITY ? 0.f : m;
+            float s = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float below = y[i] - ref;
+                s += __builtin_amdgcn_exp2f(below);
+                if constexpr (TWO) s2 += __builtin_amdgcn_exp2f(below * out.ratio);
+            }
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            if constexpr (TWO) {
+                s2 += __shfl_xor(s2, 16);
+                s2 += __shfl_xor(s2, 32);
+            }
+            const Steps st(ref, ref - least, out.deepest);
+            const int row = row0 + 16 * a + rl;
+            if (quad == 0 && row < rows) out.sums[(size_t)row * out.groups + group] = GroupSums{m, s, s2, st.size};
+            if constexpr (CODES) {
+                char *rowp = slab + (16 * (a - a0) + rl) * 128;
+                const int swz = (rl >> 1) & 7;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<u32x2_t *>(rowp + (((2 * b + (quad >> 1)) ^ swz) << 4) + (quad & 1) * 8) =
+                        u32x2_t{codes_of(y[4 * b], y[4 * b + 1], st), codes_of(y[4 * b + 2], y[4 * b + 3], st)};
+            }
+        });
+        if constexpr (CODES) {
+            // rows leave as whole 128-byte lines; a wavefront's LDS operations execute in order
+            asm volatile("" ::: "memory");
+            const int rr = el >> 3, rc = el & 7;
+#pragma unroll
+            for (int i = 0; i < PA * 2; ++i) {
+                const int row = i * 8 + rr, gi = row0 + a0 * 16 + row;
+                const u32x4_t piece = *reinterpret_cast<const u32x4_t *>(slab + row * 128 + ((rc ^ ((row >> 1) & 7)) << 4));
+                if (gi < rows) *reinterpret_cast<u32x4_t *>(out.codes + (size_t)gi * out.ld + col0 + rc * 8) = piece;
+            }
+            asm volatile("" ::: "memory");
+        }
+    });
+}
 
 // listed rows of the chunk: count - first, a device value, at most cap
 template <bool CODES, bool TWO>
@@ -52,104 +148,11 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
             j0 = bj * 256;
         },
         [&](auto &w, int, int i0, int j0) {
-                constexpr int FM = sizeof(w.acc) / sizeof(w.acc[0]), FN = 4, WM = 16 * FM;
-                char *slab = smem + (FM == LogitsFull::FM ? LogitsFull::SLABS_AT : LogitsHalf::SLABS_AT) + wave * LogitsFull::SLAB;
-                int el = lane;                               // opaque: what follows from it is not kept over the products
-                asm volatile("" : "+v"(el));
-                const int row0 = i0 + wave / 4 * WM, col0 = j0 + wave % 4 * 64, quad = el >> 4, rl = el & 15;
-                const int col = col0 + 4 * quad;             // the lane's columns: col + 16 b + e
-                const bool whole = col0 + 64 <= vocab;
-                if (col0 >= vocab && (!CODES || col0 >= out.ld)) return;
-                const int group = col0 / 64;
-                const float scale = out.inv_tau * 1.44269504088896340736f, scale2 = out.inv_tau2 * 1.44269504088896340736f;
-                constexpr int PA = 2;                        // fragment rows that the slab holds: 16 rows of 128 bytes each
-                static_for<0, FM / PA>([&](auto pass_c) {
-                    constexpr int a0 = decltype(pass_c)::value * PA;
-                    static_for<0, PA>([&](auto a_c) {
-                        constexpr int a = a0 + decltype(a_c)::value;
-                        float m = -INFINITY, least = INFINITY;
-                        if (!whole) {
-#pragma unroll
-                            for (int b = 0; b < FN; ++b)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const bool in = col + 16 * b + e < vocab;
-                                    if constexpr (CODES) least = fminf(least, in ? w.acc[a][b][e] : least);
-                                    w.acc[a][b][e] = in ? w.acc[a][b][e] : -INFINITY;
-                                }
-                        } else if constexpr (CODES) {
-#pragma unroll
-                            for (int b = 0; b < FN; ++b)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) least = fminf(least, w.acc[a][b][e]);
-                        }
-#pragma unroll
-                        for (int b = 0; b < FN; ++b)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) m = fmaxf(m, w.acc[a][b][e]);
-                        m = fmaxf(m, __shfl_xor(m, 16));
-                        m = fmaxf(m, __shfl_xor(m, 32));
-                        // a group of nothing but minus infinities: exp(-inf - 0), not exp(-inf + inf)
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        float s = 0.f, s2 = 0.f;
-#pragma unroll
-                        for (int b = 0; b < FN; ++b)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float below = w.acc[a][b][e] - ref;
-                                s += __builtin_amdgcn_exp2f(below * scale);
-                                if constexpr (TWO) s2 += __builtin_amdgcn_exp2f(below * scale2);
-                            }
-                        s += __shfl_xor(s, 16);
-                        s += __shfl_xor(s, 32);
-                        if constexpr (TWO) {
-                            s2 += __shfl_xor(s2, 16);
-                            s2 += __shfl_xor(s2, 32);
-                        }
-                        float per_step = 0.f, steps = 0.f;
-                        if constexpr (CODES) {
-                            least = fminf(least, __shfl_xor(least, 16));
-                            least = fminf(least, __shfl_xor(least, 32));
-                            // (the order of the bounds makes any spread that is not a number a finite one)
-                            const float spread = fminf(fmaxf(ref - least, 1e-3f), out.deepest);
-                            per_step = spread * (1.f / kSteps);
-                            steps = kSteps / spread;
-                        }
-                        const size_t at = (size_t)(row0 + 16 * a + rl) * out.groups + group;
-                        if (quad == 0 && row0 + 16 * a + rl < rows && group < out.groups) {
-                            out.group_max[at] = m;
-                            out.group_sum[at] = s;
-                            if constexpr (TWO) out.group_sum_tau[at] = s2;
-                            if constexpr (CODES) out.group_step[at] = per_step;
-                        }
-                        if constexpr (CODES) {
-                            char *rowp = slab + (16 * (a - a0) + rl) * 128;
-                            const int swz = (rl >> 1) & 7;
-#pragma unroll
-                            for (int b = 0; b < FN; ++b) {
-                                uint32_t c[4];
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    c[e] = (uint32_t)fminf((ref - w.acc[a][b][e]) * steps + 0.5f, 65535.f);
-                                }
-                                *reinterpret_cast<u32x2_t *>(rowp + (((2 * b + (quad >> 1)) ^ swz) << 4) + (quad & 1) * 8) =
-                                    u32x2_t{c[0] | c[1] << 16, c[2] | c[3] << 16};
-                            }
-                        }
-                    });
-                    if constexpr (CODES) {
-                        // rows leave as whole 128-byte lines; a wavefront's LDS operations execute in order
-                        asm volatile("" ::: "memory");
-                        const int rr = el >> 3, rc = el & 7;
-#pragma unroll
-                        for (int i = 0; i < PA * 2; ++i) {
-                            const int row = i * 8 + rr, gi = row0 + a0 * 16 + row;
-                            const u32x4_t piece = *reinterpret_cast<const u32x4_t *>(slab + row * 128 + ((rc ^ ((row >> 1) & 7)) << 4));
-                            if (gi < rows && col0 + rc * 8 < out.ld) *reinterpret_cast<u32x4_t *>(out.codes + (size_t)gi * out.ld + col0 + rc * 8) = piece;
-                        }
-                        asm volatile("" ::: "memory");
-                    }
-                });
+            constexpr int FM = sizeof(w.acc) / sizeof(w.acc[0]);
+            char *slab = smem + (FM == LogitsFull::FM ? LogitsFull::SLABS_AT : LogitsHalf::SLABS_AT) + wave * LogitsFull::SLAB;
+            const int row0 = i0 + wave / 4 * 16 * FM, col0 = j0 + wave % 4 * 64;
+            if (col0 + 64 <= vocab) logits_out<FM, CODES, TWO, true>(w.acc, row0, col0, rows, vocab, slab, lane, out);
+            else if (col0 < vocab) logits_out<FM, CODES, TWO, false>(w.acc, row0, col0, rows, vocab, slab, lane, out);
         });
 }
 
@@ -223,26 +226,24 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_few_kernel(const Operands
 #pragma unroll
             for (int e = 0; e < 4; ++e) sums[(wave * ROWS + 16 * f + 4 * kq + e) * 64 + 16 * c + n16] = acc[f][c][e];
     __syncthreads();
-    const float scale = out.inv_tau * 1.44269504088896340736f, scale2 = out.inv_tau2 * 1.44269504088896340736f;
     const bool in = col0 + lane < vocab;
     for (int r = wave; r < ROWS && r < rows; r += NW) {
-        float z = 0.f;
+#pragma clang fp contract(off)
+        float y = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) z += sums[(w * ROWS + r) * 64 + lane];
-        z = in ? z : -INFINITY;
-        const float m = wave_max(z), ref = m == -INFINITY ? 0.f : m, below = z - ref;
-        const float s = wave_sum(__builtin_amdgcn_exp2f(below * scale));
+        for (int w = 0; w < NW; ++w) y += sums[(w * ROWS + r) * 64 + lane];
+        y = in ? y * out.scale : -INFINITY;
+        const float m = wave_max(y), ref = m == -INFINITY ? 0.f : m, below = y - ref;
+        const float s = wave_sum(__builtin_amdgcn_exp2f(below));
         float s2 = 0.f, spread = 0.f;
-        if constexpr (TWO) s2 = wave_sum(__builtin_amdgcn_exp2f(below * scale2));
-        if constexpr (CODES) spread = fminf(fmaxf(wave_max(in ? -below : 0.f), 1e-3f), out.deepest);
+        if constexpr (TWO) s2 = wave_sum(__builtin_amdgcn_exp2f(below * out.ratio));
+        if constexpr (CODES) spread = wave_max(in ? -below : 0.f);
+        const Steps st(ref, spread, out.deepest);
         if (lane == 0) {
             const size_t at = (size_t)r * out.groups + blockIdx.x;
-            out.group_max[at] = m;
-            out.group_sum[at] = s;
-            if constexpr (TWO) out.group_sum_tau[at] = s2;
-            if constexpr (CODES) out.group_step[at] = spread * (1.f / kSteps);
+            out.sums[at] = GroupSums{m, s, s2, st.size};
         }
-        if constexpr (CODES) out.codes[(size_t)r * out.ld + col0 + lane] = (uint16_t)(uint32_t)fminf(-below * (kSteps / spread) + 0.5f, 65535.f);
+        if constexpr (CODES) out.codes[(size_t)r * out.ld + col0 + lane] = (uint16_t)(codes_of(y, y, st) & 0xffffu);
     }
 }
 
@@ -399,7 +400,7 @@ struct Plan {
     Splits dx;
     int dw_splits;
     bool dw_parts;           // dW through fp32 parts
-    size_t list, count, scale, xc, wp, gmax, gsum, gsum2, gstep, codes, dx_part, dw_part, dw_stride, total;
+    size_t list, count, scale, xc, wp, sums, codes, dx_part, dw_part, dw_stride, total;
 };
 
 Plan plan_of(const VocabArgs &a, bool grads)
@@ -429,11 +430,8 @@ Plan plan_of(const VocabArgs &a, bool grads)
         p.ldz = (size_t)p.groups * 64;
         p.xc = take((size_t)p.rows_held * p.ldx * 2);
         if (p.pack_w) p.wp = take((size_t)a.vocab * p.ldx * 2);
-        p.gmax = take((size_t)p.cap * p.groups * sizeof(float));
-        p.gsum = take((size_t)p.cap * p.groups * sizeof(float));
-        if (a.ntop && a.tau != 1.f) p.gsum2 = take((size_t)p.cap * p.groups * sizeof(float));
+        p.sums = take((size_t)p.cap * p.groups * sizeof(GroupSums));
         if (grads) {
-            p.gstep = take((size_t)p.cap * p.groups * sizeof(float));
             p.codes = take((size_t)p.rows_held * p.ldz * 2);
             p.dx = Splits{p.small ? 64 : 256, (a.d + 255) / 256, (a.vocab + pipe::BKS - 1) / pipe::BKS};
             p.dx_part = take((size_t)p.dx.rows(p.cap) * p.ldx * sizeof(float));
@@ -474,16 +472,15 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
         LM_TRY(launch_pad_rows(a.W, a.vocab, a.d, p.ldx, base + p.wp, s));
         W = (const bf16_t *)(base + p.wp);
     }
-    const bool two = p.gsum2 != 0 && a.label;
-    const float inv_tau = 1.f / a.tau;
+    const bool two = a.label && a.ntop && a.tau != 1.f;
+    const float inv_tau = 1.f / a.tau, scale = 1.44269504088896340736f * (a.label ? 1.f : inv_tau);
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap;
         LM_TRY(launch_arrange_rows(a, g, rl, first, p.rows_held, p.ldx, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
-        const LogitsOut lo{(float *)(base + p.gmax), (float *)(base + p.gsum), two ? (float *)(base + p.gsum2) : nullptr,
-                           (float *)(base + p.gstep), p.groups, codes, (long)p.ldz, a.label ? 1.f : inv_tau, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f)};
+        const LogitsOut lo{(GroupSums *)(base + p.sums), p.groups, codes, (long)p.ldz, scale, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f) * scale};
         LM_TRY(launch_logits(logits, rl.count, first, p.cap, a.vocab, lo, two, s));
-        const VocabChunk c{first, p.cap, codes, p.ldz, lo.group_max, lo.group_sum, lo.group_sum_tau, lo.group_step, p.groups, xc, p.ldx};
+        const VocabChunk c{first, p.cap, codes, p.ldz, lo.sums, two, p.groups, xc, p.ldx};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             const Operands o{codes, W, (long)p.ldz, p.ldx, p.rows_held, p.ldx, a.vocab};
@@ -513,7 +510,7 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
         LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
         LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false}, s));
-        const VocabChunk c{first, cap, z, p.ldz, nullptr, nullptr, nullptr, nullptr, 0, xc, a.d};
+        const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0, xc, a.d};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false}, s));

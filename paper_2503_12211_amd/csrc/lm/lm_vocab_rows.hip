@@ -212,8 +212,7 @@ __device__ __forceinline__ float block_sum(float v, float *red)
     return v;
 }
 
-constexpr float kLog2e = 1.44269504088896340736f;
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // One listed row a workgroup.  With p = softmax(z), p_tau = softmax(z / tau), q the teacher's shares and their entries id_j:
 //     label_loss = lse - z_label,   top_loss = sum_j q_j (log q_j - z_id_j / tau + lse_tau),
@@ -226,6 +225,8 @@ template <typename T, bool GRADS>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const VocabGrads g, const T *W, int d, float tau, const int *list, const int *count,
                                                                  const float *scale, VocabChunk c, float *label_loss, float *top_loss)
 {
+    // (no contraction: the losses have the same bits with and without gradients)
+#pragma clang fp contract(off)
     constexpr bool BF16 = sizeof(T) == 2;
     __shared__ float red[kRowWaves];
     __shared__ int ids[kMostTop + 1];        // the entries', and behind them the label's
@@ -266,19 +267,26 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
     }
     __syncthreads();
 
-    // log of the sums over the vocabulary; with one term the product keeps one sum, of that term's temperature
-    float m = -INFINITY, sum = 0.f, sum_tau = 0.f;
-    const float *gm = nullptr;
+    // log of the sums over the vocabulary; bf16 storage, in powers of two: y of VocabChunk, whose first sum is of the labels' temperature, 1, or, without
+    // labels, of the teacher's; the second is there where both are and differ
+    float m = -INFINITY, sum = 0.f, sum_tau = 0.f, lse, lse_tau;
+    float lse2 = 0.f, lse2_tau = 0.f, ratio = 1.f;
+    const GroupSums *groups = nullptr;
     if constexpr (BF16) {
-        gm = c.group_max + (size_t)r * c.groups;
-        const float *gs = c.group_sum + (size_t)r * c.groups, *gt = c.group_sum_tau ? c.group_sum_tau + (size_t)r * c.groups : nullptr;
-        for (int i = tid; i < c.groups; i += kRowThreads) m = fmaxf(m, gm[i]);
+        groups = c.sums + (size_t)r * c.groups;
+        ratio = c.two ? inv_tau : 1.f;
+        for (int i = tid; i < c.groups; i += kRowThreads) m = fmaxf(m, groups[i].m);
         m = block_max(m, red);
         for (int i = tid; i < c.groups; i += kRowThreads) {
-            const float below = gm[i] - m;
-            sum += gs[i] * exp_fast(t.label ? below : below * inv_tau);
-            if (gt) sum_tau += gt[i] * exp_fast(below * inv_tau);
+            const GroupSums g = groups[i];
+            const float below = g.m - m;
+            sum += g.sum * __builtin_amdgcn_exp2f(below);
+            if (c.two) sum_tau += g.sum_tau * __builtin_amdgcn_exp2f(below * ratio);
         }
+        sum = block_sum(sum, red);
+        sum_tau = c.two ? block_sum(sum_tau, red) : sum;
+        lse2 = m + log2f(sum), lse2_tau = m * ratio + log2f(sum_tau);
+        lse = lse2 * kLn2, lse_tau = lse2_tau * kLn2;
     } else {
         const float *Z = (const float *)codes;
         for (int v = tid; v < vocab; v += kRowThreads) m = fmaxf(m, Z[v]);
@@ -287,12 +295,10 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
             sum += expf(Z[v] - m);
             if (ntop) sum_tau += expf((Z[v] - m) * inv_tau);
         }
+        sum = block_sum(sum, red);
+        sum_tau = block_sum(sum_tau, red);
+        lse = m + logf(sum), lse_tau = m * inv_tau + logf(sum_tau);
     }
-    sum = block_sum(sum, red);
-    sum_tau = block_sum(sum_tau, red);
-    if constexpr (BF16)
-        if (!c.group_sum_tau) sum_tau = sum;
-    const float lse = m + logf(sum), lse_tau = m * inv_tau + logf(sum_tau);
 
     // the logits of the label and the teacher's entries
     if constexpr (BF16) {
@@ -371,21 +377,19 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
         const float cl = labelled && g.dlabel ? g.dlabel[row] * factor : 0.f, ct = taught && g.dtop ? g.dtop[row] * inv_tau * factor : 0.f;
         if constexpr (BF16) {
             // chunks of eight logits lie in one group of 64
-            const float *gstep = c.group_step + (size_t)r * c.groups;
             for (size_t v = (size_t)tid * 8; v < c.ld; v += kRowThreads * 8) {
                 const u32x4_t in = *reinterpret_cast<const u32x4_t *>(codes + v);
-                const float mg = gm[v / 64], step = gstep[v / 64];
-                const float at = mg - lse, at_tau = mg * inv_tau - lse_tau;
+                const float mg = groups[v / 64].m, step = groups[v / 64].step;
+                const float at = mg - lse2, at_tau = mg * ratio - lse2_tau, step_tau = step * ratio;
                 float out[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t code = (in[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-                    const float below = -(float)code * step;
                     float dz = 0.f;
-                    if (labelled) dz = cl * exp_fast(at + below);
-                    if (taught) dz = fmaf(ct, exp_fast(fmaf(below, inv_tau, at_tau)), dz);
+                    if (labelled) dz = cl * __builtin_amdgcn_exp2f(fmaf(-(float)code, step, at));
+                    if (taught) dz = fmaf(ct, __builtin_amdgcn_exp2f(fmaf(-(float)code, step_tau, at_tau)), dz);
                     // a row whose sums are not a number stays one throughout
-                    out[e] = code == 65535u && lse == lse ? 0.f : dz;
+                    out[e] = code == 65535u && m + sum == m + sum ? 0.f : dz;
                 }
                 *reinterpret_cast<u32x4_t *>(codes + v) =
                     u32x4_t{pack_bf16x2(out[0], out[1]), pack_bf16x2(out[2], out[3]), pack_bf16x2(out[4], out[5]), pack_bf16x2(out[6], out[7])};

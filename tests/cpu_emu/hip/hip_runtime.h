@@ -178,6 +178,13 @@ inline char *cpu_dyn_lds_ptr() { return emu::dyn_lds_ptr; }
 inline float __uint_as_float(uint32_t u) { float f; memcpy(&f, &u, 4); return f; }
 inline uint32_t __float_as_uint(float f) { uint32_t u; memcpy(&u, &f, 4); return u; }
 inline float rsqrtf(float x) { return 1.0f / sqrtf(x); }
+typedef unsigned short emu_u16x2 __attribute__((ext_vector_type(2)));
+inline emu_u16x2 emu_pknorm(float a, float b)
+{
+    auto one = [](float x) { return (unsigned short)(x >= 1.0f ? 65535 : x > 0.0f ? (int)nearbyintf(x * 65535.0f) : 0); };
+    return emu_u16x2{one(a), one(b)};
+}
+#define __builtin_amdgcn_cvt_pknorm_u16(a, b) emu_pknorm(a, b)
 // uniform by construction where the kernels use it
 #define __builtin_amdgcn_readfirstlane(x) (x)
 #define __builtin_amdgcn_sched_barrier(x) ((void)0)
