@@ -17,15 +17,20 @@ struct Operands {
     int Kl;
 };
 
-// Blocks in groups of GM block rows, down the columns of a group first: the 32 workgroups of an XCD, side by side in the list, then share 4 rows of
-// the first operand and 8 columns of the second in their L2 instead of 1 and 32 (4096 x 65536 x 4096: 1735 us, 2090 row by row, 1846 in groups of 16).
-constexpr int kGroupRows = 4;
-__device__ __forceinline__ void block_at(int v, int tiles_m, int tiles_n, int &bi, int &bj)
+// Blocks in groups of about four block rows, down the columns of a group first: the 32 workgroups of an XCD, side by side in the list, then share 4 rows
+// of the first operand and 8 columns of the second in their L2 instead of 1 and 32 (4096 x 65536 x 4096: 1735 us, 2090 row by row, 1846 in groups of
+// 16).  Groups are of even size: of five rows one group of five, not of four and one (1280 x 50176 x 1024: 124 us and 135).
+__device__ __forceinline__ int group_rows(int tiles_m)
 {
-    const int per = kGroupRows * tiles_n, q = v / per, rem = v - q * per;
-    const int rows = tiles_m - q * kGroupRows < kGroupRows ? tiles_m - q * kGroupRows : kGroupRows;
+    const int groups = tiles_m < 7 ? 1 : (tiles_m + 1) / 4;
+    return (tiles_m + groups - 1) / groups;
+}
+__device__ __forceinline__ void block_at(int v, int tiles_m, int tiles_n, int size, int &bi, int &bj)
+{
+    const int per = size * tiles_n, q = v / per, rem = v - q * per;
+    const int rows = tiles_m - q * size < size ? tiles_m - q * size : size;
     bj = rem / rows;
-    bi = q * kGroupRows + rem - bj * rows;
+    bi = q * size + rem - bj * rows;
 }
 
 template <int BM_, int BN_, int WAVES_M, int WAVES_N_, int NS, bool A_T, bool B_T, bool KTAIL>

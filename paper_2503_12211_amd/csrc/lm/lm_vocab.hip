@@ -137,12 +137,12 @@ __global__ __launch_bounds__(512) void vocab_logits_kernel(const Operands o, con
     int rows = *count - first;
     if (rows > cap) rows = cap;
     if (rows <= 0) return;
-    const int tiles_m = (rows + 255) / 256, tiles_n = (vocab + 255) / 256, nks = o.Kl / BKS;
+    const int tiles_m = (rows + 255) / 256, tiles_n = (vocab + 255) / 256, size = group_rows(tiles_m), nks = o.Kl / BKS;
     walk_list<LogitsFull, LogitsHalf>(
         tiles_m * tiles_n, rows, o, smem, smem_lds, wave, lane,
         [&](int v, Operands &, int &stages, int &i0, int &j0) {
             int bi, bj;
-            block_at(v, tiles_m, tiles_n, bi, bj);
+            block_at(v, tiles_m, tiles_n, size, bi, bj);
             stages = nks;
             i0 = bi * 256;
             j0 = bj * 256;
@@ -261,14 +261,14 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
     int rows = *count - first;
     if (rows > cap) rows = cap;
     if (rows <= 0) return;
-    const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
+    const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, size = group_rows(tiles_m), per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
     const size_t stride = (size_t)rows * ldx;
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
     walk(R{}, first_block(total), end_block(total), block_step(), o, smem, smem_lds, wave, lane,
          [&](int v, Operands &mine, int &n, int &i0, int &j0) {
              const int sp = v / per, s0 = begin_of(sp), s1 = begin_of(sp + 1);
              int bi, bj;
-             block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+             block_at(v - sp * per, tiles_m, tiles_n, size, bi, bj);
              mine.A += (long)s0 * BKS;
              mine.B += (long)s0 * BKS * o.ldb;
              mine.Kl = (o.Kl < s1 * BKS ? o.Kl : s1 * BKS) - s0 * BKS;
@@ -303,14 +303,14 @@ __global__ __launch_bounds__(512) void vocab_dw_kernel(const Operands o, const i
         if (ACC) return;                                     // nothing to add
         rows = 0;
     }
-    const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, per = tiles_m * tiles_n, stages = (rows + BKS - 1) / BKS;
+    const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, size = group_rows(tiles_m), per = tiles_m * tiles_n, stages = (rows + BKS - 1) / BKS;
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
     walk_list<DwFull, DwHalf>(
         per * splits, vocab, o, smem, smem_lds, wave, lane,
         [&](int v, Operands &mine, int &n, int &i0, int &j0) {
             const int sp = v / per, s0 = begin_of(sp);
             int bi, bj;
-            block_at(v - sp * per, tiles_m, tiles_n, bi, bj);
+            block_at(v - sp * per, tiles_m, tiles_n, size, bi, bj);
             mine.A += (long)s0 * BKS * o.lda;
             mine.B += (long)s0 * BKS * o.ldb;
             n = begin_of(sp + 1) - s0;
