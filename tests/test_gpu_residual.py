@@ -269,3 +269,31 @@ def test_no_rows():
     assert bool((dw == 3.0).all())
     stl.stl_residual_norm_backward(prob, None, None, None, None, None, None, None, None, None, None, None, dw, None, None, None, 0, None, 0, flags)
     assert not dw.any()
+
+
+def test_more_elements_than_32_bits_count():
+    """Rows behind the 2^31st element: the same bits as those rows alone."""
+    rows, n = 140000, 16384
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("not enough free memory")
+    p = problem(8, n, "bf16", 8, True, True, True, True, False, 91)
+    t = to_dev(p, "bf16")
+    flags = flags_of(True, True, False)
+    small = stl.ResidualProblem(8, n)
+    Xout, Z = gpu_forward(small, t, flags, "bf16")
+    got = gpu_backward(small, t, Xout, flags, "bf16")
+    big = {k: torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda") for k in ("X", "H", "dXout", "dZ")}
+    for k, v in big.items():
+        v[-8:] = t[k]
+    prob = stl.ResidualProblem(rows, n)
+    out, z = torch.empty_like(big["X"]), torch.empty_like(big["X"])
+    stl.stl_residual_norm_forward(prob, big["X"], big["H"], t["gate"], t["w_post"], None, t["w_pre"], None, out, z, flags)
+    assert torch.equal(out[-8:], Xout) and torch.equal(z[-8:], Z) and not out[:-8].any()
+    nbytes = stl.stl_residual_norm_workspace_bytes(prob, flags)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    dX, dH, dw = big["X"], z, torch.empty(n, device="cuda")
+    stl.stl_residual_norm_backward(prob, out, big["H"], t["gate"], t["w_post"], None, t["w_pre"], big["dXout"], big["dZ"], dX, dH, None, None, None, dw, None, 0,
+                                   ws, nbytes, flags)
+    assert torch.equal(dX[-8:], got["dX"]) and torch.equal(dH[-8:], got["dH"])
+    # rows of zeros add nothing: the sum of the eight rows, in another order
+    assert float((dw - got["dw_pre"]).abs().max()) <= 16 * EPS * float(got["dw_pre"].abs().max()) * 8
