@@ -68,23 +68,28 @@ __device__ __forceinline__ f32x4_t fragment(const float *tile, int row, int l0)
 }
 
 template <int GROUPS, bool A_ALONG, bool B_ALONG, bool ACC>
-__global__ __launch_bounds__(256 * GROUPS) void gemm_f32_kernel(Operand a, Operand b, int L, float *out, int tiles_n, int tiles)
+__global__ __launch_bounds__(256 * GROUPS) void gemm_f32_kernel(Operand a, Operand b, int L, float *out, int tiles_m, int tiles_n, int tiles)
 {
     extern __shared__ __align__(16) char smem[];
     const int t = (int)threadIdx.x & 255, group = (int)threadIdx.x >> 8, lane = t & 63, wave = t >> 6;
     // each XCD takes a contiguous eighth of the blocks
     const int v = (int)((long)(blockIdx.x & 7) * tiles / 8) + (int)(blockIdx.x >> 3);
     if (v >= (int)((long)((blockIdx.x & 7) + 1) * tiles / 8)) return;
-    const int i0 = v / tiles_n * BT, j0 = v % tiles_n * BT, wi = wave >> 1 << 5, wj = (wave & 1) << 5;
+    // down the columns of eight block rows first: the 128 blocks that an XCD has at a time share 8 rows of one operand and 16 columns of the other
+    const int per = 8 * tiles_n, q = v / per, rem = v - q * per, in_group = tiles_m - 8 * q < 8 ? tiles_m - 8 * q : 8;
+    const int i0 = (8 * q + rem % in_group) * BT, j0 = rem / in_group * BT, wi = wave >> 1 << 5, wj = (wave & 1) << 5;
     a.along = A_ALONG, b.along = B_ALONG;
     float *mine = reinterpret_cast<float *>(smem) + group * 4 * TILE;
     f32x16_t acc = {};
-    const int stages = (L + BK - 1) / BK, turns = (stages + GROUPS - 1) / GROUPS;
+    const int all = (L + BK - 1) / BK, s0 = (int)((long)all * blockIdx.y / gridDim.y), stages = (int)((long)all * (blockIdx.y + 1) / gridDim.y) - s0;
+    const int turns = (stages + GROUPS - 1) / GROUPS;
+    if (s0 + stages < all) L = (s0 + stages) * BK;
+    out += (size_t)blockIdx.y * a.rows * b.rows;
     Staged sa[2], sb[2];
     auto load = [&](int s, int k) {
         if (s < turns) {
-            sa[k].load(a, i0, (s * GROUPS + group) * BK, L, t);
-            sb[k].load(b, j0, (s * GROUPS + group) * BK, L, t);
+            sa[k].load(a, i0, (s0 + s * GROUPS + group) * BK, L, t);
+            sb[k].load(b, j0, (s0 + s * GROUPS + group) * BK, L, t);
         }
     };
     auto turn = [&](int s, auto k_c) {
@@ -134,36 +139,46 @@ __global__ __launch_bounds__(256 * GROUPS) void gemm_f32_kernel(Operand a, Opera
 }
 
 template <int GROUPS, bool A_ALONG, bool B_ALONG, bool ACC>
-hipError_t launch_as(const Operand &a, const Operand &b, int L, float *out, int tiles_n, int tiles, hipStream_t s)
+hipError_t launch_as(const Operand &a, const Operand &b, int L, float *out, int tiles_m, int tiles_n, int tiles, int splits, hipStream_t s)
 {
     auto kern = gemm_f32_kernel<GROUPS, A_ALONG, B_ALONG, ACC>;
     constexpr int lds = GROUPS * 4 * TILE * (int)sizeof(float);
     static std::atomic<uint64_t> granted{0};                 // of this instantiation
     if (const hipError_t e = allow_lds(reinterpret_cast<const void *>(kern), lds, lds, granted); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((tiles + 7) / 8 * 8), dim3(256 * GROUPS), lds, s, a, b, L, out, tiles_n, tiles);
+    hipLaunchKernelGGL(kern, dim3((tiles + 7) / 8 * 8, splits), dim3(256 * GROUPS), lds, s, a, b, L, out, tiles_m, tiles_n, tiles);
     return hipGetLastError();
 }
 
 }  // namespace f32
 
+int gemm_f32_splits(int I, int J, int L)
+{
+    using namespace f32;
+    const long tiles = (long)((I + BT - 1) / BT) * ((J + BT - 1) / BT);
+    const int stages = (L + BK - 1) / BK;
+    long n = tiles >= 512 ? 1 : 512 / tiles;
+    if (n > stages / 32) n = stages / 32;
+    return n > 16 ? 16 : n < 1 ? 1 : (int)n;
+}
+
 hipError_t launch_gemm_f32(const GemmF32 &g, hipStream_t s)
 {
     using namespace f32;
     const Operand a{g.A, g.a_along ? g.L : g.I, g.I, g.a_along}, b{g.B, g.b_along ? g.L : g.J, g.J, g.b_along};
-    const long tiles_n = (g.J + BT - 1) / BT, tiles = (long)((g.I + BT - 1) / BT) * tiles_n;
+    const long tiles_m = (g.I + BT - 1) / BT, tiles_n = (g.J + BT - 1) / BT, tiles = tiles_m * tiles_n;
     if (tiles > (1L << 30)) return hipErrorInvalidValue;
-    const int stages = (g.L + BK - 1) / BK;
+    const int stages = (g.L + BK - 1) / BK / g.splits;
     auto run = [&](auto groups_c) {
         constexpr int G = decltype(groups_c)::value;
-        if (g.a_along && !g.b_along) return launch_as<G, true, false, false>(a, b, g.L, g.Out, (int)tiles_n, (int)tiles, s);
-        if (g.a_along) return launch_as<G, true, true, false>(a, b, g.L, g.Out, (int)tiles_n, (int)tiles, s);
-        return g.accumulate ? launch_as<G, false, false, true>(a, b, g.L, g.Out, (int)tiles_n, (int)tiles, s)
-                            : launch_as<G, false, false, false>(a, b, g.L, g.Out, (int)tiles_n, (int)tiles, s);
+        if (g.a_along && !g.b_along) return launch_as<G, true, false, false>(a, b, g.L, g.Out, (int)tiles_m, (int)tiles_n, (int)tiles, g.splits, s);
+        if (g.a_along) return launch_as<G, true, true, false>(a, b, g.L, g.Out, (int)tiles_m, (int)tiles_n, (int)tiles, g.splits, s);
+        return g.accumulate ? launch_as<G, false, false, true>(a, b, g.L, g.Out, (int)tiles_m, (int)tiles_n, (int)tiles, g.splits, s)
+                            : launch_as<G, false, false, false>(a, b, g.L, g.Out, (int)tiles_m, (int)tiles_n, (int)tiles, g.splits, s);
     };
     if ((!g.a_along && g.b_along) || (g.accumulate && g.a_along)) return hipErrorInvalidValue;         // forms that no product here has
     // as many groups as make two blocks' worth of wavefronts a CU, where each has two stages at least
-    if (tiles < 256 && stages >= 8) return run(std::integral_constant<int, 4>{});
-    if (tiles < 512 && stages >= 4) return run(std::integral_constant<int, 2>{});
+    if (tiles * g.splits < 256 && stages >= 8) return run(std::integral_constant<int, 4>{});
+    if (tiles * g.splits < 512 && stages >= 4) return run(std::integral_constant<int, 2>{});
     return run(std::integral_constant<int, 1>{});
 }
 

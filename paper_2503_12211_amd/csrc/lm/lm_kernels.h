@@ -39,7 +39,10 @@ struct GemmF32 {
     bool b_along;
     float *Out;
     bool accumulate;         // of [l][i] and [l][j] only
+    int splits;              // of the contraction over workgroups: part s of the output lies s * I * J floats on
 };
+// as many as make two blocks a CU where there are fewer, of 32 stages at least
+int gemm_f32_splits(int I, int J, int L);
 hipError_t launch_gemm_f32(const GemmF32 &g, hipStream_t s);
 
 // ---- vocabulary loss (lm_vocab.hip, lm_vocab_rows.hip) -----------------------------------------------------------------------
@@ -102,7 +105,7 @@ hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl
 // least) as take the least time, us: rounds of blocks over the CUs of an MI355X, of 0.53 a stage and 5 beside, and 0.12 a block and run for writing its
 // fp32 part and adding it up.  Part s of `rows` rows lies s * rows * ld floats on.
 struct Splits {
-    int block_rows, tiles_n, stages;
+    int block_rows, tiles_n, stages;         // fp32 storage: 0, 0 and the number of parts, which the host knows
     static constexpr int kMost = 16, kBlocks = 1024;         // runs, and blocks of all runs where there is more than one
     __host__ __device__ int of(int rows) const
     {

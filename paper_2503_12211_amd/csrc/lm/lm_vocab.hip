@@ -452,7 +452,12 @@ Plan plan_of(const VocabArgs &a, bool grads)
         p.ldz = a.vocab;
         p.xc = take((size_t)p.cap * a.d * 4);
         p.codes = take((size_t)p.cap * p.ldz * 4);
-        if (grads) p.dx_part = take((size_t)p.cap * a.d * 4);
+        if (grads) {
+            // the last chunk has fewer rows, and may have more parts
+            const int last = a.rows - (p.chunks - 1) * p.cap;
+            const size_t some = (size_t)p.cap * gemm_f32_splits(p.cap, a.d, a.vocab), end = (size_t)last * gemm_f32_splits(last, a.d, a.vocab);
+            p.dx_part = take((some > end ? some : end) * a.d * 4);
+        }
     }
     p.total = at;
     return p;
@@ -509,14 +514,15 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
         LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, g ? g->dX : nullptr, label_loss, top_loss, s));
-        LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false}, s));
+        LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false, 1}, s));
         const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0, xc, a.d};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
-            LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false}, s));
-            LM_TRY(launch_finish_dx(false, dx, Splits{}, a.d, rl, first, cap, a.d, g->dX, s));
+            const int parts = gemm_f32_splits(cap, a.d, a.vocab);
+            LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false, parts}, s));
+            LM_TRY(launch_finish_dx(false, dx, Splits{0, 0, parts}, a.d, rl, first, cap, a.d, g->dX, s));
         }
-        if (g && g->dW) LM_TRY(launch_gemm_f32({a.vocab, a.d, cap, z, false, xc, false, (float *)g->dW, ch > 0}, s));
+        if (g && g->dW) LM_TRY(launch_gemm_f32({a.vocab, a.d, cap, z, false, xc, false, (float *)g->dW, ch > 0, 1}, s));
     }
     return hipSuccess;
 }

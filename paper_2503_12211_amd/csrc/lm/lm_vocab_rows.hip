@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, Split
     const int r = (int)blockIdx.x;
     if (r >= rows) return;
     const bool bf16 = sizeof(T) == 2;
-    finish_row(part + (size_t)r * ld, bf16 ? sp.of(rows) : 1, (size_t)rows * ld, d, bf16 ? scale[1] : 1.f, dX + (size_t)list[first + r] * d);
+    finish_row(part + (size_t)r * ld, bf16 ? sp.of(rows) : sp.stages, (size_t)(bf16 ? rows : cap) * ld, d, bf16 ? scale[1] : 1.f, dX + (size_t)list[first + r] * d);
 }
 
 hipError_t launch_finish_dx(bool bf16, const float *part, Splits sp, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s)

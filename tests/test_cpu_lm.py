@@ -151,3 +151,4 @@ def test_vocabulary_of_many_blocks(driver):
     # more blocks than the stand-in has CUs; contractions of several rounds of the ring
     vocab_case(driver, 300, 288, 1100, "bf16", ignored=0.1, seed=3)
     vocab_case(driver, 40, 256, 1700, "bf16", top=3, tau=4.0, seed=4)
+    vocab_case(driver, 20, 40, 2500, "f32", top=2, seed=5)           # dX in parts
