@@ -102,19 +102,19 @@ struct VocabChunk {
 };
 hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
 // How the contraction of dX over the vocabulary is cut, on the device, where the rows of the chunk are known: in as many runs of whole stages (16 at
-// least) as take the least time, us: rounds of blocks over the CUs of an MI355X, of 0.53 a stage and 5 beside, and 0.12 a block and run for writing its
-// fp32 part and adding it up.  Part s of `rows` rows lies s * rows * ld floats on.
+// least) as take the least time, in 10 ns: rounds of blocks over the CUs of an MI355X, of 53 a stage and 500 beside, and 12 a block and run for writing
+// its fp32 part and adding it up.  (Whole numbers: two kernels have to come to the same answer.)  Part s of `rows` rows lies s * rows * ld floats on.
 struct Splits {
     int block_rows, tiles_n, stages;         // fp32 storage: 0, 0 and the number of parts, which the host knows
     static constexpr int kMost = 16, kBlocks = 1024;         // runs, and blocks of all runs where there is more than one
     __host__ __device__ int of(int rows) const
     {
-        const int tiles = (rows + block_rows - 1) / block_rows * tiles_n;
+        const int tiles = (rows + block_rows - 1) / block_rows * tiles_n;      // at most 32 * 4096
         int best = 1;
-        float least = 0.f;
+        int64_t least = 0;
         for (int s = 1; s == 1 || (s <= kMost && s * tiles <= kBlocks && 16 * s <= stages); ++s) {
-            const float us = (float)((s * tiles + 255) / 256) * (0.53f * (float)stages / (float)s + 5.f) + 0.12f * (float)(s * tiles);
-            if (s == 1 || us < least) least = us, best = s;
+            const int64_t time = (int64_t)((s * tiles + 255) / 256) * (53 * stages / s + 500) + 12 * s * tiles;
+            if (s == 1 || time < least) least = time, best = s;
         }
         return best;
     }

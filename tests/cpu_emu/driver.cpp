@@ -29,6 +29,13 @@ emu_switch:
     ret
 )");
 
+// what the library has in stl_api.hip
+static thread_local char error_buffer[512] = "";
+namespace stl {
+char *error_text() { return error_buffer; }
+}
+extern "C" const char *stl_last_error(void) { return error_buffer; }
+
 static std::string dir;
 static std::map<std::string, double> num;
 static std::map<std::string, std::pair<void *, size_t>> outs;

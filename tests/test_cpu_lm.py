@@ -1,4 +1,4 @@
-"""The residual step and the vocabulary loss without a GPU: the library's sources compiled for the host against a stand-in for the HIP runtime that runs a
+"""The residual step and the vocabulary loss without a GPU: their sources compiled for the host against a stand-in for the HIP runtime that runs a
 workgroup's threads as fibers (tests/cpu_emu/), whole calls of the C ABI on buffers that end where their allocation ends, under AddressSanitizer,
 and their results against the oracle.  Every access of the real index arithmetic is checked, also where it depends on labels and lists."""
 import os
@@ -28,7 +28,7 @@ def driver(tmp_path_factory):
         for device, host in meet.items():
             text = text.replace(device, host)
         to.write_text(_host_source(text))
-        if f.suffix == ".hip":
+        if f.suffix == ".hip" and f.parent.name == "lm":
             srcs.append(to)
     shutil.copy(ROOT / "tests" / "cpu_emu" / "driver.cpp", work / "driver.cpp")
     srcs.append(work / "driver.cpp")
