@@ -77,8 +77,9 @@ struct RowList {
 hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s);
 // rows first .. first + cap of the list of X, side by side with ld elements each (zeros behind a row's end and behind the list's).  With the
 // first chunk also: zeros for the rows that are not listed, in dX and the losses (each may be NULL).
-// Up to kFewRows rows are listed by every workgroup of this launch for itself, and by the first of them for the launches that follow.
-constexpr int kFewRows = 256;
+// Few rows are listed by every workgroup of this launch for itself, and by the first of them for the launches that follow: 1024 labels are 8 KB for each,
+// lists of a teacher lie far apart.
+inline bool few_rows(const VocabArgs &a) { return a.rows <= (a.top_id ? 256 : 1024); }
 hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss,
                                hipStream_t s);
 // rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)

@@ -536,7 +536,7 @@ hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *lab
     const Plan p = plan_of(a, g != nullptr);
     char *base = (char *)ws;
     const RowList rl{(int *)(base + p.list), (int *)(base + p.count), (float *)(base + p.scale)};
-    if (a.rows > kFewRows) LM_TRY(launch_select_rows(a, g, rl, s));
+    if (!few_rows(a)) LM_TRY(launch_select_rows(a, g, rl, s));
     return a.bf16 ? loss_bf16(a, g, label_loss, top_loss, p, base, rl, s) : loss_f32(a, g, label_loss, top_loss, p, base, rl, s);
 }
 

@@ -125,7 +125,7 @@ __device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, 
 }
 
 // a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed.  FEW: there is no list
-// yet; a thread has a row, and every workgroup lists them.
+// yet; every workgroup goes over all rows.
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, Weights w, const T *X, int *list, int *count, float *scale, int first, int cap, int d,
                                                            int ld, T *out, int zeros, T *dX, float *label_loss, float *top_loss)
@@ -134,21 +134,28 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, We
     long from = -1;
     if constexpr (FEW) {
         __shared__ int mine;
-        const int r = (int)threadIdx.x;
-        const bool l = r < rows && t.labelled(r), q = r < rows && t.taught(r);
-        int all;
-        float top = r < rows ? w.of(r, l, q) : 0.f;
-        const int at = scan_rows<256>(l || q, all, top) - 1;
-        if (r == 0) mine = -1;
+        const int per = (rows + 255) / 256, r0 = (int)threadIdx.x * per;     // at most four rows a thread
+        int n = 0, all;
+        float top = 0.f;
+        uint32_t has = 0;
+        for (int r = r0; r < r0 + per && r < rows; ++r) {
+            const bool l = t.labelled(r), q = t.taught(r);
+            n += l || q;
+            has |= (uint32_t)(l || q) << (r - r0);
+            top = fmaxf(top, w.of(r, l, q));
+        }
+        int at = scan_rows<256>(n, all, top) - n;
+        if (threadIdx.x == 0) mine = -1;
         __syncthreads();
-        if ((l || q) && at == b) mine = r;
-        if (b == 0) {
-            if (l || q) list[at] = r;
-            if (r == 0) {
-                *count = all;
-                scale[0] = dz_scale(top);
-                scale[1] = 1.f / scale[0];
-            }
+        for (; has; has &= has - 1, ++at) {
+            const int r = r0 + __builtin_ctz(has);
+            if (at == b) mine = r;
+            if (b == 0) list[at] = r;
+        }
+        if (b == 0 && threadIdx.x == 0) {
+            *count = all;
+            scale[0] = dz_scale(top);
+            scale[1] = 1.f / scale[0];
         }
         __syncthreads();
         from = mine;
@@ -175,7 +182,7 @@ hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList 
                            first, cap, a.d, ld, (T *)out, zeros, (T *)dX, label_loss, top_loss);
         return hipGetLastError();
     };
-    const bool few = a.rows <= kFewRows;
+    const bool few = few_rows(a);
     if (a.bf16) return few ? run(arrange_rows_kernel<bf16_t, true>, (bf16_t *)nullptr) : run(arrange_rows_kernel<bf16_t, false>, (bf16_t *)nullptr);
     return few ? run(arrange_rows_kernel<float, true>, (float *)nullptr) : run(arrange_rows_kernel<float, false>, (float *)nullptr);
 }
