@@ -248,9 +248,9 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_few_kernel(const Operands
 }
 
 // ---- dX and dW -----------------------------------------------------------------------------------------------------------------------
-// dX parts: part s, rows x ldx = dz (columns of split s) W.
+// dX parts: part s, rows x ldx = dz (columns of split s) W.  The number of parts is left behind the count.
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, const int *count, int first, int cap, int d, Splits sps, float *part, int ldx)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, int *count, int first, int cap, int d, Splits sps, float *part, int ldx)
 {
     using namespace pipe;
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
@@ -263,6 +263,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
     if (rows <= 0) return;
     const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, size = group_rows(tiles_m), per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
     const size_t stride = (size_t)rows * ldx;
+    if (blockIdx.x == 0 && tid == 0) count[1] = splits;
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
     walk(R{}, first_block(total), end_block(total), block_step(), o, smem, smem_lds, wave, lane,
          [&](int v, Operands &mine, int &n, int &i0, int &j0) {
@@ -365,7 +366,7 @@ static hipError_t launch_logits(const Operands &o, const int *count, int first, 
 }
 
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-static hipError_t launch_dx(const Operands &o, const int *count, int first, int cap, int d, const Splits &sp, float *part, int ldx, hipStream_t s)
+static hipError_t launch_dx(const Operands &o, int *count, int first, int cap, int d, const Splits &sp, float *part, int ldx, hipStream_t s)
 {
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
     static std::atomic<uint64_t> granted{0};
@@ -414,7 +415,7 @@ Plan plan_of(const VocabArgs &a, bool grads)
         return here;
     };
     p.list = take((size_t)a.rows * sizeof(int));
-    p.count = take(sizeof(int));
+    p.count = take(2 * sizeof(int));
     p.scale = take(2 * sizeof(float));
     if (a.bf16) {
         // 4.3 GB of codes at most, and as many rows as fill the chip several times over
@@ -492,7 +493,7 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
             float *part = (float *)(base + p.dx_part);
             LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.dx, part, p.ldx, s)
                             : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.dx, part, p.ldx, s)));
-            LM_TRY(launch_finish_dx(true, part, p.dx, p.ldx, rl, first, p.cap, a.d, g->dX, s));
+            LM_TRY(launch_finish_dx(true, part, 0, p.ldx, rl, first, p.cap, a.d, g->dX, s));
         }
         if (g && g->dW) {
             const Operands o{codes, xc, (long)p.ldz, p.ldx, (int)p.ldz, p.ldx, 0};
@@ -520,7 +521,7 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
         if (g && g->dX) {
             const int parts = gemm_f32_splits(cap, a.d, a.vocab);
             LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false, parts}, s));
-            LM_TRY(launch_finish_dx(false, dx, Splits{0, 0, parts}, a.d, rl, first, cap, a.d, g->dX, s));
+            LM_TRY(launch_finish_dx(false, dx, parts, a.d, rl, first, cap, a.d, g->dX, s));
         }
         if (g && g->dW) LM_TRY(launch_gemm_f32({a.vocab, a.d, cap, z, false, xc, false, (float *)g->dW, ch > 0, 1}, s));
     }

@@ -109,11 +109,19 @@ hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList r
 }
 
 // ---- rows side by side ---------------------------------------------------------------------------------------------------------------
-// row `from` of `in` (none: zeros) to row `to` of `out`, zeros behind its end, by a workgroup of 256
-template <typename T>
-__device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, size_t to, int ld)
+// threads of a workgroup of 256 that share a row of d elements, eight each at a time
+__host__ __device__ inline int threads_of(int d)
 {
-    for (int c = (int)threadIdx.x * 8; c < ld; c += 2048) {
+    int n = 8;
+    while (n < 256 && n * 8 < d) n *= 2;
+    return n;
+}
+
+// row `from` of `in` (none: zeros) to row `to` of `out`, zeros behind its end, by thread t of n
+template <typename T>
+__device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, size_t to, int ld, int t, int n)
+{
+    for (int c = t * 8; c < ld; c += n * 8) {
         Chunk<T> v;
         v.fill(0.f);
         if (from >= 0 && c < d) v.load(in + (size_t)from * d + c, d - c);
@@ -162,13 +170,13 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, We
     } else {
         if (b < cap && first + b < *count) from = list[first + b];
     }
-    if (b < cap) copy_row(X, from, d, out, b, ld);
+    if (b < cap) copy_row(X, from, d, out, b, ld, (int)threadIdx.x, 256);
     if (b < zeros && !t.any(b)) {
         if (threadIdx.x == 0) {
             if (label_loss) label_loss[b] = 0.f;
             if (top_loss) top_loss[b] = 0.f;
         }
-        if (dX) copy_row(X, -1L, d, dX, b, d);
+        if (dX) copy_row(X, -1L, d, dX, b, d, (int)threadIdx.x, 256);
     }
 }
 
@@ -187,11 +195,17 @@ hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList 
     return few ? run(arrange_rows_kernel<float, true>, (float *)nullptr) : run(arrange_rows_kernel<float, false>, (float *)nullptr);
 }
 
-__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t *in, int d, bf16_t *out, int ld) { copy_row(in, blockIdx.x, d, out, blockIdx.x, ld); }
+// (a workgroup a row: 71 us for 97624 x 205, several: 34)
+__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t *in, int rows, int d, bf16_t *out, int ld)
+{
+    const int n = threads_of(ld), r = (int)blockIdx.x * (256 / n) + (int)threadIdx.x / n;
+    if (r < rows) copy_row(in, r, d, out, r, ld, (int)threadIdx.x % n, n);
+}
 
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s)
 {
-    hipLaunchKernelGGL(pad_rows_kernel, dim3(rows), dim3(256), 0, s, (const bf16_t *)in, d, (bf16_t *)out, ld);
+    const int per = 256 / threads_of(ld);
+    hipLaunchKernelGGL(pad_rows_kernel, dim3((rows + per - 1) / per), dim3(256), 0, s, (const bf16_t *)in, rows, d, (bf16_t *)out, ld);
     return hipGetLastError();
 }
 
@@ -217,6 +231,30 @@ __device__ __forceinline__ float block_sum(float v, float *red)
     v = red[0];
     for (int w = 1; w < kRowWaves; ++w) v += red[w];
     return v;
+}
+
+// f of every logit of a row of fp32 storage (STORE: which takes its place), by a workgroup: eight a thread at a time where each thread has some (40 rows of
+// 53504, three sweeps: 43 us, 86 by ones), one where there are fewer (2048 rows of 1000: 16.0 us, 19 by eights)
+template <bool STORE, class F>
+__device__ __forceinline__ void each_logit(float *Z, int vocab, F &&f)
+{
+    const int tid = (int)threadIdx.x;
+    if (vocab < kRowThreads * 8) {
+        for (int v = tid; v < vocab; v += kRowThreads) {
+            const float z = f(Z[v]);
+            if (STORE) Z[v] = z;
+        }
+        return;
+    }
+    for (int v = tid * 8; v < vocab; v += kRowThreads * 8) {
+        Chunk<float> in;
+        in.load(Z + v, vocab - v);
+        float out[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < vocab - v) out[e] = f(in.get(e));
+        if (STORE) Chunk<float>::store(Z + v, vocab - v, out);
+    }
 }
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -295,13 +333,14 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
         lse2 = m + log2f(sum), lse2_tau = m * ratio + log2f(sum_tau);
         lse = lse2 * kLn2, lse_tau = lse2_tau * kLn2;
     } else {
-        const float *Z = (const float *)codes;
-        for (int v = tid; v < vocab; v += kRowThreads) m = fmaxf(m, Z[v]);
+        float *Z = (float *)codes;
+        each_logit<false>(Z, vocab, [&](float z) { return m = fmaxf(m, z); });
         m = block_max(m, red);
-        for (int v = tid; v < vocab; v += kRowThreads) {
-            sum += expf(Z[v] - m);
-            if (ntop) sum_tau += expf((Z[v] - m) * inv_tau);
-        }
+        each_logit<false>(Z, vocab, [&](float z) {
+            sum += expf(z - m);
+            if (ntop) sum_tau += expf((z - m) * inv_tau);
+            return z;
+        });
         sum = block_sum(sum, red);
         sum_tau = block_sum(sum_tau, red);
         lse = m + logf(sum), lse_tau = m * inv_tau + logf(sum_tau);
@@ -402,13 +441,12 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
                     u32x4_t{pack_bf16x2(out[0], out[1]), pack_bf16x2(out[2], out[3]), pack_bf16x2(out[4], out[5]), pack_bf16x2(out[6], out[7])};
             }
         } else {
-            float *Z = (float *)codes;
-            for (int v = tid; v < vocab; v += kRowThreads) {
+            each_logit<true>((float *)codes, vocab, [&](float z) {
                 float dz = 0.f;
-                if (labelled) dz = cl * expf(Z[v] - lse);
-                if (taught) dz = fmaf(ct, expf(fmaf(Z[v], inv_tau, -lse_tau)), dz);
-                Z[v] = dz;
-            }
+                if (labelled) dz = cl * expf(z - lse);
+                if (taught) dz = fmaf(ct, expf(fmaf(z, inv_tau, -lse_tau)), dz);
+                return dz;
+            });
         }
         __syncthreads();                     // the sweep's stores are done before the entries' places are written again
         for (int j = tid; j <= ntop; j += kRowThreads) {
@@ -438,27 +476,41 @@ hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl
 }
 
 // ---- the gradients' last stage ---------------------------------------------------------------------------------------------------------
-// a row of `out`: the sum of its parts times `factor`, rounded once, by a workgroup of 256
-template <typename T>
-__device__ __forceinline__ void finish_row(const float *part, int parts, size_t stride, int d, float factor, T *out)
+// eight elements of a row's parts p0, p0 + step, ...: their sum
+__device__ __forceinline__ void sum_parts(const float *part, int p0, int parts, int step, size_t stride, int left, float (&f)[8])
 {
-    for (int c = (int)threadIdx.x * 8; c < d; c += 2048) {
-        float f[8] = {};
-        for (int p = 0; p < parts; ++p) {
-            Chunk<float> v;
-            v.load(part + p * stride + c, d - c);
+    constexpr int AT_ONCE = 4;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] += v.get(e);
-        }
+    for (int e = 0; e < 8; ++e) f[e] = 0.f;
+    int p = p0;
+    for (; p + (AT_ONCE - 1) * step < parts; p += AT_ONCE * step) {
+        Chunk<float> v[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= factor;
-        Chunk<T>::store(out + c, d - c, f);
+        for (int k = 0; k < AT_ONCE; ++k) v[k].load(part + (size_t)(p + k * step) * stride, left);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] += v[k].get(e);
     }
+    for (; p < parts; p += step) {
+        Chunk<float> v;
+        v.load(part + (size_t)p * stride, left);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] += v.get(e);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_scaled(T *out, int left, float (&f)[8], float factor)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= factor;
+    Chunk<T>::store(out, left, f);
 }
 
 // a workgroup a row of the chunk, to where the row came from
 template <typename T>
-__global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, Splits sp, int ld, const int *list, const int *count, const float *scale, int first,
+__global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, int known, int ld, const int *list, const int *count, const float *scale, int first,
                                                         int cap, int d, T *dX)
 {
     int rows = *count - first;
@@ -466,31 +518,62 @@ __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, Split
     const int r = (int)blockIdx.x;
     if (r >= rows) return;
     const bool bf16 = sizeof(T) == 2;
-    finish_row(part + (size_t)r * ld, bf16 ? sp.of(rows) : sp.stages, (size_t)(bf16 ? rows : cap) * ld, d, bf16 ? scale[1] : 1.f, dX + (size_t)list[first + r] * d);
+    const int parts = bf16 ? count[1] : known, n = threads_of(d), groups = 256 / n, group = (int)threadIdx.x / n, t = (int)threadIdx.x % n;
+    const size_t stride = (size_t)(bf16 ? rows : cap) * ld;
+    const float *from = part + (size_t)r * ld, factor = bf16 ? scale[1] : 1.f;
+    T *to = dX + (size_t)list[first + r] * d;
+    // short rows: several groups of threads share the parts, and the first adds them up in order
+    __shared__ f32x4_t red[512];
+    for (int c0 = 0; c0 < d; c0 += n * 8) {
+        const int c = c0 + t * 8;
+        float f[8] = {};
+        if (c < d) sum_parts(from + c, group, parts, groups, stride, d - c, f);
+        if (groups > 1) {                                    // (then c0 takes one turn)
+            red[threadIdx.x * 2] = f32x4_t{f[0], f[1], f[2], f[3]};
+            red[threadIdx.x * 2 + 1] = f32x4_t{f[4], f[5], f[6], f[7]};
+            __syncthreads();
+            if (group == 0)
+                for (int k = 1; k < groups; ++k) {
+                    const f32x4_t a = red[(k * n + t) * 2], b = red[(k * n + t) * 2 + 1];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] += a[e], f[e + 4] += b[e];
+                }
+        }
+        if (group == 0 && c < d) store_scaled(to + c, d - c, f, factor);
+    }
 }
 
-hipError_t launch_finish_dx(bool bf16, const float *part, Splits sp, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s)
+hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s)
 {
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, sp, ld, (const int *)rl.list, (const int *)rl.count, (const float *)rl.scale, first, cap, d, (T *)dX);
+        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, parts, ld, (const int *)rl.list, (const int *)rl.count, (const float *)rl.scale, first, cap, d, (T *)dX);
         return hipGetLastError();
     };
     return bf16 ? run(finish_dx_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_dx_kernel<float>, (float *)nullptr);
 }
 
+// as many rows a workgroup as it has threads for (97624 x 205, a workgroup a row: 49 us, several: 24)
 template <typename T>
-__global__ __launch_bounds__(256) void finish_dw_kernel(const float *part, int parts, size_t stride, int ld, int d, const float *scale, T *dW)
+__global__ __launch_bounds__(256) void finish_dw_kernel(const float *part, int parts, size_t stride, int ld, size_t rows, int d, const float *scale, T *dW)
 {
-    const size_t r = blockIdx.x;
-    finish_row(part + r * ld, parts, stride, d, scale[1], dW + r * d);
+    const int n = threads_of(d);
+    const size_t r = (size_t)blockIdx.x * (256 / n) + threadIdx.x / n;
+    if (r >= rows) return;
+    const float factor = scale[1];
+    for (int c = (int)threadIdx.x % n * 8; c < d; c += n * 8) {
+        float f[8];
+        sum_parts(part + r * ld + c, 0, parts, 1, stride, d - c, f);
+        store_scaled(dW + r * d + c, d - c, f, factor);
+    }
 }
 
 hipError_t launch_finish_dw(bool bf16, RowList rl, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s)
 {
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(256), 0, s, part, parts, stride, ld, d, (const float *)rl.scale, (T *)dW);
+        const size_t per = 256 / threads_of(d);
+        hipLaunchKernelGGL(kern, dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, part, parts, stride, ld, rows, d, (const float *)rl.scale, (T *)dW);
         return hipGetLastError();
     };
     return bf16 ? run(finish_dw_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_dw_kernel<float>, (float *)nullptr);
