@@ -148,6 +148,14 @@ def test_labels_and_teacher(shape, dtype, tau):
     check(*shape, dtype, tau=tau, top=16, ignored=0.3, seed=shape[0])
 
 
+# few rows and a wide vocabulary: dX's contraction in many runs, whose number is not a divisor of its stages
+@pytest.mark.parametrize("shape", [(1, 8, 70000), (34, 64, 66001), (68, 205, 40001), (257, 72, 33000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("top", [0, 3])
+def test_few_rows_of_a_wide_vocabulary(shape, dtype, top):
+    check(*shape, dtype, tau=2.0 if top else 1.0, top=top, seed=sum(shape) + top)
+
+
 @pytest.mark.parametrize("top", [1, 2, 63, 64, 65, 600, 1024])
 def test_lengths_of_the_teachers_lists(top):
     check(40, 64, 1500, "bf16", tau=2.0, top=top, seed=top)
