@@ -81,7 +81,7 @@ hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList r
 // Few rows are listed by every workgroup of this launch for itself, and by the first of them for the launches that follow: 1024 labels are 8 KB for each,
 // lists of a teacher lie far apart.
 inline bool few_rows(const VocabArgs &a) { return a.rows <= (a.top_id ? 256 : 1024); }
-hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, void *dX, float *label_loss, float *top_loss,
+hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, bool pairs, void *dX, float *label_loss, float *top_loss,
                                hipStream_t s);
 // rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
@@ -92,6 +92,7 @@ hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, h
 struct alignas(16) GroupSums {
     float m, sum, sum_tau, step;
 };
+constexpr int kPairRows = 32;                // up to so many rows the gradient in the logits of bf16 storage is held as two numbers: vocab_rows_kernel
 struct VocabChunk {
     int first, cap;                          // listed rows first .. first + cap (those that exist)
     void *codes;                             // cap x ld: 16 bits (bf16 storage) or fp32 logits; the gradient is written in their place
@@ -101,6 +102,7 @@ struct VocabChunk {
     int groups;
     const void *Xc;                          // the listed rows, ldx elements each
     int ldx;
+    bool pairs;                              // what rounding the gradient of row r leaves goes to row r + kPairRows, itself rounded
 };
 hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
 // How the contraction of dX over the vocabulary is cut, on the device, where the rows of the chunk are known: in as many runs of whole stages (16 at
@@ -128,8 +130,9 @@ struct Splits {
         return some > cap ? some : cap;
     }
 };
-// dX rows of the list from the parts (bf16 storage: as many as the product left behind the count)
-hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, void *dX, hipStream_t s);
+// dX rows of the list from the parts (bf16 storage: as many as the product left behind the count); pairs: rows r and
+// r + kPairRows of 2 kPairRows together
+hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, bool pairs, void *dX, hipStream_t s);
 // out[i][j] = sum over parts of part[p][i][j], rows of ld in the parts and of d in `out`, and 1 / scale
 hipError_t launch_finish_dw(bool bf16, RowList rl, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s);
 
