@@ -59,6 +59,10 @@ struct VocabGrads {
     void *dX, *dW;                           // storage type, either may be NULL
 };
 constexpr int kMostTop = 1024;
+// Rows of a chunk.  bf16: as many as have kChunkCodes logits (4.3 GB of codes), kChunkLeast to kChunkMost of them, which fill the chip several times
+// over; fp32: as many as have kChunkLogits (1 GiB), kChunkLeastF32 at least.
+constexpr long kChunkCodes = 1L << 31, kChunkLogits = 1L << 28;
+constexpr int kChunkLeast = 256, kChunkMost = 8192, kChunkLeastF32 = 64;
 // A logit between its product and its gradient is held (bf16 storage) in 16 bits: as one of 65534 even steps from its group's maximum down to its
 // minimum, 65535 for what is below every share that fp32 can hold (minus infinity among it).  A group of 64 normal logits spreads over five
 // deviations: at a deviation of 2 a step is 1.5e-4, that is an error of exp(z) of 4e-5 (root mean square), a fortieth of the rounding of the gradient
@@ -78,8 +82,8 @@ struct RowList {
 hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, hipStream_t s);
 // rows first .. first + cap of the list of X, side by side with ld elements each (zeros behind a row's end and behind the list's).  With the
 // first chunk also: zeros for the rows that are not listed, in dX and the losses (each may be NULL).
-// Few rows are listed by every workgroup of this launch for itself, and by the first of them for the launches that follow: 1024 labels are 8 KB for each,
-// lists of a teacher lie far apart.
+// Few rows are listed by every workgroup of the first chunk's launch for itself, and by the first of them for the launches that follow, later chunks' among
+// them: 1024 labels are 8 KB for each, lists of a teacher lie far apart.
 inline bool few_rows(const VocabArgs &a) { return a.rows <= (a.top_id ? 256 : 1024); }
 hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, bool pairs, void *dX, float *label_loss, float *top_loss,
                                hipStream_t s);

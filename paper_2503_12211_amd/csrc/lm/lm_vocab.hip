@@ -422,9 +422,8 @@ Plan plan_of(const VocabArgs &a, bool grads)
     p.count = take(2 * sizeof(int));
     p.scale = take(2 * sizeof(float));
     if (a.bf16) {
-        // 4.3 GB of codes at most, and as many rows as fill the chip several times over
-        long cap = ((long)1 << 31) / a.vocab / 256 * 256;
-        cap = cap > 8192 ? 8192 : cap < 256 ? 256 : cap;
+        long cap = kChunkCodes / a.vocab / 256 * 256;
+        cap = cap > kChunkMost ? kChunkMost : cap < kChunkLeast ? kChunkLeast : cap;
         p.cap = (int)(a.rows < cap ? a.rows : cap);
         p.chunks = (a.rows + p.cap - 1) / p.cap;
         p.small = p.cap <= 64;
@@ -450,8 +449,8 @@ Plan plan_of(const VocabArgs &a, bool grads)
             if (p.dw_parts) p.dw_part = take(p.dw_stride * p.dw_splits * sizeof(float));
         }
     } else {
-        long cap = ((long)1 << 28) / a.vocab;                // 1 GiB of logits
-        cap = cap < 64 ? 64 : cap;
+        long cap = kChunkLogits / a.vocab;
+        cap = cap < kChunkLeastF32 ? kChunkLeastF32 : cap;
         p.cap = (int)(a.rows < cap ? a.rows : cap);
         p.chunks = (a.rows + p.cap - 1) / p.cap;
         p.ldx = a.d;

@@ -133,7 +133,7 @@ __device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, 
 }
 
 // a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed.  FEW: there is no list
-// yet; every workgroup goes over all rows; pairs: and row b is to be found at b + kPairRows too.
+// yet, and first is 0; every workgroup goes over all rows; pairs: and row b is to be found at b + kPairRows too.
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, Weights w, const T *X, int *list, int *count, float *scale, int first, int cap, int d,
                                                            int ld, T *out, bool pairs, int zeros, T *dX, float *label_loss, float *top_loss)
@@ -190,7 +190,7 @@ hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList 
                            first, cap, a.d, ld, (T *)out, pairs, zeros, (T *)dX, label_loss, top_loss);
         return hipGetLastError();
     };
-    const bool few = few_rows(a);
+    const bool few = few_rows(a) && first == 0;              // later chunks have the list
     if (a.bf16) return few ? run(arrange_rows_kernel<bf16_t, true>, (bf16_t *)nullptr) : run(arrange_rows_kernel<bf16_t, false>, (bf16_t *)nullptr);
     return few ? run(arrange_rows_kernel<float, true>, (float *)nullptr) : run(arrange_rows_kernel<float, false>, (float *)nullptr);
 }
