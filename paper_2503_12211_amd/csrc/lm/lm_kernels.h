@@ -63,11 +63,16 @@ constexpr int kMostTop = 1024;
 // over; fp32: as many as have kChunkLogits (1 GiB), kChunkLeastF32 at least.
 constexpr long kChunkCodes = 1L << 31, kChunkLogits = 1L << 28;
 constexpr int kChunkLeast = 256, kChunkMost = 8192, kChunkLeastF32 = 64;
-// A logit between its product and its gradient is held (bf16 storage) in 16 bits: as one of 65534 even steps from its group's maximum down to its
-// minimum, 65535 for what is below every share that fp32 can hold (minus infinity among it).  A group of 64 normal logits spreads over five
-// deviations: at a deviation of 2 a step is 1.5e-4, that is an error of exp(z) of 4e-5 (root mean square), a fortieth of the rounding of the gradient
-// to bf16 that follows (as bf16 exponentials they would add that rounding once more).  In terms of z / tau it is 1 / tau of that.
-constexpr float kSteps = 65535.f, kLowestTau = 0.25f, kHighestTau = 16.f;
+// A logit between its product and its gradient is held (bf16 storage) in 16 bits: y = z log2(e) / t, t = 1 where there are labels and tau otherwise, in steps
+// from its group's maximum down to its minimum, 65534; 65535 is what is below every share that fp32 can hold (minus infinity among it): 2^-kNoShare.
+// One temperature: even steps over at most kNoShare; half a step is at most 1.1e-3, that is 8e-4 of a share.  A group of 64 normal logits spreads over
+// five deviations: at a deviation of 2 a step is 2.2e-4, an error of 4e-5 (root mean square), a fortieth of the rounding of the gradient to
+// bf16 that follows (as bf16 exponentials they would add that rounding once more).
+// Two temperatures that differ (their ratio is up to 16): the lower one's shares end at kNoShare min(1, tau) below the maximum, but the other's go on to
+// kNoShare max(1, tau).  A group that spreads over more than twice the first, `bend`, has half of its steps above the bend and half below, so that
+// a share of either is off by 1.6e-3 at most (even steps, tau = 16: 1.3e-2).
+constexpr float kSteps = 65535.f, kLowestTau = 0.25f, kHighestTau = 16.f, kNoShare = 150.041f;
+constexpr float kBendSteps = 32767.f;
 size_t vocab_workspace_bytes(const VocabArgs &a, bool grads);
 // label_loss, top_loss: rows fp32 or NULL; g NULL: losses alone
 hipError_t launch_vocab_loss(const VocabArgs &a, const VocabGrads *g, float *label_loss, float *top_loss, void *ws, hipStream_t s);
@@ -91,8 +96,9 @@ hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList 
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
 
 // Logits of one chunk of listed rows on their way to the gradient (storage fp32: the logits themselves).  bf16: what the product leaves for
-// every listed row and group of 64 columns, with y = z log2(e) / t, t = 1 where there are labels and tau otherwise: the largest y, m, the sums of
-// 2^(y - m) and of 2^((y - m) / tau), and with gradients y as 16-bit steps below m and the size of a step.
+// every listed row and group of 64 columns, with y as for kSteps: the largest y, m, the sums of
+// 2^(y - m) and of 2^((y - m) / tau), and with gradients y as 16-bit steps below m and the size of a step; minus the size of those below the bend
+// where there is one.
 struct alignas(16) GroupSums {
     float m, sum, sum_tau, step;
 };
@@ -103,6 +109,7 @@ struct VocabChunk {
     size_t ld;
     const GroupSums *sums;                   // cap x groups (bf16 storage)
     bool two;                                // they have the second sum: both terms are there and tau is not 1
+    float bend;
     int groups;
     const void *Xc;                          // the listed rows, ldx elements each
     int ldx;

@@ -23,24 +23,38 @@ struct LogitsOut {
     float scale;         // log2(e) over the temperature of the first sum: y = scale z
     float ratio;         // the first temperature over the second
     float deepest;       // below a group's maximum by this much in y, no share is left in fp32
+    float bend;          // as much for the lower of two temperatures (kSteps)
 };
 
 // From a group's largest y and its spread to its smallest: what a step is, and what takes y to [0, 1] for the conversion to 16 bits, in which 1
 // is 65535.  The smallest y comes to lie on 65534.  (The order of the bounds makes any spread that is not a number a finite one.)
+// TWO: of two lines the lower one is taken, the second of which has the steps below the bend; without a bend they are the same.
+template <bool TWO>
 struct Steps {
-    float size, mul, add;
-    __device__ __forceinline__ Steps(float ref, float spread, float deepest)
+    float size, mul, add, mul2, add2;
+    __device__ __forceinline__ Steps(float ref, float spread, const LogitsOut &out)
     {
-        const float whole = fminf(fmaxf(spread, 1e-3f), deepest) * (kSteps / (kSteps - 1.f));
+        const float deep = fminf(fmaxf(spread, 1e-3f), out.deepest);
+        const bool bent = TWO && deep > 2.f * out.bend;
+        const float whole = bent ? out.bend * (kSteps / kBendSteps) : deep * (kSteps / (kSteps - 1.f));
         size = whole * (1.f / kSteps);
         mul = -__builtin_amdgcn_rcpf(whole);                 // (an error of 1e-7 of it is 0.007 steps at the far end)
         add = -ref * mul;
+        if constexpr (TWO) {
+            const float below = (deep - out.bend) * (kSteps / kBendSteps);
+            mul2 = bent ? -__builtin_amdgcn_rcpf(below) : mul;
+            add2 = bent ? fmaf(out.bend - ref, mul2, kBendSteps / kSteps) : add;
+            if (bent) size = -below * (1.f / kSteps);
+        }
     }
+    __device__ __forceinline__ float at(float y) const
+    {
+        const float t = fmaf(y, mul, add);
+        if constexpr (TWO) return fminf(t, fmaf(y, mul2, add2));
+        return t;
+    }
+    __device__ __forceinline__ uint32_t codes(float y0, float y1) const { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(at(y0), at(y1))); }
 };
-__device__ __forceinline__ uint32_t codes_of(float y0, float y1, const Steps &st)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(fmaf(y0, st.mul, st.add), fmaf(y1, st.mul, st.add)));
-}
 
 typedef Ring<256, 256, 2, 4, 4, false, false, false> LogitsFull;
 typedef Ring<128, 256, 2, 4, 5, false, false, false> LogitsHalf;
@@ -99,7 +113,7 @@ __device__ __forceinline__ void logits_out(pipe::acc4_t (&acc)[FM][4], int row0,
                 s2 += __shfl_xor(s2, 16);
                 s2 += __shfl_xor(s2, 32);
             }
-            const Steps st(ref, ref - least, out.deepest);
+            const Steps<TWO> st(ref, ref - least, out);
             const int row = row0 + 16 * a + rl;
             if (quad == 0 && row < rows) out.sums[(size_t)row * out.groups + group] = GroupSums{m, s, s2, st.size};
             if constexpr (CODES) {
@@ -108,7 +122,7 @@ __device__ __forceinline__ void logits_out(pipe::acc4_t (&acc)[FM][4], int row0,
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     *reinterpret_cast<u32x2_t *>(rowp + (((2 * b + (quad >> 1)) ^ swz) << 4) + (quad & 1) * 8) =
-                        u32x2_t{codes_of(y[4 * b], y[4 * b + 1], st), codes_of(y[4 * b + 2], y[4 * b + 3], st)};
+                        u32x2_t{st.codes(y[4 * b], y[4 * b + 1]), st.codes(y[4 * b + 2], y[4 * b + 3])};
             }
         });
         if constexpr (CODES) {
@@ -238,12 +252,12 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_few_kernel(const Operands
         float s2 = 0.f, spread = 0.f;
         if constexpr (TWO) s2 = wave_sum(__builtin_amdgcn_exp2f(below * out.ratio));
         if constexpr (CODES) spread = wave_max(in ? -below : 0.f);
-        const Steps st(ref, spread, out.deepest);
+        const Steps<TWO> st(ref, spread, out);
         if (lane == 0) {
             const size_t at = (size_t)r * out.groups + blockIdx.x;
             out.sums[at] = GroupSums{m, s, s2, st.size};
         }
-        if constexpr (CODES) out.codes[(size_t)r * out.ld + col0 + lane] = (uint16_t)(codes_of(y, y, st) & 0xffffu);
+        if constexpr (CODES) out.codes[(size_t)r * out.ld + col0 + lane] = (uint16_t)(st.codes(y, y) & 0xffffu);
     }
 }
 
@@ -484,13 +498,14 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
     }
     const bool two = a.label && a.ntop && a.tau != 1.f;
     const float inv_tau = 1.f / a.tau, scale = 1.44269504088896340736f * (a.label ? 1.f : inv_tau);
+    const float deepest = kNoShare * (two ? fmaxf(1.f, a.tau) : 1.f), bend = kNoShare * (two ? fminf(1.f, a.tau) : 1.f);
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap;
         LM_TRY(launch_arrange_rows(a, g, rl, first, p.rows_held, p.ldx, xc, p.pairs, g ? g->dX : nullptr, label_loss, top_loss, s));
         const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
-        const LogitsOut lo{(GroupSums *)(base + p.sums), p.groups, codes, (long)p.ldz, scale, inv_tau, 104.f * (a.tau > 1.f ? a.tau : 1.f) * scale};
+        const LogitsOut lo{(GroupSums *)(base + p.sums), p.groups, codes, (long)p.ldz, scale, inv_tau, deepest, bend};
         LM_TRY(launch_logits(logits, rl.count, first, p.cap, a.vocab, lo, two, s));
-        const VocabChunk c{first, p.cap, codes, p.ldz, lo.sums, two, p.groups, xc, p.ldx, p.pairs};
+        const VocabChunk c{first, p.cap, codes, p.ldz, lo.sums, two, bend, p.groups, xc, p.ldx, p.pairs};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             const Operands o{codes, W, (long)p.ldz, p.ldx, p.rows_held, p.ldx, a.vocab};
@@ -520,7 +535,7 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
         LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, false, g ? g->dX : nullptr, label_loss, top_loss, s));
         LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false, 1}, s));
-        const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0, xc, a.d, false};
+        const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0.f, 0, xc, a.d, false};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             const int parts = gemm_f32_splits(cap, a.d, a.vocab);

@@ -430,31 +430,44 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
         const float factor = BF16 ? *scale : 1.f;
         const float cl = labelled && g.dlabel ? g.dlabel[row] * factor : 0.f, ct = taught && g.dtop ? g.dtop[row] * inv_tau * factor : 0.f;
         if constexpr (BF16) {
-            // chunks of eight logits lie in one group of 64
-            for (size_t v = (size_t)tid * 8; v < c.ld; v += kRowThreads * 8) {
-                const u32x4_t in = *reinterpret_cast<const u32x4_t *>(codes + v);
-                const float mg = groups[v / 64].m, step = groups[v / 64].step;
-                const float at = mg - lse2, at_tau = mg * ratio - lse2_tau, step_tau = step * ratio;
-                float out[8];
+            auto sweep = [&](auto two_c) {
+                constexpr bool TWO = decltype(two_c)::value;
+                // chunks of eight logits lie in one group of 64
+                for (size_t v = (size_t)tid * 8; v < c.ld; v += kRowThreads * 8) {
+                    const u32x4_t in = *reinterpret_cast<const u32x4_t *>(codes + v);
+                    const float mg = groups[v / 64].m, step = groups[v / 64].step;
+                    const float at = mg - lse2, at_tau = mg * ratio - lse2_tau;
+                    // two temperatures: below the maximum by the higher one of two lines (Steps)
+                    const float step1 = step > 0.f ? step : c.bend * (1.f / kBendSteps), step2 = fabsf(step), off2 = step > 0.f ? 0.f : fmaf(-kBendSteps, step2, c.bend);
+                    float out[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t code = (in[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-                    float dz = 0.f;
-                    if (labelled) dz = cl * __builtin_amdgcn_exp2f(fmaf(-(float)code, step, at));
-                    if (taught) dz = fmaf(ct, __builtin_amdgcn_exp2f(fmaf(-(float)code, step_tau, at_tau)), dz);
-                    // a row whose sums are not a number stays one throughout
-                    out[e] = code == 65535u && m + sum == m + sum ? 0.f : dz;
-                }
-                const u32x4_t packed = {pack_bf16x2(out[0], out[1]), pack_bf16x2(out[2], out[3]), pack_bf16x2(out[4], out[5]), pack_bf16x2(out[6], out[7])};
-                *reinterpret_cast<u32x4_t *>(codes + v) = packed;
-                if (c.pairs) {
-                    u32x4_t rest;
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t code = (in[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+                        float dz = 0.f;
+                        if constexpr (TWO) {
+                            const float below = fmaxf((float)code * step1, fmaf((float)code, step2, off2));
+                            if (labelled) dz = cl * __builtin_amdgcn_exp2f(at - below);
+                            if (taught) dz = fmaf(ct, __builtin_amdgcn_exp2f(fmaf(-below, ratio, at_tau)), dz);
+                        } else {
+                            if (labelled) dz = cl * __builtin_amdgcn_exp2f(fmaf(-(float)code, step, at));
+                            if (taught) dz = fmaf(ct, __builtin_amdgcn_exp2f(fmaf(-(float)code, step, at_tau)), dz);
+                        }
+                        // a row whose sums are not a number stays one throughout
+                        out[e] = code == 65535u && m + sum == m + sum ? 0.f : dz;
+                    }
+                    const u32x4_t packed = {pack_bf16x2(out[0], out[1]), pack_bf16x2(out[2], out[3]), pack_bf16x2(out[4], out[5]), pack_bf16x2(out[6], out[7])};
+                    *reinterpret_cast<u32x4_t *>(codes + v) = packed;
+                    if (c.pairs) {
+                        u32x4_t rest;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        rest[k] = pack_bf16x2(rest_of(out[2 * k], __uint_as_float(packed[k] << 16)), rest_of(out[2 * k + 1], __uint_as_float(packed[k] & 0xffff0000u)));
-                    *reinterpret_cast<u32x4_t *>(codes + v + kPairRows * c.ld) = rest;
+                        for (int k = 0; k < 4; ++k)
+                            rest[k] = pack_bf16x2(rest_of(out[2 * k], __uint_as_float(packed[k] << 16)), rest_of(out[2 * k + 1], __uint_as_float(packed[k] & 0xffff0000u)));
+                        *reinterpret_cast<u32x4_t *>(codes + v + kPairRows * c.ld) = rest;
+                    }
                 }
-            }
+            };
+            if (c.two) sweep(std::true_type{});
+            else sweep(std::false_type{});
         } else {
             each_logit<true>((float *)codes, vocab, [&](float z) {
                 float dz = 0.f;
