@@ -90,7 +90,7 @@ hipError_t launch_select_rows(const VocabArgs &a, const VocabGrads *g, RowList r
 // Few rows are listed by every workgroup of the first chunk's launch for itself, and by the first of them for the launches that follow, later chunks' among
 // them: 1024 labels are 8 KB for each, lists of a teacher lie far apart.
 inline bool few_rows(const VocabArgs &a) { return a.rows <= (a.top_id ? 256 : 1024); }
-hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, bool pairs, void *dX, float *label_loss, float *top_loss,
+hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, int held, void *dX, float *label_loss, float *top_loss,
                                hipStream_t s);
 // rows of an array, ld elements each in `out`, zeros behind a row's end (bf16)
 hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, hipStream_t s);
@@ -102,7 +102,15 @@ hipError_t launch_pad_rows(const void *in, int rows, int d, int ld, void *out, h
 struct alignas(16) GroupSums {
     float m, sum, sum_tau, step;
 };
-constexpr int kPairRows = 32;                // up to so many rows the gradient in the logits of bf16 storage is held as two numbers: vocab_rows_kernel
+// Up to so many listed rows the gradient in the logits of bf16 storage is held as two numbers (vocab_rows_kernel): what rounding that of row r leaves goes
+// to row r + second_row, itself rounded.  The errors of dX and dW over those of one rounding of each, the largest of 420 outputs of small calls (most of them
+// of 64 to 128 columns, labels, a teacher's 5 to 100 entries or both): with one number 1.60, 1.74, 1.65, 1.49, 1.50, 1.56, 1.47, 1.52 and 1.46 at 33, 48, 64, 96,
+// 128, 140, 192, 256 and 400 rows (the median is 1.33 throughout; two equal roundings give 1.41), with two 1.00.  They double the rows of dX's and dW's
+// products: 64 x 4096, vocabulary 65536: 430 -> 502 us, 100 x 4096: 479 -> 535, 64 x 64, 109807: 90 -> 97.
+constexpr int kPairRows = 128;
+__host__ __device__ inline int whole_stages(int rows) { return (rows + 31) / 32 * 32; }
+// 0: one number a row.  listed: of all chunks; held: rows of the chunk's buffers (0: no gradients), which have room for both
+__host__ __device__ inline int second_row(int listed, int held) { return listed <= kPairRows && 2 * whole_stages(listed) <= held ? whole_stages(listed) : 0; }
 struct VocabChunk {
     int first, cap;                          // listed rows first .. first + cap (those that exist)
     void *codes;                             // cap x ld: 16 bits (bf16 storage) or fp32 logits; the gradient is written in their place
@@ -113,7 +121,7 @@ struct VocabChunk {
     int groups;
     const void *Xc;                          // the listed rows, ldx elements each
     int ldx;
-    bool pairs;                              // what rounding the gradient of row r leaves goes to row r + kPairRows, itself rounded
+    int held;                                // second_row
 };
 hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, const VocabChunk &c, float *label_loss, float *top_loss, hipStream_t s);
 // How the contraction of dX over the vocabulary is cut, on the device, where the rows of the chunk are known: in as many runs of whole stages (16 at
@@ -141,9 +149,8 @@ struct Splits {
         return some > cap ? some : cap;
     }
 };
-// dX rows of the list from the parts (bf16 storage: as many as the product left behind the count); pairs: rows r and
-// r + kPairRows of 2 kPairRows together
-hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, bool pairs, void *dX, hipStream_t s);
+// dX rows of the list from the parts (bf16 storage: as many as the product left behind the count), a row and its second one (held: second_row) together
+hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, int held, void *dX, hipStream_t s);
 // out[i][j] = sum over parts of part[p][i][j], rows of ld in the parts and of d in `out`, and 1 / scale
 hipError_t launch_finish_dw(bool bf16, RowList rl, const float *part, int parts, size_t stride, int ld, size_t rows, int d, void *dW, hipStream_t s);
 

@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_few_kernel(const Operands
 // ---- dX and dW -----------------------------------------------------------------------------------------------------------------------
 // dX parts: part s, rows x ldx = dz (columns of split s) W.  The number of parts is left behind the count.
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, int *count, int first, int cap, int d, bool pairs, Splits sps, float *part, int ldx)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const Operands o, int *count, int first, int cap, int d, int held, Splits sps, float *part, int ldx)
 {
     using namespace pipe;
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64) void vocab_dx_kernel(const O
     int rows = *count - first;
     if (rows > cap) rows = cap;
     if (rows <= 0) return;
-    if (pairs) rows = 2 * kPairRows;
+    if (const int second = second_row(*count, held)) rows = 2 * second;
     const int tiles_m = (rows + BM - 1) / BM, tiles_n = sps.tiles_n, size = group_rows(tiles_m), per = tiles_m * tiles_n, splits = sps.of(rows), total = per * splits, stages = sps.stages;
     const size_t stride = (size_t)rows * ldx;
     if (blockIdx.x == 0 && tid == 0) count[1] = splits;
@@ -306,7 +306,7 @@ typedef Ring<128, 256, 2, 4, 5, true, true, false> DwHalf;
 static_assert(DwHalf::SLABS_AT <= DwFull::SLABS_AT && DwHalf::LDS_BYTES <= DwFull::LDS_BYTES, "LDS of walk_list");
 
 template <typename TO, bool ACC>
-__global__ __launch_bounds__(512) void vocab_dw_kernel(const Operands o, const int *count, const float *scale, int first, int cap, bool pairs, int vocab, int splits, TO *out,
+__global__ __launch_bounds__(512) void vocab_dw_kernel(const Operands o, const int *count, const float *scale, int first, int cap, int held, int vocab, int splits, TO *out,
                                                        size_t stride, int ldo)
 {
     using namespace pipe;
@@ -318,8 +318,8 @@ __global__ __launch_bounds__(512) void vocab_dw_kernel(const Operands o, const i
     if (rows <= 0) {
         if (ACC) return;                                     // nothing to add
         rows = 0;
-    } else if (pairs) {
-        rows = 2 * kPairRows;
+    } else if (const int second = second_row(*count, held)) {
+        rows = 2 * second;
     }
     const int tiles_m = (vocab + 255) / 256, tiles_n = (ldo + 255) / 256, size = group_rows(tiles_m), per = tiles_m * tiles_n, stages = (rows + BKS - 1) / BKS;
     auto begin_of = [&](int sp) { return (int)((long)stages * sp / splits); };
@@ -383,20 +383,20 @@ static hipError_t launch_logits(const Operands &o, const int *count, int first, 
 }
 
 template <int BM, int WAVES_M, int WAVES_N, int NS>
-static hipError_t launch_dx(const Operands &o, int *count, int first, int cap, int d, bool pairs, const Splits &sp, float *part, int ldx, hipStream_t s)
+static hipError_t launch_dx(const Operands &o, int *count, int first, int cap, int d, int held, const Splits &sp, float *part, int ldx, hipStream_t s)
 {
     typedef Ring<BM, 256, WAVES_M, WAVES_N, NS, false, true, true> R;
     static std::atomic<uint64_t> granted{0};
-    return launch_ring(vocab_dx_kernel<BM, WAVES_M, WAVES_N, NS>, granted, R::LDS_BYTES, R::THREADS, pipe::cu_count(), s, o, count, first, cap, d, pairs, sp, part, ldx);
+    return launch_ring(vocab_dx_kernel<BM, WAVES_M, WAVES_N, NS>, granted, R::LDS_BYTES, R::THREADS, pipe::cu_count(), s, o, count, first, cap, d, held, sp, part, ldx);
 }
 
 template <typename TO, bool ACC>
-static hipError_t launch_dw(const Operands &o, const RowList &rl, int first, int cap, bool pairs, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
+static hipError_t launch_dw(const Operands &o, const RowList &rl, int first, int cap, int held, int vocab, int splits, TO *out, size_t stride, int ldo, hipStream_t s)
 {
     typedef DwFull R;
     static std::atomic<uint64_t> granted{0};
     return launch_ring(vocab_dw_kernel<TO, ACC>, granted, R::LDS_BYTES, R::THREADS, 2L * ((vocab + 255) / 256) * ((ldo + 255) / 256) * splits, s, o,
-                       (const int *)rl.count, (const float *)rl.scale, first, cap, pairs, vocab, splits, out, stride, ldo);
+                       (const int *)rl.count, (const float *)rl.scale, first, cap, held, vocab, splits, out, stride, ldo);
 }
 
 // ---- the whole of a call -----------------------------------------------------------------------------------------------------------------
@@ -415,7 +415,7 @@ struct Plan {
     size_t ldz;              // elements of a row of the logits' codes / of the gradient in the logits
     int groups;
     bool small;              // blocks of 64 rows
-    bool pairs;              // VocabChunk
+    int held;                // rows that the chunk's buffers have for two numbers a row (second_row)
     Splits dx;
     int dw_splits;
     bool dw_parts;           // dW through fp32 parts
@@ -440,9 +440,11 @@ Plan plan_of(const VocabArgs &a, bool grads)
         cap = cap > kChunkMost ? kChunkMost : cap < kChunkLeast ? kChunkLeast : cap;
         p.cap = (int)(a.rows < cap ? a.rows : cap);
         p.chunks = (a.rows + p.cap - 1) / p.cap;
+        // up to 64 rows, twice: blocks of 64 (64 x 64, vocabulary 109807: 97 us, 108 in blocks of 256; 64 x 4096, 65536: 505 and 508)
         p.small = p.cap <= 64;
-        p.pairs = grads && p.cap <= kPairRows;
-        p.rows_held = (int)round_up(p.cap, p.small ? 64 : 256);
+        const int twice = grads ? 2 * whole_stages(p.cap < kPairRows ? p.cap : kPairRows) : 0, product_rows = p.cap > twice ? p.cap : twice;
+        p.rows_held = (int)round_up(product_rows, p.small ? 64 : 256);
+        p.held = grads ? p.rows_held : 0;
         p.ldx = (int)round_up(a.d, pipe::BKS);                 // whole stages of the products
         p.pack_w = p.ldx != a.d;
         p.groups = (a.vocab + 63) / 64;
@@ -453,9 +455,9 @@ Plan plan_of(const VocabArgs &a, bool grads)
         if (grads) {
             p.codes = take((size_t)p.rows_held * p.ldz * 2);
             p.dx = Splits{p.small ? 64 : 256, (a.d + 255) / 256, (a.vocab + pipe::BKS - 1) / pipe::BKS};
-            p.dx_part = take((size_t)p.dx.rows(p.pairs ? 2 * kPairRows : p.cap) * p.ldx * sizeof(float));
+            p.dx_part = take((size_t)p.dx.rows(product_rows) * p.ldx * sizeof(float));
             const long dw_blocks = (long)((a.vocab + 255) / 256) * ((a.d + 255) / 256);
-            const int row_stages = (p.cap + pipe::BKS - 1) / pipe::BKS;
+            const int row_stages = (product_rows + pipe::BKS - 1) / pipe::BKS;
             p.dw_splits = (int)(dw_blocks >= cus ? 1 : cus / dw_blocks);
             if (p.dw_splits > row_stages / 8) p.dw_splits = row_stages / 8 > 0 ? row_stages / 8 : 1;
             p.dw_parts = p.chunks > 1 || p.dw_splits > 1 || a.d % 8 != 0;
@@ -501,25 +503,25 @@ hipError_t loss_bf16(const VocabArgs &a, const VocabGrads *g, float *label_loss,
     const float deepest = kNoShare * (two ? fmaxf(1.f, a.tau) : 1.f), bend = kNoShare * (two ? fminf(1.f, a.tau) : 1.f);
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap;
-        LM_TRY(launch_arrange_rows(a, g, rl, first, p.rows_held, p.ldx, xc, p.pairs, g ? g->dX : nullptr, label_loss, top_loss, s));
+        LM_TRY(launch_arrange_rows(a, g, rl, first, p.rows_held, p.ldx, xc, p.held, g ? g->dX : nullptr, label_loss, top_loss, s));
         const Operands logits{xc, W, p.ldx, p.ldx, p.rows_held, a.vocab, p.ldx};
         const LogitsOut lo{(GroupSums *)(base + p.sums), p.groups, codes, (long)p.ldz, scale, inv_tau, deepest, bend};
         LM_TRY(launch_logits(logits, rl.count, first, p.cap, a.vocab, lo, two, s));
-        const VocabChunk c{first, p.cap, codes, p.ldz, lo.sums, two, bend, p.groups, xc, p.ldx, p.pairs};
+        const VocabChunk c{first, p.cap, codes, p.ldz, lo.sums, two, bend, p.groups, xc, p.ldx, p.held};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             const Operands o{codes, W, (long)p.ldz, p.ldx, p.rows_held, p.ldx, a.vocab};
             float *part = (float *)(base + p.dx_part);
-            LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.pairs, p.dx, part, p.ldx, s)
-                            : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.pairs, p.dx, part, p.ldx, s)));
-            LM_TRY(launch_finish_dx(true, part, 0, p.ldx, rl, first, p.cap, a.d, p.pairs, g->dX, s));
+            LM_TRY((p.small ? launch_dx<64, 1, 4, 7>(o, rl.count, first, p.cap, a.d, p.held, p.dx, part, p.ldx, s)
+                            : launch_dx<256, 2, 4, 4>(o, rl.count, first, p.cap, a.d, p.held, p.dx, part, p.ldx, s)));
+            LM_TRY(launch_finish_dx(true, part, 0, p.ldx, rl, first, p.cap, a.d, p.held, g->dX, s));
         }
         if (g && g->dW) {
             const Operands o{codes, xc, (long)p.ldz, p.ldx, (int)p.ldz, p.ldx, 0};
             float *part = (float *)(base + p.dw_part);
-            if (!p.dw_parts) LM_TRY((launch_dw<bf16_t, false>(o, rl, first, p.cap, p.pairs, a.vocab, 1, (bf16_t *)g->dW, 0, a.d, s)));
-            else if (ch == 0) LM_TRY((launch_dw<float, false>(o, rl, first, p.cap, p.pairs, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
-            else LM_TRY((launch_dw<float, true>(o, rl, first, p.cap, p.pairs, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+            if (!p.dw_parts) LM_TRY((launch_dw<bf16_t, false>(o, rl, first, p.cap, p.held, a.vocab, 1, (bf16_t *)g->dW, 0, a.d, s)));
+            else if (ch == 0) LM_TRY((launch_dw<float, false>(o, rl, first, p.cap, p.held, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
+            else LM_TRY((launch_dw<float, true>(o, rl, first, p.cap, p.held, a.vocab, p.dw_splits, part, p.dw_stride, p.ldx, s)));
         }
     }
     if (g && g->dW && p.dw_parts)
@@ -533,14 +535,14 @@ hipError_t loss_f32(const VocabArgs &a, const VocabGrads *g, float *label_loss, 
     const float *W = (const float *)a.W;
     for (int ch = 0; ch < p.chunks; ++ch) {
         const int first = ch * p.cap, cap = a.rows - first < p.cap ? a.rows - first : p.cap;
-        LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, false, g ? g->dX : nullptr, label_loss, top_loss, s));
+        LM_TRY(launch_arrange_rows(a, g, rl, first, cap, a.d, xc, 0, g ? g->dX : nullptr, label_loss, top_loss, s));
         LM_TRY(launch_gemm_f32({cap, a.vocab, a.d, xc, true, W, true, z, false, 1}, s));
-        const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0.f, 0, xc, a.d, false};
+        const VocabChunk c{first, cap, z, p.ldz, nullptr, false, 0.f, 0, xc, a.d, 0};
         LM_TRY(launch_vocab_rows(a, g, rl, c, label_loss, top_loss, s));
         if (g && g->dX) {
             const int parts = gemm_f32_splits(cap, a.d, a.vocab);
             LM_TRY(launch_gemm_f32({cap, a.d, a.vocab, z, true, W, false, dx, false, parts}, s));
-            LM_TRY(launch_finish_dx(false, dx, parts, a.d, rl, first, cap, a.d, false, g->dX, s));
+            LM_TRY(launch_finish_dx(false, dx, parts, a.d, rl, first, cap, a.d, 0, g->dX, s));
         }
         if (g && g->dW) LM_TRY(launch_gemm_f32({a.vocab, a.d, cap, z, false, xc, false, (float *)g->dW, ch > 0, 1}, s));
     }

@@ -132,11 +132,11 @@ __device__ __forceinline__ void copy_row(const T *in, long from, int d, T *out, 
     }
 }
 
-// a workgroup a row: the listed row first + b to row b of `out` (b < cap), and zeros where row b (b < zeros) is not listed.  FEW: there is no list
-// yet, and first is 0; every workgroup goes over all rows; pairs: and row b is to be found at b + kPairRows too.
+// a workgroup a row: the listed row first + b to row b of `out` (b < cap) and to its second row's place (held: second_row), and zeros where row b (b <
+// zeros) is not listed.  FEW: there is no list yet, and first is 0; every workgroup goes over all rows.
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, Weights w, const T *X, int *list, int *count, float *scale, int first, int cap, int d,
-                                                           int ld, T *out, bool pairs, int zeros, T *dX, float *label_loss, float *top_loss)
+                                                           int ld, T *out, int held, int zeros, T *dX, float *label_loss, float *top_loss)
 {
     const int b = (int)blockIdx.x;
     long from = -1;
@@ -153,11 +153,12 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, We
             top = fmaxf(top, w.of(r, l, q));
         }
         int at = scan_rows<256>(n, all, top) - n;
+        const int second = second_row(all, held), want = second && b >= second ? b - second : b;
         if (threadIdx.x == 0) mine = -1;
         __syncthreads();
         for (; has; has &= has - 1, ++at) {
             const int r = r0 + __builtin_ctz(has);
-            if (at == (pairs ? b & (kPairRows - 1) : b)) mine = r;
+            if (at == want) mine = r;
             if (b == 0) list[at] = r;
         }
         if (b == 0 && threadIdx.x == 0) {
@@ -168,7 +169,8 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, We
         __syncthreads();
         from = mine;
     } else {
-        if (b < cap && first + b < *count) from = list[first + b];
+        const int second = second_row(*count, held), want = second && b >= second ? b - second : b;
+        if (b < cap && first + want < *count) from = list[first + want];
     }
     if (b < cap) copy_row(X, from, d, out, b, ld, (int)threadIdx.x, 256);
     if (b < zeros && !t.any(b)) {
@@ -180,14 +182,14 @@ __global__ __launch_bounds__(256) void arrange_rows_kernel(Terms t, int rows, We
     }
 }
 
-hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, bool pairs, void *dX, float *label_loss, float *top_loss,
+hipError_t launch_arrange_rows(const VocabArgs &a, const VocabGrads *g, RowList rl, int first, int cap, int ld, void *out, int held, void *dX, float *label_loss, float *top_loss,
                                hipStream_t s)
 {
     const int zeros = first == 0 ? a.rows : 0;
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         hipLaunchKernelGGL(kern, dim3(cap > zeros ? cap : zeros), dim3(256), 0, s, terms_of(a), a.rows, weights_of(a, g), (const T *)a.X, rl.list, rl.count, rl.scale,
-                           first, cap, a.d, ld, (T *)out, pairs, zeros, (T *)dX, label_loss, top_loss);
+                           first, cap, a.d, ld, (T *)out, held, zeros, (T *)dX, label_loss, top_loss);
         return hipGetLastError();
     };
     const bool few = few_rows(a) && first == 0;              // later chunks have the list
@@ -268,7 +270,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // The row is written in one sweep without the label's and the entries' own terms, which then overwrite their places: their logits are taken in
 // fp32 (p - 1 of a label that is nearly certain loses everything in 16 bits).  bf16 storage: the sweep reads a logit as 16-bit steps below its group's
 // maximum (kSteps) and writes the bf16 gradient over it; the row's dot products with the label's and the entries' rows of W give their logits.
-// Few rows (c.pairs) have few entries that count, whose roundings do not average out: what rounding leaves is a second row of the products
+// Few rows (second_row) have few entries that count, whose roundings do not average out: what rounding leaves is a second row of the products
 // (the gradients' errors of 3 rows of 1216, vocabulary 103168: 2.6e-3 -> 1.7e-3, their own rounding; 16 x 4096, 65536: 362 -> 392 us).
 // What bounds it: reading and writing the row, 4 bytes a logit (bf16) or 8.
 template <typename T, bool GRADS>
@@ -283,13 +285,15 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
     __shared__ float y[kMostTop], q[kMostTop], all[kMostTop + 1], z[kMostTop + 1];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, r = (int)blockIdx.x, vocab = t.vocab;
     T *codes = (T *)c.codes + (size_t)r * c.ld;
-    if (c.first + r >= *count) {
+    const int listed = *count - c.first;
+    const size_t second = BF16 ? (size_t)second_row(*count, c.held) * c.ld : 0;           // from a row's place to its second one's
+    if (r >= listed) {
         // behind the list: the products read whole stages of 32 rows (fp32 storage: all rows of the chunk)
-        const int listed = *count - c.first, read = BF16 ? (listed + 31) / 32 * 32 : c.cap;
+        const int read = BF16 ? whole_stages(listed) : c.cap;
         if (GRADS && r < read)
             for (size_t v = tid; v < c.ld; v += kRowThreads) {
                 codes[v] = 0;
-                if (BF16 && c.pairs) codes[v + kPairRows * c.ld] = 0;
+                if (second) codes[v + second] = 0;
             }
         return;
     }
@@ -457,12 +461,12 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
                     }
                     const u32x4_t packed = {pack_bf16x2(out[0], out[1]), pack_bf16x2(out[2], out[3]), pack_bf16x2(out[4], out[5]), pack_bf16x2(out[6], out[7])};
                     *reinterpret_cast<u32x4_t *>(codes + v) = packed;
-                    if (c.pairs) {
+                    if (second) {
                         u32x4_t rest;
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             rest[k] = pack_bf16x2(rest_of(out[2 * k], __uint_as_float(packed[k] << 16)), rest_of(out[2 * k + 1], __uint_as_float(packed[k] & 0xffff0000u)));
-                        *reinterpret_cast<u32x4_t *>(codes + v + kPairRows * c.ld) = rest;
+                        *reinterpret_cast<u32x4_t *>(codes + v + second) = rest;
                     }
                 }
             };
@@ -484,9 +488,9 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(Terms t, const 
             if (labelled) dz = cl * (expf(z[j] - lse) - (ids[ntop] == v ? 1.f : 0.f));
             if (taught) dz = fmaf(ct, expf(fmaf(z[j], inv_tau, -lse_tau)) - all[j], dz);
             Elem<T>::st(codes + v, dz);
-            if (BF16 && c.pairs) {
+            if (second) {
                 const float held = __uint_as_float(pack_bf16x2(dz, 0.f) << 16);
-                Elem<T>::st(codes + v + kPairRows * c.ld, rest_of(dz, held));
+                Elem<T>::st(codes + v + second, rest_of(dz, held));
             }
         }
     }
@@ -498,7 +502,7 @@ hipError_t launch_vocab_rows(const VocabArgs &a, const VocabGrads *g, RowList rl
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         // with gradients of bf16 storage also the rows up to a whole stage of the products' contraction
-        const int rows = a.bf16 && g ? (c.cap + 31) / 32 * 32 : c.cap;
+        const int rows = a.bf16 && g ? whole_stages(c.cap) : c.cap;
         hipLaunchKernelGGL(kern, dim3(rows), dim3(kRowThreads), 0, s, terms_of(a), g ? *g : none, (const T *)a.W, a.d, a.tau, (const int *)rl.list,
                            (const int *)rl.count, (const float *)rl.scale, c, label_loss, top_loss);
         return hipGetLastError();
@@ -543,7 +547,7 @@ __device__ __forceinline__ void store_scaled(T *out, int left, float (&f)[8], fl
 // a workgroup a row of the chunk, to where the row came from
 template <typename T>
 __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, int known, int ld, const int *list, const int *count, const float *scale, int first,
-                                                        int cap, int d, bool pairs, T *dX)
+                                                        int cap, int d, int held, T *dX)
 {
     int rows = *count - first;
     if (rows > cap) rows = cap;
@@ -551,7 +555,8 @@ __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, int k
     if (r >= rows) return;
     const bool bf16 = sizeof(T) == 2;
     const int parts = bf16 ? count[1] : known, n = threads_of(d), groups = 256 / n, group = (int)threadIdx.x / n, t = (int)threadIdx.x % n;
-    const size_t stride = (size_t)(pairs ? 2 * kPairRows : bf16 ? rows : cap) * ld;
+    const int second = bf16 ? second_row(*count, held) : 0;
+    const size_t stride = (size_t)(second ? 2 * second : bf16 ? rows : cap) * ld;
     const float *from = part + (size_t)r * ld, factor = bf16 ? scale[1] : 1.f;
     T *to = dX + (size_t)list[first + r] * d;
     // short rows: several groups of threads share the parts, and the first adds them up in order
@@ -561,9 +566,9 @@ __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, int k
         float f[8] = {};
         if (c < d) {
             sum_parts(from + c, group, parts, groups, stride, d - c, f);
-            if (pairs) {
+            if (second) {
                 float rest[8];
-                sum_parts(from + (size_t)kPairRows * ld + c, group, parts, groups, stride, d - c, rest);
+                sum_parts(from + (size_t)second * ld + c, group, parts, groups, stride, d - c, rest);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] += rest[e];
             }
@@ -583,11 +588,11 @@ __global__ __launch_bounds__(256) void finish_dx_kernel(const float *part, int k
     }
 }
 
-hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, bool pairs, void *dX, hipStream_t s)
+hipError_t launch_finish_dx(bool bf16, const float *part, int parts, int ld, RowList rl, int first, int cap, int d, int held, void *dX, hipStream_t s)
 {
     auto run = [&](auto kern, auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, parts, ld, (const int *)rl.list, (const int *)rl.count, (const float *)rl.scale, first, cap, d, pairs, (T *)dX);
+        hipLaunchKernelGGL(kern, dim3(cap), dim3(256), 0, s, part, parts, ld, (const int *)rl.list, (const int *)rl.count, (const float *)rl.scale, first, cap, d, held, (T *)dX);
         return hipGetLastError();
     };
     return bf16 ? run(finish_dx_kernel<bf16_t>, (bf16_t *)nullptr) : run(finish_dx_kernel<float>, (float *)nullptr);
