@@ -27,7 +27,7 @@ class _ResidualNorm(torch.autograd.Function):
     def forward(ctx, X, H, gate, w_post, w_pre, scale, flags):
         X, H = X.contiguous(), H.contiguous()
         rows, n = X.shape
-        prob = stl.ResidualProblem(rows, n, -(-rows // gate.shape[0]), 1.0, scale, 1e-6, _DT[X.dtype])
+        prob = stl.ResidualProblem(rows, n, max(1, -(-rows // gate.shape[0])), 1.0, scale, 1e-6, _DT[X.dtype])
         Xout, Z = torch.empty_like(X), torch.empty_like(X)
         stl.stl_residual_norm_forward(prob, X, H, gate, w_post, None, w_pre, None, Xout, Z, flags)
         ctx.prob, ctx.flags = prob, flags
@@ -39,7 +39,8 @@ class _ResidualNorm(torch.autograd.Function):
         Xout, H, gate, w_post, w_pre = ctx.saved_tensors
         dXout, dZ = dXout.contiguous(), dZ.contiguous()
         dX, dH = torch.empty_like(Xout), torch.empty_like(Xout)
-        sums = [torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in (gate, w_post, w_pre)]
+        # (without rows there is no row of the gate that the library would write)
+        sums = [(torch.empty if ctx.prob.rows else torch.zeros)(t.shape, dtype=torch.float32, device=t.device) for t in (gate, w_post, w_pre)]
         nbytes = stl.stl_residual_norm_workspace_bytes(ctx.prob, ctx.flags)
         stl.stl_residual_norm_backward(ctx.prob, Xout, H, gate, w_post, None, w_pre, dXout, dZ, dX, dH, sums[0], sums[1], None, sums[2], None, 0,
                                        _scratch(nbytes, Xout.device), nbytes, ctx.flags)
@@ -47,7 +48,11 @@ class _ResidualNorm(torch.autograd.Function):
 
 
 def residual_norm(X, H, gate, w_post, w_pre, scale=1.0, center=False):
-    """(X + scale gate * norm(H) w_post, norm of that times w_pre) for X, H (rows, n), gate (groups of rows, n); differentiable in the five tensors."""
+    """(X + scale gate * norm(H) w_post, norm of that times w_pre) for X, H (rows, n), gate (groups of rows, n); differentiable in the five tensors.  The
+    groups have ceil(rows / groups) rows each, the last one what is left, which has to be some."""
+    rows, groups = X.shape[0], gate.shape[0]
+    if groups < 1 or rows and -(-rows // -(-rows // groups)) != groups:
+        raise ValueError(f"{rows} rows in groups of {-(-rows // max(groups, 1))} do not take {groups} rows of the gate")
     flags = stl.STL_FLAG_POST_NORM | stl.STL_FLAG_PRE_NORM | (stl.STL_FLAG_CENTER if center else 0)
     return _ResidualNorm.apply(X, H, gate, w_post, w_pre, scale, flags)
 
