@@ -22,10 +22,26 @@ import paper_2503_12211_amd as stl
 from .stl_linear import _DT, STLLinear, _scratch
 
 
+def _like(name, t, shape, dtype, X):
+    """The library reads plain pointers: a tensor of another type or size, or on another device, would be read as what it is not."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape) or t.device != X.device:
+        raise ValueError(f"{name} of {tuple(t.shape)} on {t.device}, not {tuple(shape)} on {X.device}")
+
+
+def _states(X):
+    if X.dtype not in _DT:
+        raise TypeError(f"X is {X.dtype}: float32 or bfloat16")
+    if X.dim() != 2:
+        raise ValueError(f"X of {tuple(X.shape)}: rows and columns")
+    return X.shape
+
+
 class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, H, gate, w_post, w_pre, scale, flags):
-        X, H = X.contiguous(), H.contiguous()
+        X, H, gate, w_post, w_pre = (t.contiguous() for t in (X, H, gate, w_post, w_pre))
         rows, n = X.shape
         prob = stl.ResidualProblem(rows, n, max(1, -(-rows // gate.shape[0])), 1.0, scale, 1e-6, _DT[X.dtype])
         Xout, Z = torch.empty_like(X), torch.empty_like(X)
@@ -50,7 +66,10 @@ class _ResidualNorm(torch.autograd.Function):
 def residual_norm(X, H, gate, w_post, w_pre, scale=1.0, center=False):
     """(X + scale gate * norm(H) w_post, norm of that times w_pre) for X, H (rows, n), gate (groups of rows, n); differentiable in the five tensors.  The
     groups have ceil(rows / groups) rows each, the last one what is left, which has to be some."""
-    rows, groups = X.shape[0], gate.shape[0]
+    rows, n = _states(X)
+    groups = gate.shape[0]
+    for name, t, shape in (("H", H, (rows, n)), ("gate", gate, (groups, n)), ("w_post", w_post, (n,)), ("w_pre", w_pre, (n,))):
+        _like(name, t, shape, X.dtype, X)
     if groups < 1 or rows and -(-rows // -(-rows // groups)) != groups:
         raise ValueError(f"{rows} rows in groups of {-(-rows // max(groups, 1))} do not take {groups} rows of the gate")
     flags = stl.STL_FLAG_POST_NORM | stl.STL_FLAG_PRE_NORM | (stl.STL_FLAG_CENTER if center else 0)
@@ -60,7 +79,7 @@ def residual_norm(X, H, gate, w_post, w_pre, scale=1.0, center=False):
 class _VocabLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W, label, top_id, top_logit, label_weight, top_weight, temperature):
-        X, W = X.contiguous(), W.contiguous()
+        X, W, label, top_id, top_logit = (None if t is None else t.contiguous() for t in (X, W, label, top_id, top_logit))
         rows, d = X.shape
         ntop = 0 if top_id is None else top_id.shape[1]
         prob = stl.VocabProblem(rows, d, W.shape[0], ntop, temperature, _DT[X.dtype])
@@ -91,9 +110,16 @@ class _VocabLoss(torch.autograd.Function):
 def vocab_loss(X, W, label=None, top_id=None, top_logit=None, temperature=1.0, distill=1.0):
     """Mean cross entropy of the rows with a label, plus `distill` times the mean divergence from the teacher's top logits over the rows; X (rows, d), W
     (vocab, d), label (rows,) int64, top_id and top_logit (rows, ntop) int64 and float32.  Differentiable in X and W."""
-    rows = X.shape[0]
+    rows, d = _states(X)
+    _like("W", W, (W.shape[0], d), X.dtype, X)
     label_weight = top_weight = None
+    if (top_id is None) != (top_logit is None):
+        raise ValueError("top_id and top_logit go together")
+    if top_id is not None:
+        _like("top_id", top_id, (rows, top_id.shape[-1]), torch.int64, X)
+        _like("top_logit", top_logit, top_id.shape, torch.float32, X)
     if label is not None:
+        _like("label", label, (rows,), torch.int64, X)
         has = (label >= 0) & (label < W.shape[0])
         label_weight = (has / has.sum().clamp_min(1)).float()
     if top_id is not None:

@@ -76,3 +76,55 @@ def test_step_without_rows(calls):
     assert Xout.shape == Z.shape == (0, 8)
     (Xout.sum() + Z.sum()).backward()
     assert not t[2].grad.any() and not t[3].grad.any()
+
+
+def bad_step(**kw):
+    t = dict(zip(("X", "H", "gate", "w_post", "w_pre"), step()))
+    t.update(kw)
+    return t
+
+
+@pytest.mark.parametrize("kw,error", [
+    (dict(w_post=torch.ones(8, dtype=torch.bfloat16)), TypeError), (dict(H=torch.ones(12, 8, dtype=torch.float64)), TypeError),
+    (dict(gate=torch.ones(3, 8, dtype=torch.bfloat16)), TypeError), (dict(w_pre=torch.ones(8, dtype=torch.float16)), TypeError),
+    (dict(H=torch.ones(11, 8)), ValueError), (dict(H=torch.ones(12, 9)), ValueError), (dict(gate=torch.ones(3, 4)), ValueError), (dict(gate=torch.ones(8)), ValueError),
+    (dict(w_post=torch.ones(9)), ValueError), (dict(w_pre=torch.ones(1, 8)), ValueError), (dict(X=torch.ones(2, 6, 8)), ValueError),
+    (dict(H=torch.ones(12, 8, device="meta")), ValueError)])
+def test_step_arguments_that_are_refused(calls, kw, error):
+    with pytest.raises(error):
+        stl_lm.residual_norm(**bad_step(**kw))
+    assert not calls
+
+
+def test_step_arguments_are_passed_dense(calls):
+    t = bad_step(gate=torch.ones(1, 8).expand(3, 8), w_post=torch.ones(16)[::2], w_pre=torch.ones(1).expand(8), H=torch.ones(8, 12).t())
+    t["X"] = t["X"].detach().requires_grad_()
+    stl_lm.residual_norm(**t)
+    assert all(calls[0][1][k].is_contiguous() for k in ("X", "H", "gate", "w_post", "w_pre"))
+
+
+def scored(rows=6, d=8, vocab=20, ntop=3, dtype=torch.float32):
+    g = torch.Generator().manual_seed(1)
+    return dict(X=torch.randn((rows, d), generator=g).to(dtype), W=torch.randn((vocab, d), generator=g).to(dtype), label=torch.randint(0, vocab, (rows,), generator=g),
+                top_id=torch.randint(0, vocab, (rows, ntop), generator=g), top_logit=torch.randn((rows, ntop), generator=g))
+
+
+@pytest.mark.parametrize("kw,error", [
+    (dict(label=torch.zeros(6, dtype=torch.int32)), TypeError), (dict(top_id=torch.zeros(6, 3, dtype=torch.int32)), TypeError),
+    (dict(top_logit=torch.zeros(6, 3, dtype=torch.bfloat16)), TypeError), (dict(W=torch.zeros(20, 8, dtype=torch.bfloat16)), TypeError),
+    (dict(label=torch.zeros(5, dtype=torch.int64)), ValueError), (dict(label=torch.zeros(6, 1, dtype=torch.int64)), ValueError),
+    (dict(top_id=torch.zeros(5, 3, dtype=torch.int64)), ValueError), (dict(top_id=torch.zeros(6, dtype=torch.int64)), ValueError), (dict(top_logit=torch.zeros(6, 2)), ValueError), (dict(top_logit=None), ValueError),
+    (dict(top_id=None), ValueError), (dict(W=torch.zeros(20, 9)), ValueError), (dict(X=torch.zeros(2, 3, 8)), ValueError),
+    (dict(label=torch.zeros(6, dtype=torch.int64, device="meta")), ValueError)])
+def test_loss_arguments_that_are_refused(calls, kw, error):
+    with pytest.raises(error):
+        stl_lm.vocab_loss(**{**scored(), **kw})
+    assert not calls
+
+
+def test_loss_arguments_are_passed_dense(calls):
+    s = scored()
+    s.update(X=torch.ones(8, 6).t(), W=torch.ones(8, 20).t(), label=torch.zeros(12, dtype=torch.int64)[::2], top_id=torch.zeros(6, 1, dtype=torch.int64).expand(6, 3),
+             top_logit=torch.zeros(3, 6).t())
+    stl_lm.vocab_loss(**s)
+    assert all(calls[0][1][k].is_contiguous() for k in ("X", "W", "label", "top_id", "top_logit"))
