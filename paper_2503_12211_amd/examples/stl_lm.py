@@ -104,7 +104,9 @@ class _VocabLoss(torch.autograd.Function):
     @staticmethod
     def backward(ctx, upstream):
         dX, dW = ctx.saved_tensors
-        return upstream.to(dX.dtype) * dX, upstream.to(dW.dtype) * dW, None, None, None, None, None, None
+        # (in fp32: the factor rounded to bf16 would be an error that all gradients have in common)
+        scaled = lambda t: (t.float() * upstream).to(t.dtype)  # noqa: E731
+        return scaled(dX), scaled(dW), None, None, None, None, None, None
 
 
 def vocab_loss(X, W, label=None, top_id=None, top_logit=None, temperature=1.0, distill=1.0):

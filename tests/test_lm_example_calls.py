@@ -128,3 +128,16 @@ def test_loss_arguments_are_passed_dense(calls):
              top_logit=torch.zeros(3, 6).t())
     stl_lm.vocab_loss(**s)
     assert all(calls[0][1][k].is_contiguous() for k in ("X", "W", "label", "top_id", "top_logit"))
+
+
+def test_loss_gradients_take_the_upstream_factor_in_fp32(calls):
+    """A factor that bf16 does not hold (a third is 0.2 % off there) is multiplied in fp32, and the gradient rounded behind it."""
+    s = scored(dtype=torch.bfloat16)
+    for k in "XW":
+        s[k].requires_grad_()
+    (stl_lm.vocab_loss(**s) / 3).backward()
+    got = calls[0][1]
+    factor = torch.tensor(1.0) / 3
+    for k in "XW":
+        assert s[k].grad.dtype == torch.bfloat16
+        assert torch.equal(s[k].grad, (got["d" + k].float() * factor).to(torch.bfloat16)), k
