@@ -16,6 +16,7 @@ from __future__ import annotations
 import argparse
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2503_12211_amd as stl
 
@@ -51,6 +52,7 @@ class _ResidualNorm(torch.autograd.Function):
         return Xout, Z
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dXout, dZ):
         Xout, H, gate, w_post, w_pre = ctx.saved_tensors
         dXout, dZ = dXout.contiguous(), dZ.contiguous()
@@ -102,6 +104,7 @@ class _VocabLoss(torch.autograd.Function):
         return total
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, upstream):
         dX, dW = ctx.saved_tensors
         # (in fp32: the factor rounded to bf16 would be an error that all gradients have in common)

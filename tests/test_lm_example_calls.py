@@ -141,3 +141,17 @@ def test_loss_gradients_take_the_upstream_factor_in_fp32(calls):
     for k in "XW":
         assert s[k].grad.dtype == torch.bfloat16
         assert torch.equal(s[k].grad, (got["d" + k].float() * factor).to(torch.bfloat16)), k
+
+
+def test_second_derivatives_are_refused(calls):
+    """Neither function's gradients come with their own graph: a second derivative would lack their terms."""
+    s = scored()
+    X, W = s["X"].requires_grad_(), s["W"].requires_grad_()
+    scale = torch.ones((), requires_grad=True)
+    g = torch.autograd.grad(stl_lm.vocab_loss(**{**s, "X": X, "W": W}) * scale, X, create_graph=True)[0]
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
+    t = step()
+    g = torch.autograd.grad(sum(o.square().sum() for o in stl_lm.residual_norm(*t)), t[0], create_graph=True)[0]
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
