@@ -80,19 +80,19 @@ def residual_norm(X, H, gate, w_post, w_pre, scale=1.0, center=False):
 
 class _VocabLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, X, W, label, top_id, top_logit, label_weight, top_weight, temperature):
+    def forward(ctx, X, W, label, top_id, top_logit, label_weight, top_weight, temperature, want_x, want_w):
         X, W, label, top_id, top_logit = (None if t is None else t.contiguous() for t in (X, W, label, top_id, top_logit))
         rows, d = X.shape
         ntop = 0 if top_id is None else top_id.shape[1]
         prob = stl.VocabProblem(rows, d, W.shape[0], ntop, temperature, _DT[X.dtype])
         losses = [torch.empty(rows, dtype=torch.float32, device=X.device) if t is not None else None for t in (label, top_id)]
         inputs = (prob, X, W, label, top_id, top_logit)
-        train = ctx.needs_input_grad[0] or ctx.needs_input_grad[1]
+        train = want_x or want_w
         nbytes = stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_BACKWARD if train else stl.STL_OP_FORWARD)
         ws = _scratch(nbytes, X.device)
         if train:
             # the row weights are known here: losses and gradients come from one call, which forms the logits once
-            dX, dW = torch.empty_like(X), torch.empty_like(W)
+            dX, dW = torch.empty_like(X) if want_x else None, torch.empty_like(W) if want_w else None
             stl.stl_vocab_loss_backward(*inputs, label_weight, top_weight, *losses, dX, dW, ws, nbytes)
             ctx.save_for_backward(dX, dW)
         else:
@@ -108,8 +108,8 @@ class _VocabLoss(torch.autograd.Function):
     def backward(ctx, upstream):
         dX, dW = ctx.saved_tensors
         # (in fp32: the factor rounded to bf16 would be an error that all gradients have in common)
-        scaled = lambda t: (t.float() * upstream).to(t.dtype)  # noqa: E731
-        return scaled(dX), scaled(dW), None, None, None, None, None, None
+        scaled = lambda t: None if t is None else (t.float() * upstream).to(t.dtype)  # noqa: E731
+        return scaled(dX), scaled(dW), *[None] * 8
 
 
 def vocab_loss(X, W, label=None, top_id=None, top_logit=None, temperature=1.0, distill=1.0):
@@ -129,7 +129,9 @@ def vocab_loss(X, W, label=None, top_id=None, top_logit=None, temperature=1.0, d
         label_weight = (has / has.sum().clamp_min(1)).float()
     if top_id is not None:
         top_weight = torch.full((rows,), distill / max(rows, 1), dtype=torch.float32, device=X.device)
-    return _VocabLoss.apply(X, W, label, top_id, top_logit, label_weight, top_weight, temperature)
+    # (asked here: the function's own needs_input_grad is set for a parameter under no_grad too)
+    want = [torch.is_grad_enabled() and t.requires_grad for t in (X, W)]
+    return _VocabLoss.apply(X, W, label, top_id, top_logit, label_weight, top_weight, temperature, *want)
 
 
 class STLLanguageModel(torch.nn.Module):

@@ -155,3 +155,23 @@ def test_second_derivatives_are_refused(calls):
     g = torch.autograd.grad(sum(o.square().sum() for o in stl_lm.residual_norm(*t)), t[0], create_graph=True)[0]
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("grad_x,grad_w", [(True, True), (True, False), (False, True)])
+def test_loss_gradients_are_formed_where_they_are_asked_for(calls, grad_x, grad_w):
+    s = scored()
+    X, W = s["X"].requires_grad_(grad_x), s["W"].requires_grad_(grad_w)
+    stl_lm.vocab_loss(**s).backward()
+    assert calls.names() == ["vocab_backward"]
+    assert (calls[0][1]["dX"] is not None) == grad_x and (calls[0][1]["dW"] is not None) == grad_w
+    assert (X.grad is not None) == grad_x and (W.grad is not None) == grad_w
+
+
+def test_scoring_is_the_forward_call(calls):
+    """A parameter's requires_grad is set under no_grad too."""
+    s = scored()
+    s["W"] = torch.nn.Parameter(s["W"])
+    with torch.no_grad():
+        assert not stl_lm.vocab_loss(**s).requires_grad
+    stl_lm.vocab_loss(**{**s, "W": s["W"].detach()})
+    assert calls.names() == ["vocab_forward"] * 2
