@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 from pathlib import Path
 
 _HERE = Path(__file__).resolve().parent
@@ -56,6 +56,11 @@ class Problem:
         return _CProblem(self.m, self.k, self.n, self.t, self.r, self.dtype)
 
 
+def _rebuilt(self):
+    """__reduce__ of a problem that keeps its C form, which neither pickle nor deepcopy takes: made again from the fields."""
+    return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
+
 class _CResidual(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("rows_per_gate", ctypes.c_int64), ("skip", ctypes.c_float),
                 ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
@@ -77,6 +82,8 @@ class ResidualProblem:
         per = self.rows_per_gate if self.rows_per_gate is not None else max(self.rows, 1)
         object.__setattr__(self, "ref", ctypes.byref(_CResidual(self.rows, self.n, per, self.skip, self.scale, self.eps, self.dtype)))
 
+    __reduce__ = _rebuilt
+
 
 class _CVocab(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ntop", ctypes.c_int64),
@@ -95,6 +102,8 @@ class VocabProblem:
 
     def __post_init__(self):
         object.__setattr__(self, "ref", ctypes.byref(_CVocab(self.rows, self.d, self.vocab, self.ntop, self.temperature, self.dtype)))
+
+    __reduce__ = _rebuilt
 
 
 _lib = None

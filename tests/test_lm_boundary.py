@@ -96,3 +96,17 @@ def test_vocabulary_arguments_that_are_refused():
 def test_vocabulary_workspace_is_bounded_in_the_rows():
     sizes = [stl.stl_vocab_loss_workspace_bytes(stl.VocabProblem(rows, 4096, 131072), stl.STL_OP_BACKWARD) for rows in (8192, 16384, 1 << 20)]
     assert sizes[0] < 4 << 30 and sizes[2] - sizes[1] < 8 << 20 and sizes[2] < 6 << 30
+
+
+@pytest.mark.parametrize("prob", [stl.ResidualProblem(5, 64), stl.ResidualProblem(5, 64, 2, 0.5, 2.0, 1e-5, stl.STL_F32), stl.VocabProblem(7, 32, 100, 4, 2.0, stl.STL_F32)])
+def test_problems_are_copied_and_sent(prob):
+    """As stl.Problem is: with a module that keeps one, or to another process."""
+    import copy
+    import pickle
+    flags = stl.STL_FLAG_PRE_NORM
+    for twin in (copy.copy(prob), copy.deepcopy(prob), pickle.loads(pickle.dumps(prob))):
+        assert twin == prob
+        if isinstance(prob, stl.VocabProblem):
+            assert stl.stl_vocab_loss_workspace_bytes(twin, stl.STL_OP_BACKWARD) == stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_BACKWARD) > 0
+        else:
+            assert stl.stl_residual_norm_workspace_bytes(twin, flags) == stl.stl_residual_norm_workspace_bytes(prob, flags) > 0
