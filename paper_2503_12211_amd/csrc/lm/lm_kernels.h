@@ -60,9 +60,10 @@ struct VocabGrads {
 };
 constexpr int kMostTop = 1024;
 // Rows of a chunk.  bf16: as many as have kChunkCodes logits (4.3 GB of codes), kChunkLeast to kChunkMost of them, which fill the chip several times
-// over; fp32: as many as have kChunkLogits (1 GiB), kChunkLeastF32 at least.
+// over; fp32: as many as have kChunkLogits (1 GiB), kChunkLeastF32 at least, and no more than kChunkMostF32: a launch of a workgroup of 512 a row has fewer
+// than 2^32 threads.
 constexpr long kChunkCodes = 1L << 31, kChunkLogits = 1L << 28;
-constexpr int kChunkLeast = 256, kChunkMost = 8192, kChunkLeastF32 = 64;
+constexpr int kChunkLeast = 256, kChunkMost = 8192, kChunkLeastF32 = 64, kChunkMostF32 = 1 << 22;
 // A logit between its product and its gradient is held (bf16 storage) in 16 bits: y = z log2(e) / t, t = 1 where there are labels and tau otherwise, in steps
 // from its group's maximum down to its minimum, 65534; 65535 is what is below every share that fp32 can hold (minus infinity among it): 2^-kNoShare.
 // One temperature: even steps over at most kNoShare; half a step is at most 1.1e-3, that is 8e-4 of a share.  A group of 64 normal logits spreads over

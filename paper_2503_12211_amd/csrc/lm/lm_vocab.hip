@@ -466,7 +466,7 @@ Plan plan_of(const VocabArgs &a, bool grads)
         }
     } else {
         long cap = kChunkLogits / a.vocab;
-        cap = cap < kChunkLeastF32 ? kChunkLeastF32 : cap;
+        cap = cap < kChunkLeastF32 ? kChunkLeastF32 : cap > kChunkMostF32 ? kChunkMostF32 : cap;
         p.cap = (int)(a.rows < cap ? a.rows : cap);
         p.chunks = (a.rows + p.cap - 1) / p.cap;
         p.ldx = a.d;

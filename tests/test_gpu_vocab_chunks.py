@@ -80,3 +80,25 @@ def test_rows_of_every_chunk(rows, d, vocab, dtype, label, top):
     assert float(((dX.double() - want_dx).norm(dim=1) / want_dx.norm(dim=1).clamp_min(1e-30))[~none].max()) <= 4 * bar          # of a single row
     assert float((dX.double() - want_dx).norm() / want_dx.norm()) <= bar
     assert float((dW.double() - want_dw).norm() / want_dw.norm()) <= bar
+
+
+def test_more_rows_than_a_launch_has_workgroups_for():
+    """8.4 million rows of two classes in fp32: 512 threads a row would be 2^32 and more of them."""
+    rows, d, vocab = (1 << 23) + 5000, 3, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X, W = torch.randn((rows, d), generator=g, device="cuda"), torch.randn((vocab, d), generator=g, device="cuda")
+    label = torch.randint(-1, vocab, (rows,), generator=g, device="cuda")
+    prob = stl.VocabProblem(rows, d, vocab, dtype=stl.STL_F32)
+    n = stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+    ws, loss = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.full((rows,), float("nan"), device="cuda")
+    dX, dW, weight = torch.full_like(X, float("nan")), torch.empty_like(W), torch.full((rows,), 1.0, device="cuda")
+    stl.stl_vocab_loss_backward(prob, X, W, label, None, None, weight, None, loss, None, dX, dW, ws, n)
+    has = (label >= 0).double()
+    lp = torch.log_softmax(X.double() @ W.double().t().contiguous(), 1)
+    p = lp.exp().scatter_add_(1, label.clamp(0)[:, None], torch.full((rows, 1), -1.0, dtype=torch.float64, device="cuda")) * has[:, None]
+    # logits below 20 in size: 16 roundings of 20; sums of 4 million terms of either sign, in chains of 2^22 / 512 and blocks of 32
+    assert float((loss.double() + lp.gather(1, label.clamp(0)[:, None])[:, 0] * has).abs().max()) <= 16 * 20 * 2.0 ** -24
+    assert float((dX.double() - p @ W.double()).abs().max()) <= 64 * 20 * 2.0 ** -24
+    want = p.t().contiguous() @ X.double()
+    size = p.abs().t().contiguous() @ X.double().abs()
+    assert bool(((dW.double() - want).abs() <= 1e-4 * size).all())
