@@ -323,7 +323,9 @@ stl_status_t stl_residual_norm_forward(const stl_residual_t *prob, const void *X
  * dXout, dZ: storage dtype, either may be NULL (zeros).  dX, dH: storage dtype; dgate (the gate's shape), dw_post, db_post, dw_pre, db_pre:
  * fp32; any may be NULL.  The gradient of what the flags or a missing gate leave out: INVALID_ARG.  dX may be dXout.
  * accumulate: 0 overwrites the fp32 gradients, 1 adds into them (no rows: zeros, or nothing).  The same bits from run to run.
- * ws / ws_bytes: at least stl_residual_norm_workspace_bytes(prob, flags).
+ * ws / ws_bytes: at least stl_residual_norm_workspace_bytes(prob, flags): 16 n bytes for each of up to 256 workgroups and, where 1 < rows_per_gate
+ * (with a gate or without), fp32 sums of one to 256 / groups parts of every group of rows, that is at least the gate's shape (2^20 x 4096, two
+ * rows a gate row: 8 GiB).
  */
 size_t stl_residual_norm_workspace_bytes(const stl_residual_t *prob, int flags);
 stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *Xout, const void *H, const void *gate, const void *w_post,
@@ -332,19 +334,23 @@ stl_status_t stl_residual_norm_backward(const stl_residual_t *prob, const void *
                                         int flags, void *stream);
 
 /*
- * Loss over a vocabulary from hidden states, without the logits z = X W^T in memory.  Up to two terms for every row t:
+ * Loss over a vocabulary from hidden states; the logits z = X W^T are formed for a chunk of the rows at a time.  Up to two terms for every row t:
  *     label_loss[t] = log sum_v exp z_tv - z_t,label[t]                                     (label not NULL)
  *     top_loss[t]   = sum_j q_j (log q_j - log softmax(z_t / tau)[top_id[t][j]])           (ntop > 0)
  * the second being distillation from a teacher's `ntop` largest logits: q = softmax over j of top_logit[t][j] / tau.  A label outside
  * 0 .. vocab-1 (such as -100) is none; so is an entry with an id outside, or a logit of minus infinity, and a row may have none.  A row
- * without a term has that loss 0 and no gradient from it; where it has neither its X is not looked at (whatever it holds) and costs no products.
+ * without a term has that loss 0 and no gradient from it; where it has neither its X is not looked at (whatever it holds) and costs no products
+ * in bf16 storage (in fp32 it costs what the others do).
  * An id may stand in a row more than once: it is one entry with the sum of its shares.
  * X: rows x d, W: vocab x d (storage dtype).  label: rows; top_id, top_logit: rows x ntop.  label_loss, top_loss: rows fp32 (out) or NULL.
  * Sums are fp32; bf16 logits are fp32 sums of exact products, fp32 logits fp32 products.
  * 0 <= rows <= STL_MAX_DIM (0: pointers of what has rows may be NULL), 1 <= d <= STL_VOCAB_WIDEST, 1 <= vocab <= STL_VOCAB_MOST,
  * 0 <= ntop <= STL_VOCAB_MOST_TOP, 0.25 <= temperature <= 16 (not read without a teacher).  At least one term.
- * ws / ws_bytes: at least stl_vocab_loss_workspace_bytes(prob, STL_OP_FORWARD or STL_OP_BACKWARD); rows are taken in chunks, so that it is
- * bounded by a few GB however many there are.
+ * ws / ws_bytes: at least stl_vocab_loss_workspace_bytes(prob, STL_OP_FORWARD or STL_OP_BACKWARD).  Rows are taken in chunks -- bf16 of 256 to 8192 with up to
+ * 2^31 logits, fp32 of 64 to 2^22 with up to 2^28 -- and behind the first chunk a row adds 4 bytes.  A chunk's logits take 4 bytes each in fp32 storage; in bf16
+ * storage none for a loss alone, 2 with gradients, and a quarter of a byte for sums.  Beside them: its rows of X; with gradients dX in fp32 parts (bf16: 268 MB
+ * or the chunk's dX); and in bf16 storage W again where 32 does not divide d, and dW in fp32 where 8 does not divide d, where there is more than one chunk, and
+ * where it has 128 blocks of 256 x 256 or fewer and its rows are summed in parts.
  */
 typedef struct {
     int64_t rows, d, vocab, ntop;
@@ -363,7 +369,10 @@ stl_status_t stl_vocab_loss_forward(const stl_vocab_t *prob, const void *X, cons
  *     dz_tv = dlabel[t] (softmax(z_t)[v] - [v = label[t]]) + dtop[t] / tau (softmax(z_t / tau)[v] - sum_{j: top_id[t][j] = v} q_j)
  *     dX = dz W,   dW = dz^T X.
  * dlabel, dtop: rows fp32; NULL stands for zeros (one of them at least).  dX: rows x d, dW: vocab x d (out, storage dtype), either may be NULL
- * (not both).  bf16: dz is rounded to bf16 once for the two products, dX and dW once.  The same bits from run to run.
+ * (not both).  The same bits from run to run.  bf16 storage: between its product and dz a logit is held in 16 bits, in steps of its group of 64 columns' range
+ * (a share of the softmax is off by 8e-4 of itself at most, 1.6e-3 with two temperatures, and by 4e-5 where logits have a deviation of 2); dz is rounded to
+ * bf16 once for the two products, or, up to 128 rows with a term, held as two bf16 numbers; dX and dW are rounded once.  So their relative errors are 1.7e-3 up to
+ * 128 rows, the outputs' own rounding, and 1.9e-3 to 2.5e-3 above.
  */
 stl_status_t stl_vocab_loss_backward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
                                      const float *top_logit, const float *dlabel, const float *dtop, float *label_loss, float *top_loss, void *dX,

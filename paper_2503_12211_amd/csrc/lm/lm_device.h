@@ -35,7 +35,7 @@ __device__ __forceinline__ float wave_max(float v)
     return last_lane(v);
 }
 
-// Eight consecutive elements of a row, held as loaded; `left` of them (or fewer) are in the row, the others read as `fill` bits.  Rows start at
+// Eight consecutive elements of a row, held as loaded; `left` of them (or fewer) are in the row, the others are zeros.  Rows start at
 // any element: gfx950 loads and stores 16 bytes at any address, and the last, incomplete chunk of a row goes element by element.
 template <typename T> struct Chunk;
 template <> struct Chunk<bf16_t> {

@@ -4,8 +4,9 @@
 // What bounds it: the matrix cores, 64 cycles a product of 32 x 32 x 2 (157 TFLOP/s at 2.4 GHz).  A workgroup has a block of 64 x 64 outputs, a quarter
 // for each of four wavefronts; where there are fewer than two blocks a CU, two or four groups of four wavefronts share a block's contraction,
 // each with every second or fourth stage, and add their sums up in LDS.  (Blocks of 32 x 32 as in ../stl_gemm_generic.hip move twice the
-// bytes through LDS; 2048 rows of 768, 1000 classes, us of the three products under the profiler: 80, 64 and 62 there, 51, 56 and 58 here, the
-// whole call 192 and 151.  The matrix cores are busy for two thirds of the time that wavefronts are there.)  A stage holds 32 elements
+// bytes through LDS; 2048 rows of 768, 1000 classes, us of the three products under the profiler: 80, 64 and 62 there, 52, 64 and 68 here, the
+// whole call 192 and 153.  The matrix cores are busy for 60, 61 and 59 % of the time that CUs have wavefronts, and for 45, 39 and 37 % of the three launches:
+// 512, 384 and 192 equal blocks on 256 CUs.)  A stage holds 32 elements
 // of the contraction; the next two's are on their way through registers while it is multiplied, into the other half of LDS.  Operands keep their orientation in LDS,
 // with rows padded so that a fragment's lanes fall on all banks: [row][l] 36 floats (a lane reads four l at once, one for each of four
 // products), [l][row] 72.

@@ -86,11 +86,11 @@ static inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t residual_workspace_bytes(int rows, int n, int per_gate)
 {
     if (rows == 0) return 0;
-    // with a gate or without one: the vectors' partials of at most 512 workgroups and the gate's, one an item
-    int grid = 0, grid1 = 0;
-    const ResidualItems it = residual_items(rows, n, per_gate, true, &grid), no = residual_items(rows, n, per_gate, false, &grid1);
-    (void)no;
-    const size_t vec = round256((size_t)(grid > grid1 ? grid : grid1) * 4 * n * sizeof(float));
+    // with a gate or without one: the vectors' partials of at most 256 workgroups and the gate's, one an item
+    int grid = 0, gateless = 0;
+    const ResidualItems it = residual_items(rows, n, per_gate, true, &grid);
+    residual_items(rows, n, per_gate, false, &gateless);
+    const size_t vec = round256((size_t)(grid > gateless ? grid : gateless) * 4 * n * sizeof(float));
     return vec + (it.gate_rows ? 0 : round256((size_t)it.groups * it.pieces * n * sizeof(float)));
 }
 

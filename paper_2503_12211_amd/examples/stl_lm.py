@@ -1,6 +1,6 @@
 """A small language model whose linear maps are STL layers, trained through the library end to end: residual steps between its blocks
 (`stl_residual_norm_forward` / `_backward`) and the loss over its vocabulary (`stl_vocab_loss_backward`), from labels and from the stored
-top logits of a dense teacher, without the logits in memory.
+top logits of a dense teacher, the logits formed for a chunk of the tokens at a time.
 
 The three `torch.autograd.Function`s here marshal arguments, as `stl_linear.py` does; PyTorch supplies device memory, the embedding's rows, the mixing
 of neighbouring tokens, the autograd graph and the optimiser.
@@ -91,7 +91,8 @@ class _VocabLoss(torch.autograd.Function):
         nbytes = stl.stl_vocab_loss_workspace_bytes(prob, stl.STL_OP_BACKWARD if train else stl.STL_OP_FORWARD)
         ws = _scratch(nbytes, X.device)
         if train:
-            # the row weights are known here: losses and gradients come from one call, which forms the logits once
+            # the row weights are known here: losses and gradients come from one call, which forms the logits once (a factor that comes later, such as that of
+            # a scaled loss, is multiplied into the rounded gradients)
             dX, dW = torch.empty_like(X) if want_x else None, torch.empty_like(W) if want_w else None
             stl.stl_vocab_loss_backward(*inputs, label_weight, top_weight, *losses, dX, dW, ws, nbytes)
             ctx.save_for_backward(dX, dW)
