@@ -1,12 +1,11 @@
-"""Up to 128 rows with a term hold the gradient in the logits of bf16 storage as two bf16 numbers: every entry, as in tests/test_cpu_lm_pairs.py, and the errors of
+"""Up to 128 rows with a term hold the gradient in the logits of bf16 storage as two bf16 numbers: every entry, as in tests/test_cpu_lm_far_logits.py, and the errors of
 dX and dW against one rounding of the exact ones."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2503_12211_amd as stl
-from test_cpu_lm_far_logits import B, case, check
-from test_cpu_lm_pairs import unlabelled
+from test_cpu_lm_far_logits import B, case, check, unlabelled
 from oracle import lm
 from test_gpu_vocab import check as against_oracle, problem
 
