@@ -13,7 +13,7 @@
  * Letters: X is m x k, W is k x n, C is m x n; M=m/t, K=k/t, N=n/t tile counts.
  *
  * Conventions for every entry point
- *  - All matrices are dense, row-major, without strides.  vec() of a tile is
+ *  - All matrices are dense, row-major, without strides (but for those that a description below gives a distance between rows).  vec() of a tile is
  *    row-major: vec(T)[a*t+b] = T[a][b].  E_X, E_W, D are r x t^2 row-major
  *    (Definition 3.1); the decoder is applied as D^T.
  *  - Weight-side plane tensors (What, dWhat) are plane-major: [p][row tile][col tile].
@@ -26,7 +26,7 @@
  *    the plane products.)  Callers that only pass Xhat_save / Yhat_save from stl_forward to stl_backward
  *    never need to know.
  *  - Every data pointer is a DEVICE pointer owned by the caller, 16-byte aligned
- *    (STL_ERR_INVALID_ARG otherwise).
+ *    (STL_ERR_INVALID_ARG otherwise) where nothing else is said.
  *    The library allocates and frees no device memory: scratch comes from `ws`
  *    (size from stl_workspace_bytes).  Outputs must not alias inputs or `ws`.
  *  - Calls only enqueue work on `stream` (a hipStream_t passed as void*; NULL is
@@ -97,8 +97,9 @@ enum {
     STL_FLAG_GELU = 0x100,  /* C <- gelu(C) (exact erf form) applied in fp32 before the final rounding */
     STL_FLAG_B_TRANSPOSED = 0x200,  /* stl_aa_*: the second operand is stored transposed, (nbatch*n) x k */
     STL_FLAG_POST_NORM = 0x400,     /* stl_residual_norm_*: the block's output is normalised before the residual sum */
-    STL_FLAG_PRE_NORM = 0x800,      /* stl_residual_norm_*: the sum is normalised for the next block */
-    STL_FLAG_CENTER = 0x1000        /* stl_residual_norm_*: both norms subtract the mean (layer norm); without it root mean square */
+    STL_FLAG_PRE_NORM = 0x800,      /* stl_residual_norm_*: the sum is normalised for the next block; stl_head_norm_*: heads are normalised */
+    STL_FLAG_CENTER = 0x1000,       /* stl_residual_norm_*: both norms subtract the mean (layer norm); without it root mean square */
+    STL_FLAG_ADJACENT = 0x2000      /* stl_head_norm_*: elements 2 p and 2 p + 1 of a head are turned together, without it p and p + rot / 2 */
 };
 
 /* Bytes of device scratch `ws` needed by op (STL_OP_*) with `flags`; 0 on invalid problem. */
@@ -377,6 +378,102 @@ stl_status_t stl_vocab_loss_forward(const stl_vocab_t *prob, const void *X, cons
 stl_status_t stl_vocab_loss_backward(const stl_vocab_t *prob, const void *X, const void *W, const int64_t *label, const int64_t *top_id,
                                      const float *top_logit, const float *dlabel, const float *dtop, float *label_loss, float *top_loss, void *dX,
                                      void *dW, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Rows of a vocabulary by token, X[i] = scale W[token[i]].  A token outside 0 .. vocab-1 (such as -100) is none: its row is zeros.
+ * token: rows int64.  W: vocab x d, X: rows x d (storage dtype), the product in fp32, rounded once.
+ * 0 <= rows <= STL_MAX_DIM (0: nothing is done and the pointers of what has rows may be NULL), 1 <= d <= STL_VOCAB_WIDEST,
+ * 1 <= vocab <= STL_VOCAB_MOST.
+ */
+typedef struct {
+    int64_t rows, d, vocab;
+    float scale;
+    int32_t dtype;     /* stl_dtype_t */
+} stl_embed_t;
+stl_status_t stl_embed_forward(const stl_embed_t *prob, const int64_t *token, const void *W, void *X, void *stream);
+/*
+ * Backward: dW[v] = scale * sum of dX[i] over the rows i with token[i] = v, in fp32 and in the order of the rows, rounded once.  The same bits from run
+ * to run.  dX: rows x d, dW: vocab x d (out, storage dtype).
+ * accumulate: 0 writes all of dW, zeros for ids that no row has (also with no rows); 1 adds to the rows of dW whose ids occur and leaves the others alone, as
+ * tied weights need it behind stl_vocab_loss_backward.
+ * ws / ws_bytes: at least stl_embed_workspace_bytes(prob): 8 bytes a row and fp32 sums of 8 d bytes for each 16 rows, at most 2048 times.
+ */
+size_t stl_embed_workspace_bytes(const stl_embed_t *prob);
+stl_status_t stl_embed_backward(const stl_embed_t *prob, const int64_t *token, const void *dX, void *dW, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Norm of every query and key head and its rotation by position, in one pass:
+ *     y = x / sqrt(mean(x^2) + eps) * w                                                          (STL_FLAG_PRE_NORM; y = x without)
+ *     (y_a, y_b) <- (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position base^(-2 p / rot),  for the pairs p = 0 .. rot / 2 - 1
+ * of the first `rot` elements of a head, (a, b) = (p, p + rot / 2) or, with STL_FLAG_ADJACENT, (2 p, 2 p + 1); the others stay.  position: rows int64, any
+ * values (angles are formed in 64 bits), or NULL: nothing is turned.
+ * Q: rows of `heads` heads of d elements next to each other, ld_q elements from row to row; K: kv_heads (0: none, K NULL), ld_k; outputs alike with
+ * ld_qout, ld_kout.  So they may be parts of the rows of one matrix; an output may be its input (with the same distance).  These pointers are aligned to an
+ * element, w_q, w_k (d elements or NULL: ones; not read without the norm) and position to 16 bytes.  Storage dtype, each output rounded once.
+ * 0 <= rows <= STL_MAX_DIM (0: nothing is done), heads and kv_heads at most 65536, 1 <= d <= STL_HEAD_WIDEST (UNSUPPORTED above), rot even and at most d
+ * (0 without a position), ld at least the row's elements, base > 0, eps > 0.
+ */
+typedef struct {
+    int64_t rows, heads, kv_heads, d, rot;
+    int64_t ld_q, ld_k, ld_qout, ld_kout;
+    float base, eps;
+    int32_t dtype;     /* stl_dtype_t */
+} stl_head_norm_t;
+#define STL_HEAD_WIDEST 1024
+stl_status_t stl_head_norm_forward(const stl_head_norm_t *prob, const void *Q, const void *K, const void *w_q, const void *w_k, const int64_t *position,
+                                   void *Qout, void *Kout, int flags, void *stream);
+/*
+ * Backward of <dQout, Qout> + <dKout, Kout>.  With dy the gradient turned back and x^ = x / sqrt(...):
+ *     dx = (dy w - x^ mean(dy w x^)) / sqrt(...) (dy without the norm),   dw = sum over rows and heads of dy x^.
+ * Q, K: as in the forward call (not read without the norm).  dQout, dKout: ld_qout, ld_kout; NULL stands for zeros.  dQ, dK: ld_q, ld_k, storage dtype; dw_q, dw_k: d fp32,
+ * INVALID_ARG without the norm; any output may be NULL.  dQ may be dQout, dK dKout (with the same distance).
+ * accumulate: 0 overwrites dw_q, dw_k (no rows: zeros), 1 adds into them.  The same bits from run to run.
+ * ws / ws_bytes: at least stl_head_norm_workspace_bytes(prob, flags): 8 d bytes for each of up to 1024 workgroups.
+ */
+size_t stl_head_norm_workspace_bytes(const stl_head_norm_t *prob, int flags);
+stl_status_t stl_head_norm_backward(const stl_head_norm_t *prob, const void *Q, const void *K, const void *w_q, const void *w_k, const int64_t *position,
+                                    const void *dQout, const void *dKout, void *dQ, void *dK, float *dw_q, float *dw_k, int accumulate, void *ws,
+                                    size_t ws_bytes, int flags, void *stream);
+
+/*
+ * Attention whose past decays: each head of each sequence has a state S, dk x dv, and with lambda = exp(log_decay[head])
+ *     S_t = lambda S_{t-1} + k_t v_t^T,      o_t = scale q_t S_t          (o_t = scale sum_{s <= t} lambda^(t-s) (q_t . k_s) v_s  for S_{-1} = 0).
+ * One call takes any number of tokens: a prompt, a part of one, or a token at a time, and states go from call to call.
+ * Q: rows of `heads` heads of dk elements, ld_q from row to row; K: kv_heads heads of dk (head h of Q reads head h / (heads / kv_heads) of K and V), V: kv_heads of
+ * dv, O: heads of dv.  They may be parts of the rows of one matrix; these pointers are aligned to an element, the others to 16 bytes.  Storage dtype; states fp32,
+ * sequences x heads x dk x dv, decays fp32, -infinity (the present token alone) to 0; NULL: zeros.
+ * Which rows: offset NULL: token t of sequence b is row b seq_step + t token_step, all sequences have `length` tokens.  seq_step >= length with token_step 1 has one
+ * sequence after the other, token_step >= sequences with seq_step 1 one position after the other; rows that two tokens share are refused.
+ * offset (sequences + 1 int64, ascending): sequence b has the rows offset[b] .. offset[b + 1] - 1, the first `length` of them if there are more; it may have
+ * none.  Offsets are on the device: what lies outside 0 .. rows is cut off.  Rows that no sequence has are not read and left as they are.
+ * state_in: NULL (zeros) or the states in front of the first tokens; state_out: NULL or the states behind the last (state_in's where there is no token).
+ * state_out may be state_in.  Sums and states are fp32; for BF16 an operand formed in fp32 goes to the matrix cores as two bf16 numbers (2^-16), three (2^-24) for
+ * what is added to a state.  A value that is no finite number reaches its own and later tokens alone, whose results may then be NaN where the formula gives
+ * an infinity.
+ * 0 <= rows <= STL_MAX_DIM, 1 <= sequences, 0 <= length (0: states are copied), sequences * heads <= 4194304, 1 <= kv_heads dividing heads,
+ * 1 <= dk, dv <= STL_DECAY_WIDEST (UNSUPPORTED above), ld at least the row's elements, scale finite and not 0.
+ * ws / ws_bytes: at least stl_decay_attention_workspace_bytes(prob, STL_OP_FORWARD or STL_OP_BACKWARD).
+ */
+typedef struct {
+    int64_t rows, sequences, length, heads, kv_heads, dk, dv;
+    int64_t seq_step, token_step;
+    int64_t ld_q, ld_k, ld_v, ld_o;
+    float scale;
+    int32_t dtype;     /* stl_dtype_t */
+} stl_decay_attention_t;
+#define STL_DECAY_WIDEST 256
+size_t stl_decay_attention_workspace_bytes(const stl_decay_attention_t *prob, int op);
+stl_status_t stl_decay_attention_forward(const stl_decay_attention_t *prob, const void *Q, const void *K, const void *V, const float *log_decay,
+                                         const int64_t *offset, const float *state_in, void *O, float *state_out, void *ws, size_t ws_bytes, void *stream);
+/*
+ * Backward of <dO, O> + <dstate_out, state_out> (decays are constants):
+ *     G_t = scale q_t do_t^T + lambda G_{t+1} (dstate_out behind the last),  dq_t = scale S_t do_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  dstate_in = lambda G_0,
+ * dk and dv summed over the heads that share them.  Inputs as in the forward call; dO: ld_o; dstate_out: NULL stands for zeros.  dQ, dK, dV: ld_q, ld_k, ld_v,
+ * storage dtype; dstate_in: fp32; any of the four may be NULL.  No output may be an input.  The same bits from run to run.
+ */
+stl_status_t stl_decay_attention_backward(const stl_decay_attention_t *prob, const void *Q, const void *K, const void *V, const float *log_decay,
+                                          const int64_t *offset, const float *state_in, const void *dO, const float *dstate_out, void *dQ, void *dK, void *dV,
+                                          float *dstate_in, void *ws, size_t ws_bytes, void *stream);
 
 /* Static text for a status code. */
 const char *stl_status_string(stl_status_t status);

@@ -12,4 +12,7 @@ from .binding import (  # noqa: F401
     stl_workspace_bytes,
     STL_MAX_DIM, STL_FLAG_CENTER, STL_FLAG_POST_NORM, STL_FLAG_PRE_NORM, ResidualProblem, stl_residual_norm_backward, stl_residual_norm_forward,
     stl_residual_norm_workspace_bytes, VocabProblem, stl_vocab_loss_backward, stl_vocab_loss_forward, stl_vocab_loss_workspace_bytes,
+    STL_FLAG_ADJACENT, EmbedProblem, stl_embed_backward, stl_embed_forward, stl_embed_workspace_bytes, HeadNormProblem, stl_head_norm_backward,
+    stl_head_norm_forward, stl_head_norm_workspace_bytes, DecayAttentionProblem, stl_decay_attention_backward, stl_decay_attention_forward,
+    stl_decay_attention_workspace_bytes,
 )

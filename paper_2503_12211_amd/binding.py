@@ -19,6 +19,7 @@ STL_FLAG_AUTO, STL_FLAG_UNFUSED, STL_FLAG_EPILOGUE, STL_FLAG_FUSED, STL_FLAG_PIP
 STL_FLAG_GELU = 0x100
 STL_FLAG_B_TRANSPOSED = 0x200
 STL_FLAG_POST_NORM, STL_FLAG_PRE_NORM, STL_FLAG_CENTER = 0x400, 0x800, 0x1000
+STL_FLAG_ADJACENT = 0x2000
 
 # every symbol include/stl.h declares
 SYMBOLS = (
@@ -28,6 +29,9 @@ SYMBOLS = (
     "stl_ragged_workspace_bytes", "stl_ragged_forward", "stl_ragged_backward",
     "stl_residual_norm_workspace_bytes", "stl_residual_norm_forward", "stl_residual_norm_backward",
     "stl_vocab_loss_workspace_bytes", "stl_vocab_loss_forward", "stl_vocab_loss_backward",
+    "stl_embed_workspace_bytes", "stl_embed_forward", "stl_embed_backward",
+    "stl_head_norm_workspace_bytes", "stl_head_norm_forward", "stl_head_norm_backward",
+    "stl_decay_attention_workspace_bytes", "stl_decay_attention_forward", "stl_decay_attention_backward",
     "stl_status_string", "stl_last_error", "stl_version",
 )
 
@@ -106,6 +110,91 @@ class VocabProblem:
     __reduce__ = _rebuilt
 
 
+class _CEmbed(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int64), ("vocab", ctypes.c_int64), ("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class EmbedProblem:
+    """Sizes of stl_embed_*."""
+    rows: int
+    d: int
+    vocab: int
+    scale: float = 1.0
+    dtype: int = STL_BF16
+
+    def __post_init__(self):
+        object.__setattr__(self, "ref", ctypes.byref(_CEmbed(self.rows, self.d, self.vocab, self.scale, self.dtype)))
+
+    __reduce__ = _rebuilt
+
+
+class _CHeadNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "heads", "kv_heads", "d", "rot", "ld_q", "ld_k", "ld_qout", "ld_kout")] + [
+        ("base", ctypes.c_float), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class HeadNormProblem:
+    """Sizes and constants of stl_head_norm_*; rot None: all of a head is turned; ld_* None: rows next to each other."""
+    rows: int
+    heads: int
+    kv_heads: int
+    d: int
+    rot: int | None = None
+    ld_q: int | None = None
+    ld_k: int | None = None
+    ld_qout: int | None = None
+    ld_kout: int | None = None
+    base: float = 10000.0
+    eps: float = 1e-6
+    dtype: int = STL_BF16
+
+    def __post_init__(self):
+        q, k = self.heads * self.d, self.kv_heads * self.d
+        ld = [given if given is not None else wide for given, wide in ((self.ld_q, q), (self.ld_k, k), (self.ld_qout, q), (self.ld_kout, k))]
+        object.__setattr__(self, "ref", ctypes.byref(_CHeadNorm(self.rows, self.heads, self.kv_heads, self.d, self.rot if self.rot is not None else self.d, *ld,
+                                                                self.base, self.eps, self.dtype)))
+
+    __reduce__ = _rebuilt
+
+
+class _CDecayAttention(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "sequences", "length", "heads", "kv_heads", "dk", "dv", "seq_step", "token_step", "ld_q", "ld_k", "ld_v",
+                                              "ld_o")] + [("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class DecayAttentionProblem:
+    """Sizes of stl_decay_attention_*; kv_heads, dv None: as heads, dk; seq_step None: one sequence after the other; ld_* None: rows next to each other."""
+    rows: int
+    sequences: int
+    length: int
+    heads: int
+    kv_heads: int | None = None
+    dk: int = 128
+    dv: int | None = None
+    seq_step: int | None = None
+    token_step: int = 1
+    ld_q: int | None = None
+    ld_k: int | None = None
+    ld_v: int | None = None
+    ld_o: int | None = None
+    scale: float = 1.0
+    dtype: int = STL_BF16
+
+    def __post_init__(self):
+        kv = self.kv_heads if self.kv_heads is not None else self.heads
+        dv = self.dv if self.dv is not None else self.dk
+        step = self.seq_step if self.seq_step is not None else self.length * self.token_step
+        ld = [given if given is not None else wide for given, wide in ((self.ld_q, self.heads * self.dk), (self.ld_k, kv * self.dk), (self.ld_v, kv * dv),
+                                                                       (self.ld_o, self.heads * dv))]
+        object.__setattr__(self, "ref", ctypes.byref(_CDecayAttention(self.rows, self.sequences, self.length, self.heads, kv, self.dk, dv, step, self.token_step, *ld,
+                                                                      self.scale, self.dtype)))
+
+    __reduce__ = _rebuilt
+
+
 _lib = None
 _P = ctypes.c_void_p
 
@@ -158,6 +247,15 @@ def _load():
     lib.stl_vocab_loss_workspace_bytes.argtypes = [vp, ctypes.c_int]
     lib.stl_vocab_loss_forward.argtypes = [vp] + [_P] * 8 + [ctypes.c_size_t, _P]
     lib.stl_vocab_loss_backward.argtypes = [vp] + [_P] * 12 + [ctypes.c_size_t, _P]
+    ep, hp, dp = ctypes.POINTER(_CEmbed), ctypes.POINTER(_CHeadNorm), ctypes.POINTER(_CDecayAttention)
+    size, whole = ctypes.c_size_t, ctypes.c_int
+    for name, restype, argtypes in (
+            ("stl_embed_workspace_bytes", size, [ep]), ("stl_embed_forward", whole, [ep] + [_P] * 4), ("stl_embed_backward", whole, [ep] + [_P] * 3 + [whole, _P, size, _P]),
+            ("stl_head_norm_workspace_bytes", size, [hp, whole]), ("stl_head_norm_forward", whole, [hp] + [_P] * 7 + [whole, _P]),
+            ("stl_head_norm_backward", whole, [hp] + [_P] * 11 + [whole, _P, size, whole, _P]),
+            ("stl_decay_attention_workspace_bytes", size, [dp, whole]), ("stl_decay_attention_forward", whole, [dp] + [_P] * 9 + [size, _P]),
+            ("stl_decay_attention_backward", whole, [dp] + [_P] * 13 + [size, _P])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = restype, argtypes
     for name in ("stl_vocab_loss_forward", "stl_vocab_loss_backward", "stl_residual_norm_forward", "stl_residual_norm_backward", "stl_ragged_forward", "stl_ragged_backward", "stl_aa_forward", "stl_aa_backward", "stl_encode_weight", "stl_forward", "stl_backward", "stl_encode_activation", "stl_plane_matmul",
                  "stl_decode", "stl_mlp_forward", "stl_recode", "stl_encode_weight_backward"):
         getattr(lib, name).restype = ctypes.c_int
@@ -349,3 +447,44 @@ def stl_vocab_loss_backward(prob: VocabProblem, X, W, label, top_id, top_logit, 
                             stream=None) -> None:
     _check(_load().stl_vocab_loss_backward(prob.ref, _ptr(X), _ptr(W), _ptr(label), _ptr(top_id), _ptr(top_logit), _ptr(dlabel), _ptr(dtop),
                                            _ptr(label_loss), _ptr(top_loss), _ptr(dX), _ptr(dW), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def stl_embed_workspace_bytes(prob: EmbedProblem) -> int:
+    return int(_load().stl_embed_workspace_bytes(prob.ref))
+
+
+def stl_embed_forward(prob: EmbedProblem, token, W, X, stream=None) -> None:
+    _check(_load().stl_embed_forward(prob.ref, _ptr(token), _ptr(W), _ptr(X), _stream(stream)))
+
+
+def stl_embed_backward(prob: EmbedProblem, token, dX, dW, accumulate: int = 0, ws=None, ws_bytes: int = 0, stream=None) -> None:
+    _check(_load().stl_embed_backward(prob.ref, _ptr(token), _ptr(dX), _ptr(dW), accumulate, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def stl_head_norm_workspace_bytes(prob: HeadNormProblem, flags: int = STL_FLAG_PRE_NORM) -> int:
+    return int(_load().stl_head_norm_workspace_bytes(prob.ref, flags))
+
+
+def stl_head_norm_forward(prob: HeadNormProblem, Q, K, w_q, w_k, position, Qout, Kout, flags: int = STL_FLAG_PRE_NORM, stream=None) -> None:
+    _check(_load().stl_head_norm_forward(prob.ref, _ptr(Q), _ptr(K), _ptr(w_q), _ptr(w_k), _ptr(position), _ptr(Qout), _ptr(Kout), flags, _stream(stream)))
+
+
+def stl_head_norm_backward(prob: HeadNormProblem, Q, K, w_q, w_k, position, dQout, dKout, dQ, dK, dw_q, dw_k, accumulate: int = 0, ws=None, ws_bytes: int = 0,
+                           flags: int = STL_FLAG_PRE_NORM, stream=None) -> None:
+    _check(_load().stl_head_norm_backward(prob.ref, _ptr(Q), _ptr(K), _ptr(w_q), _ptr(w_k), _ptr(position), _ptr(dQout), _ptr(dKout), _ptr(dQ), _ptr(dK),
+                                          _ptr(dw_q), _ptr(dw_k), accumulate, _ptr(ws), ws_bytes, flags, _stream(stream)))
+
+
+def stl_decay_attention_workspace_bytes(prob: DecayAttentionProblem, op: int = STL_OP_FORWARD) -> int:
+    return int(_load().stl_decay_attention_workspace_bytes(prob.ref, op))
+
+
+def stl_decay_attention_forward(prob: DecayAttentionProblem, Q, K, V, log_decay, offset, state_in, O, state_out, ws=None, ws_bytes: int = 0, stream=None) -> None:
+    _check(_load().stl_decay_attention_forward(prob.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(offset), _ptr(state_in), _ptr(O), _ptr(state_out),
+                                               _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def stl_decay_attention_backward(prob: DecayAttentionProblem, Q, K, V, log_decay, offset, state_in, dO, dstate_out, dQ, dK, dV, dstate_in, ws=None,
+                                 ws_bytes: int = 0, stream=None) -> None:
+    _check(_load().stl_decay_attention_backward(prob.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(offset), _ptr(state_in), _ptr(dO), _ptr(dstate_out),
+                                                _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dstate_in), _ptr(ws), ws_bytes, _stream(stream)))

@@ -21,7 +21,7 @@ FLAGS = [
 
 
 def sources():
-    return sorted(CSRC.glob("*.hip")) + sorted((CSRC / "lm").glob("*.hip"))
+    return sorted(CSRC.glob("*.hip")) + sorted((CSRC / "lm").glob("*.hip")) + sorted((CSRC / "seq").glob("*.hip"))
 
 
 def build(force: bool = True, verbose: bool = False) -> Path:

@@ -1,0 +1,339 @@
+// Norms of queries and keys for each head, and their rotation by position, in one pass (gfx950).
+//
+//   y = x / sqrt(mean x^2 + eps) w over the d elements of a head,   (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin) for its pairs
+//
+// with the angle position base^(-2 p / rot) for pair p.  Memory bound: every element is read once and written once.  A lane holds a unit of
+// sixteen elements of a head, both of each of its eight pairs, so that the rotation needs no other lane and the norm a sum over the few lanes of a head.
+// Angles are formed in 64 bits as parts of a turn (a position of 100000 has lost 0.004 rad in 32), once for a row and a pair, by one thread
+// of the workgroup; all heads of the row take cosine and sine from LDS.
+// Backward: with dy the gradient turned back, x^ = x / sqrt(...): dw = sum dy x^ over rows and heads, dx = r (dy w - x^ mean(dy w x^)).  A workgroup keeps
+// its sums for the weights in registers over all of its rows; a second launch adds up the workgroups'.
+#include "seq_kernels.h"
+#include "../lm/lm_device.h"
+
+namespace stl {
+namespace seq {
+
+using lm::Chunk;
+
+// Pairs 0 .. rot / 2 - 1 are turned; those behind them are the other elements two by two (the second of the last one may not exist), left as they are.
+struct Pair {
+    int a, b;
+};
+template <bool ADJ>
+__device__ __forceinline__ Pair pair_of(int p, int rot)
+{
+    const int half = rot / 2;
+    if (p >= half || ADJ) return Pair{2 * p, 2 * p + 1};
+    return Pair{p, p + half};
+}
+
+// The sixteen elements of a unit (pairs 8 u .. 8 u + 7) in registers.  VEC: as two chunks of 8, where 16 divides d and rot.
+// ADJ: pair k is (x[2 k], x[2 k + 1]), otherwise (x[k], x[8 + k]).
+template <typename T, bool ADJ, bool VEC>
+struct Unit {
+    static __device__ __forceinline__ int second_chunk(int u, int rot)
+    {
+        return ADJ || 16 * u >= rot ? 16 * u + 8 : rot / 2 + 8 * u;
+    }
+    static __device__ __forceinline__ int first_chunk(int u, int rot) { return ADJ || 16 * u >= rot ? 16 * u : 8 * u; }
+    static __device__ __forceinline__ void load(const T *p, int u, int d, int rot, float *x)
+    {
+        if constexpr (VEC) {
+            Chunk<T> a, b;
+            a.load(p + first_chunk(u, rot), 8);
+            b.load(p + second_chunk(u, rot), 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = a.get(e), x[8 + e] = b.get(e);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const Pair at = pair_of<ADJ>(8 * u + k, rot);
+                x[ADJ ? 2 * k : k] = at.a < d ? Elem<T>::ld(p + at.a) : 0.f;
+                x[ADJ ? 2 * k + 1 : 8 + k] = at.b < d ? Elem<T>::ld(p + at.b) : 0.f;
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(T *p, int u, int d, int rot, const float *x)
+    {
+        if constexpr (VEC) {
+            Chunk<T>::store(p + first_chunk(u, rot), 8, x);
+            Chunk<T>::store(p + second_chunk(u, rot), 8, x + 8);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const Pair at = pair_of<ADJ>(8 * u + k, rot);
+                if (at.a < d) Elem<T>::st(p + at.a, x[ADJ ? 2 * k : k]);
+                if (at.b < d) Elem<T>::st(p + at.b, x[ADJ ? 2 * k + 1 : 8 + k]);
+            }
+        }
+    }
+    // the first n pairs turned by the angles whose cosines and sines lie at `cs`, or back
+    static __device__ __forceinline__ void turn(const f32x2_t *cs, int n, float *x, float back)
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k >= n) break;
+            float &a = x[ADJ ? 2 * k : k], &b = x[ADJ ? 2 * k + 1 : 8 + k];
+            const f32x2_t t = cs[k];
+            const float s = back * t[1], was = a;
+            a = fmaf(was, t[0], -(b * s));
+            b = fmaf(was, s, b * t[0]);
+        }
+    }
+};
+
+// sum over groups of `lanes` lanes next to each other (a power of two), in every one of them
+__device__ __forceinline__ float group_sum(float v, int lanes)
+{
+    if (lanes > 1) v += lm::dpp<0xb1, 0xf>(v, 0.f);
+    if (lanes > 2) v += lm::dpp<0x4e, 0xf>(v, 0.f);
+    if (lanes > 4) v += lm::dpp<0x141, 0xf>(v, 0.f);
+    if (lanes > 8) v += lm::dpp<0x140, 0xf>(v, 0.f);
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+struct HeadPlan {
+    int units, lanes, together;              // of a head; rows whose angles are formed together
+    int grid;
+    bool vec;
+};
+HeadPlan head_plan(const HeadArgs &a)
+{
+    HeadPlan p;
+    p.units = ((a.d + 1) / 2 + 7) / 8;
+    p.lanes = 1;
+    while (p.lanes < p.units) p.lanes *= 2;
+    p.together = a.rows >= 8192 ? 8 : a.rows >= 4096 ? 4 : a.rows >= 2048 ? 2 : 1;
+    const int turns = (a.rows + p.together - 1) / p.together;
+    p.grid = turns < 1024 ? turns : 1024;
+    p.vec = a.d % 16 == 0 && a.rot % 16 == 0;
+    return p;
+}
+
+// cosines and sines of the pairs of `rows` rows from `row` on, 8 units pairs a row (those that are not turned: 1 and 0)
+__device__ __forceinline__ void angles(const HeadArgs &a, int pairs, int row, int rows, f32x2_t *table)
+{
+    const int half = a.rot / 2;
+    for (int i = (int)threadIdx.x; i < rows * pairs; i += 256) {
+        const int r = i / pairs, p = i % pairs;
+        f32x2_t cs = {1.f, 0.f};
+        if (p < half) {
+            // quarters of a turn, position base^(-2 p / rot) 2 / pi: whole ones in 64 bits, so that what is left is small and the smaller of cosine and sine as
+            // exact, relative to itself, as the larger
+            const double quarters = (double)a.position[row + r] * (exp2(-a.log2_base * (2.0 * p / a.rot)) * 0.63661977236758134308), n = rint(quarters);
+            float s, c;
+            sincospif(0.5f * (float)(quarters - n), &s, &c);
+            const int q = (int)(n - 4.0 * floor(0.25 * n));
+            if (q & 1) {
+                const float was = c;
+                c = -s, s = was;
+            }
+            if (q & 2) c = -c, s = -s;
+            cs = f32x2_t{c, s};
+        }
+        table[i] = cs;
+    }
+}
+
+template <typename T, bool ADJ, bool VEC>
+__global__ __launch_bounds__(256) void head_kernel(const HeadArgs a, const HeadPlan plan, T *out_q, T *out_k)
+{
+    extern __shared__ __align__(16) char smem[];
+    f32x2_t *table = reinterpret_cast<f32x2_t *>(smem);
+    using U = Unit<T, ADJ, VEC>;
+    const int lanes = plan.lanes, pairs = 8 * plan.units;
+    const int u = (int)threadIdx.x % lanes, group = (int)threadIdx.x / lanes, groups = 256 / lanes;
+    const bool mine = u < plan.units;
+    float w[2][16];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[side][e] = 1.f;
+        if (a.w[side] && mine) U::load((const T *)a.w[side], u, a.d, a.rot, w[side]);
+    }
+    const float inv = 1.f / (float)a.d;
+    for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
+        const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
+        __syncthreads();
+        angles(a, pairs, (int)row, rows, table);
+        __syncthreads();
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const int heads = a.heads[side];
+            T *out = side ? out_k : out_q;
+            // (every lane takes part in the sums)
+            for (int from = 0; from < rows * heads; from += groups) {
+                const int i = from + group, r = i / heads, h = i - r * heads;
+                const bool live = mine && i < rows * heads;
+                float x[16] = {};
+                if (live) U::load((const T *)a.in[side] + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, x);
+                if (a.norm) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum = fmaf(x[e], x[e], sum);
+                    const float by = rsqrtf(fmaf(group_sum(sum, lanes), inv, a.eps));
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] *= by * w[side][e];
+                }
+                if (live) {
+                    U::turn(table + r * pairs + 8 * u, a.rot / 2 - 8 * u, x, 1.f);
+                    U::store(out + (row + r) * a.ld_out[side] + (size_t)h * a.d, u, a.d, a.rot, x);
+                }
+            }
+        }
+    }
+}
+
+// parts: for each workgroup the sums for the two weights, d each
+template <typename T, bool ADJ, bool VEC>
+__global__ __launch_bounds__(256) void head_back_kernel(const HeadArgs a, const HeadGrads g, const HeadPlan plan, float *parts)
+{
+    extern __shared__ __align__(16) char smem[];
+    f32x2_t *table = reinterpret_cast<f32x2_t *>(smem);
+    using U = Unit<T, ADJ, VEC>;
+    const int lanes = plan.lanes, pairs = 8 * plan.units;
+    const int u = (int)threadIdx.x % lanes, group = (int)threadIdx.x / lanes, groups = 256 / lanes;
+    const bool mine = u < plan.units;
+    float dw[2][16] = {};
+    const float inv = 1.f / (float)a.d;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int heads = a.heads[side];
+        float w[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = 1.f;
+        if (a.w[side] && mine) U::load((const T *)a.w[side], u, a.d, a.rot, w);
+        T *out = (T *)g.d_in[side];
+        if (heads == 0 || (!out && !g.dw[side])) continue;
+        for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
+            const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
+            __syncthreads();
+            angles(a, pairs, (int)row, rows, table);
+            __syncthreads();
+            for (int from = 0; from < rows * heads; from += groups) {
+                const int i = from + group, r = i / heads, h = i - r * heads;
+                const bool live = mine && i < rows * heads;
+                float x[16] = {}, t[16] = {};
+                if (live) {
+                    if (a.norm) U::load((const T *)a.in[side] + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, x);
+                    if (g.up[side]) U::load((const T *)g.up[side] + (row + r) * a.ld_out[side] + (size_t)h * a.d, u, a.d, a.rot, t);
+                    U::turn(table + r * pairs + 8 * u, a.rot / 2 - 8 * u, t, -1.f);
+                }
+                if (a.norm) {
+                    float squares = 0.f, dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) squares = fmaf(x[e], x[e], squares);
+                    const float by = rsqrtf(fmaf(group_sum(squares, lanes), inv, a.eps));
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] *= by;
+                        dw[side][e] = fmaf(t[e], x[e], dw[side][e]);
+                        t[e] *= w[e];
+                        dot = fmaf(t[e], x[e], dot);
+                    }
+                    dot = group_sum(dot, lanes) * inv;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) t[e] = by * fmaf(-x[e], dot, t[e]);
+                }
+                if (live && out) U::store(out + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, t);
+            }
+        }
+    }
+    if (!g.dw[0] && !g.dw[1]) return;
+    // over the groups of a wavefront, then over the wavefronts, in an order of their own each
+    float *red = reinterpret_cast<float *>(smem);                 // [wavefront][unit][16]
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float v = dw[side][e];
+            for (int n = lanes; n < 64; n *= 2) v += __shfl_xor(v, n);
+            if (lane < lanes && mine) red[(wave * plan.units + u) * 16 + e] = v;
+        }
+        __syncthreads();
+        if (g.dw[side])
+            for (int i = (int)threadIdx.x; i < 16 * plan.units; i += 256) {
+                float v = 0.f;
+                for (int k = 0; k < 4; ++k) v += red[k * plan.units * 16 + i];
+                const int unit = i / 16, e = i % 16;
+                int at;
+                if (VEC) at = (e < 8 ? U::first_chunk(unit, a.rot) : U::second_chunk(unit, a.rot)) + e % 8;
+                else {
+                    const Pair p = pair_of<ADJ>(8 * unit + (ADJ ? e / 2 : e % 8), a.rot);
+                    at = (ADJ ? e % 2 : e / 8) ? p.b : p.a;
+                }
+                if (at < a.d) parts[((size_t)blockIdx.x * 2 + side) * a.d + at] = v;
+            }
+    }
+}
+
+// dw (+)= sum over `n` workgroups' parts; 16 columns, 16 threads a column that take every sixteenth part
+__global__ __launch_bounds__(256) void head_sum_kernel(const float *parts, int n, int d, float *dw_q, float *dw_k, int accumulate)
+{
+    __shared__ float red[16][17];
+    const int x = (int)threadIdx.x & 15, y = (int)threadIdx.x >> 4, c = (int)blockIdx.x * 16 + x, side = (int)blockIdx.y;
+    float *dw = side ? dw_k : dw_q;
+    if (!dw) return;
+    float v = 0.f;
+    if (c < d)
+        for (int b = y; b < n; b += 16) v += parts[((size_t)b * 2 + side) * d + c];
+    red[y][x] = v;
+    __syncthreads();
+    if (y == 0 && c < d) {
+        for (int k = 1; k < 16; ++k) v += red[k][x];
+        dw[c] = accumulate ? dw[c] + v : v;
+    }
+}
+
+size_t head_workspace_bytes(const HeadArgs &a)
+{
+    return ((size_t)head_plan(a).grid * 2 * a.d * 4 + 255) / 256 * 256;
+}
+
+template <typename T, bool ADJ, bool VEC>
+hipError_t forward(const HeadArgs &a, const HeadPlan &p, void *const out[2], hipStream_t s)
+{
+    hipLaunchKernelGGL((head_kernel<T, ADJ, VEC>), dim3(p.grid), dim3(256), p.together * 64 * p.units, s, a, p, (T *)out[0], (T *)out[1]);
+    return hipGetLastError();
+}
+template <typename T, bool ADJ, bool VEC>
+hipError_t backward(const HeadArgs &a, const HeadGrads &g, const HeadPlan &p, float *parts, hipStream_t s)
+{
+    const int table = p.together * 64 * p.units, sums = 4 * 64 * p.units;
+    hipLaunchKernelGGL((head_back_kernel<T, ADJ, VEC>), dim3(p.grid), dim3(256), table > sums ? table : sums, s, a, g, p, parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!g.dw[0] && !g.dw[1])) return e;
+    hipLaunchKernelGGL(head_sum_kernel, dim3((a.d + 15) / 16, 2), dim3(256), 0, s, parts, p.grid, a.d, g.dw[0], g.dw[1], g.accumulate);
+    return hipGetLastError();
+}
+
+// f(a value of the storage type, whether pairs are adjacent, whether heads are whole chunks)
+template <typename F>
+hipError_t by_kind(int dtype, bool adjacent, bool vec, F f)
+{
+    auto rest = [&](auto t) {
+        if (adjacent) return vec ? f(t, std::true_type(), std::true_type()) : f(t, std::true_type(), std::false_type());
+        return vec ? f(t, std::false_type(), std::true_type()) : f(t, std::false_type(), std::false_type());
+    };
+    return dtype ? rest(bf16_t()) : rest(float());
+}
+
+hipError_t launch_head_forward(int dtype, const HeadArgs &a, void *const out[2], hipStream_t s)
+{
+    const HeadPlan p = head_plan(a);
+    return by_kind(dtype, a.adjacent, p.vec, [&](auto t, auto adj, auto vec) { return forward<decltype(t), adj.value, vec.value>(a, p, out, s); });
+}
+
+hipError_t launch_head_backward(int dtype, const HeadArgs &a, const HeadGrads &g, void *ws, hipStream_t s)
+{
+    const HeadPlan p = head_plan(a);
+    return by_kind(dtype, a.adjacent, p.vec, [&](auto t, auto adj, auto vec) { return backward<decltype(t), adj.value, vec.value>(a, g, p, (float *)ws, s); });
+}
+
+}  // namespace seq
+}  // namespace stl

@@ -1,0 +1,33 @@
+// The stand-in for the HIP runtime that runs kernels as they are meant to run (tests/cpu_emu/), with what the kernels of csrc/seq use beside.
+#pragma once
+#include "../../cpu_emu/hip/hip_runtime.h"
+inline unsigned long long __ballot(int v)
+{
+    int *s = emu::Exchange<int>::all(v != 0);
+    unsigned long long r = 0;
+    for (int l = 0; l < 64; ++l) r |= (unsigned long long)(s[l] != 0) << l;
+    emu::Exchange<int>::release();
+    return r;
+}
+inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
+inline int atomicAdd(int *p, int v) { const int old = *p; *p += v; return old; }
+inline void sincospif(float x, float *s, float *c) { *s = (float)sin(M_PI * (double)x), *c = (float)cos(M_PI * (double)x); }
+// D[i][j] += sum_k A[i][k] B[k][j]: a lane holds row (column) lane % 32, k = 8 (lane / 32) ..., and of D column lane % 32, rows 8 (e / 4) + 4 (lane / 32) + e % 4
+inline emu_f32x16 emu_mfma32(emu_bf16x8 a, emu_bf16x8 b, emu_f32x16 c)
+{
+    struct Both { EmuBits8 a, b; } mine;
+    memcpy(&mine.a, &a, 16);
+    memcpy(&mine.b, &b, 16);
+    Both *s = emu::Exchange<Both>::all(mine);
+    const int l = emu::lane();
+    for (int e = 0; e < 16; ++e) {
+        const int i = 8 * (e >> 2) + 4 * (l / 32) + (e & 3), j = l % 32;
+        float t = c[e];
+        for (int k = 0; k < 16; ++k) t += emu_bf16(s[i + 32 * (k / 8)].a.v[k % 8]) * emu_bf16(s[j + 32 * (k / 8)].b.v[k % 8]);
+        c[e] = t;
+    }
+    emu::Exchange<Both>::release();
+    return c;
+}
+#undef __builtin_amdgcn_mfma_f32_32x32x16_bf16
+#define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) emu_mfma32(a, b, c)
