@@ -7,7 +7,9 @@
 // so that all but the masking is matrix products.  The gradients are the same thing with other operands: dQ is this attention of (dO, V, K), and, with
 // time reversed, dV that of (K, Q, dO) and dK that of (V, dO, Q) (DecayPass).
 //
-// A workgroup takes a head of a sequence (and 128 columns of v at most) from its first token to its last.  A wavefront owns 32 columns of v: its part of S
+// A workgroup takes a segment of a sequence, a head and 128 columns of v at most, chunk after chunk.  Where there are too few heads to fill the chip, a sequence has
+// several segments: a sweep without outputs first forms what each adds to the state, a small kernel joins these in order to the state in front of each
+// segment (decay_join_kernel), and all segments run at once.  That reads K and V twice (from the last-level cache, if they fit there).  A wavefront owns 32 columns of v: its part of S
 // stays in accumulators (dk x 32, fp32) all along.  Products are formed so that accumulators are the next product's operand as they lie:
 //   P^T = K Q^T (tokens j x i)   ->   O^T += V^T P^T,      S (dk x columns) as S^T in   O^T = S^T Q^T
 // An accumulator's lane holds rows 8 (e / 4) + 4 h + e % 4 of its column (h = lane / 32), an operand's lane eight elements of the contraction, whose
@@ -50,6 +52,10 @@ struct DecayPass {
     bool turned;
     float init_scale, last_scale;
     int init_power, last_power;
+    // segments of seg_tokens (a multiple of 32).  starts [sequence][head][segments][da dv]: number s holds what segment s adds to the state, and behind decay_join_kernel
+    // the state in front of segment s + 1; the last one `init` as it was, where the last state may be written over it.
+    int segments, seg_tokens;
+    float *starts;
 };
 
 // tokens of sequence b: the row of the first, and how many (never outside the rows there are, whatever the offsets are)
@@ -205,31 +211,58 @@ template <> struct Ops<float> {
 // a lane's row within 32 of accumulator element e
 __device__ __forceinline__ int acc_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
 
-constexpr int kDecayColumns = 128;           // of v, of a workgroup
-template <typename T, int KT>                // 32 KT: width of queries and keys in LDS
+constexpr int kDecayColumns = 128;           // of v, of a workgroup, 32 a wavefront
+constexpr int kChunk = 32;
+template <typename T, int KT, int NW>        // 32 KT: width of queries and keys in LDS; NW wavefronts
 struct DecayShape {
-    static constexpr int C = sizeof(T) == 2 && KT < 8 ? 64 : 32;
-    static constexpr int ld = 32 * KT + Ops<T>::kPad;
-    static int lds(int columns) { return (2 * C * ld + C * (columns + Ops<T>::kPad)) * (int)sizeof(T) + (C + 1) * 4 + 16; }
+    static constexpr int columns = 32 * NW, ld = 32 * KT + Ops<T>::kPad, ldv = columns + Ops<T>::kPad;
+    static constexpr int lds(bool outputs) { return (((outputs ? 2 : 1) * ld + ldv) * kChunk * (int)sizeof(T) + 15) / 16 * 16 + (kChunk + 1) * 4 + 8; }
 };
+// 256 registers, two workgroups a CU, where a wavefront's state and the next chunk fit
+constexpr int decay_waves(size_t element, int KT) { return element == 2 && KT <= 4 ? 2 : 1; }
 
-template <typename T, int KT>
-__global__ __launch_bounds__(256, KT < 8 ? 2 : 1) void decay_kernel(const DecayPass p)
+// up to four elements of a row of outputs
+template <typename T>
+__device__ __forceinline__ void put4(T *to, int left, f32x4_t v)
+{
+    if (left >= 4) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t *>(to) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else *reinterpret_cast<f32x4_any_t *>(to) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < left) Elem<T>::st(to + e, v[e]);
+    }
+}
+
+// OUT: with outputs; without, what a segment adds to the state
+template <typename T, int KT, int NW, bool OUT>
+__device__ __forceinline__ void decay_body(const DecayPass &p)
 {
     extern __shared__ __align__(16) char smem[];
-    using S = DecayShape<T, KT>;
+    using S = DecayShape<T, KT, NW>;
     using O = Ops<T>;
     using Frag = typename O::Frag;
-    constexpr int C = S::C, CT = C / 32, ld = S::ld;
-    const int threads = (int)blockDim.x, columns = threads / 2, ldv = columns + O::kPad;
-    T *lA = reinterpret_cast<T *>(smem), *lB = lA + C * ld, *lV = lB + C * ld;
-    float *fade = reinterpret_cast<float *>(lV + C * ldv);       // lambda^n, n = 0 .. C
-    int *bad = reinterpret_cast<int *>(fade + C + 1);
+    constexpr int ld = S::ld, ldv = S::ldv, threads = 64 * NW;
+    T *lB = reinterpret_cast<T *>(smem), *lV = lB + kChunk * ld, *lA = lV + kChunk * ldv;
+    float *fade = reinterpret_cast<float *>(smem + S::lds(OUT) - (kChunk + 1) * 4 - 8);      // lambda^n, n = 0 .. 32
+    int *bad = reinterpret_cast<int *>(fade + kChunk + 1);
 
     const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
-    const int z = (int)blockIdx.x % blocks, bh = (int)blockIdx.x / blocks, b = bh / p.heads, head = bh % p.heads;
+    int at = (int)blockIdx.x;
+    const int z = at % blocks;
+    at /= blocks;
+    const int seg = at % p.segments;
+    at /= p.segments;
+    const int b = at / p.heads, head = at % p.heads;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
     const Tokens tokens = tokens_of(p, b);
+    const int begin = seg * p.seg_tokens;
+    // the segment that has the last token (the first one where there is none)
+    const bool final = OUT && (seg == 0 || begin < tokens.count) && tokens.count <= begin + p.seg_tokens;
+    const int end = tokens.count < begin + p.seg_tokens ? tokens.count : begin + p.seg_tokens;
+    if (OUT ? begin >= tokens.count && !final : begin + p.seg_tokens >= tokens.count) return;
+
     const T *gA = (const T *)p.A + (size_t)(head / p.share_a) * p.da, *gB = (const T *)p.B + (size_t)(head / p.share_b) * p.da;
     const T *gV = (const T *)p.V + (size_t)(head / p.share_v) * p.dv + z * kDecayColumns;
     const int vleft = p.dv - z * kDecayColumns;                  // columns of v from this workgroup's first on
@@ -238,74 +271,92 @@ __global__ __launch_bounds__(256, KT < 8 ? 2 : 1) void decay_kernel(const DecayP
 
     double a = p.log_decay ? (double)p.log_decay[head] : 0.0;
     a = a < -1e5 ? -1e5 : a;
-    for (int i = (int)threadIdx.x; i <= C; i += threads) fade[i] = (float)power(a, i);
+    if (threadIdx.x <= kChunk) fade[threadIdx.x] = (float)power(a, (int)threadIdx.x);
     if (threadIdx.x == 0) bad[0] = bad[1] = 0;
-    const double whole = power(a, C);
+    const double whole = power(a, kChunk);
 
     // the state, element e of tile k: row 32 k + acc_row(e), column n
     f32x16_t state[KT];
-    const size_t state_at = ((size_t)b * p.heads + head) * p.da * p.dv;
+    const size_t each = (size_t)p.da * p.dv, state_at = ((size_t)b * p.heads + head) * each;
+    const float *init = p.init;
+    float init_scale = p.init_scale;
+    size_t init_at = state_at;
+    int power_of_first = p.init_power;                           // of lambda, from the state to the next token
+    if (!OUT) init = nullptr;
+    if (OUT && p.segments > 1 && (seg > 0 || (init && p.last))) {
+        init = p.starts;
+        init_at = (((size_t)b * p.heads + head) * p.segments + (seg > 0 ? seg - 1 : p.segments - 1)) * each;
+        if (seg > 0) init_scale = 1.f, power_of_first = 1;
+    }
     auto at_state = [&](int k, int e) {
         const int i = 32 * k + acc_row(e, h), j = z * kDecayColumns + col + n;
-        return i < p.da && j < p.dv ? (p.turned ? (int64_t)j * p.da + i : (int64_t)i * p.dv + j) : (int64_t)-1;
+        return i < p.da && j < p.dv ? (p.turned ? j * p.da + i : i * p.dv + j) : -1;
     };
 #pragma unroll
     for (int k = 0; k < KT; ++k)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int64_t at = p.init ? at_state(k, e) : -1;
-            state[k][e] = at >= 0 ? p.init_scale * p.init[state_at + at] : 0.f;
+            const int i = init ? at_state(k, e) : -1;
+            state[k][e] = i >= 0 ? init_scale * init[init_at + i] : 0.f;
         }
-    bool any = p.init != nullptr;                                // whether the state may differ from zero
-    int power_of_first = p.init_power;                           // of lambda, from the state to the next token
+    bool any = init != nullptr;                                  // whether the state may differ from zero
 
-    int from = 0, turn = 0;
-    while (from < tokens.count) {
-        int count = tokens.count - from < C ? tokens.count - from : C;
+    // the next chunk on its way: 16 elements of a row of A and of B, 8 of V at a time
+    constexpr int kUnits = 2 * KT * kChunk, kPer = (kUnits + threads - 1) / threads, kPerV = kChunk * S::columns / 8 / threads;
+    Chunk<T> na[OUT ? kPer : 1][2], nb[kPer][2], nv[kPerV];
+    auto fetch = [&](int from, int count) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int unit = i * threads + (int)threadIdx.x, r = unit / (2 * KT), u = unit % (2 * KT), left = r < count ? p.da - 16 * u : 0;
+            const size_t row = left > 0 ? row_of(from + r) : 0;
+            if (OUT) {
+                na[i][0].load(gA + row * p.lda + 16 * u, left);
+                na[i][1].load(gA + row * p.lda + 16 * u + 8, left - 8);
+            }
+            nb[i][0].load(gB + row * p.ldb + 16 * u, left);
+            nb[i][1].load(gB + row * p.ldb + 16 * u + 8, left - 8);
+        }
+#pragma unroll
+        for (int i = 0; i < kPerV; ++i) {
+            const int unit = i * threads + (int)threadIdx.x, r = unit / (S::columns / 8), u = unit % (S::columns / 8), left = r < count ? vleft - 8 * u : 0;
+            nv[i].load(gV + (left > 0 ? row_of(from + r) : 0) * p.ldv + 8 * u, left);
+        }
+    };
+
+    int from = begin, count = end - from < kChunk ? end - from : kChunk, turn = 0, singles = 0;
+    if (count > 0) fetch(from, count);
+    while (count > 0) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int unit = i * threads + (int)threadIdx.x, r = unit / (2 * KT), u = unit % (2 * KT);
+            if (kUnits % threads && unit >= kUnits) break;
+            if (OUT) O::put(lA + r * ld + 16 * u, na[i][0], na[i][1]);
+            O::put(lB + r * ld + 16 * u, nb[i][0], nb[i][1]);
+        }
+        bool ok = true;
+#pragma unroll
+        for (int i = 0; i < kPerV; ++i) {
+            const int unit = i * threads + (int)threadIdx.x, r = unit / (S::columns / 8), u = unit % (S::columns / 8);
+            ok &= O::finite(nv[i]);
+            O::put_plain(lV + r * ldv + 8 * u, nv[i]);
+        }
+        if (!ok) bad[turn] = 1;
         __syncthreads();
         // A value that is no finite number must not reach earlier tokens, as it would with a zero of the masked P: a chunk with one goes token by token.
-        for (int only = 0; only < 2; ++only) {
-            for (int i = (int)threadIdx.x; i < C * 2 * KT; i += threads) {
-                const int r = i / (2 * KT), u = i % (2 * KT);
-                Chunk<T> c[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) c[k].fill(0.f);
-                if (r < count) {
-                    const size_t row = row_of(from + r);
-                    const int left = p.da - 16 * u;
-                    c[0].load(gA + row * p.lda + 16 * u, left);
-                    c[1].load(gA + row * p.lda + 16 * u + 8, left - 8);
-                    c[2].load(gB + row * p.ldb + 16 * u, left);
-                    c[3].load(gB + row * p.ldb + 16 * u + 8, left - 8);
-                }
-                O::put(lA + r * ld + 16 * u, c[0], c[1]);
-                O::put(lB + r * ld + 16 * u, c[2], c[3]);
-            }
-            bool ok = true;
-            for (int i = (int)threadIdx.x; i < C * (columns / 8); i += threads) {
-                const int r = i / (columns / 8), u = i % (columns / 8);
-                Chunk<T> c;
-                c.fill(0.f);
-                if (r < count) c.load(gV + row_of(from + r) * p.ldv + 8 * u, vleft - 8 * u);
-                ok &= O::finite(c);
-                O::put_plain(lV + r * ldv + 8 * u, c);
-            }
-            if (!ok) bad[turn] = 1;
-            __syncthreads();
-            if (!bad[turn] || count == 1) break;
-            count = 1;
-            __syncthreads();
-        }
+        const bool again = bad[turn] && count > 1;
         if (threadIdx.x == 0) bad[turn ^ 1] = 0;
         turn ^= 1;
-
-        if (p.O) {
-#pragma unroll
-            for (int i = 0; i < CT; ++i) {
-                if (32 * i >= count) break;
+        if (again) singles = from + count;
+        const int next = again ? from : from + count;
+        int next_count = end - next < kChunk ? end - next : kChunk;
+        if (next < singles) next_count = 1;
+        if (next_count > 0) fetch(next, next_count);
+        if (!again) {
+            if (OUT && p.O) {
                 Frag q[KT];
 #pragma unroll
-                for (int k = 0; k < KT; ++k) q[k] = O::along(lA + (32 * i + n) * ld + 32 * k, h);
+                for (int k = 0; k < KT; ++k) q[k] = O::along(lA + n * ld + 32 * k, h);
                 f32x16_t out = {};
                 if (any) {
 #pragma unroll
@@ -318,124 +369,126 @@ __global__ __launch_bounds__(256, KT < 8 ? 2 : 1) void decay_kernel(const DecayP
 #pragma unroll
                         for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q[k], out);
                     }
-                    out *= fade[32 * i + n + (power_of_first ? 1 : 0)];
+                    out *= fade[n + (power_of_first ? 1 : 0)];
                 }
+                f32x16_t prob = {};
 #pragma unroll
-                for (int j = 0; j < CT; ++j) {
-                    if (j > i) break;
-                    f32x16_t prob = {};
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) prob = O::mma(O::along(lB + (32 * j + n) * ld + 32 * k, h), q[k], prob);
-                    float x[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int ago = 32 * (i - j) + n - acc_row(e, h);
-                        x[e] = ago >= 0 ? prob[e] * fade[ago] : 0.f;
-                    }
-                    Frag parts[O::kOutParts];
-                    O::template split<O::kOutParts>(x, parts);
-                    const Frag v = O::template across<false>(lV + 32 * j * ldv + col, ldv, lane);
-#pragma unroll
-                    for (int m = 0; m < O::kOutParts; ++m) out = O::mma(v, parts[m], out);
-                }
-                if (32 * i + n < count) {
-                    const size_t row = row_of(from + 32 * i + n);
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int c = col + 8 * g + 4 * h, left = vleft - c;
-                        f32x4_t v = {out[4 * g], out[4 * g + 1], out[4 * g + 2], out[4 * g + 3]};
-                        v *= p.out_scale;
-                        const size_t at = row * p.ldo + (size_t)head * p.dv + z * kDecayColumns + c;
-                        if (p.out32) {
-                            float *to = (float *)p.O + at;
-                            if (left >= 4) *reinterpret_cast<f32x4_any_t *>(to) = v;
-                            else
-#pragma unroll
-                                for (int e = 0; e < 3; ++e)
-                                    if (e < left) to[e] = v[e];
-                        } else {
-                            T *to = (T *)p.O + at;
-                            if (left >= 4) {
-                                if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t *>(to) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                                else *reinterpret_cast<f32x4_any_t *>(to) = v;
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 3; ++e)
-                                    if (e < left) Elem<T>::st(to + e, v[e]);
-                            }
-                        }
-                    }
-                }
-            }
-        }
-        // the state behind the chunk's last token (not needed behind the sequence's last one if nobody asks for it)
-        if (from + count < tokens.count || p.last) {
-            const int steps = count - 1 + power_of_first;
-            const double fall = steps == C ? whole : power(a, steps);
-            const float fall_hi = (float)fall, fall_lo = (float)(fall - (double)fall_hi);
-            if (any)
-#pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) state[k][e] = fmaf(state[k][e], fall_hi, state[k][e] * fall_lo);
-#pragma unroll
-            for (int j = 0; j < CT; ++j) {
-                if (32 * j >= count) break;
-                const Frag v = O::template across<false>(lV + 32 * j * ldv + col, ldv, lane);
+                for (int k = 0; k < KT; ++k) prob = O::mma(O::along(lB + n * ld + 32 * k, h), q[k], prob);
                 float x[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int left = count - 1 - 32 * j - acc_row(e, h);
-                    x[e] = left >= 0 ? O::get(v, e) * fade[left] : 0.f;
+                    const int ago = n - acc_row(e, h);
+                    x[e] = ago >= 0 ? prob[e] * fade[ago >= 0 ? ago : 0] : 0.f;
+                }
+                Frag parts[O::kOutParts];
+                O::template split<O::kOutParts>(x, parts);
+                const Frag v = O::template across<false>(lV + col, ldv, lane);
+#pragma unroll
+                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(v, parts[m], out);
+                if (n < count) {
+                    const size_t row = row_of(from + n);
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int c = col + 8 * g + 4 * h, left = vleft - c;
+                        f32x4_t w = {out[4 * g], out[4 * g + 1], out[4 * g + 2], out[4 * g + 3]};
+                        w *= p.out_scale;
+                        const size_t to = row * p.ldo + (size_t)head * p.dv + z * kDecayColumns + c;
+                        if (p.out32) put4((float *)p.O + to, left, w);
+                        else put4((T *)p.O + to, left, w);
+                    }
+                }
+            }
+            // the state behind the chunk's last token (not needed behind the sequence's last one if nobody asks for it)
+            if (!OUT || next < end || (final && p.last)) {
+                const int steps = count - 1 + power_of_first;
+                const double fall = steps == kChunk ? whole : power(a, steps);
+                const float fall_hi = (float)fall, fall_lo = (float)(fall - (double)fall_hi);
+                if (any)
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) state[k][e] = fmaf(state[k][e], fall_hi, state[k][e] * fall_lo);
+                const Frag v = O::template across<false>(lV + col, ldv, lane);
+                float x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int left = count - 1 - acc_row(e, h);
+                    x[e] = left >= 0 ? O::get(v, e) * fade[left >= 0 ? left : 0] : 0.f;
                 }
                 Frag parts[O::kStateParts];
                 O::template split<O::kStateParts>(x, parts);
 #pragma unroll
                 for (int k = 0; k < KT; ++k) {
-                    const Frag key = O::template across<true>(lB + 32 * j * ld + 32 * k, ld, lane);
+                    const Frag key = O::template across<true>(lB + 32 * k, ld, lane);
 #pragma unroll
                     for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key, parts[m], state[k]);
                 }
+                any = true;
             }
-            any = true;
+            power_of_first = 1;
         }
-        power_of_first = 1;
-        from += count;
+        from = next;
+        count = next_count;
     }
-    if (p.last) {
-        const float by = (float)(p.last_scale * (tokens.count > 0 ? power(a, p.last_power) : 1.0));
+    if (OUT ? final && p.last : true) {
+        float *to = OUT ? p.last + state_at : p.starts + (((size_t)b * p.heads + head) * p.segments + seg) * each;
+        const float by = OUT ? (float)(p.last_scale * (tokens.count > 0 ? power(a, p.last_power) : 1.0)) : 1.f;
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int64_t at = at_state(k, e);
-                if (at >= 0) p.last[state_at + at] = by * state[k][e];
+                const int i = at_state(k, e);
+                if (i >= 0) to[i] = by * state[k][e];
             }
     }
 }
 
-template <typename T, int KT>
-hipError_t launch_pass(const DecayPass &p, hipStream_t s)
+// sweeps of the same widths, one beside the other (blockIdx.y)
+constexpr int kMostSweeps = 3;
+struct DecaySweeps {
+    DecayPass pass[kMostSweeps];
+    int count;
+};
+template <typename T, int KT, int NW, bool OUT>
+__global__ __launch_bounds__(64 * NW, decay_waves(sizeof(T), KT)) void decay_kernel(const DecaySweeps s)
 {
-    static std::atomic<uint64_t> granted{0};
-    const int columns = p.dv >= kDecayColumns ? kDecayColumns : (p.dv + 31) / 32 * 32, blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
-    const int bytes = DecayShape<T, KT>::lds(columns);
-    const hipError_t e = allow_lds((const void *)decay_kernel<T, KT>, bytes, DecayShape<T, KT>::lds(kDecayColumns), granted);
+    decay_body<T, KT, NW, OUT>(s.pass[blockIdx.y]);
+}
+
+template <typename T, int KT, int NW>
+hipError_t launch_shape(const DecaySweeps &sw, bool outputs, hipStream_t s)
+{
+    using S = DecayShape<T, KT, NW>;
+    static std::atomic<uint64_t> granted[2];
+    const DecayPass &p = sw.pass[0];
+    const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns, bytes = S::lds(outputs);
+    const hipError_t e = allow_lds(outputs ? (const void *)decay_kernel<T, KT, NW, true> : (const void *)decay_kernel<T, KT, NW, false>, bytes, bytes, granted[outputs]);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((decay_kernel<T, KT>), dim3((unsigned)((size_t)p.sequences * p.heads * blocks)), dim3(2 * columns), bytes, s, p);
+    const dim3 grid((unsigned)((size_t)p.sequences * p.heads * p.segments * blocks), sw.count);
+    if (outputs) hipLaunchKernelGGL((decay_kernel<T, KT, NW, true>), grid, dim3(64 * NW), bytes, s, sw);
+    else hipLaunchKernelGGL((decay_kernel<T, KT, NW, false>), grid, dim3(64 * NW), bytes, s, sw);
     return hipGetLastError();
 }
 
+inline int key_tiles(int da) { return da <= 32 ? 1 : da <= 64 ? 2 : da <= 128 ? 4 : 8; }
+inline int value_waves(int dv) { return dv <= 64 ? 2 : 4; }
+
+// sweeps with the same key_tiles, value_waves, blocks of columns and segments
 template <typename T>
-hipError_t decay_pass(const DecayPass &p, hipStream_t s)
+hipError_t decay_sweeps(const DecaySweeps &sw, bool outputs, hipStream_t s)
 {
-    if (p.da <= 32) return launch_pass<T, 1>(p, s);
-    if (p.da <= 64) return launch_pass<T, 2>(p, s);
-    if (p.da <= 128) return launch_pass<T, 4>(p, s);
-    return launch_pass<T, 8>(p, s);
+    auto wide = [&](auto nw) {
+        switch (key_tiles(sw.pass[0].da)) {
+        case 1: return launch_shape<T, 1, decltype(nw)::value>(sw, outputs, s);
+        case 2: return launch_shape<T, 2, decltype(nw)::value>(sw, outputs, s);
+        case 4: return launch_shape<T, 4, decltype(nw)::value>(sw, outputs, s);
+        }
+        return launch_shape<T, 8, decltype(nw)::value>(sw, outputs, s);
+    };
+    return value_waves(sw.pass[0].dv) == 2 ? wide(std::integral_constant<int, 2>()) : wide(std::integral_constant<int, 4>());
 }
-hipError_t decay_pass_bf16(const DecayPass &p, hipStream_t s);   // seq_decay.hip
-hipError_t decay_pass_f32(const DecayPass &p, hipStream_t s);    // seq_decay_f32.hip
+hipError_t decay_sweeps_bf16(const DecaySweeps &sw, bool outputs, hipStream_t s);   // seq_decay_bf16.hip
+hipError_t decay_sweeps_f32(const DecaySweeps &sw, bool outputs, hipStream_t s);    // seq_decay_f32.hip
 
 }  // namespace seq
 }  // namespace stl

@@ -1,26 +1,113 @@
-// Attention with decay: bf16 storage, and what the forward and the backward call make of the sweeps.
+// Attention with decay: what the forward and the backward call make of the sweeps, single tokens, and the small kernels around.
 #include "seq_decay.h"
 
 namespace stl {
 namespace seq {
 
-hipError_t decay_pass_bf16(const DecayPass &p, hipStream_t s) { return decay_pass<bf16_t>(p, s); }
+// Up to so many tokens a sequence go one by one, with the state in registers (decay_few_kernel): a sweep's chunk is 32 tokens whatever it holds.
+constexpr int kFewTokens = 8;
 
-namespace {
-
-DecayPass common(const DecayArgs &a)
+// A few tokens: memory bound by the state, which is read once and written once.  A thread has four columns of every RG-th row (RG: groups of COLS / 4 threads), RPT
+// rows; for each token q and k go through LDS, o is the sum over the rows: lanes, then wavefronts.
+template <typename T, int COLS, int RPT>
+__global__ __launch_bounds__(256) void decay_few_kernel(const DecayArgs a, T *O, float *state_out)
 {
+    constexpr int LC = COLS / 4, RG = 256 / LC;
+    __shared__ float lq[kDecayWidest], lk[kDecayWidest];
+    __shared__ __align__(16) float sums[4][COLS];
+    const int blocks = (a.dv + COLS - 1) / COLS, z = (int)blockIdx.x % blocks, bh = (int)blockIdx.x / blocks, b = bh / a.heads, head = bh % a.heads;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, col = z * COLS + 4 * (tid % LC), group = tid / LC, left = a.dv - col;
     DecayPass p{};
-    p.rows = a.rows, p.sequences = a.sequences, p.length = a.length, p.heads = a.heads, p.seq_step = a.seq_step, p.token_step = a.token_step;
-    p.log_decay = a.log_decay, p.offset = a.offset;
-    p.share_a = p.share_b = p.share_v = 1;
-    p.out_scale = a.scale, p.init_scale = p.last_scale = 1.f;
-    return p;
+    p.rows = a.rows, p.length = a.length, p.seq_step = a.seq_step, p.offset = a.offset;
+    const Tokens tokens = tokens_of(p, b);
+    const size_t at = (size_t)bh * a.dk * a.dv;
+    f32x4_t state[RPT];
+#pragma unroll
+    for (int r = 0; r < RPT; ++r) {
+        const int i = r * RG + group;
+        state[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (a.state && i < a.dk) state[r] = load4(a.state + at + (size_t)i * a.dv + col, left);
+    }
+    double fall = a.log_decay ? (double)a.log_decay[head] : 0.0;
+    fall = power(fall < -1e5 ? -1e5 : fall, 1);
+    const float by = (float)fall;
+    const int share = a.heads / a.kv_heads;
+    for (int t = 0; t < tokens.count; ++t) {
+        const size_t row = (size_t)(tokens.first + (int64_t)t * (a.offset ? 1 : a.token_step));
+        if (tid < a.dk) {
+            lq[tid] = a.scale * Elem<T>::ld((const T *)a.Q + row * a.ld_q + (size_t)head * a.dk + tid);
+            lk[tid] = Elem<T>::ld((const T *)a.K + row * a.ld_k + (size_t)(head / share) * a.dk + tid);
+        }
+        const f32x4_t v = load4((const T *)a.V + row * a.ld_v + (size_t)(head / share) * a.dv + col, left);
+        __syncthreads();
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const int i = r * RG + group;
+            const float k = lk[i], q = lq[i];                    // (there is LDS behind the last row too, and any value does)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                state[r][e] = fmaf(state[r][e], by, k * v[e]);
+                sum[e] = i < a.dk ? fmaf(q, state[r][e], sum[e]) : sum[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            for (int n = LC; n < 64; n *= 2) sum[e] += __shfl_xor(sum[e], n);
+        if (lane < LC) *reinterpret_cast<f32x4_t *>(&sums[wave][4 * lane]) = sum;
+        __syncthreads();
+        if (tid < COLS && z * COLS + tid < a.dv)
+            Elem<T>::st(O + row * a.ld_o + (size_t)head * a.dv + z * COLS + tid, (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]));
+    }
+    if (!state_out || (tokens.count == 0 && state_out == a.state)) return;
+#pragma unroll
+    for (int r = 0; r < RPT; ++r) {
+        const int i = r * RG + group;
+        if (i < a.dk) put4(state_out + at + (size_t)i * a.dv + col, left, state[r]);
+    }
 }
 
-size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+template <typename T, int COLS>
+hipError_t few_tokens(const DecayArgs &a, void *O, float *state_out, hipStream_t s)
+{
+    constexpr int RG = 256 / (COLS / 4);
+    const dim3 grid((unsigned)((size_t)a.sequences * a.heads * ((a.dv + COLS - 1) / COLS)));
+    const int each = (a.dk + RG - 1) / RG;
+    if (each <= 64 / RG) hipLaunchKernelGGL((decay_few_kernel<T, COLS, 64 / RG>), grid, dim3(256), 0, s, a, (T *)O, state_out);
+    else if (each <= 128 / RG) hipLaunchKernelGGL((decay_few_kernel<T, COLS, 128 / RG>), grid, dim3(256), 0, s, a, (T *)O, state_out);
+    else hipLaunchKernelGGL((decay_few_kernel<T, COLS, 256 / RG>), grid, dim3(256), 0, s, a, (T *)O, state_out);
+    return hipGetLastError();
+}
 
-}  // namespace
+// What segments add to the state -> the state in front of each.  Four elements a thread; the elements of a state in whichever order they lie.
+__global__ __launch_bounds__(256) void decay_join_kernel(const DecaySweeps s)
+{
+    const DecayPass &p = s.pass[blockIdx.z];
+    const int each = p.da * p.dv, bh = (int)blockIdx.x, at = 4 * ((int)blockIdx.y * 256 + (int)threadIdx.x), left = each - at;
+    if (left <= 0) return;
+    const Tokens tokens = tokens_of(p, bh / p.heads);
+    double a = p.log_decay ? (double)p.log_decay[bh % p.heads] : 0.0;
+    a = a < -1e5 ? -1e5 : a;
+    float *starts = p.starts + (size_t)bh * p.segments * each + at;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    if (p.init) {
+        v = load4(p.init + (size_t)bh * each + at, left);
+        put4(starts + (size_t)(p.segments - 1) * each, left, v);
+        v *= p.init_scale;
+    }
+    int steps = p.seg_tokens - 1 + p.init_power;
+    const int full = (tokens.count - 1) / p.seg_tokens;          // segments with another behind them
+    f32x4_t next = full > 0 ? load4(starts, left) : v;
+    for (int k = 0; k < full; ++k) {
+        const f32x4_t add = next;
+        if (k + 1 < full) next = load4(starts + (size_t)(k + 1) * each, left);
+        const float fall = (float)power(a, steps);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], fall, add[e]);
+        put4(starts + (size_t)k * each, left, v);
+        steps = p.seg_tokens;
+    }
+}
 
 // Gradients of key heads that several heads share: out[row][g] = sum over the heads of group g of part[row][head], rows of the sequences alone.
 template <typename T>
@@ -40,16 +127,94 @@ __global__ __launch_bounds__(256) void decay_share_kernel(const DecayPass p, con
     }
 }
 
+namespace {
+
+size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+
+// Segments of a sequence: as many as give every CU two workgroups, of 128 tokens at least; at most so many, and how they come out.
+int most_segments(const DecayArgs &a)
+{
+    const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns);
+    int64_t n = 512 / groups;
+    if (n > a.length / 128) n = a.length / 128;
+    return n < 1 ? 1 : (int)n;
+}
+void cut(const DecayArgs &a, int *segments, int *tokens)
+{
+    const int64_t n = most_segments(a);
+    *tokens = n > 1 ? (int)((a.length + n * kChunk - 1) / (n * kChunk)) * kChunk : a.length > 0 ? a.length : 1;
+    *segments = a.length > 0 ? (a.length + *tokens - 1) / *tokens : 1;
+}
+
+DecayPass common(const DecayArgs &a)
+{
+    DecayPass p{};
+    p.rows = a.rows, p.sequences = a.sequences, p.length = a.length, p.heads = a.heads, p.seq_step = a.seq_step, p.token_step = a.token_step;
+    p.log_decay = a.log_decay, p.offset = a.offset;
+    p.share_a = p.share_b = p.share_v = 1;
+    p.out_scale = a.scale, p.init_scale = p.last_scale = 1.f;
+    cut(a, &p.segments, &p.seg_tokens);
+    return p;
+}
+
+size_t starts_bytes(const DecayArgs &a)
+{
+    // (never less for a longer sequence)
+    const int segments = most_segments(a);
+    return segments > 1 ? whole((size_t)a.sequences * a.heads * segments * a.dk * a.dv * 4) : 0;
+}
+size_t parts_bytes(const DecayArgs &a, int width) { return a.heads != a.kv_heads ? whole((size_t)a.rows * a.heads * width * 4) : 0; }
+
+hipError_t sweep(int dtype, const DecaySweeps &sw, bool outputs, hipStream_t s)
+{
+    return dtype ? decay_sweeps_bf16(sw, outputs, s) : decay_sweeps_f32(sw, outputs, s);
+}
+hipError_t join(const DecaySweeps &sw, hipStream_t s)
+{
+    const DecayPass &p = sw.pass[0];
+    hipLaunchKernelGGL(decay_join_kernel, dim3(p.sequences * p.heads, (p.da * p.dv + 1023) / 1024, sw.count), dim3(256), 0, s, sw);
+    return hipGetLastError();
+}
+
+hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const float *part, void *out, size_t ld, int width, hipStream_t s)
+{
+    const int64_t elements = (int64_t)a.length * a.kv_heads * width;
+    int64_t blocks = (elements + 2047) / 2048;
+    if (blocks > 4096) blocks = 4096;
+    for (int b = 0; b < a.sequences; b += 65535) {
+        DecayPass q = p;
+        const dim3 grid((unsigned)blocks, a.sequences - b < 65535 ? a.sequences - b : 65535);
+        if (q.offset) q.offset += b;
+        const size_t skip = q.offset ? 0 : (size_t)b * a.seq_step;
+        const float *from = part + skip * a.heads * width;
+        if (dtype) hipLaunchKernelGGL(decay_share_kernel<bf16_t>, grid, dim3(256), 0, s, q, from, (bf16_t *)out + skip * ld, ld, width, a.heads / a.kv_heads);
+        else hipLaunchKernelGGL(decay_share_kernel<float>, grid, dim3(256), 0, s, q, from, (float *)out + skip * ld, ld, width, a.heads / a.kv_heads);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
 size_t decay_workspace_bytes(int dtype, const DecayArgs &a, bool grads)
 {
-    size_t n = 0;
-    if (grads && a.heads != a.kv_heads) n += whole((size_t)a.rows * a.heads * (a.dk > a.dv ? a.dk : a.dv) * 4);
-    return n;
+    if (!grads) return a.length > kFewTokens ? starts_bytes(a) : 0;
+    return 2 * starts_bytes(a) + parts_bytes(a, a.dk) + parts_bytes(a, a.dv);
 }
 
 hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *state_out, void *ws, hipStream_t s)
 {
-    DecayPass p = common(a);
+    if (a.length <= kFewTokens) {
+        // 32 columns a workgroup where 128 would leave CUs without one
+        const bool narrow = (int64_t)a.sequences * a.heads * ((a.dv + 127) / 128) < 1024;
+        if (dtype) return narrow ? few_tokens<bf16_t, 32>(a, O, state_out, s) : few_tokens<bf16_t, 128>(a, O, state_out, s);
+        return narrow ? few_tokens<float, 32>(a, O, state_out, s) : few_tokens<float, 128>(a, O, state_out, s);
+    }
+    DecaySweeps sw{};
+    DecayPass &p = sw.pass[0];
+    sw.count = 1;
+    p = common(a);
     p.da = a.dk, p.dv = a.dv;
     p.A = a.Q, p.lda = a.ld_q;
     p.B = a.K, p.ldb = a.ld_k, p.V = a.V, p.ldv = a.ld_v;
@@ -57,75 +222,86 @@ hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *s
     p.O = O, p.ldo = a.ld_o;
     p.init = a.state, p.last = state_out;
     p.init_power = 1;
-    return dtype ? decay_pass_bf16(p, s) : decay_pass_f32(p, s);
+    p.starts = (float *)ws;
+    if (p.segments > 1) {
+        hipError_t e = sweep(dtype, sw, false, s);
+        if (e == hipSuccess) e = join(sw, s);
+        if (e != hipSuccess) return e;
+    }
+    return sweep(dtype, sw, true, s);
 }
 
 hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads &g, void *ws, hipStream_t s)
 {
     const int share = a.heads / a.kv_heads;
-    auto sweep = [&](const DecayPass &p) { return dtype ? decay_pass_bf16(p, s) : decay_pass_f32(p, s); };
-    // what belongs to a key head: by head in fp32 first where heads share it
-    auto shared = [&](DecayPass p, void *out, size_t ld, int width) {
-        if (share == 1 || !out) {
-            p.O = out, p.ldo = ld;
-            return sweep(p);
-        }
-        p.O = ws, p.ldo = (size_t)a.heads * width, p.out32 = true;
-        hipError_t e = sweep(p);
-        if (e != hipSuccess) return e;
-        const int64_t elements = (int64_t)a.length * a.kv_heads * width;
-        int64_t blocks = (elements + 2047) / 2048;
-        if (blocks > 4096) blocks = 4096;
-        for (int b = 0; b < a.sequences; b += 65535) {
-            DecayPass q = p;
-            const int some = a.sequences - b < 65535 ? a.sequences - b : 65535;
-            const dim3 grid((unsigned)blocks, some);
-            float *part = (float *)ws;
-            if (q.offset) q.offset += b;
-            const size_t skip = q.offset ? 0 : (size_t)b * a.seq_step;
-            part += skip * a.heads * width;
-            if (dtype) hipLaunchKernelGGL(decay_share_kernel<bf16_t>, grid, dim3(256), 0, s, q, (const float *)part, (bf16_t *)out + skip * ld, ld, width, share);
-            else hipLaunchKernelGGL(decay_share_kernel<float>, grid, dim3(256), 0, s, q, (const float *)part, (float *)out + skip * ld, ld, width, share);
-            e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        return hipSuccess;
+    char *at = (char *)ws;
+    auto take = [&](size_t n) {
+        char *was = at;
+        at += n;
+        return (float *)was;
     };
+    float *starts[2] = {take(starts_bytes(a)), take(starts_bytes(a))}, *part_k = take(parts_bytes(a, a.dk)), *part_v = take(parts_bytes(a, a.dv));
+    // the state forward in time, from K and V
+    DecayPass f = common(a);
+    f.da = a.dk, f.dv = a.dv;
+    f.B = a.K, f.ldb = a.ld_k, f.V = a.V, f.ldv = a.ld_v;
+    f.share_b = f.share_v = share;
+    f.init = a.state, f.init_power = 1;
+    f.starts = starts[0];
+    // its gradient backward in time, from Q and dO, held without the factor c, which its outputs have
+    DecayPass r = common(a);
+    r.reverse = true;
+    r.da = a.dk, r.dv = a.dv;
+    r.B = a.Q, r.ldb = a.ld_q, r.V = g.dO, r.ldv = a.ld_o;
+    r.init = g.dstate_out, r.init_scale = 1.f / a.scale;
+    r.last_scale = a.scale, r.last_power = 1;
+    r.starts = starts[1];
+    const bool back = g.dK || g.dV || g.dstate_in;
     hipError_t e = hipSuccess;
+    if (f.segments > 1) {
+        // (the last state is written over none of them: `init` need not be kept, but for dstate_in, which is the last state of the sweep for dV)
+        DecaySweeps sw{};
+        if (g.dQ) sw.pass[sw.count++] = f;
+        if (back) sw.pass[sw.count++] = r;
+        e = sweep(dtype, sw, false, s);
+        if (e == hipSuccess) e = join(sw, s);
+        if (e != hipSuccess) return e;
+    }
+    DecaySweeps sw{};
     if (g.dQ) {
-        DecayPass p = common(a);
-        p.da = a.dv, p.dv = a.dk;
+        DecayPass p = f;
+        p.da = a.dv, p.dv = a.dk, p.turned = true;
         p.A = g.dO, p.lda = a.ld_o;
         p.B = a.V, p.ldb = a.ld_v, p.V = a.K, p.ldv = a.ld_k;
-        p.share_b = p.share_v = share;
         p.O = g.dQ, p.ldo = a.ld_q;
-        p.init = a.state, p.turned = true;
-        p.init_power = 1;
-        e = sweep(p);
-        if (e != hipSuccess) return e;
-    }
-    // the state's gradient is held without the factor c, which its outputs have
-    DecayPass p = common(a);
-    p.reverse = true;
-    p.init = g.dstate_out, p.init_scale = 1.f / a.scale;
-    p.last_scale = a.scale, p.last_power = 1;
-    if (g.dV || g.dstate_in) {
-        DecayPass v = p;
-        v.da = a.dk, v.dv = a.dv;
-        v.A = a.K, v.lda = a.ld_k, v.share_a = share;
-        v.B = a.Q, v.ldb = a.ld_q, v.V = g.dO, v.ldv = a.ld_o;
-        v.last = g.dstate_in;
-        e = shared(v, g.dV, a.ld_v, a.dv);
-        if (e != hipSuccess) return e;
+        sw.pass[sw.count++] = p;
     }
     if (g.dK) {
-        DecayPass k = p;
-        k.da = a.dv, k.dv = a.dk;
-        k.A = a.V, k.lda = a.ld_v, k.share_a = share;
-        k.B = g.dO, k.ldb = a.ld_o, k.V = a.Q, k.ldv = a.ld_q;
-        k.turned = true;
-        e = shared(k, g.dK, a.ld_k, a.dk);
+        DecayPass p = r;
+        p.da = a.dv, p.dv = a.dk, p.turned = true;
+        p.A = a.V, p.lda = a.ld_v, p.share_a = share;
+        p.B = g.dO, p.ldb = a.ld_o, p.V = a.Q, p.ldv = a.ld_q;
+        p.O = share > 1 ? (void *)part_k : g.dK, p.ldo = share > 1 ? (size_t)a.heads * a.dk : a.ld_k, p.out32 = share > 1;
+        sw.pass[sw.count++] = p;
     }
+    if (g.dV || g.dstate_in) {
+        DecayPass p = r;
+        p.A = a.K, p.lda = a.ld_k, p.share_a = share;
+        p.O = share > 1 && g.dV ? (void *)part_v : g.dV, p.ldo = share > 1 ? (size_t)a.heads * a.dv : a.ld_v, p.out32 = share > 1;
+        p.last = g.dstate_in;
+        sw.pass[sw.count++] = p;
+    }
+    // one launch for sweeps of the same widths
+    for (int i = 0; i < sw.count;) {
+        DecaySweeps some{};
+        do some.pass[some.count++] = sw.pass[i++];
+        while (i < sw.count && key_tiles(sw.pass[i].da) == key_tiles(some.pass[0].da) && value_waves(sw.pass[i].dv) == value_waves(some.pass[0].dv) &&
+               (sw.pass[i].dv + kDecayColumns - 1) / kDecayColumns == (some.pass[0].dv + kDecayColumns - 1) / kDecayColumns);
+        e = sweep(dtype, some, true, s);
+        if (e != hipSuccess) return e;
+    }
+    if (share > 1 && g.dK) e = share_out(dtype, a, r, part_k, g.dK, a.ld_k, a.dk, s);
+    if (share > 1 && g.dV && e == hipSuccess) e = share_out(dtype, a, r, part_v, g.dV, a.ld_v, a.dv, s);
     return e;
 }
 
