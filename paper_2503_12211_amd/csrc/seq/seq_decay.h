@@ -13,8 +13,14 @@
 // stays in accumulators (dk x 32, fp32) all along.  Products are formed so that accumulators are the next product's operand as they lie:
 //   P^T = K Q^T (tokens j x i)   ->   O^T += V^T P^T,      S (dk x columns) as S^T in   O^T = S^T Q^T
 // An accumulator's lane holds rows 8 (e / 4) + 4 h + e % 4 of its column (h = lane / 32), an operand's lane eight elements of the contraction, whose
-// order is free as long as both operands have it: the contraction goes in the accumulators' order, and Q and K lie in LDS with the middle two of every
-// four groups of four elements exchanged, so that a lane still reads 16 bytes at once.
+// order is free as long as both operands have it.  Contractions over tokens go in the accumulators' order; those over columns in the order of memory, as
+// columns are dealt to lanes such that the accumulators have it too (dealt).
+//
+// Chunks of 32 tokens come through a ring of LDS stages, loaded without a register between (rows of whole 16-byte pieces at such addresses; others go through
+// registers and one stage).
+//
+// A value of V that is no finite number must not reach earlier tokens, as it would with a zero of the masked P: it is multiplied as a zero, and its column
+// of the outputs from its token on, and of the state, becomes NaN.
 //
 // bf16 storage: operands that come from fp32 (P, S, V scaled by the decay up to the chunk's end) are given to the matrix cores as sums of bf16 numbers, two of
 // them (a relative error of 2^-16) for what goes into outputs that are rounded to bf16, three (2^-24) for what goes into the fp32 state.  With one, P's
@@ -22,6 +28,7 @@
 #pragma once
 #include "seq_kernels.h"
 #include "../lm/lm_device.h"
+#include "../stl_gemm_pipe.h"
 
 #include <atomic>
 
@@ -29,8 +36,7 @@ namespace stl {
 namespace seq {
 
 using lm::Chunk;
-typedef short v4i16_t __attribute__((ext_vector_type(4)));
-#define SEQ_LDS(p) ((__attribute__((address_space(3))) char *)(p))
+using pipe::v4i16_t;
 
 // One sweep: "queries" A, "keys" B (width da), "values" V (width dv); forward in time, or backward.  Heads of A, B and V that several heads
 // share: head h takes h / share.
@@ -56,6 +62,7 @@ struct DecayPass {
     // the state in front of segment s + 1; the last one `init` as it was, where the last state may be written over it.
     int segments, seg_tokens;
     float *starts;
+    bool ring;                               // rows are whole 16-byte pieces at such addresses
 };
 
 // tokens of sequence b: the row of the first, and how many (never outside the rows there are, whatever the offsets are)
@@ -75,11 +82,26 @@ __device__ __forceinline__ Tokens tokens_of(const DecayPass &p, int b)
 // lambda^n, a not below -100000 (where it is 0 for every n > 0)
 __device__ __forceinline__ double power(double a, int n) { return n == 0 ? 1.0 : exp(a * n); }
 
+
+constexpr int kChunk = 32;                   // tokens
+
+// 32 rows of an operand in LDS, in groups of four 16-byte pieces of every row (64 bytes a row, 2 KB a group).  Piece c of row r lies in its row's place
+// c % 4 ^ r / 4 % 4: a read of one piece of 32 rows, or of four pieces of four rows, meets every bank alike, and group and operand are constants of an address.
+constexpr int kGroupBytes = 64 * kChunk;
+__device__ __forceinline__ int piece_at(int r, int c) { return kGroupBytes * (c >> 2) + 64 * r + 16 * ((c ^ r >> 2) & 3); }
+
+// a lane's row within 32 of accumulator element e
+__device__ __forceinline__ int acc_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
+// Columns of an operand that is read across its rows are dealt to lanes with bits 2 and 3 swapped, so that a lane's accumulator elements 8 b .. 8 b + 7 are
+// columns next to each other, 16 b + 8 h ..: eight outputs, or the contraction's order of a 16-byte piece (Ops::along).
+__device__ __forceinline__ int dealt(int n) { return (n & ~12) | (n & 4) << 1 | (n & 8) >> 1; }
+__device__ __forceinline__ int dealt_row(int e, int h) { return 16 * (e >> 3) + 8 * h + (e & 7); }
+
 template <typename T> struct Ops;
 
 template <> struct Ops<bf16_t> {
-    static constexpr int kPad = 8, kOutParts = 2, kStateParts = 3;
-    // operand for a contraction of 32 in the accumulators' order
+    static constexpr int kOutParts = 2, kStateParts = 3;
+    // operand for a contraction of 32
     struct Frag {
         bf16x8_t f[2];
     };
@@ -88,41 +110,33 @@ template <> struct Ops<bf16_t> {
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.f[0], b.f[0], c, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.f[1], b.f[1], c, 0, 0, 0);
     }
-    // contraction along a row of LDS (rows as put() leaves them), p at the row's 32 elements
-    static __device__ __forceinline__ Frag along(const bf16_t *p, int h)
+    // A lane's places: of its pieces of row n, and of what it gives to the transposing reads.
+    struct Places {
+        int row[2], across[2];
+    };
+    static __device__ __forceinline__ Places places(int lane)
+    {
+        const int n = lane & 31, h = lane >> 5, q = lane & 15, r = 4 * h + (q >> 2), c = 2 * (lane >> 4 & 1) + (q & 1);
+        return Places{{piece_at(n, h), piece_at(n, 2 + h)}, {piece_at(r, c) + 4 * (q & 2), piece_at(r + 8, c) + 4 * (q & 2)}};
+    }
+    // contraction along the rows, elements 32 k + dealt_row(e, h) of row lane % 32
+    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k)
     {
         Frag r;
-        r.f[0] = *reinterpret_cast<const bf16x8_t *>(p + 8 * h);
-        r.f[1] = *reinterpret_cast<const bf16x8_t *>(p + 16 + 8 * h);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) r.f[b] = *reinterpret_cast<const bf16x8_t *>(rows + at.row[b] + kGroupBytes * k);
         return r;
     }
-    // contraction over 32 rows of LDS, the lane's column of the 32 from p on; PUT: rows as put() leaves them
-    template <bool PUT>
-    static __device__ __forceinline__ Frag across(const bf16_t *p, int stride, int lane)
+    // contraction over the rows in the accumulators' order, column 32 k + dealt(lane % 32)
+    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int k)
     {
-        const int h = lane >> 5, q = lane & 15, piece = PUT ? (q & 3) == 1 ? 2 : (q & 3) == 2 ? 1 : q & 3 : q & 3;
-        const bf16_t *at = p + (4 * h + (q >> 2)) * stride + 16 * (lane >> 4 & 1) + 4 * piece;
         struct { v4i16_t lo, hi; } two[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            two[b].lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)SEQ_LDS((char *)(at + 16 * b * stride)));
-            two[b].hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)SEQ_LDS((char *)(at + (16 * b + 8) * stride)));
+            two[b].lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(rows + at.across[0] + kGroupBytes * k + 1024 * b));
+            two[b].hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(rows + at.across[1] + kGroupBytes * k + 1024 * b));
         }
         return Frag{{__builtin_bit_cast(bf16x8_t, two[0]), __builtin_bit_cast(bf16x8_t, two[1])}};
-    }
-    // sixteen elements of a row on their way to LDS: groups of four in the order 0 2 1 3
-    static __device__ __forceinline__ void put(bf16_t *p, const Chunk<bf16_t> &a, const Chunk<bf16_t> &b)
-    {
-        *reinterpret_cast<u32x4_t *>(p) = u32x4_t{a.v[0], a.v[1], b.v[0], b.v[1]};
-        *reinterpret_cast<u32x4_t *>(p + 8) = u32x4_t{a.v[2], a.v[3], b.v[2], b.v[3]};
-    }
-    static __device__ __forceinline__ void put_plain(bf16_t *p, const Chunk<bf16_t> &a) { *reinterpret_cast<u32x4_t *>(p) = a.v; }
-    static __device__ __forceinline__ bool finite(const Chunk<bf16_t> &a)
-    {
-        bool ok = true;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ok &= (a.v[i] & 0x7f80u) != 0x7f80u && (a.v[i] & 0x7f800000u) != 0x7f800000u;
-        return ok;
     }
     // the sum of N operands, the last of them rounded
     template <int N>
@@ -150,10 +164,41 @@ template <> struct Ops<bf16_t> {
         const u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[e >> 3]);
         return __uint_as_float(e & 1 ? w[e >> 1 & 3] & 0xffff0000u : w[e >> 1 & 3] << 16);
     }
+    // (an exponent of ones carries into its sign bit)
+    static __device__ __forceinline__ bool finite(const Frag &a)
+    {
+        uint32_t carry = 0;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[b]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) carry |= (w[i] & 0x7f807f80u) + 0x00800080u;
+        }
+        return !(carry & 0x80008000u);
+    }
+    // zeros in the place of what is no finite number; the first row of such an element, 32 if there is none
+    static __device__ __forceinline__ int clean(Frag &a, int h)
+    {
+        int first = kChunk;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[b]);
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const uint32_t half = i & 1 ? 0xffff0000u : 0xffffu, ones = half & 0x7f807f80u;
+                if ((w[i >> 1] & ones) != ones) continue;
+                w[i >> 1] &= ~half;
+                const int row = acc_row(8 * b + i, h);
+                first = row < first ? row : first;
+            }
+            a.f[b] = __builtin_bit_cast(bf16x8_t, w);
+        }
+        return first;
+    }
 };
 
 template <> struct Ops<float> {
-    static constexpr int kPad = 4, kOutParts = 1, kStateParts = 1;
+    static constexpr int kOutParts = 1, kStateParts = 1;
     struct Frag {
         float f[16];
     };
@@ -163,41 +208,31 @@ template <> struct Ops<float> {
         for (int e = 0; e < 16; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[e], b.f[e], c, 0, 0, 0);
         return c;
     }
-    static __device__ __forceinline__ Frag along(const float *p, int h)
+    struct Places {
+        int row[2], across[2];
+    };
+    static __device__ __forceinline__ Places places(int lane)
+    {
+        const int n = lane & 31, h = lane >> 5, column = dealt(n), c = column >> 2;
+        return Places{{piece_at(n, 2 * h), piece_at(n, 2 * h + 1)}, {piece_at(4 * h, c) + 4 * (column & 3), piece_at(8 + 4 * h, c) + 4 * (column & 3)}};
+    }
+    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k)
     {
         Frag r;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(p + 8 * g + 4 * h);
+            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(rows + at.row[g & 1] + kGroupBytes * (2 * k + (g >> 1)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) r.f[4 * g + e] = v[e];
         }
         return r;
     }
-    template <bool PUT>
-    static __device__ __forceinline__ Frag across(const float *p, int stride, int lane)
+    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int k)
     {
         Frag r;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) r.f[e] = p[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * stride + (lane & 31)];
+        for (int e = 0; e < 16; ++e) r.f[e] = *reinterpret_cast<const float *>(rows + at.across[e >> 2 & 1] + 2 * kGroupBytes * k + 1024 * (e >> 3) + 64 * (e & 3));
         return r;
-    }
-    static __device__ __forceinline__ void put(float *p, const Chunk<float> &a, const Chunk<float> &b)
-    {
-        put_plain(p, a);
-        put_plain(p + 8, b);
-    }
-    static __device__ __forceinline__ void put_plain(float *p, const Chunk<float> &a)
-    {
-        *reinterpret_cast<f32x4_t *>(p) = a.a;
-        *reinterpret_cast<f32x4_t *>(p + 4) = a.b;
-    }
-    static __device__ __forceinline__ bool finite(const Chunk<float> &a)
-    {
-        bool ok = true;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ok &= (__float_as_uint(a.get(e)) & 0x7f800000u) != 0x7f800000u;
-        return ok;
     }
     template <int N>
     static __device__ __forceinline__ void split(const float *x, Frag *out)
@@ -206,19 +241,40 @@ template <> struct Ops<float> {
         for (int e = 0; e < 16; ++e) out[0].f[e] = x[e];
     }
     static __device__ __forceinline__ float get(const Frag &a, int e) { return a.f[e]; }
+    static __device__ __forceinline__ bool finite(const Frag &a)
+    {
+        uint32_t carry = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) carry |= (__float_as_uint(a.f[e]) & 0x7f800000u) + 0x00800000u;
+        return !(carry & 0x80000000u);
+    }
+    static __device__ __forceinline__ int clean(Frag &a, int h)
+    {
+        int first = kChunk;
+#pragma unroll
+        for (int e = 15; e >= 0; --e) {
+            if ((__float_as_uint(a.f[e]) & 0x7f800000u) != 0x7f800000u) continue;
+            a.f[e] = 0.f;
+            first = acc_row(e, h);
+        }
+        return first;
+    }
 };
-
-// a lane's row within 32 of accumulator element e
-__device__ __forceinline__ int acc_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
 
 constexpr int kDecayColumns = 128;           // of v, of a workgroup, 32 a wavefront
-constexpr int kChunk = 32;
-template <typename T, int KT, int NW>        // 32 KT: width of queries and keys in LDS; NW wavefronts
+// 32 KT: width of queries and keys in LDS; NW wavefronts; OUT: with outputs; RING: loaded by LDS-DMA
+template <typename T, int KT, int NW, bool OUT, bool RING>
 struct DecayShape {
-    static constexpr int columns = 32 * NW, ld = 32 * KT + Ops<T>::kPad, ldv = columns + Ops<T>::kPad;
-    static constexpr int lds(bool outputs) { return (((outputs ? 2 : 1) * ld + ldv) * kChunk * (int)sizeof(T) + 15) / 16 * 16 + (kChunk + 1) * 4 + 8; }
+    static constexpr int columns = 32 * NW, threads = 64 * NW, in_group = 64 / (int)sizeof(T);
+    static constexpr int groups = 32 * KT / in_group, groups_v = columns / in_group;
+    static constexpr int bytes = kGroupBytes * groups, bytes_v = kGroupBytes * groups_v, stage = (OUT ? 2 : 1) * bytes + bytes_v;
+    // 256 registers and half of the LDS, so that two workgroups share a CU, where a wavefront's state fits
+    static constexpr int waves = sizeof(T) == 2 && KT <= 4 ? 2 : 1;
+    static constexpr int room = 160 * 1024 / waves - 512, fit = room / stage;
+    static constexpr int stages = RING ? fit < 4 ? fit : 4 : 1;
+    static constexpr int lds = stages * stage + 4 * (2 * kChunk + 4);
+    static_assert(stages >= (RING ? 2 : 1), "a ring has two stages at least");
 };
-// 256 registers, two workgroups a CU, where a wavefront's state and the next chunk fit
 constexpr int decay_waves(size_t element, int KT) { return element == 2 && KT <= 4 ? 2 : 1; }
 
 // up to four elements of a row of outputs
@@ -235,18 +291,76 @@ __device__ __forceinline__ void put4(T *to, int left, f32x4_t v)
     }
 }
 
-// OUT: with outputs; without, what a segment adds to the state
-template <typename T, int KT, int NW, bool OUT>
+// all but the N youngest loads and stores are done, and all LDS reads
+template <int N>
+__device__ __forceinline__ void wait_all_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// eight elements of row r, from element 8 u on, to where they lie in LDS
+__device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<bf16_t> &c) { *reinterpret_cast<u32x4_t *>(rows + piece_at(r, u)) = c.v; }
+__device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<float> &c)
+{
+    *reinterpret_cast<f32x4_t *>(rows + piece_at(r, 2 * u)) = c.a;
+    *reinterpret_cast<f32x4_t *>(rows + piece_at(r, 2 * u + 1)) = c.b;
+}
+
+// One operand's share of a stage that a wavefront loads by LDS-DMA.  Instruction i brings 64 pieces, one a lane: four of each of 16 rows.  Where the row
+// ends before the groups do, or instructions are no multiple of the wavefronts, some of them bring the same again: all wavefronts issue as many.
+template <typename T, int GROUPS, int NW>
+struct RingSource {
+    static constexpr int kAll = 2 * GROUPS, kPer = (kAll + NW - 1) / NW;
+    const char *first;                       // of the sequence's first row
+    int64_t step;                            // bytes from token to token
+    uint32_t which, off[kPer];               // a bit for each instruction: whether this lane's piece lies within the row; its place from the chunk's lowest row on
+    int instruction[kPer];
+    __device__ __forceinline__ int row(int j, int lane) const { return 16 * (instruction[j] & 1) + (lane >> 2); }
+    __device__ __forceinline__ int piece(int j, int lane) const { return 4 * (instruction[j] >> 1) + ((lane ^ row(j, lane) >> 2) & 3); }
+    __device__ __forceinline__ void init(const T *base, size_t ld, const Tokens &tokens, int token_step, int wave, int lane, int wide, bool reverse)
+    {
+        constexpr int in_group = 64 / (int)sizeof(T);
+        const int there = 2 * ((wide + in_group - 1) / in_group);
+        first = reinterpret_cast<const char *>(base + (size_t)tokens.first * ld);
+        step = (int64_t)token_step * (int64_t)(ld * sizeof(T));
+        which = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            int i = j * NW + wave;
+            i = i < kAll ? i : kAll - 1;
+            instruction[j] = i < there ? i : there - 1;
+            if (piece(j, lane) * (16 / (int)sizeof(T)) < wide) which |= 1u << j;
+            const int r = row(j, lane);
+            off[j] = (uint32_t)(reverse ? kChunk - 1 - r : r) * (uint32_t)step + 16 * piece(j, lane);
+        }
+    }
+    // tokens from .. from + count - 1 of `all`.  Rows past them take the last one's values, which are finite where those are
+    __device__ __forceinline__ void load(int from, int count, int all, bool reverse, uint32_t lds, int lane)
+    {
+        const char *base = first + step * (reverse ? all - from - count : from);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            uint32_t at = off[j];
+            if (count < kChunk) {
+                int r = row(j, lane);
+                r = r < count ? r : count - 1;
+                at = (uint32_t)(reverse ? count - 1 - r : r) * (uint32_t)step + 16 * piece(j, lane);
+            }
+            if (which >> j & 1) pipe::dma16(reinterpret_cast<const bf16_t *>(base + at), lds + 1024 * instruction[j]);
+        }
+    }
+};
+
+template <typename T, int KT, int NW, bool OUT, bool RING>
 __device__ __forceinline__ void decay_body(const DecayPass &p)
 {
     extern __shared__ __align__(16) char smem[];
-    using S = DecayShape<T, KT, NW>;
+    using S = DecayShape<T, KT, NW, OUT, RING>;
     using O = Ops<T>;
     using Frag = typename O::Frag;
-    constexpr int ld = S::ld, ldv = S::ldv, threads = 64 * NW;
-    T *lB = reinterpret_cast<T *>(smem), *lV = lB + kChunk * ld, *lA = lV + kChunk * ldv;
-    float *fade = reinterpret_cast<float *>(smem + S::lds(OUT) - (kChunk + 1) * 4 - 8);      // lambda^n, n = 0 .. 32
-    int *bad = reinterpret_cast<int *>(fade + kChunk + 1);
+    constexpr int threads = S::threads;
+    // lambda^n, n = 0 .. 32, and behind them lambda^(31 - n), n = 0 .. 31
+    float *fade = reinterpret_cast<float *>(smem + S::stages * S::stage), *rising = fade + kChunk + 4;
 
     const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
     int at = (int)blockIdx.x;
@@ -267,179 +381,264 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     const T *gV = (const T *)p.V + (size_t)(head / p.share_v) * p.dv + z * kDecayColumns;
     const int vleft = p.dv - z * kDecayColumns;                  // columns of v from this workgroup's first on
     const int col = 32 * wave;                                   // this wavefront's first among them
-    auto row_of = [&](int t) { return (size_t)(tokens.first + (int64_t)(p.reverse ? tokens.count - 1 - t : t) * (p.offset ? 1 : p.token_step)); };
+    const int token_step = p.offset ? 1 : p.token_step;
+    auto row_of = [&](int t) { return (size_t)(tokens.first + (int64_t)(p.reverse ? tokens.count - 1 - t : t) * token_step); };
+
+    // pieces behind a row's end are never loaded
+    if (RING && (p.da % S::in_group || p.da < 32 * KT || vleft < S::columns)) {
+        for (int i = (int)threadIdx.x; i < S::stages * S::stage / 16; i += threads) *reinterpret_cast<u32x4_t *>(smem + 16 * i) = u32x4_t{0u, 0u, 0u, 0u};
+        __syncthreads();
+    }
+    RingSource<T, S::groups, NW> ring_a, ring_b;
+    RingSource<T, S::groups_v, NW> ring_v;
+    constexpr int kLoads = (OUT ? 2 : 1) * RingSource<T, S::groups, NW>::kPer + RingSource<T, S::groups_v, NW>::kPer;       // a stage, of a wavefront
+    if (RING) {
+        if (OUT) ring_a.init(gA, p.lda, tokens, token_step, wave, lane, p.da, p.reverse);
+        ring_b.init(gB, p.ldb, tokens, token_step, wave, lane, p.da, p.reverse);
+        ring_v.init(gV, p.ldv, tokens, token_step, wave, lane, vleft < S::columns ? vleft : S::columns, p.reverse);
+    }
+    // or the next chunk on its way through registers: 8 elements of a row at a time
+    constexpr int kPieces8 = 4 * KT, kPer = (kPieces8 * kChunk + threads - 1) / threads, kPerV = kChunk * S::columns / 8 / threads;
+    Chunk<T> na[OUT && !RING ? kPer : 1], nb[RING ? 1 : kPer], nv[RING ? 1 : kPerV];
+    auto lds_of = [&](int stage) { return (uint32_t)(uintptr_t)STL_LDS(smem) + stage * S::stage; };
+    auto fetch = [&](int from, int stage) {
+        const int count = end - from < kChunk ? end - from : kChunk;
+        if constexpr (RING) {
+            const uint32_t to = lds_of(stage);
+            ring_b.load(from, count, tokens.count, p.reverse, to, lane);
+            ring_v.load(from, count, tokens.count, p.reverse, to + S::bytes, lane);
+            if (OUT) ring_a.load(from, count, tokens.count, p.reverse, to + S::bytes + S::bytes_v, lane);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int unit = i * threads + (int)threadIdx.x, r = unit / kPieces8, u = unit % kPieces8, left = r < count ? p.da - 8 * u : 0;
+                const size_t row = left > 0 ? row_of(from + r) : 0;
+                if (OUT) na[i].load(gA + row * p.lda + 8 * u, left);
+                nb[i].load(gB + row * p.ldb + 8 * u, left);
+            }
+#pragma unroll
+            for (int i = 0; i < kPerV; ++i) {
+                const int unit = i * threads + (int)threadIdx.x, r = unit / (S::columns / 8), u = unit % (S::columns / 8), left = r < count ? vleft - 8 * u : 0;
+                nv[i].load(gV + (left > 0 ? row_of(from + r) : 0) * p.ldv + 8 * u, left);
+            }
+        }
+    };
+    const int chunks = end > begin ? (end - begin + kChunk - 1) / kChunk : 0;
+#pragma unroll
+    for (int c = 0; c < (RING ? S::stages - 1 : 1); ++c)
+        if (c < chunks) fetch(begin + c * kChunk, c);
 
     double a = p.log_decay ? (double)p.log_decay[head] : 0.0;
     a = a < -1e5 ? -1e5 : a;
-    if (threadIdx.x <= kChunk) fade[threadIdx.x] = (float)power(a, (int)threadIdx.x);
-    if (threadIdx.x == 0) bad[0] = bad[1] = 0;
+    for (int i = (int)threadIdx.x; i <= kChunk; i += threads) {
+        const float f = (float)power(a, i);
+        fade[i] = f;
+        if (i < kChunk) rising[kChunk - 1 - i] = f;
+    }
     const double whole = power(a, kChunk);
 
-    // the state, element e of tile k: row 32 k + acc_row(e), column n
+    // the state, element e of tile k: row 32 k + dealt_row(e), column dealt(n)
     f32x16_t state[KT];
     const size_t each = (size_t)p.da * p.dv, state_at = ((size_t)b * p.heads + head) * each;
-    const float *init = p.init;
+    const float *init = OUT ? p.init : nullptr;
     float init_scale = p.init_scale;
     size_t init_at = state_at;
     int power_of_first = p.init_power;                           // of lambda, from the state to the next token
-    if (!OUT) init = nullptr;
     if (OUT && p.segments > 1 && (seg > 0 || (init && p.last))) {
         init = p.starts;
         init_at = (((size_t)b * p.heads + head) * p.segments + (seg > 0 ? seg - 1 : p.segments - 1)) * each;
         if (seg > 0) init_scale = 1.f, power_of_first = 1;
     }
-    auto at_state = [&](int k, int e) {
-        const int i = 32 * k + acc_row(e, h), j = z * kDecayColumns + col + n;
-        return i < p.da && j < p.dv ? (p.turned ? j * p.da + i : i * p.dv + j) : -1;
-    };
+    // (loads of elements that there are not go to the last ones and are dropped: without a branch all of them are in flight at once)
+    const int j = z * kDecayColumns + col + dealt(n), j_in = j < p.dv ? j : p.dv - 1;
+    if (init) {
+        if (p.turned) {
+            const float *row = init + init_at + (size_t)j_in * p.da;
+            if (p.da == 32 * KT) {
 #pragma unroll
-    for (int k = 0; k < KT; ++k)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int i = init ? at_state(k, e) : -1;
-            state[k][e] = i >= 0 ? init_scale * init[init_at + i] : 0.f;
-        }
-    bool any = init != nullptr;                                  // whether the state may differ from zero
-
-    // the next chunk on its way: 16 elements of a row of A and of B, 8 of V at a time
-    constexpr int kUnits = 2 * KT * kChunk, kPer = (kUnits + threads - 1) / threads, kPerV = kChunk * S::columns / 8 / threads;
-    Chunk<T> na[OUT ? kPer : 1][2], nb[kPer][2], nv[kPerV];
-    auto fetch = [&](int from, int count) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int unit = i * threads + (int)threadIdx.x, r = unit / (2 * KT), u = unit % (2 * KT), left = r < count ? p.da - 16 * u : 0;
-            const size_t row = left > 0 ? row_of(from + r) : 0;
-            if (OUT) {
-                na[i][0].load(gA + row * p.lda + 16 * u, left);
-                na[i][1].load(gA + row * p.lda + 16 * u + 8, left - 8);
-            }
-            nb[i][0].load(gB + row * p.ldb + 16 * u, left);
-            nb[i][1].load(gB + row * p.ldb + 16 * u + 8, left - 8);
-        }
-#pragma unroll
-        for (int i = 0; i < kPerV; ++i) {
-            const int unit = i * threads + (int)threadIdx.x, r = unit / (S::columns / 8), u = unit % (S::columns / 8), left = r < count ? vleft - 8 * u : 0;
-            nv[i].load(gV + (left > 0 ? row_of(from + r) : 0) * p.ldv + 8 * u, left);
-        }
-    };
-
-    int from = begin, count = end - from < kChunk ? end - from : kChunk, turn = 0, singles = 0;
-    if (count > 0) fetch(from, count);
-    while (count > 0) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int unit = i * threads + (int)threadIdx.x, r = unit / (2 * KT), u = unit % (2 * KT);
-            if (kUnits % threads && unit >= kUnits) break;
-            if (OUT) O::put(lA + r * ld + 16 * u, na[i][0], na[i][1]);
-            O::put(lB + r * ld + 16 * u, nb[i][0], nb[i][1]);
-        }
-        bool ok = true;
-#pragma unroll
-        for (int i = 0; i < kPerV; ++i) {
-            const int unit = i * threads + (int)threadIdx.x, r = unit / (S::columns / 8), u = unit % (S::columns / 8);
-            ok &= O::finite(nv[i]);
-            O::put_plain(lV + r * ldv + 8 * u, nv[i]);
-        }
-        if (!ok) bad[turn] = 1;
-        __syncthreads();
-        // A value that is no finite number must not reach earlier tokens, as it would with a zero of the masked P: a chunk with one goes token by token.
-        const bool again = bad[turn] && count > 1;
-        if (threadIdx.x == 0) bad[turn ^ 1] = 0;
-        turn ^= 1;
-        if (again) singles = from + count;
-        const int next = again ? from : from + count;
-        int next_count = end - next < kChunk ? end - next : kChunk;
-        if (next < singles) next_count = 1;
-        if (next_count > 0) fetch(next, next_count);
-        if (!again) {
-            if (OUT && p.O) {
-                Frag q[KT];
-#pragma unroll
-                for (int k = 0; k < KT; ++k) q[k] = O::along(lA + n * ld + 32 * k, h);
-                f32x16_t out = {};
-                if (any) {
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) {
-                        float x[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = state[k][e];
-                        Frag parts[O::kOutParts];
-                        O::template split<O::kOutParts>(x, parts);
-#pragma unroll
-                        for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q[k], out);
-                    }
-                    out *= fade[n + (power_of_first ? 1 : 0)];
-                }
-                f32x16_t prob = {};
-#pragma unroll
-                for (int k = 0; k < KT; ++k) prob = O::mma(O::along(lB + n * ld + 32 * k, h), q[k], prob);
-                float x[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int ago = n - acc_row(e, h);
-                    x[e] = ago >= 0 ? prob[e] * fade[ago >= 0 ? ago : 0] : 0.f;
-                }
-                Frag parts[O::kOutParts];
-                O::template split<O::kOutParts>(x, parts);
-                const Frag v = O::template across<false>(lV + col, ldv, lane);
-#pragma unroll
-                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(v, parts[m], out);
-                if (n < count) {
-                    const size_t row = row_of(from + n);
+                for (int k = 0; k < KT; ++k)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const int c = col + 8 * g + 4 * h, left = vleft - c;
-                        f32x4_t w = {out[4 * g], out[4 * g + 1], out[4 * g + 2], out[4 * g + 3]};
-                        w *= p.out_scale;
-                        const size_t to = row * p.ldo + (size_t)head * p.dv + z * kDecayColumns + c;
-                        if (p.out32) put4((float *)p.O + to, left, w);
-                        else put4((T *)p.O + to, left, w);
+                        const f32x4_t v = *reinterpret_cast<const f32x4_any_t *>(row + 32 * k + 16 * (g >> 1) + 8 * h + 4 * (g & 1));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) state[k][4 * g + e] = v[e];
                     }
-                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int i = 32 * k + dealt_row(e, h);
+                        state[k][e] = row[i < p.da ? i : p.da - 1];
+                    }
             }
-            // the state behind the chunk's last token (not needed behind the sequence's last one if nobody asks for it)
-            if (!OUT || next < end || (final && p.last)) {
-                const int steps = count - 1 + power_of_first;
-                const double fall = steps == kChunk ? whole : power(a, steps);
-                const float fall_hi = (float)fall, fall_lo = (float)(fall - (double)fall_hi);
-                if (any)
+        } else {
+            const float *column = init + init_at + j_in;
 #pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) state[k][e] = fmaf(state[k][e], fall_hi, state[k][e] * fall_lo);
-                const Frag v = O::template across<false>(lV + col, ldv, lane);
-                float x[16];
+            for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int left = count - 1 - acc_row(e, h);
-                    x[e] = left >= 0 ? O::get(v, e) * fade[left >= 0 ? left : 0] : 0.f;
+                    const int i = 32 * k + dealt_row(e, h);
+                    state[k][e] = column[(size_t)(i < p.da ? i : p.da - 1) * p.dv];
                 }
-                Frag parts[O::kStateParts];
-                O::template split<O::kStateParts>(x, parts);
-#pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    const Frag key = O::template across<true>(lB + 32 * k, ld, lane);
-#pragma unroll
-                    for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key, parts[m], state[k]);
-                }
-                any = true;
-            }
-            power_of_first = 1;
         }
-        from = next;
-        count = next_count;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) state[k][e] = 32 * k + dealt_row(e, h) < p.da && j < p.dv ? init_scale * state[k][e] : 0.f;
+    } else {
+#pragma unroll
+        for (int k = 0; k < KT; ++k) state[k] = f32x16_t{};
+    }
+    __syncthreads();
+
+    // what does not change from chunk to chunk
+    const typename O::Places places = O::places(lane);
+    float near[OUT ? 16 : 1];                                    // c lambda^(n - j) for this lane's j = acc_row(e)
+    if (OUT)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int ago = n - acc_row(e, h);
+            near[e] = p.out_scale * fade[ago >= 0 ? ago : 0];
+        }
+    float since = OUT ? p.out_scale * fade[n + power_of_first] : 0.f;
+    double owed = 0.0;                                           // what the roundings of lambda^32 to fp32 have left out: made good by the next ones
+
+    for (int c = 0; c < chunks; ++c) {
+        const int from = begin + c * kChunk, count = end - from < kChunk ? end - from : kChunk;
+        const int stage = RING ? c % S::stages : 0;
+        if constexpr (RING) {
+            // this chunk's loads are done (younger ones: those of the stages - 2 chunks behind it, and outputs), everybody's after the barrier, where everybody is
+            // also done with the chunk before, whose stage takes the next loads
+            if (c + S::stages - 1 <= chunks) wait_all_but<kLoads *(S::stages - 2)>();
+            else wait_all_but<0>();
+            pipe::block_barrier();
+            if (c + S::stages - 1 < chunks) fetch(from + (S::stages - 1) * kChunk, (c + S::stages - 1) % S::stages);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int unit = i * threads + (int)threadIdx.x, r = unit / kPieces8, u = unit % kPieces8;
+                if (kPieces8 * kChunk % threads && unit >= kPieces8 * kChunk) break;
+                put8(smem, r, u, nb[i]);
+                if (OUT) put8(smem + S::bytes + S::bytes_v, r, u, na[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kPerV; ++i) {
+                const int unit = i * threads + (int)threadIdx.x;
+                put8(smem + S::bytes, unit / (S::columns / 8), unit % (S::columns / 8), nv[i]);
+            }
+            __syncthreads();
+            if (c + 1 < chunks) fetch(from + kChunk, 0);
+        }
+        const char *lB = smem + stage * S::stage, *lV = lB + S::bytes, *lA = lV + S::bytes_v;
+
+        Frag values = O::across(lV, places, wave);
+        const bool unclean = __ballot(!O::finite(values)) != 0;
+        int bad = kChunk;                                        // the first token whose value in this lane's column is no finite number
+        if (unclean) {
+            bad = O::clean(values, h);
+            const int other = __shfl_xor(bad, 32);
+            bad = other < bad ? other : bad;
+        }
+        if (OUT && p.O) {
+            f32x16_t out = {}, prob = {};
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                const Frag q = O::along(lA, places, k);
+                prob = O::mma(O::along(lB, places, k), q, prob);
+                float x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = state[k][e];
+                Frag parts[O::kOutParts];
+                O::template split<O::kOutParts>(x, parts);
+#pragma unroll
+                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q, out);
+            }
+            out *= since;
+            int token = n;
+            asm volatile("" : "+v"(token));                      // (compared anew in every chunk: the 16 masks would take the scalar registers)
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = token >= acc_row(e, h) ? prob[e] * near[e] : 0.f;
+            Frag parts[O::kOutParts];
+            O::template split<O::kOutParts>(x, parts);
+#pragma unroll
+            for (int m = 0; m < O::kOutParts; ++m) out = O::mma(values, parts[m], out);
+            if (unclean)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int from_token = __shfl(bad, acc_row(e, h));
+                    if (n >= from_token) out[e] = __uint_as_float(0x7fc00000u);
+                }
+            if (n < count) {
+                const size_t to = row_of(from + n) * p.ldo + (size_t)head * p.dv + z * kDecayColumns;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int at_col = col + 16 * g + 8 * h;
+                    float w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = out[8 * g + e];
+                    if (vleft <= at_col) continue;
+                    if (p.out32) Chunk<float>::store((float *)p.O + to + at_col, vleft - at_col, w);
+                    else Chunk<T>::store((T *)p.O + to + at_col, vleft - at_col, w);
+                }
+            }
+        }
+        // the state behind the last token (not needed behind the sequence's last one if nobody asks for it)
+        if (!OUT || c + 1 < chunks || (final && p.last)) {
+            float x[16];
+            double exact;
+            if (count == kChunk && power_of_first) {
+                exact = whole + owed;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4_t left = *reinterpret_cast<const f32x4_t *>(rising + acc_row(4 * g, h));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[4 * g + e] = O::get(values, 4 * g + e) * left[e];
+                }
+            } else {
+                exact = power(a, count - 1 + power_of_first) + owed;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = acc_row(e, h);
+                    x[e] = row < count ? O::get(values, e) * fade[row < count ? count - 1 - row : 0] : 0.f;
+                }
+            }
+            const float fall = (float)exact;
+            owed = exact - (double)fall;
+#pragma unroll
+            for (int k = 0; k < KT; ++k) state[k] *= fall;
+            Frag parts[O::kStateParts];
+            O::template split<O::kStateParts>(x, parts);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                const Frag key = O::across(lB, places, k);
+#pragma unroll
+                for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key, parts[m], state[k]);
+            }
+            if (bad < kChunk)
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) state[k][e] = __uint_as_float(0x7fc00000u);
+        }
+        if (OUT && !power_of_first) since = p.out_scale * fade[n + 1];
+        power_of_first = 1;
     }
     if (OUT ? final && p.last : true) {
         float *to = OUT ? p.last + state_at : p.starts + (((size_t)b * p.heads + head) * p.segments + seg) * each;
         const float by = OUT ? (float)(p.last_scale * (tokens.count > 0 ? power(a, p.last_power) : 1.0)) : 1.f;
+        float *column = to + j * (p.turned ? p.da : 1);
+        const size_t step_i = p.turned ? 1 : p.dv;
+        if (j < p.dv)
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+            for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = at_state(k, e);
-                if (i >= 0) to[i] = by * state[k][e];
-            }
+                for (int e = 0; e < 16; ++e) {
+                    const int i = 32 * k + dealt_row(e, h);
+                    if (i < p.da) column[i * step_i] = by * state[k][e];
+                }
     }
 }
 
@@ -449,46 +648,54 @@ struct DecaySweeps {
     DecayPass pass[kMostSweeps];
     int count;
 };
-template <typename T, int KT, int NW, bool OUT>
+template <typename T, int KT, int NW, bool OUT, bool RING>
 __global__ __launch_bounds__(64 * NW, decay_waves(sizeof(T), KT)) void decay_kernel(const DecaySweeps s)
 {
-    decay_body<T, KT, NW, OUT>(s.pass[blockIdx.y]);
+    decay_body<T, KT, NW, OUT, RING>(s.pass[blockIdx.y]);
 }
 
-template <typename T, int KT, int NW>
-hipError_t launch_shape(const DecaySweeps &sw, bool outputs, hipStream_t s)
+template <typename T, int KT, int NW, bool OUT, bool RING>
+hipError_t launch_shape(const DecaySweeps &sw, hipStream_t s)
 {
-    using S = DecayShape<T, KT, NW>;
-    static std::atomic<uint64_t> granted[2];
+    using S = DecayShape<T, KT, NW, OUT, RING>;
+    static std::atomic<uint64_t> granted{0};
     const DecayPass &p = sw.pass[0];
-    const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns, bytes = S::lds(outputs);
-    const hipError_t e = allow_lds(outputs ? (const void *)decay_kernel<T, KT, NW, true> : (const void *)decay_kernel<T, KT, NW, false>, bytes, bytes, granted[outputs]);
+    const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
+    const hipError_t e = allow_lds((const void *)decay_kernel<T, KT, NW, OUT, RING>, S::lds, S::lds, granted);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((size_t)p.sequences * p.heads * p.segments * blocks), sw.count);
-    if (outputs) hipLaunchKernelGGL((decay_kernel<T, KT, NW, true>), grid, dim3(64 * NW), bytes, s, sw);
-    else hipLaunchKernelGGL((decay_kernel<T, KT, NW, false>), grid, dim3(64 * NW), bytes, s, sw);
+    hipLaunchKernelGGL((decay_kernel<T, KT, NW, OUT, RING>), grid, dim3(S::threads), S::lds, s, sw);
     return hipGetLastError();
 }
 
-inline int key_tiles(int da) { return da <= 32 ? 1 : da <= 64 ? 2 : da <= 128 ? 4 : 8; }
+inline int key_tiles(int da) { return da <= 128 ? (da + 31) / 32 : 8; }
 inline int value_waves(int dv) { return dv <= 64 ? 2 : 4; }
 
-// sweeps with the same key_tiles, value_waves, blocks of columns and segments
-template <typename T>
-hipError_t decay_sweeps(const DecaySweeps &sw, bool outputs, hipStream_t s)
+// sweeps with the same key_tiles, value_waves, blocks of columns, segments and kind of rows
+template <typename T, bool OUT>
+hipError_t decay_sweeps(const DecaySweeps &sw, hipStream_t s)
 {
-    auto wide = [&](auto nw) {
-        switch (key_tiles(sw.pass[0].da)) {
-        case 1: return launch_shape<T, 1, decltype(nw)::value>(sw, outputs, s);
-        case 2: return launch_shape<T, 2, decltype(nw)::value>(sw, outputs, s);
-        case 4: return launch_shape<T, 4, decltype(nw)::value>(sw, outputs, s);
-        }
-        return launch_shape<T, 8, decltype(nw)::value>(sw, outputs, s);
+    const int tiles = key_tiles(sw.pass[0].da);
+    constexpr bool wide = sizeof(T) == 2;                        // fp32: a ring of rows of 256 does not fit
+    if (!sw.pass[0].ring || (!wide && tiles == 8)) {
+        if (tiles == 8) return launch_shape<T, 8, 4, OUT, false>(sw, s);
+        return tiles > 2 ? launch_shape<T, 4, 4, OUT, false>(sw, s) : launch_shape<T, 2, 4, OUT, false>(sw, s);
+    }
+    auto ring = [&](auto nw) {
+        constexpr int NW = decltype(nw)::value;
+        if constexpr (wide)
+            if (tiles == 8) return launch_shape<T, 8, NW, OUT, true>(sw, s);
+        if (tiles == 4) return launch_shape<T, 4, NW, OUT, true>(sw, s);
+        if (tiles == 3) return launch_shape<T, 3, NW, OUT, true>(sw, s);
+        return tiles == 2 ? launch_shape<T, 2, NW, OUT, true>(sw, s) : launch_shape<T, 1, NW, OUT, true>(sw, s);
     };
-    return value_waves(sw.pass[0].dv) == 2 ? wide(std::integral_constant<int, 2>()) : wide(std::integral_constant<int, 4>());
+    return value_waves(sw.pass[0].dv) == 2 ? ring(std::integral_constant<int, 2>()) : ring(std::integral_constant<int, 4>());
 }
-hipError_t decay_sweeps_bf16(const DecaySweeps &sw, bool outputs, hipStream_t s);   // seq_decay_bf16.hip
-hipError_t decay_sweeps_f32(const DecaySweeps &sw, bool outputs, hipStream_t s);    // seq_decay_f32.hip
+// seq_decay_bf16.hip, seq_decay_f32.hip; seq_decay_states_*.hip: what segments add to the state
+hipError_t decay_sweeps_bf16(const DecaySweeps &sw, hipStream_t s);
+hipError_t decay_sweeps_f32(const DecaySweeps &sw, hipStream_t s);
+hipError_t decay_states_bf16(const DecaySweeps &sw, hipStream_t s);
+hipError_t decay_states_f32(const DecaySweeps &sw, hipStream_t s);
 
 }  // namespace seq
 }  // namespace stl

@@ -165,9 +165,20 @@ size_t starts_bytes(const DecayArgs &a)
 }
 size_t parts_bytes(const DecayArgs &a, int width) { return a.heads != a.kv_heads ? whole((size_t)a.rows * a.heads * width * 4) : 0; }
 
-hipError_t sweep(int dtype, const DecaySweeps &sw, bool outputs, hipStream_t s)
+// rows are whole 16-byte pieces at such addresses, and a chunk's bytes are counted by 31 bits
+bool whole_rows(int dtype, const DecayPass &p)
 {
-    return dtype ? decay_sweeps_bf16(sw, outputs, s) : decay_sweeps_f32(sw, outputs, s);
+    const size_t each = dtype ? 8 : 4, step = p.offset || p.token_step < 1 ? 1 : p.token_step, most = ((size_t)1 << 31) / (16 / each) / kChunk / step;
+    auto ok = [&](const void *at, size_t ld) { return !at || ((uintptr_t)at % 16 == 0 && ld % each == 0 && ld < most); };
+    return ok(p.A, p.lda) && ok(p.B, p.ldb) && ok(p.V, p.ldv) && p.da % each == 0 && p.dv % each == 0;
+}
+hipError_t sweep(int dtype, DecaySweeps &sw, bool outputs, hipStream_t s)
+{
+    bool ring = true;
+    for (int i = 0; i < sw.count; ++i) ring = ring && whole_rows(dtype, sw.pass[i]);
+    for (int i = 0; i < sw.count; ++i) sw.pass[i].ring = ring;
+    if (outputs) return dtype ? decay_sweeps_bf16(sw, s) : decay_sweeps_f32(sw, s);
+    return dtype ? decay_states_bf16(sw, s) : decay_states_f32(sw, s);
 }
 hipError_t join(const DecaySweeps &sw, hipStream_t s)
 {

@@ -4,7 +4,7 @@
 namespace stl {
 namespace seq {
 
-hipError_t decay_sweeps_bf16(const DecaySweeps &sw, bool outputs, hipStream_t s) { return decay_sweeps<bf16_t>(sw, outputs, s); }
+hipError_t decay_sweeps_bf16(const DecaySweeps &sw, hipStream_t s) { return decay_sweeps<bf16_t, true>(sw, s); }
 
 }  // namespace seq
 }  // namespace stl

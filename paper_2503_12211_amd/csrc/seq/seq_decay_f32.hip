@@ -4,7 +4,7 @@
 namespace stl {
 namespace seq {
 
-hipError_t decay_sweeps_f32(const DecaySweeps &sw, bool outputs, hipStream_t s) { return decay_sweeps<float>(sw, outputs, s); }
+hipError_t decay_sweeps_f32(const DecaySweeps &sw, hipStream_t s) { return decay_sweeps<float, true>(sw, s); }
 
 }  // namespace seq
 }  // namespace stl

@@ -9,6 +9,7 @@ inline unsigned long long __ballot(int v)
     emu::Exchange<int>::release();
     return r;
 }
+inline int __shfl(int v, int from) { return emu::from_lane(v, [&](int) { return from; }); }
 inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
 inline int atomicAdd(int *p, int v) { const int old = *p; *p += v; return old; }
 inline void sincospif(float x, float *s, float *c) { *s = (float)sin(M_PI * (double)x), *c = (float)cos(M_PI * (double)x); }
