@@ -79,6 +79,9 @@ __device__ __forceinline__ Tokens tokens_of(const DecayPass &p, int b)
     return Tokens{lo, hi - lo < p.length ? (int)(hi - lo) : p.length};
 }
 
+// a b, and zero where either is zero, whatever the other is (v_mul_legacy_f32, which has no builtin)
+__device__ float fmul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
 // lambda^n, a not below -100000 (where it is 0 for every n > 0)
 __device__ __forceinline__ double power(double a, int n) { return n == 0 ? 1.0 : exp(a * n); }
 
@@ -96,6 +99,13 @@ __device__ __forceinline__ int acc_row(int e, int h) { return 8 * (e >> 2) + 4 *
 // columns next to each other, 16 b + 8 h ..: eight outputs, or the contraction's order of a 16-byte piece (Ops::along).
 __device__ __forceinline__ int dealt(int n) { return (n & ~12) | (n & 4) << 1 | (n & 8) >> 1; }
 __device__ __forceinline__ int dealt_row(int e, int h) { return 16 * (e >> 3) + 8 * h + (e & 7); }
+
+// The tile of probabilities (tokens i of the queries by tokens j of the keys) is formed by a workgroup's wavefronts in quarters of 16 by 16: 0, 1 and 2 are (i, j) from
+// (0, 0), (16, 0) and (16, 16) on, and the fourth is all masked.  A lane has one i and four j from `j` on.
+struct Quarter {
+    int i, j;
+    __device__ __forceinline__ Quarter(int which, int lane) : i((which > 0 ? 16 : 0) + (lane & 15)), j((which > 1 ? 16 : 0) + 4 * (lane >> 4)) {}
+};
 
 template <typename T> struct Ops;
 
@@ -159,22 +169,43 @@ template <> struct Ops<bf16_t> {
             for (int n = 0; n < N; ++n) out[n].f[b] = __builtin_bit_cast(bf16x8_t, u32x4_t{w[n][0], w[n][1], w[n][2], w[n][3]});
         }
     }
+    // Probabilities, q_i . k_j times `near`: products by 16 x 16 x 32, two parts of four bf16 numbers a lane to where probabilities() finds them.
+    template <int KT>
+    static __device__ __forceinline__ void quarter(const char *queries, const char *keys, int which, int lane, const float *near, char *probs)
+    {
+        const Quarter at(which, lane);
+        const char *q = queries + piece_at(at.i, lane >> 4), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), lane >> 4);
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < KT; ++g)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8_t *>(k + kGroupBytes * g), *reinterpret_cast<const bf16x8_t *>(q + kGroupBytes * g), sum, 0, 0, 0);
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmul_legacy(near[e], sum[e]);                     // (zero times anything is zero: the masked ones)
+        char *to = probs + piece_at(at.i, 2 * (at.j >> 4) + (at.j >> 2 & 1)) + 8 * (at.j >> 3 & 1);
+#pragma unroll
+        for (int m = 0; m < kOutParts; ++m) {
+            const u32x2_t w = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+            *reinterpret_cast<u32x2_t *>(to + kGroupBytes * m) = w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] -= __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        }
+    }
+    // part m of them, contraction over j in the accumulators' order, column i = lane % 32
+    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int m) { return along(probs, at, m); }
     static __device__ __forceinline__ float get(const Frag &a, int e)
     {
         const u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[e >> 3]);
         return __uint_as_float(e & 1 ? w[e >> 1 & 3] & 0xffff0000u : w[e >> 1 & 3] << 16);
     }
-    // (an exponent of ones carries into its sign bit)
+    // zero times them by the matrix cores: two instructions in the place of two dozen
     static __device__ __forceinline__ bool finite(const Frag &a)
     {
-        uint32_t carry = 0;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[b]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) carry |= (w[i] & 0x7f807f80u) + 0x00800080u;
-        }
-        return !(carry & 0x80008000u);
+        const bf16x8_t none = __builtin_bit_cast(bf16x8_t, u32x4_t{0u, 0u, 0u, 0u});
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, a.f[0], sum, 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, a.f[1], sum, 0, 0, 0);
+        return sum[0] == 0.f;
     }
     // zeros in the place of what is no finite number; the first row of such an element, 32 if there is none
     static __device__ __forceinline__ int clean(Frag &a, int h)
@@ -209,12 +240,12 @@ template <> struct Ops<float> {
         return c;
     }
     struct Places {
-        int row[2], across[2];
+        int row[2], across[2], prob[2];
     };
     static __device__ __forceinline__ Places places(int lane)
     {
         const int n = lane & 31, h = lane >> 5, column = dealt(n), c = column >> 2;
-        return Places{{piece_at(n, 2 * h), piece_at(n, 2 * h + 1)}, {piece_at(4 * h, c) + 4 * (column & 3), piece_at(8 + 4 * h, c) + 4 * (column & 3)}};
+        return Places{{piece_at(n, 2 * h), piece_at(n, 2 * h + 1)}, {piece_at(4 * h, c) + 4 * (column & 3), piece_at(8 + 4 * h, c) + 4 * (column & 3)}, {piece_at(n, h), piece_at(n, 2 + h)}};
     }
     static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k)
     {
@@ -240,7 +271,36 @@ template <> struct Ops<float> {
 #pragma unroll
         for (int e = 0; e < 16; ++e) out[0].f[e] = x[e];
     }
+    // (products by 16 x 16 x 4, the contraction in the order 4 (lane / 16) + e for e = 0 .. 3)
+    template <int KT>
+    static __device__ __forceinline__ void quarter(const char *queries, const char *keys, int which, int lane, const float *near, char *probs)
+    {
+        const Quarter at(which, lane);
+        const char *q = queries + piece_at(at.i, lane >> 4), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), lane >> 4);
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < 2 * KT; ++g) {
+            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(k + kGroupBytes * g), v = *reinterpret_cast<const f32x4_t *>(q + kGroupBytes * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(u[e], v[e], sum, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = fmul_legacy(near[e], sum[e]);
+        *reinterpret_cast<f32x4_t *>(probs + piece_at(at.i, at.j >> 2)) = sum;
+    }
+    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int m)
+    {
+        Frag r;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(probs + at.prob[g & 1] + kGroupBytes * (g >> 1));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.f[4 * g + e] = v[e];
+        }
+        return r;
+    }
     static __device__ __forceinline__ float get(const Frag &a, int e) { return a.f[e]; }
+    // (an exponent of ones carries into its sign bit)
     static __device__ __forceinline__ bool finite(const Frag &a)
     {
         uint32_t carry = 0;
@@ -270,9 +330,10 @@ struct DecayShape {
     static constexpr int bytes = kGroupBytes * groups, bytes_v = kGroupBytes * groups_v, stage = (OUT ? 2 : 1) * bytes + bytes_v;
     // 256 registers and half of the LDS, so that two workgroups share a CU, where a wavefront's state fits
     static constexpr int waves = sizeof(T) == 2 && KT <= 4 ? 2 : 1;
-    static constexpr int room = 160 * 1024 / waves - 512, fit = room / stage;
+    static constexpr int tables = 512, tile = OUT ? 2 * kGroupBytes : 0;
+    static constexpr int room = 160 * 1024 / waves - tables - tile, fit = room / stage;
     static constexpr int stages = RING ? fit < 4 ? fit : 4 : 1;
-    static constexpr int lds = stages * stage + 4 * (2 * kChunk + 4);
+    static constexpr int lds = stages * stage + tables + tile;
     static_assert(stages >= (RING ? 2 : 1), "a ring has two stages at least");
 };
 constexpr int decay_waves(size_t element, int KT) { return element == 2 && KT <= 4 ? 2 : 1; }
@@ -298,6 +359,9 @@ __device__ __forceinline__ void wait_all_but()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
+// all LDS reads and writes are done
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // eight elements of row r, from element 8 u on, to where they lie in LDS
 __device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<bf16_t> &c) { *reinterpret_cast<u32x4_t *>(rows + piece_at(r, u)) = c.v; }
 __device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<float> &c)
@@ -308,46 +372,63 @@ __device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<float
 
 // One operand's share of a stage that a wavefront loads by LDS-DMA.  Instruction i brings 64 pieces, one a lane: four of each of 16 rows.  Where the row
 // ends before the groups do, or instructions are no multiple of the wavefronts, some of them bring the same again: all wavefronts issue as many.
+__device__ __forceinline__ void dma16_at(const char *base, uint32_t off, uint32_t lds_wave_base)
+{
+    const uint32_t l = __builtin_amdgcn_readfirstlane(lds_wave_base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");
+}
+
 template <typename T, int GROUPS, int NW>
 struct RingSource {
-    static constexpr int kAll = 2 * GROUPS, kPer = (kAll + NW - 1) / NW;
-    const char *first;                       // of the sequence's first row
-    int64_t step;                            // bytes from token to token
-    uint32_t which, off[kPer];               // a bit for each instruction: whether this lane's piece lies within the row; its place from the chunk's lowest row on
-    int instruction[kPer];
-    __device__ __forceinline__ int row(int j, int lane) const { return 16 * (instruction[j] & 1) + (lane >> 2); }
-    __device__ __forceinline__ int piece(int j, int lane) const { return 4 * (instruction[j] >> 1) + ((lane ^ row(j, lane) >> 2) & 3); }
-    __device__ __forceinline__ void init(const T *base, size_t ld, const Tokens &tokens, int token_step, int wave, int lane, int wide, bool reverse)
+    static constexpr int kAll = 2 * GROUPS, kPer = (kAll + NW - 1) / NW, kInGroup = 64 / (int)sizeof(T);
+    const char *next;                        // where the next chunk's lowest row is, if it is whole
+    int64_t advance;                         // bytes from there to the one behind it
+    uint32_t off[kPer];                      // of a lane's pieces, from the chunk's lowest row on
+    uint32_t which, step;                    // a bit for each instruction: whether this lane's piece lies within the row; bytes from token to token
+    int there, whole;                        // instructions that bring something; whether rows end where a group does
+    __device__ __forceinline__ int instruction(int j, int wave) const
     {
-        constexpr int in_group = 64 / (int)sizeof(T);
-        const int there = 2 * ((wide + in_group - 1) / in_group);
-        first = reinterpret_cast<const char *>(base + (size_t)tokens.first * ld);
-        step = (int64_t)token_step * (int64_t)(ld * sizeof(T));
+        const int i = j * NW + wave;
+        return i < there ? i : there - 1;
+    }
+    static __device__ __forceinline__ int row(int i, int lane) { return 16 * (i & 1) + (lane >> 2); }
+    static __device__ __forceinline__ int piece(int i, int lane) { return 4 * (i >> 1) + ((lane ^ row(i, lane) >> 2) & 3); }
+    __device__ __forceinline__ void init(const T *base, size_t ld, const Tokens &tokens, int token_step, int from, int wave, int lane, int wide, bool reverse)
+    {
+        there = 2 * ((wide + kInGroup - 1) / kInGroup), whole = wide % kInGroup == 0;
+        const int64_t bytes = (int64_t)token_step * (int64_t)(ld * sizeof(T));
+        step = (uint32_t)bytes;
+        next = reinterpret_cast<const char *>(base + (size_t)tokens.first * ld) + bytes * (reverse ? tokens.count - from - kChunk : from);
+        advance = (reverse ? -kChunk : kChunk) * bytes;
         which = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            int i = j * NW + wave;
-            i = i < kAll ? i : kAll - 1;
-            instruction[j] = i < there ? i : there - 1;
-            if (piece(j, lane) * (16 / (int)sizeof(T)) < wide) which |= 1u << j;
-            const int r = row(j, lane);
-            off[j] = (uint32_t)(reverse ? kChunk - 1 - r : r) * (uint32_t)step + 16 * piece(j, lane);
+            const int i = instruction(j, wave), r = row(i, lane), c = piece(i, lane);
+            if (c * (16 / (int)sizeof(T)) < wide) which |= 1u << j;
+            off[j] = (uint32_t)(reverse ? kChunk - 1 - r : r) * step + 16 * c;
         }
     }
-    // tokens from .. from + count - 1 of `all`.  Rows past them take the last one's values, which are finite where those are
-    __device__ __forceinline__ void load(int from, int count, int all, bool reverse, uint32_t lds, int lane)
+    // the next `count` tokens.  Rows past them take the last one's values, which are finite where those are
+    __device__ __forceinline__ void load(int count, bool reverse, uint32_t lds, int wave, int lane)
     {
-        const char *base = first + step * (reverse ? all - from - count : from);
+        if (there == kAll && kAll % NW == 0 && count == kChunk && whole) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            uint32_t at = off[j];
-            if (count < kChunk) {
-                int r = row(j, lane);
-                r = r < count ? r : count - 1;
-                at = (uint32_t)(reverse ? count - 1 - r : r) * (uint32_t)step + 16 * piece(j, lane);
+            for (int j = 0; j < kPer; ++j) dma16_at(next, off[j], lds + 1024 * (j * NW + wave));
+        } else {
+            const char *base = next + (reverse ? (int64_t)(kChunk - count) * step : 0);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int i = instruction(j, wave);
+                uint32_t at = off[j];
+                if (count < kChunk) {
+                    int r = row(i, lane);
+                    r = r < count ? r : count - 1;
+                    at = (uint32_t)(reverse ? count - 1 - r : r) * step + 16 * piece(i, lane);
+                }
+                if (which >> j & 1) dma16_at(base, at, lds + 1024 * i);
             }
-            if (which >> j & 1) pipe::dma16(reinterpret_cast<const bf16_t *>(base + at), lds + 1024 * instruction[j]);
         }
+        next += advance;
     }
 };
 
@@ -359,8 +440,9 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     using O = Ops<T>;
     using Frag = typename O::Frag;
     constexpr int threads = S::threads;
-    // lambda^n, n = 0 .. 32, and behind them lambda^(31 - n), n = 0 .. 31
-    float *fade = reinterpret_cast<float *>(smem + S::stages * S::stage), *rising = fade + kChunk + 4;
+    // lambda^n, n = 0 .. 32; lambda^(31 - n), n = 0 .. 31; the same for the last chunk's tokens, and zeros behind them
+    float *fade = reinterpret_cast<float *>(smem + S::stages * S::stage), *rising = fade + kChunk + 4, *ending = rising + kChunk;
+    char *probs = smem + S::stages * S::stage + S::tables;       // the tile of probabilities of a chunk
 
     const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
     int at = (int)blockIdx.x;
@@ -382,8 +464,12 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     const int vleft = p.dv - z * kDecayColumns;                  // columns of v from this workgroup's first on
     const int col = 32 * wave;                                   // this wavefront's first among them
     const int token_step = p.offset ? 1 : p.token_step;
-    auto row_of = [&](int t) { return (size_t)(tokens.first + (int64_t)(p.reverse ? tokens.count - 1 - t : t) * token_step); };
+    const bool reverse = p.reverse;
+    auto row_of = [&](int t) { return (size_t)(tokens.first + (int64_t)(reverse ? tokens.count - 1 - t : t) * token_step); };
 
+    // the quarter of the tile whose tokens j are behind all of its i
+    if (OUT)
+        for (int i = (int)threadIdx.x; i < S::tile / 16; i += threads) *reinterpret_cast<u32x4_t *>(probs + 16 * i) = u32x4_t{0u, 0u, 0u, 0u};
     // pieces behind a row's end are never loaded
     if (RING && (p.da % S::in_group || p.da < 32 * KT || vleft < S::columns)) {
         for (int i = (int)threadIdx.x; i < S::stages * S::stage / 16; i += threads) *reinterpret_cast<u32x4_t *>(smem + 16 * i) = u32x4_t{0u, 0u, 0u, 0u};
@@ -393,9 +479,9 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     RingSource<T, S::groups_v, NW> ring_v;
     constexpr int kLoads = (OUT ? 2 : 1) * RingSource<T, S::groups, NW>::kPer + RingSource<T, S::groups_v, NW>::kPer;       // a stage, of a wavefront
     if (RING) {
-        if (OUT) ring_a.init(gA, p.lda, tokens, token_step, wave, lane, p.da, p.reverse);
-        ring_b.init(gB, p.ldb, tokens, token_step, wave, lane, p.da, p.reverse);
-        ring_v.init(gV, p.ldv, tokens, token_step, wave, lane, vleft < S::columns ? vleft : S::columns, p.reverse);
+        if (OUT) ring_a.init(gA, p.lda, tokens, token_step, begin, wave, lane, p.da, reverse);
+        ring_b.init(gB, p.ldb, tokens, token_step, begin, wave, lane, p.da, reverse);
+        ring_v.init(gV, p.ldv, tokens, token_step, begin, wave, lane, vleft < S::columns ? vleft : S::columns, reverse);
     }
     // or the next chunk on its way through registers: 8 elements of a row at a time
     constexpr int kPieces8 = 4 * KT, kPer = (kPieces8 * kChunk + threads - 1) / threads, kPerV = kChunk * S::columns / 8 / threads;
@@ -405,9 +491,9 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
         const int count = end - from < kChunk ? end - from : kChunk;
         if constexpr (RING) {
             const uint32_t to = lds_of(stage);
-            ring_b.load(from, count, tokens.count, p.reverse, to, lane);
-            ring_v.load(from, count, tokens.count, p.reverse, to + S::bytes, lane);
-            if (OUT) ring_a.load(from, count, tokens.count, p.reverse, to + S::bytes + S::bytes_v, lane);
+            ring_b.load(count, reverse, to, wave, lane);
+            ring_v.load(count, reverse, to + S::bytes, wave, lane);
+            if (OUT) ring_a.load(count, reverse, to + S::bytes + S::bytes_v, wave, lane);
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -433,9 +519,15 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     for (int i = (int)threadIdx.x; i <= kChunk; i += threads) {
         const float f = (float)power(a, i);
         fade[i] = f;
-        if (i < kChunk) rising[kChunk - 1 - i] = f;
+        if (i < kChunk) {
+            const int last = (end - begin - 1) % kChunk - i;      // (no chunk: nobody reads it)
+            rising[kChunk - 1 - i] = f;
+            if (last >= 0) ending[last] = f;
+            else ending[kChunk + last] = 0.f;
+        }
     }
-    const double whole = power(a, kChunk);
+    const double through = power(a, kChunk);
+    const float whole = (float)through, whole_rest = (float)(through - (double)whole);
 
     // the state, element e of tile k: row 32 k + dealt_row(e), column dealt(n)
     f32x16_t state[KT];
@@ -494,26 +586,40 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
 
     // what does not change from chunk to chunk
     const typename O::Places places = O::places(lane);
-    float near[OUT ? 16 : 1];                                    // c lambda^(n - j) for this lane's j = acc_row(e)
-    if (OUT)
+    constexpr int kQuarters = OUT ? (3 + NW - 1) / NW : 0;       // of the probabilities' tile, of a wavefront at most
+    float near[kQuarters ? kQuarters : 1][4];                    // c lambda^(i - j) for this lane's i and j, 0 for j > i
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int ago = n - acc_row(e, h);
-            near[e] = p.out_scale * fade[ago >= 0 ? ago : 0];
+    for (int i = 0; i < kQuarters; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const Quarter at(wave + i * NW, lane);
+            const int ago = at.i - at.j - e;
+            near[i][e] = ago >= 0 ? p.out_scale * fade[ago >= 0 ? ago : 0] : 0.f;
         }
     float since = OUT ? p.out_scale * fade[n + power_of_first] : 0.f;
-    double owed = 0.0;                                           // what the roundings of lambda^32 to fp32 have left out: made good by the next ones
+    // where this lane's outputs of the next chunk go, and how many of its columns there are (none: no outputs); bit 0: in fp32, bit 1: not all columns of the wavefront
+    char *out_at = nullptr;
+    int64_t out_advance = 0;
+    const int out_left = OUT && p.O ? vleft - col - 8 * h : 0;
+    int out_kind = (p.out32 ? 1 : 0) | (p.O && vleft - col >= 32 ? 0 : 2);
+    asm volatile("" : "+s"(out_kind));                           // (kept, and not read from the arguments again in each chunk)
+    if (OUT && p.O) {
+        const int64_t size = p.out32 ? 4 : (int64_t)sizeof(T), row = tokens.first + (int64_t)(reverse ? tokens.count - 1 - begin - n : begin + n) * token_step;
+        out_at = (char *)p.O + (row * (int64_t)p.ldo + (int64_t)head * p.dv + z * kDecayColumns + col + 8 * h) * size;
+        out_advance = (reverse ? -kChunk : kChunk) * token_step * (int64_t)p.ldo * size;
+    }
+    float owed = 0.f;                                            // what the roundings of lambda^32 to fp32 have left out: made good by the next ones
 
+    int stage = 0;
     for (int c = 0; c < chunks; ++c) {
         const int from = begin + c * kChunk, count = end - from < kChunk ? end - from : kChunk;
-        const int stage = RING ? c % S::stages : 0;
         if constexpr (RING) {
             // this chunk's loads are done (younger ones: those of the stages - 2 chunks behind it, and outputs), everybody's after the barrier, where everybody is
             // also done with the chunk before, whose stage takes the next loads
             if (c + S::stages - 1 <= chunks) wait_all_but<kLoads *(S::stages - 2)>();
             else wait_all_but<0>();
             pipe::block_barrier();
-            if (c + S::stages - 1 < chunks) fetch(from + (S::stages - 1) * kChunk, (c + S::stages - 1) % S::stages);
+            if (c + S::stages - 1 < chunks) fetch(from + (S::stages - 1) * kChunk, stage > 0 ? stage - 1 : S::stages - 1);
         } else {
             __syncthreads();
 #pragma unroll
@@ -541,90 +647,92 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
             const int other = __shfl_xor(bad, 32);
             bad = other < bad ? other : bad;
         }
-        if (OUT && p.O) {
-            f32x16_t out = {}, prob = {};
+        float high = whole, low = whole_rest;
+        if (count < kChunk || !power_of_first) {
+            const double exact = power(a, count - 1 + power_of_first);
+            high = (float)exact, low = (float)(exact - (double)high);
+        }
+        low += owed;
+        const float fall = high + low;
+        owed = low - (fall - high);
+        const float *weight = count < kChunk ? ending : rising;
+        // all products of a chunk in one piece of straight code, so that vector and matrix instructions overlap (the state behind the last token too, which
+        // is not always needed)
+        f32x16_t out = {};
+        Frag key[2];                                             // (operands are read a step ahead; the fences keep the compiler from reading further)
+        if (OUT) {
+            Frag q[2];
+            q[0] = O::along(lA, places, 0);
+#pragma unroll
+            for (int i = 0; i < kQuarters; ++i)
+                if (wave + i * NW < 3) O::template quarter<KT>(lA, lB, wave + i * NW, lane, near[i], probs);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                const Frag q = O::along(lA, places, k);
-                prob = O::mma(O::along(lB, places, k), q, prob);
+                if (k + 1 < KT) q[k + 1 & 1] = O::along(lA, places, k + 1);
+                else key[0] = O::across(lB, places, 0);
+                __builtin_amdgcn_sched_barrier(0);
                 float x[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[e] = state[k][e];
                 Frag parts[O::kOutParts];
                 O::template split<O::kOutParts>(x, parts);
 #pragma unroll
-                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q, out);
+                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q[k & 1], out);
             }
             out *= since;
-            int token = n;
-            asm volatile("" : "+v"(token));                      // (compared anew in every chunk: the 16 masks would take the scalar registers)
-            float x[16];
+            wait_lds();
+            pipe::block_barrier();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = token >= acc_row(e, h) ? prob[e] * near[e] : 0.f;
-            Frag parts[O::kOutParts];
-            O::template split<O::kOutParts>(x, parts);
-#pragma unroll
-            for (int m = 0; m < O::kOutParts; ++m) out = O::mma(values, parts[m], out);
-            if (unclean)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int from_token = __shfl(bad, acc_row(e, h));
-                    if (n >= from_token) out[e] = __uint_as_float(0x7fc00000u);
-                }
-            if (n < count) {
-                const size_t to = row_of(from + n) * p.ldo + (size_t)head * p.dv + z * kDecayColumns;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int at_col = col + 16 * g + 8 * h;
-                    float w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = out[8 * g + e];
-                    if (vleft <= at_col) continue;
-                    if (p.out32) Chunk<float>::store((float *)p.O + to + at_col, vleft - at_col, w);
-                    else Chunk<T>::store((T *)p.O + to + at_col, vleft - at_col, w);
-                }
-            }
+            for (int m = 0; m < O::kOutParts; ++m) out = O::mma(values, O::probabilities(probs, places, m), out);
+        } else {
+            key[0] = O::across(lB, places, 0);
         }
-        // the state behind the last token (not needed behind the sequence's last one if nobody asks for it)
-        if (!OUT || c + 1 < chunks || (final && p.last)) {
-            float x[16];
-            double exact;
-            if (count == kChunk && power_of_first) {
-                exact = whole + owed;
+        float x[16];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4_t left = *reinterpret_cast<const f32x4_t *>(rising + acc_row(4 * g, h));
+        for (int g = 0; g < 4; ++g) {
+            const f32x4_t left = *reinterpret_cast<const f32x4_t *>(weight + acc_row(4 * g, h));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * g + e] = O::get(values, 4 * g + e) * left[e];
-                }
-            } else {
-                exact = power(a, count - 1 + power_of_first) + owed;
+            for (int e = 0; e < 4; ++e) x[4 * g + e] = O::get(values, 4 * g + e) * left[e];
+        }
+        Frag parts[O::kStateParts];
+        O::template split<O::kStateParts>(x, parts);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int row = acc_row(e, h);
-                    x[e] = row < count ? O::get(values, e) * fade[row < count ? count - 1 - row : 0] : 0.f;
-                }
-            }
-            const float fall = (float)exact;
-            owed = exact - (double)fall;
+        for (int k = 0; k < KT; ++k) {
+            if (k + 1 < KT) key[k + 1 & 1] = O::across(lB, places, k + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            state[k] *= fall;
 #pragma unroll
-            for (int k = 0; k < KT; ++k) state[k] *= fall;
-            Frag parts[O::kStateParts];
-            O::template split<O::kStateParts>(x, parts);
+            for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key[k & 1], parts[m], state[k]);
+        }
+        if (unclean) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k) {
-                const Frag key = O::across(lB, places, k);
-#pragma unroll
-                for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key, parts[m], state[k]);
-            }
+            for (int e = 0; e < 16; ++e)
+                if (n >= __shfl(bad, acc_row(e, h))) out[e] = __uint_as_float(0x7fc00000u);
             if (bad < kChunk)
 #pragma unroll
                 for (int k = 0; k < KT; ++k)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) state[k][e] = __uint_as_float(0x7fc00000u);
         }
+        if (OUT && n < count) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int left = out_left - 16 * g;
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = out[8 * g + e];
+                if (out_kind == 0) Chunk<T>::store((T *)out_at + 16 * g, 8, w);
+                else if (out_kind == 1) Chunk<float>::store((float *)out_at + 16 * g, 8, w);
+                else if (left <= 0) continue;
+                else if (out_kind == 2) Chunk<T>::store((T *)out_at + 16 * g, left, w);
+                else Chunk<float>::store((float *)out_at + 16 * g, left, w);
+            }
+        }
+        if (OUT) out_at += out_advance;
         if (OUT && !power_of_first) since = p.out_scale * fade[n + 1];
         power_of_first = 1;
+        if (RING) stage = stage + 1 < S::stages ? stage + 1 : 0;
     }
     if (OUT ? final && p.last : true) {
         float *to = OUT ? p.last + state_at : p.starts + (((size_t)b * p.heads + head) * p.segments + seg) * each;

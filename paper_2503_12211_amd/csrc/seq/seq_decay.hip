@@ -109,21 +109,22 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecaySweeps s)
     }
 }
 
-// Gradients of key heads that several heads share: out[row][g] = sum over the heads of group g of part[row][head], rows of the sequences alone.
+// Gradients of key heads that several heads share: out[row][g] = sum over the heads of group g of part[row][head], rows of the sequences alone.  A workgroup takes
+// whole rows.
 template <typename T>
 __global__ __launch_bounds__(256) void decay_share_kernel(const DecayPass p, const float *part, T *out, size_t ld, int width, int share)
 {
-    const int b = (int)blockIdx.y;
-    const Tokens tokens = tokens_of(p, b);
-    const int groups = p.heads / share, wide = groups * width;
-    const int64_t all = (int64_t)tokens.count * wide;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int t = (int)(i / wide), c = (int)(i % wide), g = c / width, e = c % width;
+    const Tokens tokens = tokens_of(p, (int)blockIdx.y);
+    const int wide = p.heads / share * width;
+    for (int t = (int)blockIdx.x; t < tokens.count; t += (int)gridDim.x) {
         const size_t row = (size_t)(tokens.first + (int64_t)t * (p.offset ? 1 : p.token_step));
-        const float *from = part + (row * p.heads + (size_t)g * share) * width + e;
-        float v = 0.f;
-        for (int k = 0; k < share; ++k) v += from[(size_t)k * width];
-        Elem<T>::st(out + row * ld + c, v);
+        for (int c = (int)threadIdx.x; c < wide; c += 256) {
+            const int g = c / width, e = c - g * width;
+            const float *from = part + (row * p.heads + (size_t)g * share) * width + e;
+            float v = 0.f;
+            for (int k = 0; k < share; ++k) v += from[(size_t)k * width];
+            Elem<T>::st(out + row * ld + c, v);
+        }
     }
 }
 
@@ -131,36 +132,35 @@ namespace {
 
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 
-// Segments of a sequence: as many as give every CU two workgroups, of 128 tokens at least; at most so many, and how they come out.
-int most_segments(const DecayArgs &a)
+// Segments of a sequence.  They cost a sweep more, so only where a head has four of them at least for 512 workgroups in all (for each of the gradients' three sweeps 256),
+// and of 128 tokens (fp32, whose products take three times as long: 64).  13 sequences of up to 777 tokens x 16 heads: 46 us in one piece, 76 us in two; 4 x 2048
+// tokens x 16 heads, gradients: 156 us in four pieces, 168 us in two, 182 us in eight.
+int most_segments(int dtype, const DecayArgs &a, bool grads)
 {
-    const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns);
-    int64_t n = 512 / groups;
-    if (n > a.length / 128) n = a.length / 128;
-    return n < 1 ? 1 : (int)n;
+    const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns), most = (grads ? 256 : 512) / groups, fit = a.length / (dtype ? 128 : 64);
+    return most < 4 || fit < 4 ? 1 : (int)(most < fit ? most : fit);
 }
-void cut(const DecayArgs &a, int *segments, int *tokens)
+void cut(const DecayArgs &a, int64_t n, int *segments, int *tokens)
 {
-    const int64_t n = most_segments(a);
     *tokens = n > 1 ? (int)((a.length + n * kChunk - 1) / (n * kChunk)) * kChunk : a.length > 0 ? a.length : 1;
     *segments = a.length > 0 ? (a.length + *tokens - 1) / *tokens : 1;
 }
 
-DecayPass common(const DecayArgs &a)
+DecayPass common(int dtype, const DecayArgs &a, bool grads)
 {
     DecayPass p{};
     p.rows = a.rows, p.sequences = a.sequences, p.length = a.length, p.heads = a.heads, p.seq_step = a.seq_step, p.token_step = a.token_step;
     p.log_decay = a.log_decay, p.offset = a.offset;
     p.share_a = p.share_b = p.share_v = 1;
     p.out_scale = a.scale, p.init_scale = p.last_scale = 1.f;
-    cut(a, &p.segments, &p.seg_tokens);
+    cut(a, most_segments(dtype, a, grads), &p.segments, &p.seg_tokens);
     return p;
 }
 
-size_t starts_bytes(const DecayArgs &a)
+size_t starts_bytes(int dtype, const DecayArgs &a, bool grads)
 {
     // (never less for a longer sequence)
-    const int segments = most_segments(a);
+    const int segments = most_segments(dtype, a, grads);
     return segments > 1 ? whole((size_t)a.sequences * a.heads * segments * a.dk * a.dv * 4) : 0;
 }
 size_t parts_bytes(const DecayArgs &a, int width) { return a.heads != a.kv_heads ? whole((size_t)a.rows * a.heads * width * 4) : 0; }
@@ -189,9 +189,7 @@ hipError_t join(const DecaySweeps &sw, hipStream_t s)
 
 hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const float *part, void *out, size_t ld, int width, hipStream_t s)
 {
-    const int64_t elements = (int64_t)a.length * a.kv_heads * width;
-    int64_t blocks = (elements + 2047) / 2048;
-    if (blocks > 4096) blocks = 4096;
+    const int blocks = a.length < 4096 ? a.length : 4096;
     for (int b = 0; b < a.sequences; b += 65535) {
         DecayPass q = p;
         const dim3 grid((unsigned)blocks, a.sequences - b < 65535 ? a.sequences - b : 65535);
@@ -210,8 +208,8 @@ hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const fl
 
 size_t decay_workspace_bytes(int dtype, const DecayArgs &a, bool grads)
 {
-    if (!grads) return a.length > kFewTokens ? starts_bytes(a) : 0;
-    return 2 * starts_bytes(a) + parts_bytes(a, a.dk) + parts_bytes(a, a.dv);
+    if (!grads) return a.length > kFewTokens ? starts_bytes(dtype, a, false) : 0;
+    return 2 * starts_bytes(dtype, a, true) + parts_bytes(a, a.dk) + parts_bytes(a, a.dv);
 }
 
 hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *state_out, void *ws, hipStream_t s)
@@ -225,7 +223,7 @@ hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *s
     DecaySweeps sw{};
     DecayPass &p = sw.pass[0];
     sw.count = 1;
-    p = common(a);
+    p = common(dtype, a, false);
     p.da = a.dk, p.dv = a.dv;
     p.A = a.Q, p.lda = a.ld_q;
     p.B = a.K, p.ldb = a.ld_k, p.V = a.V, p.ldv = a.ld_v;
@@ -251,16 +249,16 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
         at += n;
         return (float *)was;
     };
-    float *starts[2] = {take(starts_bytes(a)), take(starts_bytes(a))}, *part_k = take(parts_bytes(a, a.dk)), *part_v = take(parts_bytes(a, a.dv));
+    float *starts[2] = {take(starts_bytes(dtype, a, true)), take(starts_bytes(dtype, a, true))}, *part_k = take(parts_bytes(a, a.dk)), *part_v = take(parts_bytes(a, a.dv));
     // the state forward in time, from K and V
-    DecayPass f = common(a);
+    DecayPass f = common(dtype, a, true);
     f.da = a.dk, f.dv = a.dv;
     f.B = a.K, f.ldb = a.ld_k, f.V = a.V, f.ldv = a.ld_v;
     f.share_b = f.share_v = share;
     f.init = a.state, f.init_power = 1;
     f.starts = starts[0];
     // its gradient backward in time, from Q and dO, held without the factor c, which its outputs have
-    DecayPass r = common(a);
+    DecayPass r = common(dtype, a, true);
     r.reverse = true;
     r.da = a.dk, r.dv = a.dv;
     r.B = a.Q, r.ldb = a.ld_q, r.V = g.dO, r.ldv = a.ld_o;

@@ -6,9 +6,9 @@
 // The gradient is formed without floating-point atomics, so that its bits do not depend on the order in which workgroups run.  Three launches:
 //  1. the rows sorted by id.  The vocabulary is cut into ranges, a workgroup each.  It reads all tokens twice: once to count its ids (and, for the place at
 //     which its rows begin, the tokens of lower ids), once to write its rows down, in order.  A wavefront walks over consecutive tokens and has counts of
-//     its own, so the order of rows with one id is that of the batch.  The same workgroup writes zeros for its ids that do not occur: most of dW.
+//     its own, so the order of rows with one id is that of the batch.  Ids that do not occur are noted as bits.
 //  2. sums over the sorted rows, cut into segments of equal length whatever the ids: a common token's many rows are shared by many workgroups.
-//     A run of one id that lies in one segment is finished there; parts of others go to the workspace in fp32.
+//     A run of one id that lies in one segment is finished there; parts of others go to the workspace in fp32.  Zeros for absent ids beside them.
 //  3. parts of a run that several segments share are added up in order.
 #include "seq_kernels.h"
 #include "../lm/lm_device.h"
@@ -51,9 +51,8 @@ __device__ __forceinline__ void each_id(int rel, int width, F f)
     }
 }
 
-template <typename T>
 __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs a, const EmbedPlan plan, const int64_t *token, int *order, int *ids, int *total,
-                                                                 T *dW, int zeros)
+                                                                 uint64_t *absent)
 {
     __shared__ int count[kWaves][kMostWidth];
     __shared__ int below[kWaves];
@@ -107,10 +106,9 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs
         }
     }
     if ((int)blockIdx.x == plan.ranges - 1 && threadIdx.x == 64 * kWaves - 1) *total = base + upto;
-    // ids that do not occur, for the zeros below: kept as a bit a lane before the places move on
-    __shared__ uint64_t absent[kWaves];
+    // ids that do not occur, a bit each, for the zeros that the sums' launch writes
     const uint64_t gone = __ballot(id < width && mine == 0);
-    if (lane == 0) absent[wave] = gone;
+    if (lane == 0) absent[(size_t)blockIdx.x * kWaves + wave] = gone;
     __syncthreads();
     for (int step = begin; step < end; step += 8) {
         int got[8];
@@ -133,20 +131,32 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs
             });
         }
     }
-    if (!zeros) return;
-    for (int i = wave; i < width; i += kWaves) {
-        if (!(absent[i >> 6] >> (i & 63) & 1)) continue;
-        T *out = dW + (size_t)(first + i) * a.d;
-        const float none[8] = {};
+}
+
+// zeros for the absent ones of 64 ids
+template <typename T>
+__device__ __forceinline__ void write_zeros(const EmbedArgs &a, const EmbedPlan &plan, int some, const uint64_t *absent, T *dW)
+{
+    const int each = (plan.width + 63) / 64, range = some / each, word = some % each, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const uint64_t bits = absent[(size_t)range * kWaves + word];
+    const float none[8] = {};
+    for (int i = wave; i < 64; i += 4) {
+        if (!(bits >> i & 1)) continue;
+        T *out = dW + ((size_t)range * plan.width + 64 * word + i) * a.d;
         for (int at = 8 * lane; at < a.d; at += 512) Chunk<T>::store(out + at, a.d - at, none);
     }
 }
 
 // A chunk of 8 columns a thread.  parts[2 s]: the sum of segment s's rows that go on from segment s - 1; parts[2 s + 1]: of those that go on behind it.
+// Workgroups behind the segments': zeros for up to 64 ids that do not occur, most of dW, while the sums wait for their rows.
 template <typename T>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const EmbedPlan plan, const int *order, const int *ids, const int *total, const T *dX, T *dW,
-                                                        float *parts, int accumulate)
+__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const EmbedPlan plan, const int *order, const int *ids, const int *total,
+                                                        const uint64_t *absent, const T *dX, T *dW, float *parts, int accumulate)
 {
+    if ((int)blockIdx.x >= plan.segments) {
+        if (blockIdx.y == 0) write_zeros(a, plan, (int)blockIdx.x - plan.segments, absent, dW);
+        return;
+    }
     const int seg = (int)blockIdx.x, col = 8 * ((int)blockIdx.y * 256 + (int)threadIdx.x), left = a.d - col;
     const int count = *total;
     const int64_t first = (int64_t)seg * plan.length;
@@ -187,12 +197,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
     }
 }
 
-// The run that begins in this segment and goes on behind it, if there is one
+// The run that begins in this segment and goes on behind it, if there is one: a wavefront has 512 columns, the four of a workgroup take the run's segments eight at a
+// time in turn, and their sums are added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedArgs a, const EmbedPlan plan, const int *ids, const int *total, const float *parts, T *dW,
                                                          int accumulate)
 {
-    const int seg = (int)blockIdx.x, col = 8 * ((int)blockIdx.y * 256 + (int)threadIdx.x), left = a.d - col;
+    constexpr int kStep = 8;
+    __shared__ __align__(16) float sums[3][512];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const int seg = (int)blockIdx.x, col = 512 * (int)blockIdx.y + 8 * lane, left = a.d - col;
     const int count = *total;
     const int64_t next = ((int64_t)seg + 1) * plan.length;
     if (next >= count) return;
@@ -200,18 +214,35 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedArgs a, cons
     if (ids[next - 1] != id) return;
     // (a run that covers all of this segment and begins before it is another segment's)
     if (ids[begin] == id && begin > 0 && ids[begin - 1] == id) return;
-    if (left <= 0) return;
-    Chunk<float> c;
-    c.load(parts + (2 * (size_t)seg + 1) * a.d + col, left);
-    float sum[8];
+    float sum[8] = {};
+    if (wave == 0) {
+        Chunk<float> c;
+        c.load(parts + (2 * (size_t)seg + 1) * a.d + col, left);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = c.get(e);
-    // segments whose first row is the run's
-    for (int64_t at = next; at < count && ids[at] == id; at += plan.length) {
-        c.load(parts + 2 * (size_t)(at / plan.length) * a.d + col, left);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += c.get(e);
+        for (int e = 0; e < 8; ++e) sum[e] = c.get(e);
     }
+    // segments whose first row is the run's
+    for (int64_t at = (int64_t)seg + 1 + kStep * wave; at * plan.length < count && ids[at * plan.length] == id; at += 4 * kStep) {
+        Chunk<float> c[kStep];
+        bool more[kStep];
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+            const int64_t row = (at + u) * plan.length;
+            more[u] = row < count && ids[row < count ? row : 0] == id;
+            c[u].load(parts + 2 * (size_t)(row < count ? at + u : at) * a.d + col, left);
+        }
+#pragma unroll
+        for (int u = 0; u < kStep; ++u)
+            if (more[u])
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += c[u].get(e);
+    }
+    if (wave > 0) Chunk<float>::store(&sums[wave - 1][8 * lane], 8, sum);
+    __syncthreads();
+    if (wave > 0 || left <= 0) return;
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += sums[w][8 * lane + e];
     T *out = dW + (size_t)id * a.d + col;
     Chunk<T> old;
     old.fill(0.f);
@@ -233,7 +264,8 @@ EmbedPlan embed_plan(const EmbedArgs &a)
     p.segments = (a.rows + p.length - 1) / p.length;
     auto whole = [](size_t n) { return (n + 255) / 256 * 256; };
     p.ids_at = 256 + whole((size_t)a.rows * 4);
-    p.parts_at = p.ids_at + whole((size_t)a.rows * 4);
+    p.absent_at = p.ids_at + whole((size_t)a.rows * 4);
+    p.parts_at = p.absent_at + whole((size_t)p.ranges * kWaves * 8);
     p.bytes = p.parts_at + whole((size_t)p.segments * 2 * a.d * 4);
     return p;
 }
@@ -254,15 +286,17 @@ hipError_t backward(const EmbedArgs &a, const int64_t *token, const void *dX, vo
 {
     const EmbedPlan p = embed_plan(a);
     int *total = (int *)ws, *order = (int *)((char *)ws + 256), *ids = (int *)((char *)ws + p.ids_at);
+    uint64_t *absent = (uint64_t *)((char *)ws + p.absent_at);
     float *parts = (float *)((char *)ws + p.parts_at);
-    hipLaunchKernelGGL(embed_sort_kernel<T>, dim3(p.ranges), dim3(64 * kWaves), 0, s, a, p, token, order, ids, total, (T *)dW, accumulate ? 0 : 1);
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(p.ranges), dim3(64 * kWaves), 0, s, a, p, token, order, ids, total, absent);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 grid(p.segments, (a.d + 2047) / 2048);
-    hipLaunchKernelGGL(embed_sum_kernel<T>, grid, dim3(256), 0, s, a, p, order, ids, total, (const T *)dX, (T *)dW, parts, accumulate);
+    const int zeros = accumulate ? 0 : p.ranges * ((p.width + 63) / 64);
+    hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(p.segments + zeros, (a.d + 2047) / 2048), dim3(256), 0, s, a, p, order, ids, total, absent, (const T *)dX, (T *)dW, parts,
+                       accumulate);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embed_join_kernel<T>, grid, dim3(256), 0, s, a, p, ids, total, parts, (T *)dW, accumulate);
+    hipLaunchKernelGGL(embed_join_kernel<T>, dim3(p.segments, (a.d + 511) / 512), dim3(256), 0, s, a, p, ids, total, parts, (T *)dW, accumulate);
     return hipGetLastError();
 }
 

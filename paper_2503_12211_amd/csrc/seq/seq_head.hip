@@ -37,22 +37,42 @@ struct Unit {
         return ADJ || 16 * u >= rot ? 16 * u + 8 : rot / 2 + 8 * u;
     }
     static __device__ __forceinline__ int first_chunk(int u, int rot) { return ADJ || 16 * u >= rot ? 16 * u : 8 * u; }
-    static __device__ __forceinline__ void load(const T *p, int u, int d, int rot, float *x)
+    // as loaded, and as numbers
+    struct Raw {
+        Chunk<T> c[VEC ? 2 : 1];
+        float f[VEC ? 1 : 16];
+    };
+    static __device__ __forceinline__ void load(const T *p, int u, int d, int rot, Raw &r)
     {
         if constexpr (VEC) {
-            Chunk<T> a, b;
-            a.load(p + first_chunk(u, rot), 8);
-            b.load(p + second_chunk(u, rot), 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = a.get(e), x[8 + e] = b.get(e);
+            r.c[0].load(p + first_chunk(u, rot), 8);
+            r.c[1].load(p + second_chunk(u, rot), 8);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const Pair at = pair_of<ADJ>(8 * u + k, rot);
-                x[ADJ ? 2 * k : k] = at.a < d ? Elem<T>::ld(p + at.a) : 0.f;
-                x[ADJ ? 2 * k + 1 : 8 + k] = at.b < d ? Elem<T>::ld(p + at.b) : 0.f;
+                r.f[ADJ ? 2 * k : k] = at.a < d ? Elem<T>::ld(p + at.a) : 0.f;
+                r.f[ADJ ? 2 * k + 1 : 8 + k] = at.b < d ? Elem<T>::ld(p + at.b) : 0.f;
             }
         }
+    }
+    static __device__ __forceinline__ void clear(Raw &r)
+    {
+        r.c[0].fill(0.f);
+        if constexpr (VEC) r.c[1].fill(0.f);
+#pragma unroll
+        for (int e = 0; e < (VEC ? 1 : 16); ++e) r.f[e] = 0.f;
+    }
+    static __device__ __forceinline__ void numbers(const Raw &r, float *x)
+    {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = VEC ? r.c[e >> 3 & (VEC ? 1 : 0)].get(e & 7) : r.f[VEC ? 0 : e];
+    }
+    static __device__ __forceinline__ void load(const T *p, int u, int d, int rot, float *x)
+    {
+        Raw r;
+        load(p, u, d, rot, r);
+        numbers(r, x);
     }
     static __device__ __forceinline__ void store(T *p, int u, int d, int rot, const float *x)
     {
@@ -100,15 +120,18 @@ struct HeadPlan {
     int grid;
     bool vec;
 };
-HeadPlan head_plan(const HeadArgs &a)
+HeadPlan head_plan(const HeadArgs &a, bool back)
 {
     HeadPlan p;
     p.units = ((a.d + 1) / 2 + 7) / 8;
     p.lanes = 1;
     while (p.lanes < p.units) p.lanes *= 2;
     p.together = a.rows >= 8192 ? 8 : a.rows >= 4096 ? 4 : a.rows >= 2048 ? 2 : 1;
-    const int turns = (a.rows + p.together - 1) / p.together;
-    p.grid = turns < 1024 ? turns : 1024;
+    // (backward, few heads: twice as many where the heads of these rows leave workgroups with idle lanes and there are 512 of them all the same.  64 x 197 rows of 2 x 12
+    // heads of 64: 48 us with 8 rows, a quarter of the lanes idle)
+    if (back && p.together * a.heads[0] % (256 / p.lanes) && a.rows / (2 * p.together) >= 512) p.together *= 2;
+    const int turns = (a.rows + p.together - 1) / p.together, each = (turns + 1023) / 1024;
+    p.grid = (turns + each - 1) / each;                          // every workgroup as many turns, but for the last
     p.vec = a.d % 16 == 0 && a.rot % 16 == 0;
     return p;
 }
@@ -197,31 +220,46 @@ __global__ __launch_bounds__(256) void head_back_kernel(const HeadArgs a, const 
     const int lanes = plan.lanes, pairs = 8 * plan.units;
     const int u = (int)threadIdx.x % lanes, group = (int)threadIdx.x / lanes, groups = 256 / lanes;
     const bool mine = u < plan.units;
-    float dw[2][16] = {};
+    float dw[2][16] = {}, w[2][16];
     const float inv = 1.f / (float)a.d;
+    bool wanted[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        const int heads = a.heads[side];
-        float w[16];
+        wanted[side] = a.heads[side] > 0 && (g.d_in[side] || g.dw[side]);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = 1.f;
-        if (a.w[side] && mine) U::load((const T *)a.w[side], u, a.d, a.rot, w);
-        T *out = (T *)g.d_in[side];
-        if (heads == 0 || (!out && !g.dw[side])) continue;
-        for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
-            const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
-            __syncthreads();
-            angles(a, pairs, (int)row, rows, table);
-            __syncthreads();
+        for (int e = 0; e < 16; ++e) w[side][e] = 1.f;
+        if (a.w[side] && mine) U::load((const T *)a.w[side], u, a.d, a.rot, w[side]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
+        const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
+        // a group of lanes has one head at a time; the next one's elements are on their way meanwhile, the first ones' while angles are formed
+        typename U::Raw x_next, t_next;
+        auto fetch = [&](int side, int from) __attribute__((always_inline)) {
+            const int heads = a.heads[side], i = from + group, r = i / heads, h = i - r * heads;
+            U::clear(x_next), U::clear(t_next);
+            if (!mine || i >= rows * heads) return;
+            if (a.norm) U::load((const T *)a.in[side] + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, x_next);
+            if (g.up[side]) U::load((const T *)g.up[side] + (row + r) * a.ld_out[side] + (size_t)h * a.d, u, a.d, a.rot, t_next);
+        };
+        if (wanted[0]) fetch(0, 0);
+        else if (wanted[1]) fetch(1, 0);
+        __syncthreads();
+        angles(a, pairs, (int)row, rows, table);
+        __syncthreads();
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            if (!wanted[side]) continue;
+            const int heads = a.heads[side];
+            T *out = (T *)g.d_in[side];
             for (int from = 0; from < rows * heads; from += groups) {
                 const int i = from + group, r = i / heads, h = i - r * heads;
                 const bool live = mine && i < rows * heads;
-                float x[16] = {}, t[16] = {};
-                if (live) {
-                    if (a.norm) U::load((const T *)a.in[side] + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, x);
-                    if (g.up[side]) U::load((const T *)g.up[side] + (row + r) * a.ld_out[side] + (size_t)h * a.d, u, a.d, a.rot, t);
-                    U::turn(table + r * pairs + 8 * u, a.rot / 2 - 8 * u, t, -1.f);
-                }
+                float x[16], t[16];
+                U::numbers(x_next, x);
+                U::numbers(t_next, t);
+                if (from + groups < rows * heads) fetch(side, from + groups);
+                else if (side == 0 && wanted[1]) fetch(1, 0);
+                if (live) U::turn(table + r * pairs + 8 * u, a.rot / 2 - 8 * u, t, -1.f);
                 if (a.norm) {
                     float squares = 0.f, dot = 0.f;
 #pragma unroll
@@ -231,7 +269,7 @@ __global__ __launch_bounds__(256) void head_back_kernel(const HeadArgs a, const 
                     for (int e = 0; e < 16; ++e) {
                         x[e] *= by;
                         dw[side][e] = fmaf(t[e], x[e], dw[side][e]);
-                        t[e] *= w[e];
+                        t[e] *= w[side][e];
                         dot = fmaf(t[e], x[e], dot);
                     }
                     dot = group_sum(dot, lanes) * inv;
@@ -272,27 +310,30 @@ __global__ __launch_bounds__(256) void head_back_kernel(const HeadArgs a, const 
     }
 }
 
-// dw (+)= sum over `n` workgroups' parts; 16 columns, 16 threads a column that take every sixteenth part
+// dw (+)= sum over `n` workgroups' parts; four columns, 64 threads a column that take every 64th part
 __global__ __launch_bounds__(256) void head_sum_kernel(const float *parts, int n, int d, float *dw_q, float *dw_k, int accumulate)
 {
-    __shared__ float red[16][17];
-    const int x = (int)threadIdx.x & 15, y = (int)threadIdx.x >> 4, c = (int)blockIdx.x * 16 + x, side = (int)blockIdx.y;
+    __shared__ float red[4][4];
+    const int x = (int)threadIdx.x & 3, y = (int)threadIdx.x >> 2, c = (int)blockIdx.x * 4 + x, side = (int)blockIdx.y;
     float *dw = side ? dw_k : dw_q;
     if (!dw) return;
     float v = 0.f;
-    if (c < d)
-        for (int b = y; b < n; b += 16) v += parts[((size_t)b * 2 + side) * d + c];
-    red[y][x] = v;
+    if (c < d) {
+#pragma unroll 4
+        for (int b = y; b < n; b += 64) v += parts[((size_t)b * 2 + side) * d + c];
+    }
+    for (int m = 4; m < 64; m *= 2) v += __shfl_xor(v, m);
+    if ((y & 15) == 0) red[y >> 4][x] = v;
     __syncthreads();
     if (y == 0 && c < d) {
-        for (int k = 1; k < 16; ++k) v += red[k][x];
+        v = (red[0][x] + red[1][x]) + (red[2][x] + red[3][x]);
         dw[c] = accumulate ? dw[c] + v : v;
     }
 }
 
 size_t head_workspace_bytes(const HeadArgs &a)
 {
-    return ((size_t)head_plan(a).grid * 2 * a.d * 4 + 255) / 256 * 256;
+    return ((size_t)head_plan(a, true).grid * 2 * a.d * 4 + 255) / 256 * 256;
 }
 
 template <typename T, bool ADJ, bool VEC>
@@ -308,7 +349,7 @@ hipError_t backward(const HeadArgs &a, const HeadGrads &g, const HeadPlan &p, fl
     hipLaunchKernelGGL((head_back_kernel<T, ADJ, VEC>), dim3(p.grid), dim3(256), table > sums ? table : sums, s, a, g, p, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!g.dw[0] && !g.dw[1])) return e;
-    hipLaunchKernelGGL(head_sum_kernel, dim3((a.d + 15) / 16, 2), dim3(256), 0, s, parts, p.grid, a.d, g.dw[0], g.dw[1], g.accumulate);
+    hipLaunchKernelGGL(head_sum_kernel, dim3((a.d + 3) / 4, 2), dim3(256), 0, s, parts, p.grid, a.d, g.dw[0], g.dw[1], g.accumulate);
     return hipGetLastError();
 }
 
@@ -325,13 +366,13 @@ hipError_t by_kind(int dtype, bool adjacent, bool vec, F f)
 
 hipError_t launch_head_forward(int dtype, const HeadArgs &a, void *const out[2], hipStream_t s)
 {
-    const HeadPlan p = head_plan(a);
+    const HeadPlan p = head_plan(a, false);
     return by_kind(dtype, a.adjacent, p.vec, [&](auto t, auto adj, auto vec) { return forward<decltype(t), adj.value, vec.value>(a, p, out, s); });
 }
 
 hipError_t launch_head_backward(int dtype, const HeadArgs &a, const HeadGrads &g, void *ws, hipStream_t s)
 {
-    const HeadPlan p = head_plan(a);
+    const HeadPlan p = head_plan(a, true);
     return by_kind(dtype, a.adjacent, p.vec, [&](auto t, auto adj, auto vec) { return backward<decltype(t), adj.value, vec.value>(a, g, p, (float *)ws, s); });
 }
 

@@ -30,5 +30,19 @@ inline emu_f32x16 emu_mfma32(emu_bf16x8 a, emu_bf16x8 b, emu_f32x16 c)
     emu::Exchange<Both>::release();
     return c;
 }
+inline float fmul_legacy(float a, float b) { return a == 0.0f || b == 0.0f ? 0.0f : a * b; }
+// the same of 16 x 16 by 4 contractions: a lane holds row (column) lane % 16, k = lane / 16, and of D column lane % 16, rows 4 (lane / 16) + e
+inline emu_f32x4 emu_mfma16f(float a, float b, emu_f32x4 c)
+{
+    struct Two { float a, b; };
+    Two *s = emu::Exchange<Two>::all(Two{a, b});
+    const int l = emu::lane();
+    for (int e = 0; e < 4; ++e)
+        for (int k = 0; k < 4; ++k) c[e] += s[4 * (l / 16) + e + 16 * k].a * s[l % 16 + 16 * k].b;
+    emu::Exchange<Two>::release();
+    return c;
+}
+#undef __builtin_amdgcn_mfma_f32_16x16x4f32
+#define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) emu_mfma16f(a, b, c)
 #undef __builtin_amdgcn_mfma_f32_32x32x16_bf16
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) emu_mfma32(a, b, c)

@@ -19,7 +19,9 @@ def driver(tmp_path_factory):
     (work / "csrc").mkdir()
     (work / "include").mkdir()
     shutil.copy(ROOT / "include" / "stl.h", work / "include" / "stl.h")
-    meet = {'asm volatile("s_barrier" ::: "memory");': "emu_barrier();", 'asm volatile("" ::: "memory");': "emu_wave();"}
+    meet = {'asm volatile("s_barrier" ::: "memory");': "emu_barrier();", 'asm volatile("" ::: "memory");': "emu_wave();",
+            'asm volatile("" : "+s"(out_kind));': ";", '__device__ float fmul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");': "",
+            r'asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");': "cpu_touch16(base + off, l);"}
     srcs = []
     for f in sorted(CSRC.glob("**/*.hip")) + sorted(CSRC.glob("**/*.h")):
         to = work / "csrc" / f.relative_to(CSRC)
