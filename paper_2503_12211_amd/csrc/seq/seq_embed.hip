@@ -58,7 +58,8 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs
     __shared__ int below[kWaves];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int first = (int)blockIdx.x * plan.width, width = a.vocab - first < plan.width ? a.vocab - first : plan.width;
-    for (int i = (int)threadIdx.x; i < kWaves * kMostWidth; i += 64 * kWaves) (&count[0][0])[i] = 0;
+    for (int w = 0; w < kWaves; ++w)
+        if ((int)threadIdx.x < width) count[w][threadIdx.x] = 0;
     __syncthreads();
     // tokens of this wavefront: whole steps of 64
     const int steps = (a.rows + 63) / 64, per = (steps + kWaves - 1) / kWaves;
@@ -139,11 +140,17 @@ __device__ __forceinline__ void write_zeros(const EmbedArgs &a, const EmbedPlan 
 {
     const int each = (plan.width + 63) / 64, range = some / each, word = some % each, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const uint64_t bits = absent[(size_t)range * kWaves + word];
-    const float none[8] = {};
+    constexpr int per16 = 16 / (int)sizeof(T);
     for (int i = wave; i < 64; i += 4) {
         if (!(bits >> i & 1)) continue;
         T *out = dW + ((size_t)range * plan.width + 64 * word + i) * a.d;
-        for (int at = 8 * lane; at < a.d; at += 512) Chunk<T>::store(out + at, a.d - at, none);
+        // whole 16-byte pieces at such addresses, lane by lane, and single elements in front of them and behind
+        int head = (int)(-(uintptr_t)out % 16 / sizeof(T));
+        head = head < a.d ? head : a.d;
+        const int pieces = (a.d - head) / per16, rest = a.d - head - pieces * per16;
+        for (int c = lane; c < pieces; c += 64) *reinterpret_cast<u32x4_t *>(out + head + c * per16) = u32x4_t{0u, 0u, 0u, 0u};
+        if (lane < head) Elem<T>::st(out + lane, 0.f);
+        if (lane < rest) Elem<T>::st(out + a.d - 1 - lane, 0.f);
     }
 }
 
@@ -207,13 +214,23 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedArgs a, cons
     __shared__ __align__(16) float sums[3][512];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const int seg = (int)blockIdx.x, col = 512 * (int)blockIdx.y + 8 * lane, left = a.d - col;
-    const int count = *total;
-    const int64_t next = ((int64_t)seg + 1) * plan.length;
-    if (next >= count) return;
-    const int begin = seg * plan.length, id = ids[next];
-    if (ids[next - 1] != id) return;
+    // (all at once: what lies behind the last sorted row is no id, and not used)
+    const int64_t begin = (int64_t)seg * plan.length, next = begin + plan.length, mine = next + (int64_t)plan.length * lane;
+    const int count = *total, id = ids[next], before = ids[next - 1], first = ids[begin], earlier = begin > 0 ? ids[begin - 1] : -1;
+    int there = ids[mine < a.rows ? mine : begin];
+    if (next >= count || before != id) return;
     // (a run that covers all of this segment and begins before it is another segment's)
-    if (ids[begin] == id && begin > 0 && ids[begin - 1] == id) return;
+    if (first == id && earlier == id) return;
+    // segments whose first row is the run's, 64 at a time
+    int more = 0;
+    for (;;) {
+        const int64_t row = next + (int64_t)plan.length * (more + lane);
+        const uint64_t other = ~__ballot(row < count && there == id);
+        more += other ? (int)__builtin_ctzll(other) : 64;
+        if (other) break;
+        const int64_t ahead = next + (int64_t)plan.length * (more + lane);
+        there = ids[ahead < a.rows ? ahead : begin];
+    }
     float sum[8] = {};
     if (wave == 0) {
         Chunk<float> c;
@@ -221,19 +238,13 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedArgs a, cons
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] = c.get(e);
     }
-    // segments whose first row is the run's
-    for (int64_t at = (int64_t)seg + 1 + kStep * wave; at * plan.length < count && ids[at * plan.length] == id; at += 4 * kStep) {
+    for (int at = kStep * wave; at < more; at += 4 * kStep) {
         Chunk<float> c[kStep];
-        bool more[kStep];
 #pragma unroll
-        for (int u = 0; u < kStep; ++u) {
-            const int64_t row = (at + u) * plan.length;
-            more[u] = row < count && ids[row < count ? row : 0] == id;
-            c[u].load(parts + 2 * (size_t)(row < count ? at + u : at) * a.d + col, left);
-        }
+        for (int u = 0; u < kStep; ++u) c[u].load(parts + 2 * (size_t)(seg + 1 + (at + u < more ? at + u : at)) * a.d + col, left);
 #pragma unroll
         for (int u = 0; u < kStep; ++u)
-            if (more[u])
+            if (at + u < more)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += c[u].get(e);
     }
@@ -296,7 +307,8 @@ hipError_t backward(const EmbedArgs &a, const int64_t *token, const void *dX, vo
                        accumulate);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embed_join_kernel<T>, dim3(p.segments, (a.d + 511) / 512), dim3(256), 0, s, a, p, ids, total, parts, (T *)dW, accumulate);
+    if (p.segments == 1) return hipSuccess;
+    hipLaunchKernelGGL(embed_join_kernel<T>, dim3(p.segments - 1, (a.d + 511) / 512), dim3(256), 0, s, a, p, ids, total, parts, (T *)dW, accumulate);
     return hipGetLastError();
 }
 

@@ -91,9 +91,10 @@ struct Unit {
     // the first n pairs turned by the angles whose cosines and sines lie at `cs`, or back
     static __device__ __forceinline__ void turn(const f32x2_t *cs, int n, float *x, float back)
     {
+        if (VEC && n <= 0) return;                               // (whole units are turned, or none of it)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            if (k >= n) break;
+            if (!VEC && k >= n) break;
             float &a = x[ADJ ? 2 * k : k], &b = x[ADJ ? 2 * k + 1 : 8 + k];
             const f32x2_t t = cs[k];
             const float s = back * t[1], was = a;
@@ -210,103 +211,106 @@ __global__ __launch_bounds__(256) void head_kernel(const HeadArgs a, const HeadP
     }
 }
 
-// parts: for each workgroup the sums for the two weights, d each
+// parts: for each workgroup the sums for the two weights, d each.  Queries first, then keys: with one side's weights and sums at a time four workgroups share a CU
 template <typename T, bool ADJ, bool VEC>
-__global__ __launch_bounds__(256) void head_back_kernel(const HeadArgs a, const HeadGrads g, const HeadPlan plan, float *parts)
+__global__ __launch_bounds__(256, VEC && sizeof(T) == 2 ? 4 : 2) void head_back_kernel(const HeadArgs a, const HeadGrads g, const HeadPlan plan, float *parts)
 {
     extern __shared__ __align__(16) char smem[];
     f32x2_t *table = reinterpret_cast<f32x2_t *>(smem);
     using U = Unit<T, ADJ, VEC>;
     const int lanes = plan.lanes, pairs = 8 * plan.units;
     const int u = (int)threadIdx.x % lanes, group = (int)threadIdx.x / lanes, groups = 256 / lanes;
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const bool mine = u < plan.units;
-    float dw[2][16] = {}, w[2][16];
     const float inv = 1.f / (float)a.d;
-    bool wanted[2];
-#pragma unroll
+    float *red = reinterpret_cast<float *>(smem + plan.together * 64 * plan.units);          // [wavefront][unit][16]
+    float *weights = red + 4 * 16 * plan.units;                  // [unit][16]: in registers they would cost a workgroup of four on a CU
+    bool formed = false;                                         // whether the angles of all of this workgroup's rows are in LDS
+#pragma unroll 1
     for (int side = 0; side < 2; ++side) {
-        wanted[side] = a.heads[side] > 0 && (g.d_in[side] || g.dw[side]);
+        const int heads = a.heads[side];
+        const T *in = (const T *)a.in[side], *up = (const T *)g.up[side];
+        T *out = (T *)g.d_in[side];
+        if (heads == 0 || (!out && !g.dw[side])) continue;
+        const size_t ld_in = a.ld_in[side], ld_up = a.ld_out[side];
+        float dw[16] = {};
+        if ((int)threadIdx.x < plan.units) {
+            float w[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[side][e] = 1.f;
-        if (a.w[side] && mine) U::load((const T *)a.w[side], u, a.d, a.rot, w[side]);
-    }
-    for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
-        const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
-        // a group of lanes has one head at a time; the next one's elements are on their way meanwhile, the first ones' while angles are formed
-        typename U::Raw x_next, t_next;
-        auto fetch = [&](int side, int from) __attribute__((always_inline)) {
-            const int heads = a.heads[side], i = from + group, r = i / heads, h = i - r * heads;
-            U::clear(x_next), U::clear(t_next);
-            if (!mine || i >= rows * heads) return;
-            if (a.norm) U::load((const T *)a.in[side] + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, x_next);
-            if (g.up[side]) U::load((const T *)g.up[side] + (row + r) * a.ld_out[side] + (size_t)h * a.d, u, a.d, a.rot, t_next);
-        };
-        if (wanted[0]) fetch(0, 0);
-        else if (wanted[1]) fetch(1, 0);
-        __syncthreads();
-        angles(a, pairs, (int)row, rows, table);
-        __syncthreads();
+            for (int e = 0; e < 16; ++e) w[e] = 1.f;
+            if (a.w[side]) U::load((const T *)a.w[side], (int)threadIdx.x, a.d, a.rot, w);
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            if (!wanted[side]) continue;
-            const int heads = a.heads[side];
-            T *out = (T *)g.d_in[side];
+            for (int e = 0; e < 16; ++e) weights[16 * threadIdx.x + e] = w[e];
+        }
+        __syncthreads();
+        for (int64_t row = (int64_t)blockIdx.x * plan.together; row < a.rows; row += (int64_t)gridDim.x * plan.together) {
+            const int rows = a.rows - row < plan.together ? (int)(a.rows - row) : plan.together;
+            // a group of lanes has one head at a time
+            typename U::Raw x_raw, t_raw;
+            auto fetch = [&](int from) __attribute__((always_inline)) {
+                const int i = from + group, r = i / heads, h = i - r * heads;
+                U::clear(x_raw), U::clear(t_raw);
+                if (!mine || i >= rows * heads) return;
+                if (a.norm) U::load(in + (row + r) * ld_in + (size_t)h * a.d, u, a.d, a.rot, x_raw);
+                if (up) U::load(up + (row + r) * ld_up + (size_t)h * a.d, u, a.d, a.rot, t_raw);
+            };
+            if (!formed) {
+                __syncthreads();
+                angles(a, pairs, (int)row, rows, table);
+                __syncthreads();
+                formed = (int)gridDim.x * plan.together >= a.rows;
+            }
+            fetch(0);
             for (int from = 0; from < rows * heads; from += groups) {
                 const int i = from + group, r = i / heads, h = i - r * heads;
                 const bool live = mine && i < rows * heads;
                 float x[16], t[16];
-                U::numbers(x_next, x);
-                U::numbers(t_next, t);
-                if (from + groups < rows * heads) fetch(side, from + groups);
-                else if (side == 0 && wanted[1]) fetch(1, 0);
+                U::numbers(x_raw, x);
+                U::numbers(t_raw, t);
                 if (live) U::turn(table + r * pairs + 8 * u, a.rot / 2 - 8 * u, t, -1.f);
                 if (a.norm) {
                     float squares = 0.f, dot = 0.f;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) squares = fmaf(x[e], x[e], squares);
                     const float by = rsqrtf(fmaf(group_sum(squares, lanes), inv, a.eps));
+                    const float *w = weights + 16 * (mine ? u : 0);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         x[e] *= by;
-                        dw[side][e] = fmaf(t[e], x[e], dw[side][e]);
-                        t[e] *= w[side][e];
+                        dw[e] = fmaf(t[e], x[e], dw[e]);
+                        t[e] *= w[e];
                         dot = fmaf(t[e], x[e], dot);
                     }
                     dot = group_sum(dot, lanes) * inv;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) t[e] = by * fmaf(-x[e], dot, t[e]);
                 }
-                if (live && out) U::store(out + (row + r) * a.ld_in[side] + (size_t)h * a.d, u, a.d, a.rot, t);
+                if (live && out) U::store(out + (row + r) * ld_in + (size_t)h * a.d, u, a.d, a.rot, t);
+                if (from + groups < rows * heads) fetch(from + groups);
             }
         }
-    }
-    if (!g.dw[0] && !g.dw[1]) return;
-    // over the groups of a wavefront, then over the wavefronts, in an order of their own each
-    float *red = reinterpret_cast<float *>(smem);                 // [wavefront][unit][16]
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        __syncthreads();
+        if (!g.dw[side]) continue;
+        // over the groups of a wavefront, then over the wavefronts, in an order of their own each
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            float v = dw[side][e];
+            float v = dw[e];
             for (int n = lanes; n < 64; n *= 2) v += __shfl_xor(v, n);
             if (lane < lanes && mine) red[(wave * plan.units + u) * 16 + e] = v;
         }
         __syncthreads();
-        if (g.dw[side])
-            for (int i = (int)threadIdx.x; i < 16 * plan.units; i += 256) {
-                float v = 0.f;
-                for (int k = 0; k < 4; ++k) v += red[k * plan.units * 16 + i];
-                const int unit = i / 16, e = i % 16;
-                int at;
-                if (VEC) at = (e < 8 ? U::first_chunk(unit, a.rot) : U::second_chunk(unit, a.rot)) + e % 8;
-                else {
-                    const Pair p = pair_of<ADJ>(8 * unit + (ADJ ? e / 2 : e % 8), a.rot);
-                    at = (ADJ ? e % 2 : e / 8) ? p.b : p.a;
-                }
-                if (at < a.d) parts[((size_t)blockIdx.x * 2 + side) * a.d + at] = v;
+        for (int i = (int)threadIdx.x; i < 16 * plan.units; i += 256) {
+            float v = 0.f;
+            for (int k = 0; k < 4; ++k) v += red[k * plan.units * 16 + i];
+            const int unit = i / 16, e = i % 16;
+            int at;
+            if (VEC) at = (e < 8 ? U::first_chunk(unit, a.rot) : U::second_chunk(unit, a.rot)) + e % 8;
+            else {
+                const Pair p = pair_of<ADJ>(8 * unit + (ADJ ? e / 2 : e % 8), a.rot);
+                at = (ADJ ? e % 2 : e / 8) ? p.b : p.a;
             }
+            if (at < a.d) parts[((size_t)blockIdx.x * 2 + side) * a.d + at] = v;
+        }
+        __syncthreads();
     }
 }
 
@@ -345,8 +349,7 @@ hipError_t forward(const HeadArgs &a, const HeadPlan &p, void *const out[2], hip
 template <typename T, bool ADJ, bool VEC>
 hipError_t backward(const HeadArgs &a, const HeadGrads &g, const HeadPlan &p, float *parts, hipStream_t s)
 {
-    const int table = p.together * 64 * p.units, sums = 4 * 64 * p.units;
-    hipLaunchKernelGGL((head_back_kernel<T, ADJ, VEC>), dim3(p.grid), dim3(256), table > sums ? table : sums, s, a, g, p, parts);
+    hipLaunchKernelGGL((head_back_kernel<T, ADJ, VEC>), dim3(p.grid), dim3(256), (p.together + 5) * 64 * p.units, s, a, g, p, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!g.dw[0] && !g.dw[1])) return e;
     hipLaunchKernelGGL(head_sum_kernel, dim3((a.d + 3) / 4, 2), dim3(256), 0, s, parts, p.grid, a.d, g.dw[0], g.dw[1], g.accumulate);
