@@ -93,12 +93,8 @@ constexpr int kChunk = 32;                   // tokens
 constexpr int kGroupBytes = 64 * kChunk;
 __device__ __forceinline__ int piece_at(int r, int c) { return kGroupBytes * (c >> 2) + 64 * r + 16 * ((c ^ r >> 2) & 3); }
 
-// a lane's row within 32 of accumulator element e
-__device__ __forceinline__ int acc_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
-// Columns of an operand that is read across its rows are dealt to lanes with bits 2 and 3 swapped, so that a lane's accumulator elements 8 b .. 8 b + 7 are
-// columns next to each other, 16 b + 8 h ..: eight outputs, or the contraction's order of a 16-byte piece (Ops::along).
-__device__ __forceinline__ int dealt(int n) { return (n & ~12) | (n & 4) << 1 | (n & 8) >> 1; }
-__device__ __forceinline__ int dealt_row(int e, int h) { return 16 * (e >> 3) + 8 * h + (e & 7); }
+// The state's row, within 32, of element e of a lane's accumulators of tile t (g = lane / 16), and so the order of a contraction along the rows.
+__device__ __forceinline__ int state_row(int g, int t, int e) { return 16 * t + 4 * g + e; }
 
 // The tile of probabilities (tokens i of the queries by tokens j of the keys) is formed by a workgroup's wavefronts in quarters of 16 by 16: 0, 1 and 2 are (i, j) from
 // (0, 0), (16, 0) and (16, 16) on, and the fourth is all masked.  A lane has one i and four j from `j` on.
@@ -111,78 +107,65 @@ template <typename T> struct Ops;
 
 template <> struct Ops<bf16_t> {
     static constexpr int kOutParts = 2, kStateParts = 3;
-    // operand for a contraction of 32
-    struct Frag {
-        bf16x8_t f[2];
-    };
-    static __device__ __forceinline__ f32x16_t mma(const Frag &a, const Frag &b, f32x16_t c)
-    {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.f[0], b.f[0], c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.f[1], b.f[1], c, 0, 0, 0);
-    }
-    // A lane's places: of its pieces of row n, and of what it gives to the transposing reads.
+    typedef bf16x8_t Frag;                   // operand: row or column lane % 16, eight elements of a contraction of 32
+    static __device__ __forceinline__ f32x4_t mma(const Frag &a, const Frag &b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    // a lane's places: of its two times four elements of row lane % 16; of its piece of that row; and of what it gives to the transposing reads of a matrix'
+    // first 16 columns, for rows 8 g .. and 8 g + 4 ..
     struct Places {
-        int row[2], across[2];
+        int row[2], piece, across[2];
     };
     static __device__ __forceinline__ Places places(int lane)
     {
-        const int n = lane & 31, h = lane >> 5, q = lane & 15, r = 4 * h + (q >> 2), c = 2 * (lane >> 4 & 1) + (q & 1);
-        return Places{{piece_at(n, h), piece_at(n, 2 + h)}, {piece_at(r, c) + 4 * (q & 2), piece_at(r + 8, c) + 4 * (q & 2)}};
+        const int n = lane & 15, g = lane >> 4, r = 8 * g + (n >> 2), c = n >> 1 & 1;
+        return Places{{piece_at(n, g >> 1) + 8 * (g & 1), piece_at(n, 2 + (g >> 1)) + 8 * (g & 1)}, piece_at(n, -g & 3), {piece_at(r, c) + 8 * (n & 1), piece_at(r + 4, c) + 8 * (n & 1)}};
     }
-    // contraction along the rows, elements 32 k + dealt_row(e, h) of row lane % 32
-    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k)
+    // contraction along the rows, columns 32 k + state_row(g, t, e); row lane % 16 + 16 half
+    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k, int half)
     {
-        Frag r;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) r.f[b] = *reinterpret_cast<const bf16x8_t *>(rows + at.row[b] + kGroupBytes * k);
-        return r;
+        const char *from = rows + kGroupBytes * k + kGroupBytes / 2 * half;
+        const u32x2_t lo = *reinterpret_cast<const u32x2_t *>(from + at.row[0]), hi = *reinterpret_cast<const u32x2_t *>(from + at.row[1]);
+        return __builtin_bit_cast(Frag, u32x4_t{lo[0], lo[1], hi[0], hi[1]});
     }
-    // contraction over the rows in the accumulators' order, column 32 k + dealt(lane % 32)
-    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int k)
+    static __device__ __forceinline__ Frag transposed(const char *lo, const char *hi)
     {
-        struct { v4i16_t lo, hi; } two[2];
+        struct { v4i16_t lo, hi; } two;
+        two.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(lo));
+        two.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(hi));
+        return __builtin_bit_cast(Frag, two);
+    }
+    // contraction over the rows, column 16 c + lane % 16  (the other half of a row's 64 bytes: its places with bit 5 the other way round)
+    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int c)
+    {
+        const int other = 32 * (c & 1);
+        rows += kGroupBytes * (c >> 1);
+        return transposed(rows + (at.across[0] ^ other), rows + (at.across[1] ^ other));
+    }
+    // x rounded, and x less by that
+    static __device__ __forceinline__ Frag part(float *x)
+    {
+        u32x4_t w;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            two[b].lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(rows + at.across[0] + kGroupBytes * k + 1024 * b));
-            two[b].hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t *)STL_LDS(rows + at.across[1] + kGroupBytes * k + 1024 * b));
+        for (int k = 0; k < 4; ++k) {
+            w[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
+            x[2 * k] -= __uint_as_float(w[k] << 16);
+            x[2 * k + 1] -= __uint_as_float(w[k] & 0xffff0000u);
         }
-        return Frag{{__builtin_bit_cast(bf16x8_t, two[0]), __builtin_bit_cast(bf16x8_t, two[1])}};
+        return __builtin_bit_cast(Frag, w);
     }
-    // the sum of N operands, the last of them rounded
-    template <int N>
-    static __device__ __forceinline__ void split(const float *x, Frag *out)
-    {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            uint32_t w[N][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float u = x[8 * b + 2 * k], v = x[8 * b + 2 * k + 1];
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    w[n][k] = pack_bf16x2(u, v);
-                    u -= __uint_as_float(w[n][k] << 16);
-                    v -= __uint_as_float(w[n][k] & 0xffff0000u);
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < N; ++n) out[n].f[b] = __builtin_bit_cast(bf16x8_t, u32x4_t{w[n][0], w[n][1], w[n][2], w[n][3]});
-        }
-    }
-    // Probabilities, q_i . k_j times `near`: products by 16 x 16 x 32, two parts of four bf16 numbers a lane to where probabilities() finds them.
+    // Probabilities, q_i . k_j times `near`: two parts of four bf16 numbers a lane to where probabilities() finds them.
     template <int KT>
     static __device__ __forceinline__ void quarter(const char *queries, const char *keys, int which, int lane, const float *near, char *probs)
     {
         const Quarter at(which, lane);
-        const char *q = queries + piece_at(at.i, lane >> 4), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), lane >> 4);
+        const int c = -(lane >> 4) & 3;
+        const char *q = queries + piece_at(at.i, c), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), c);
         f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int g = 0; g < KT; ++g)
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8_t *>(k + kGroupBytes * g), *reinterpret_cast<const bf16x8_t *>(q + kGroupBytes * g), sum, 0, 0, 0);
+        for (int i = 0; i < KT; ++i) sum = mma(*reinterpret_cast<const Frag *>(k + kGroupBytes * i), *reinterpret_cast<const Frag *>(q + kGroupBytes * i), sum);
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = fmul_legacy(near[e], sum[e]);                     // (zero times anything is zero: the masked ones)
-        char *to = probs + piece_at(at.i, 2 * (at.j >> 4) + (at.j >> 2 & 1)) + 8 * (at.j >> 3 & 1);
+        char *to = probs + piece_at(at.i, -(at.j >> 3) & 3) + 8 * (at.j >> 2 & 1);
 #pragma unroll
         for (int m = 0; m < kOutParts; ++m) {
             const u32x2_t w = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
@@ -191,39 +174,34 @@ template <> struct Ops<bf16_t> {
             for (int e = 0; e < 4; ++e) y[e] -= __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
         }
     }
-    // part m of them, contraction over j in the accumulators' order, column i = lane % 32
-    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int m) { return along(probs, at, m); }
+    // part m of them, contraction over j, column i = lane % 16 + 16 half
+    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int m, int half)
+    {
+        return *reinterpret_cast<const Frag *>(probs + at.piece + kGroupBytes * m + kGroupBytes / 2 * half);
+    }
     static __device__ __forceinline__ float get(const Frag &a, int e)
     {
-        const u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[e >> 3]);
-        return __uint_as_float(e & 1 ? w[e >> 1 & 3] & 0xffff0000u : w[e >> 1 & 3] << 16);
+        const u32x4_t w = __builtin_bit_cast(u32x4_t, a);
+        return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     }
-    // zero times them by the matrix cores: two instructions in the place of two dozen
+    // zero times them by the matrix cores: one instruction in the place of a dozen
     static __device__ __forceinline__ bool finite(const Frag &a)
     {
-        const bf16x8_t none = __builtin_bit_cast(bf16x8_t, u32x4_t{0u, 0u, 0u, 0u});
-        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, a.f[0], sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, a.f[1], sum, 0, 0, 0);
-        return sum[0] == 0.f;
+        return mma(__builtin_bit_cast(Frag, u32x4_t{0u, 0u, 0u, 0u}), a, f32x4_t{0.f, 0.f, 0.f, 0.f})[0] == 0.f;
     }
     // zeros in the place of what is no finite number; the first row of such an element, 32 if there is none
-    static __device__ __forceinline__ int clean(Frag &a, int h)
+    static __device__ __forceinline__ int clean(Frag &a, int g)
     {
         int first = kChunk;
+        u32x4_t w = __builtin_bit_cast(u32x4_t, a);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            u32x4_t w = __builtin_bit_cast(u32x4_t, a.f[b]);
-#pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                const uint32_t half = i & 1 ? 0xffff0000u : 0xffffu, ones = half & 0x7f807f80u;
-                if ((w[i >> 1] & ones) != ones) continue;
-                w[i >> 1] &= ~half;
-                const int row = acc_row(8 * b + i, h);
-                first = row < first ? row : first;
-            }
-            a.f[b] = __builtin_bit_cast(bf16x8_t, w);
+        for (int e = 7; e >= 0; --e) {
+            const uint32_t half = e & 1 ? 0xffff0000u : 0xffffu, ones = half & 0x7f807f80u;
+            if ((w[e >> 1] & ones) != ones) continue;
+            w[e >> 1] &= ~half;
+            first = 8 * g + e;
         }
+        a = __builtin_bit_cast(Frag, w);
         return first;
     }
 };
@@ -231,73 +209,69 @@ template <> struct Ops<bf16_t> {
 template <> struct Ops<float> {
     static constexpr int kOutParts = 1, kStateParts = 1;
     struct Frag {
-        float f[16];
+        float f[8];
     };
-    static __device__ __forceinline__ f32x16_t mma(const Frag &a, const Frag &b, f32x16_t c)
+    // (four contractions at a time: number 8 (lane / 16) + e of 32 with the e-th instruction)
+    static __device__ __forceinline__ f32x4_t mma(const Frag &a, const Frag &b, f32x4_t c)
     {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[e], b.f[e], c, 0, 0, 0);
+        for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[e], b.f[e], c, 0, 0, 0);
         return c;
     }
+    // where piece c of the probabilities lies: four lanes' pieces 2 (lane / 16) of sixteen rows in places that meet every bank alike
+    static __device__ __forceinline__ int gray(int c) { return c ^ (c >> 1 & 1); }
     struct Places {
-        int row[2], across[2], prob[2];
+        int row[2], piece[2], across[2];
     };
     static __device__ __forceinline__ Places places(int lane)
     {
-        const int n = lane & 31, h = lane >> 5, column = dealt(n), c = column >> 2;
-        return Places{{piece_at(n, 2 * h), piece_at(n, 2 * h + 1)}, {piece_at(4 * h, c) + 4 * (column & 3), piece_at(8 + 4 * h, c) + 4 * (column & 3)}, {piece_at(n, h), piece_at(n, 2 + h)}};
+        const int n = lane & 15, g = lane >> 4, r = 8 * g, c = n >> 2, x = 4 * (n & 3);
+        return Places{{piece_at(n, g), piece_at(n, 4 + g)}, {piece_at(n, gray(2 * g)), piece_at(n, gray(2 * g + 1))}, {piece_at(r, c) + x, piece_at(r + 4, c) + x}};
     }
-    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k)
+    static __device__ __forceinline__ Frag two(const char *first, const char *second)
+    {
+        const f32x4_t u = *reinterpret_cast<const f32x4_t *>(first), v = *reinterpret_cast<const f32x4_t *>(second);
+        return Frag{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
+    }
+    static __device__ __forceinline__ Frag along(const char *rows, const Places &at, int k, int half)
+    {
+        rows += 2 * kGroupBytes * k + kGroupBytes / 2 * half;
+        return two(rows + at.row[0], rows + at.row[1]);
+    }
+    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int c)
     {
         Frag r;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(rows + at.row[g & 1] + kGroupBytes * (2 * k + (g >> 1)));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r.f[4 * g + e] = v[e];
-        }
+        for (int e = 0; e < 8; ++e) r.f[e] = *reinterpret_cast<const float *>(rows + at.across[e >> 2] + kGroupBytes * c + 64 * (e & 3));
         return r;
     }
-    static __device__ __forceinline__ Frag across(const char *rows, const Places &at, int k)
+    static __device__ __forceinline__ Frag part(const float *x)
     {
         Frag r;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) r.f[e] = *reinterpret_cast<const float *>(rows + at.across[e >> 2 & 1] + 2 * kGroupBytes * k + 1024 * (e >> 3) + 64 * (e & 3));
+        for (int e = 0; e < 8; ++e) r.f[e] = x[e];
         return r;
     }
-    template <int N>
-    static __device__ __forceinline__ void split(const float *x, Frag *out)
-    {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) out[0].f[e] = x[e];
-    }
-    // (products by 16 x 16 x 4, the contraction in the order 4 (lane / 16) + e for e = 0 .. 3)
     template <int KT>
     static __device__ __forceinline__ void quarter(const char *queries, const char *keys, int which, int lane, const float *near, char *probs)
     {
         const Quarter at(which, lane);
-        const char *q = queries + piece_at(at.i, lane >> 4), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), lane >> 4);
+        const int c = -(lane >> 4) & 3;
+        const char *q = queries + piece_at(at.i, c), *k = keys + piece_at((which > 1 ? 16 : 0) + (lane & 15), c);
         f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int g = 0; g < 2 * KT; ++g) {
-            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(k + kGroupBytes * g), v = *reinterpret_cast<const f32x4_t *>(q + kGroupBytes * g);
+        for (int i = 0; i < 2 * KT; ++i) {
+            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(k + kGroupBytes * i), v = *reinterpret_cast<const f32x4_t *>(q + kGroupBytes * i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(u[e], v[e], sum, 0, 0, 0);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = fmul_legacy(near[e], sum[e]);
-        *reinterpret_cast<f32x4_t *>(probs + piece_at(at.i, at.j >> 2)) = sum;
+        *reinterpret_cast<f32x4_t *>(probs + piece_at(at.i, gray(at.j >> 2))) = sum;
     }
-    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int m)
+    static __device__ __forceinline__ Frag probabilities(const char *probs, const Places &at, int, int half)
     {
-        Frag r;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(probs + at.prob[g & 1] + kGroupBytes * (g >> 1));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r.f[4 * g + e] = v[e];
-        }
-        return r;
+        return two(probs + at.piece[0] + kGroupBytes / 2 * half, probs + at.piece[1] + kGroupBytes / 2 * half);
     }
     static __device__ __forceinline__ float get(const Frag &a, int e) { return a.f[e]; }
     // (an exponent of ones carries into its sign bit)
@@ -305,38 +279,39 @@ template <> struct Ops<float> {
     {
         uint32_t carry = 0;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) carry |= (__float_as_uint(a.f[e]) & 0x7f800000u) + 0x00800000u;
+        for (int e = 0; e < 8; ++e) carry |= (__float_as_uint(a.f[e]) & 0x7f800000u) + 0x00800000u;
         return !(carry & 0x80000000u);
     }
-    static __device__ __forceinline__ int clean(Frag &a, int h)
+    static __device__ __forceinline__ int clean(Frag &a, int g)
     {
         int first = kChunk;
 #pragma unroll
-        for (int e = 15; e >= 0; --e) {
+        for (int e = 7; e >= 0; --e) {
             if ((__float_as_uint(a.f[e]) & 0x7f800000u) != 0x7f800000u) continue;
             a.f[e] = 0.f;
-            first = acc_row(e, h);
+            first = 8 * g + e;
         }
         return first;
     }
 };
 
-constexpr int kDecayColumns = 128;           // of v, of a workgroup, 32 a wavefront
+constexpr int kDecayColumns = 128;           // of v, of a workgroup, 16 a wavefront
 // 32 KT: width of queries and keys in LDS; NW wavefronts; OUT: with outputs; RING: loaded by LDS-DMA
 template <typename T, int KT, int NW, bool OUT, bool RING>
 struct DecayShape {
-    static constexpr int columns = 32 * NW, threads = 64 * NW, in_group = 64 / (int)sizeof(T);
+    static constexpr int columns = 16 * NW, threads = 64 * NW, in_group = 64 / (int)sizeof(T);
     static constexpr int groups = 32 * KT / in_group, groups_v = columns / in_group;
     static constexpr int bytes = kGroupBytes * groups, bytes_v = kGroupBytes * groups_v, stage = (OUT ? 2 : 1) * bytes + bytes_v;
-    // 256 registers and half of the LDS, so that two workgroups share a CU, where a wavefront's state fits
-    static constexpr int waves = sizeof(T) == 2 && KT <= 4 ? 2 : 1;
+    // half of the LDS, so that two workgroups share a CU, where two stages fit into it
     static constexpr int tables = 512, tile = OUT ? 2 * kGroupBytes : 0;
-    static constexpr int room = 160 * 1024 / waves - tables - tile, fit = room / stage;
+    static constexpr int sharing = 2 * stage + tables + tile <= 80 * 1024 ? 2 : 1;
+    static constexpr int room = 160 * 1024 / sharing - tables - tile, fit = room / stage;
     static constexpr int stages = RING ? fit < 4 ? fit : 4 : 1;
     static constexpr int lds = stages * stage + tables + tile;
     static_assert(stages >= (RING ? 2 : 1), "a ring has two stages at least");
 };
-constexpr int decay_waves(size_t element, int KT) { return element == 2 && KT <= 4 ? 2 : 1; }
+// wavefronts of a SIMD, whose registers they share: two workgroups'
+constexpr int decay_waves(size_t element, int KT) { return KT <= (element == 2 ? 4 : 3) ? 4 : 2; }
 
 // up to four elements of a row of outputs
 template <typename T>
@@ -411,9 +386,9 @@ struct RingSource {
     // the next `count` tokens.  Rows past them take the last one's values, which are finite where those are
     __device__ __forceinline__ void load(int count, bool reverse, uint32_t lds, int wave, int lane)
     {
-        if (there == kAll && kAll % NW == 0 && count == kChunk && whole) {
+        if (there == kAll && count == kChunk && whole) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) dma16_at(next, off[j], lds + 1024 * (j * NW + wave));
+            for (int j = 0; j < kPer; ++j) dma16_at(next, off[j], lds + 1024 * instruction(j, wave));
         } else {
             const char *base = next + (reverse ? (int64_t)(kChunk - count) * step : 0);
 #pragma unroll
@@ -431,6 +406,12 @@ struct RingSource {
         next += advance;
     }
 };
+
+struct Two {
+    float high, low;
+};
+// the same in all lanes: to a scalar register
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
 
 template <typename T, int KT, int NW, bool OUT, bool RING>
 __device__ __forceinline__ void decay_body(const DecayPass &p)
@@ -451,7 +432,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     const int seg = at % p.segments;
     at /= p.segments;
     const int b = at / p.heads, head = at % p.heads;
-    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
     const Tokens tokens = tokens_of(p, b);
     const int begin = seg * p.seg_tokens;
     // the segment that has the last token (the first one where there is none)
@@ -462,7 +443,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     const T *gA = (const T *)p.A + (size_t)(head / p.share_a) * p.da, *gB = (const T *)p.B + (size_t)(head / p.share_b) * p.da;
     const T *gV = (const T *)p.V + (size_t)(head / p.share_v) * p.dv + z * kDecayColumns;
     const int vleft = p.dv - z * kDecayColumns;                  // columns of v from this workgroup's first on
-    const int col = 32 * wave;                                   // this wavefront's first among them
+    const int col = 16 * wave;                                   // this wavefront's first among them
     const int token_step = p.offset ? 1 : p.token_step;
     const bool reverse = p.reverse;
     auto row_of = [&](int t) { return (size_t)(tokens.first + (int64_t)(reverse ? tokens.count - 1 - t : t) * token_step); };
@@ -484,7 +465,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
         ring_v.init(gV, p.ldv, tokens, token_step, begin, wave, lane, vleft < S::columns ? vleft : S::columns, reverse);
     }
     // or the next chunk on its way through registers: 8 elements of a row at a time
-    constexpr int kPieces8 = 4 * KT, kPer = (kPieces8 * kChunk + threads - 1) / threads, kPerV = kChunk * S::columns / 8 / threads;
+    constexpr int kPieces8 = 4 * KT, kPer = (kPieces8 * kChunk + threads - 1) / threads, kPerV = (kChunk * S::columns / 8 + threads - 1) / threads;
     Chunk<T> na[OUT && !RING ? kPer : 1], nb[RING ? 1 : kPer], nv[RING ? 1 : kPerV];
     auto lds_of = [&](int stage) { return (uint32_t)(uintptr_t)STL_LDS(smem) + stage * S::stage; };
     auto fetch = [&](int from, int stage) {
@@ -526,11 +507,9 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
             else ending[kChunk + last] = 0.f;
         }
     }
-    const double through = power(a, kChunk);
-    const float whole = (float)through, whole_rest = (float)(through - (double)whole);
 
-    // the state, element e of tile k: row 32 k + dealt_row(e), column dealt(n)
-    f32x16_t state[KT];
+    // the state, element e of tile t of 32 rows k: row 32 k + state_row(g, t, e), column n
+    f32x4_t state[KT][2];
     const size_t each = (size_t)p.da * p.dv, state_at = ((size_t)b * p.heads + head) * each;
     const float *init = OUT ? p.init : nullptr;
     float init_scale = p.init_scale;
@@ -542,71 +521,66 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
         if (seg > 0) init_scale = 1.f, power_of_first = 1;
     }
     // (loads of elements that there are not go to the last ones and are dropped: without a branch all of them are in flight at once)
-    const int j = z * kDecayColumns + col + dealt(n), j_in = j < p.dv ? j : p.dv - 1;
+    const int j = z * kDecayColumns + col + n, j_in = j < p.dv ? j : p.dv - 1;
     if (init) {
-        if (p.turned) {
-            const float *row = init + init_at + (size_t)j_in * p.da;
-            if (p.da == 32 * KT) {
-#pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const f32x4_t v = *reinterpret_cast<const f32x4_any_t *>(row + 32 * k + 16 * (g >> 1) + 8 * h + 4 * (g & 1));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) state[k][4 * g + e] = v[e];
-                    }
-            } else {
-#pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int i = 32 * k + dealt_row(e, h);
-                        state[k][e] = row[i < p.da ? i : p.da - 1];
-                    }
-            }
-        } else {
-            const float *column = init + init_at + j_in;
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int i = 32 * k + dealt_row(e, h);
-                    state[k][e] = column[(size_t)(i < p.da ? i : p.da - 1) * p.dv];
-                }
-        }
+        const float *column = init + init_at + (size_t)j_in * (p.turned ? p.da : 1);
+        const size_t step_i = p.turned ? 1 : p.dv;
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) state[k][e] = 32 * k + dealt_row(e, h) < p.da && j < p.dv ? init_scale * state[k][e] : 0.f;
+            for (int t = 0; t < 2; ++t) {
+                const int i = 32 * k + state_row(g, t, 0);
+                if (p.turned && i + 4 <= p.da) {
+                    state[k][t] = *reinterpret_cast<const f32x4_any_t *>(column + i);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) state[k][t][e] = column[(i + e < p.da ? i + e : p.da - 1) * step_i];
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) state[k][t][e] = 32 * k + state_row(g, t, e) < p.da && j < p.dv ? init_scale * state[k][t][e] : 0.f;
     } else {
 #pragma unroll
-        for (int k = 0; k < KT; ++k) state[k] = f32x16_t{};
+        for (int k = 0; k < KT; ++k) state[k][0] = state[k][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     __syncthreads();
 
+    // lambda to a chunk's tokens, in two numbers: of the first one (from the state on), of whole ones, and of the last one
+    auto two = [&](int steps) {
+        const double exact = power(a, steps);
+        const float high = (float)exact;
+        return Two{uniform(high), uniform((float)(exact - (double)high))};
+    };
+    const int last_count = chunks > 0 ? end - begin - (chunks - 1) * kChunk : 0;
+    const Two through_first = two((chunks > 1 ? kChunk : last_count) - 1 + power_of_first), through = two(kChunk), through_last = two(last_count);
     // what does not change from chunk to chunk
     const typename O::Places places = O::places(lane);
-    constexpr int kQuarters = OUT ? (3 + NW - 1) / NW : 0;       // of the probabilities' tile, of a wavefront at most
-    float near[kQuarters ? kQuarters : 1][4];                    // c lambda^(i - j) for this lane's i and j, 0 for j > i
-#pragma unroll
-    for (int i = 0; i < kQuarters; ++i)
+    float near[4] = {};                                          // c lambda^(i - j) for this lane's i and j, 0 for j > i
+    if (OUT && wave < 3) {
+        const Quarter at(wave, lane);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const Quarter at(wave + i * NW, lane);
             const int ago = at.i - at.j - e;
-            near[i][e] = ago >= 0 ? p.out_scale * fade[ago >= 0 ? ago : 0] : 0.f;
+            near[e] = ago >= 0 ? p.out_scale * fade[ago >= 0 ? ago : 0] : 0.f;
         }
-    float since = OUT ? p.out_scale * fade[n + power_of_first] : 0.f;
-    // where this lane's outputs of the next chunk go, and how many of its columns there are (none: no outputs); bit 0: in fp32, bit 1: not all columns of the wavefront
+    }
+    float since[2] = {};                                         // c lambda^(tokens from the state to n and n + 16)
+    if (OUT) since[0] = p.out_scale * fade[n + power_of_first], since[1] = p.out_scale * fade[n + 16 + power_of_first];
+    // where this lane's outputs of the next chunk go (and those of 16 tokens on), and how many of its columns there are (none: no outputs); bit 0: in fp32,
+    // bit 1: not all columns of the wavefront
     char *out_at = nullptr;
-    int64_t out_advance = 0;
-    const int out_left = OUT && p.O ? vleft - col - 8 * h : 0;
-    int out_kind = (p.out32 ? 1 : 0) | (p.O && vleft - col >= 32 ? 0 : 2);
+    int64_t out_advance = 0, out_half = 0;
+    const int out_left = OUT && p.O ? vleft - col - 4 * g : 0;
+    int out_kind = (p.out32 ? 1 : 0) | (p.O && vleft - col >= 16 ? 0 : 2);
     asm volatile("" : "+s"(out_kind));                           // (kept, and not read from the arguments again in each chunk)
     if (OUT && p.O) {
         const int64_t size = p.out32 ? 4 : (int64_t)sizeof(T), row = tokens.first + (int64_t)(reverse ? tokens.count - 1 - begin - n : begin + n) * token_step;
-        out_at = (char *)p.O + (row * (int64_t)p.ldo + (int64_t)head * p.dv + z * kDecayColumns + col + 8 * h) * size;
-        out_advance = (reverse ? -kChunk : kChunk) * token_step * (int64_t)p.ldo * size;
+        out_at = (char *)p.O + (row * (int64_t)p.ldo + (int64_t)head * p.dv + z * kDecayColumns + col + 4 * g) * size;
+        out_advance = (reverse ? -kChunk : kChunk) * token_step * (int64_t)p.ldo * size, out_half = out_advance / 2;
     }
     float owed = 0.f;                                            // what the roundings of lambda^32 to fp32 have left out: made good by the next ones
 
@@ -643,94 +617,86 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
         const bool unclean = __ballot(!O::finite(values)) != 0;
         int bad = kChunk;                                        // the first token whose value in this lane's column is no finite number
         if (unclean) {
-            bad = O::clean(values, h);
-            const int other = __shfl_xor(bad, 32);
-            bad = other < bad ? other : bad;
+            bad = O::clean(values, g);
+            for (int m = 16; m < 64; m *= 2) {
+                const int other = __shfl_xor(bad, m);
+                bad = other < bad ? other : bad;
+            }
         }
-        float high = whole, low = whole_rest;
-        if (count < kChunk || !power_of_first) {
-            const double exact = power(a, count - 1 + power_of_first);
-            high = (float)exact, low = (float)(exact - (double)high);
-        }
-        low += owed;
-        const float fall = high + low;
-        owed = low - (fall - high);
+        const Two by = c == 0 ? through_first : c + 1 == chunks ? through_last : through;
+        const float low = by.low + owed, fall = by.high + low;
+        owed = low - (fall - by.high);
         const float *weight = count < kChunk ? ending : rising;
         // all products of a chunk in one piece of straight code, so that vector and matrix instructions overlap (the state behind the last token too, which
         // is not always needed)
-        f32x16_t out = {};
-        Frag key[2];                                             // (operands are read a step ahead; the fences keep the compiler from reading further)
+        f32x4_t out[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};                       // of tokens n and n + 16
         if (OUT) {
-            Frag q[2];
-            q[0] = O::along(lA, places, 0);
-#pragma unroll
-            for (int i = 0; i < kQuarters; ++i)
-                if (wave + i * NW < 3) O::template quarter<KT>(lA, lB, wave + i * NW, lane, near[i], probs);
-            __builtin_amdgcn_sched_barrier(0);
+            if (wave < 3) O::template quarter<KT>(lA, lB, wave, lane, near, probs);
+            Frag q[2][2] = {{O::along(lA, places, 0, 0), O::along(lA, places, 0, 1)}};       // (operands are read a step ahead)
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                if (k + 1 < KT) q[k + 1 & 1] = O::along(lA, places, k + 1);
-                else key[0] = O::across(lB, places, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                float x[16];
+                if (k + 1 < KT) q[k + 1 & 1][0] = O::along(lA, places, k + 1, 0), q[k + 1 & 1][1] = O::along(lA, places, k + 1, 1);
+                float x[8];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = state[k][e];
-                Frag parts[O::kOutParts];
-                O::template split<O::kOutParts>(x, parts);
+                for (int e = 0; e < 8; ++e) x[e] = state[k][e >> 2][e & 3];
 #pragma unroll
-                for (int m = 0; m < O::kOutParts; ++m) out = O::mma(parts[m], q[k & 1], out);
+                for (int m = 0; m < O::kOutParts; ++m) {
+                    const Frag part = O::part(x);
+                    out[0] = O::mma(part, q[k & 1][0], out[0]);
+                    out[1] = O::mma(part, q[k & 1][1], out[1]);
+                }
             }
-            out *= since;
+            out[0] *= since[0], out[1] *= since[1];
             wait_lds();
             pipe::block_barrier();
 #pragma unroll
-            for (int m = 0; m < O::kOutParts; ++m) out = O::mma(values, O::probabilities(probs, places, m), out);
-        } else {
-            key[0] = O::across(lB, places, 0);
+            for (int m = 0; m < O::kOutParts; ++m)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) out[half] = O::mma(values, O::probabilities(probs, places, m, half), out[half]);
         }
-        float x[16];
+        float x[8];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4_t left = *reinterpret_cast<const f32x4_t *>(weight + acc_row(4 * g, h));
+        for (int i = 0; i < 2; ++i) {
+            const f32x4_t left = *reinterpret_cast<const f32x4_t *>(weight + 8 * g + 4 * i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * g + e] = O::get(values, 4 * g + e) * left[e];
+            for (int e = 0; e < 4; ++e) x[4 * i + e] = O::get(values, 4 * i + e) * left[e];
         }
         Frag parts[O::kStateParts];
-        O::template split<O::kStateParts>(x, parts);
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            if (k + 1 < KT) key[k + 1 & 1] = O::across(lB, places, k + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            state[k] *= fall;
+        for (int m = 0; m < O::kStateParts; ++m) parts[m] = O::part(x);
+        Frag key[2] = {O::across(lB, places, 0)};
 #pragma unroll
-            for (int m = 0; m < O::kStateParts; ++m) state[k] = O::mma(key[k & 1], parts[m], state[k]);
+        for (int c = 0; c < 2 * KT; ++c) {
+            if (c + 1 < 2 * KT) key[c + 1 & 1] = O::across(lB, places, c + 1);
+            f32x4_t &tile = state[c >> 1][c & 1];
+            tile *= fall;
+#pragma unroll
+            for (int m = 0; m < O::kStateParts; ++m) tile = O::mma(key[c & 1], parts[m], tile);
         }
         if (unclean) {
+            const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (n >= __shfl(bad, acc_row(e, h))) out[e] = __uint_as_float(0x7fc00000u);
+            for (int e = 0; e < 4; ++e) {
+                const int first = __shfl(bad, 4 * g + e);
+                if (n >= first) out[0][e] = nan;
+                if (n + 16 >= first) out[1][e] = nan;
+            }
             if (bad < kChunk)
 #pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) state[k][e] = __uint_as_float(0x7fc00000u);
+                for (int k = 0; k < KT; ++k) state[k][0] = state[k][1] = f32x4_t{nan, nan, nan, nan};
         }
-        if (OUT && n < count) {
+        if (OUT)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int left = out_left - 16 * g;
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = out[8 * g + e];
-                if (out_kind == 0) Chunk<T>::store((T *)out_at + 16 * g, 8, w);
-                else if (out_kind == 1) Chunk<float>::store((float *)out_at + 16 * g, 8, w);
-                else if (left <= 0) continue;
-                else if (out_kind == 2) Chunk<T>::store((T *)out_at + 16 * g, left, w);
-                else Chunk<float>::store((float *)out_at + 16 * g, left, w);
+            for (int half = 0; half < 2; ++half) {
+                if (n + 16 * half >= count) continue;
+                char *to = out_at + (half ? out_half : 0);
+                if (out_kind == 0) put4((T *)to, 4, out[half]);
+                else if (out_kind == 1) put4((float *)to, 4, out[half]);
+                else if (out_kind == 2) put4((T *)to, out_left, out[half]);
+                else put4((float *)to, out_left, out[half]);
             }
-        }
         if (OUT) out_at += out_advance;
-        if (OUT && !power_of_first) since = p.out_scale * fade[n + 1];
+        if (OUT && !power_of_first) since[0] = p.out_scale * fade[n + 1], since[1] = p.out_scale * fade[n + 17];
         power_of_first = 1;
         if (RING) stage = stage + 1 < S::stages ? stage + 1 : 0;
     }
@@ -743,9 +709,9 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int i = 32 * k + dealt_row(e, h);
-                    if (i < p.da) column[i * step_i] = by * state[k][e];
+                for (int e = 0; e < 8; ++e) {
+                    const int i = 32 * k + state_row(g, e >> 2, e & 3);
+                    if (i < p.da) column[i * step_i] = by * state[k][e >> 2][e & 3];
                 }
     }
 }
@@ -777,17 +743,17 @@ hipError_t launch_shape(const DecaySweeps &sw, hipStream_t s)
 }
 
 inline int key_tiles(int da) { return da <= 128 ? (da + 31) / 32 : 8; }
-inline int value_waves(int dv) { return dv <= 64 ? 2 : 4; }
+inline int value_waves(int dv) { return dv <= 64 ? 4 : 8; }
 
 // sweeps with the same key_tiles, value_waves, blocks of columns, segments and kind of rows
 template <typename T, bool OUT>
 hipError_t decay_sweeps(const DecaySweeps &sw, hipStream_t s)
 {
-    const int tiles = key_tiles(sw.pass[0].da);
+    const int tiles = key_tiles(sw.pass[0].da), waves = value_waves(sw.pass[0].dv);
     constexpr bool wide = sizeof(T) == 2;                        // fp32: a ring of rows of 256 does not fit
     if (!sw.pass[0].ring || (!wide && tiles == 8)) {
-        if (tiles == 8) return launch_shape<T, 8, 4, OUT, false>(sw, s);
-        return tiles > 2 ? launch_shape<T, 4, 4, OUT, false>(sw, s) : launch_shape<T, 2, 4, OUT, false>(sw, s);
+        if (tiles == 8) return launch_shape<T, 8, 8, OUT, false>(sw, s);
+        return tiles > 2 ? launch_shape<T, 4, 8, OUT, false>(sw, s) : launch_shape<T, 2, 8, OUT, false>(sw, s);
     }
     auto ring = [&](auto nw) {
         constexpr int NW = decltype(nw)::value;
@@ -797,7 +763,7 @@ hipError_t decay_sweeps(const DecaySweeps &sw, hipStream_t s)
         if (tiles == 3) return launch_shape<T, 3, NW, OUT, true>(sw, s);
         return tiles == 2 ? launch_shape<T, 2, NW, OUT, true>(sw, s) : launch_shape<T, 1, NW, OUT, true>(sw, s);
     };
-    return value_waves(sw.pass[0].dv) == 2 ? ring(std::integral_constant<int, 2>()) : ring(std::integral_constant<int, 4>());
+    return waves == 4 ? ring(std::integral_constant<int, 4>()) : ring(std::integral_constant<int, 8>());
 }
 // seq_decay_bf16.hip, seq_decay_f32.hip; seq_decay_states_*.hip: what segments add to the state
 hipError_t decay_sweeps_bf16(const DecaySweeps &sw, hipStream_t s);

@@ -109,13 +109,22 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecaySweeps s)
     }
 }
 
-// Gradients of key heads that several heads share: out[row][g] = sum over the heads of group g of part[row][head], rows of the sequences alone.  A workgroup takes
-// whole rows.
+// Gradients of key heads that several heads share: out[row][g] = sum over the heads of group g of part[row][head], rows of the sequences alone, of keys and of
+// values (blockIdx.z).  A workgroup takes whole rows.
+struct Shared {
+    const float *part[2];
+    void *out[2];
+    size_t ld[2];
+    int width[2];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void decay_share_kernel(const DecayPass p, const float *part, T *out, size_t ld, int width, int share)
+__global__ __launch_bounds__(256) void decay_share_kernel(const DecayPass p, const Shared what, int share)
 {
     const Tokens tokens = tokens_of(p, (int)blockIdx.y);
-    const int wide = p.heads / share * width;
+    const int z = (int)blockIdx.z, width = what.width[z], wide = p.heads / share * width;
+    const float *part = what.part[z];
+    T *out = (T *)what.out[z];
+    if (!out) return;
     for (int t = (int)blockIdx.x; t < tokens.count; t += (int)gridDim.x) {
         const size_t row = (size_t)(tokens.first + (int64_t)t * (p.offset ? 1 : p.token_step));
         for (int c = (int)threadIdx.x; c < wide; c += 256) {
@@ -123,7 +132,7 @@ __global__ __launch_bounds__(256) void decay_share_kernel(const DecayPass p, con
             const float *from = part + (row * p.heads + (size_t)g * share) * width + e;
             float v = 0.f;
             for (int k = 0; k < share; ++k) v += from[(size_t)k * width];
-            Elem<T>::st(out + row * ld + c, v);
+            Elem<T>::st(out + row * what.ld[z] + c, v);
         }
     }
 }
@@ -132,12 +141,12 @@ namespace {
 
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 
-// Segments of a sequence.  They cost a sweep more, so only where a head has four of them at least for 512 workgroups in all (for each of the gradients' three sweeps 256),
-// and of 128 tokens (fp32, whose products take three times as long: 64).  13 sequences of up to 777 tokens x 16 heads: 46 us in one piece, 76 us in two; 4 x 2048
-// tokens x 16 heads, gradients: 156 us in four pieces, 168 us in two, 182 us in eight.
-int most_segments(int dtype, const DecayArgs &a, bool grads)
+// Segments of a sequence.  They cost a sweep more, so only where a head has four of them at least for a workgroup a CU (and sweep), and of 128 tokens (fp32, whose
+// products take three times as long: 64).  More of them, of 8192 tokens x 32 heads: 132 us in 8, 138 in 16, 145 in 12; 4 x 2048 tokens x 16 heads, gradients: 156 us in
+// four, 168 in two, 182 in eight; 13 sequences of up to 777 tokens x 16 heads: 46 us in one piece, 76 in two.
+int most_segments(int dtype, const DecayArgs &a)
 {
-    const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns), most = (grads ? 256 : 512) / groups, fit = a.length / (dtype ? 128 : 64);
+    const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns), most = 256 / groups, fit = a.length / (dtype ? 128 : 64);
     return most < 4 || fit < 4 ? 1 : (int)(most < fit ? most : fit);
 }
 void cut(const DecayArgs &a, int64_t n, int *segments, int *tokens)
@@ -146,21 +155,21 @@ void cut(const DecayArgs &a, int64_t n, int *segments, int *tokens)
     *segments = a.length > 0 ? (a.length + *tokens - 1) / *tokens : 1;
 }
 
-DecayPass common(int dtype, const DecayArgs &a, bool grads)
+DecayPass common(int dtype, const DecayArgs &a)
 {
     DecayPass p{};
     p.rows = a.rows, p.sequences = a.sequences, p.length = a.length, p.heads = a.heads, p.seq_step = a.seq_step, p.token_step = a.token_step;
     p.log_decay = a.log_decay, p.offset = a.offset;
     p.share_a = p.share_b = p.share_v = 1;
     p.out_scale = a.scale, p.init_scale = p.last_scale = 1.f;
-    cut(a, most_segments(dtype, a, grads), &p.segments, &p.seg_tokens);
+    cut(a, most_segments(dtype, a), &p.segments, &p.seg_tokens);
     return p;
 }
 
-size_t starts_bytes(int dtype, const DecayArgs &a, bool grads)
+size_t starts_bytes(int dtype, const DecayArgs &a)
 {
     // (never less for a longer sequence)
-    const int segments = most_segments(dtype, a, grads);
+    const int segments = most_segments(dtype, a);
     return segments > 1 ? whole((size_t)a.sequences * a.heads * segments * a.dk * a.dv * 4) : 0;
 }
 size_t parts_bytes(const DecayArgs &a, int width) { return a.heads != a.kv_heads ? whole((size_t)a.rows * a.heads * width * 4) : 0; }
@@ -187,17 +196,20 @@ hipError_t join(const DecaySweeps &sw, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const float *part, void *out, size_t ld, int width, hipStream_t s)
+hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const Shared &all, hipStream_t s)
 {
+    const size_t size = dtype ? 2 : 4;
     const int blocks = a.length < 4096 ? a.length : 4096;
     for (int b = 0; b < a.sequences; b += 65535) {
         DecayPass q = p;
-        const dim3 grid((unsigned)blocks, a.sequences - b < 65535 ? a.sequences - b : 65535);
+        Shared what = all;
+        const dim3 grid((unsigned)blocks, a.sequences - b < 65535 ? a.sequences - b : 65535, 2);
         if (q.offset) q.offset += b;
         const size_t skip = q.offset ? 0 : (size_t)b * a.seq_step;
-        const float *from = part + skip * a.heads * width;
-        if (dtype) hipLaunchKernelGGL(decay_share_kernel<bf16_t>, grid, dim3(256), 0, s, q, from, (bf16_t *)out + skip * ld, ld, width, a.heads / a.kv_heads);
-        else hipLaunchKernelGGL(decay_share_kernel<float>, grid, dim3(256), 0, s, q, from, (float *)out + skip * ld, ld, width, a.heads / a.kv_heads);
+        for (int i = 0; i < 2; ++i)
+            if (what.out[i]) what.part[i] += skip * a.heads * what.width[i], what.out[i] = (char *)what.out[i] + skip * what.ld[i] * size;
+        if (dtype) hipLaunchKernelGGL(decay_share_kernel<bf16_t>, grid, dim3(256), 0, s, q, what, a.heads / a.kv_heads);
+        else hipLaunchKernelGGL(decay_share_kernel<float>, grid, dim3(256), 0, s, q, what, a.heads / a.kv_heads);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -208,8 +220,8 @@ hipError_t share_out(int dtype, const DecayArgs &a, const DecayPass &p, const fl
 
 size_t decay_workspace_bytes(int dtype, const DecayArgs &a, bool grads)
 {
-    if (!grads) return a.length > kFewTokens ? starts_bytes(dtype, a, false) : 0;
-    return 2 * starts_bytes(dtype, a, true) + parts_bytes(a, a.dk) + parts_bytes(a, a.dv);
+    if (!grads) return a.length > kFewTokens ? starts_bytes(dtype, a) : 0;
+    return 2 * starts_bytes(dtype, a) + parts_bytes(a, a.dk) + parts_bytes(a, a.dv);
 }
 
 hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *state_out, void *ws, hipStream_t s)
@@ -223,7 +235,7 @@ hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *s
     DecaySweeps sw{};
     DecayPass &p = sw.pass[0];
     sw.count = 1;
-    p = common(dtype, a, false);
+    p = common(dtype, a);
     p.da = a.dk, p.dv = a.dv;
     p.A = a.Q, p.lda = a.ld_q;
     p.B = a.K, p.ldb = a.ld_k, p.V = a.V, p.ldv = a.ld_v;
@@ -249,16 +261,16 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
         at += n;
         return (float *)was;
     };
-    float *starts[2] = {take(starts_bytes(dtype, a, true)), take(starts_bytes(dtype, a, true))}, *part_k = take(parts_bytes(a, a.dk)), *part_v = take(parts_bytes(a, a.dv));
+    float *starts[2] = {take(starts_bytes(dtype, a)), take(starts_bytes(dtype, a))}, *part_k = take(parts_bytes(a, a.dk)), *part_v = take(parts_bytes(a, a.dv));
     // the state forward in time, from K and V
-    DecayPass f = common(dtype, a, true);
+    DecayPass f = common(dtype, a);
     f.da = a.dk, f.dv = a.dv;
     f.B = a.K, f.ldb = a.ld_k, f.V = a.V, f.ldv = a.ld_v;
     f.share_b = f.share_v = share;
     f.init = a.state, f.init_power = 1;
     f.starts = starts[0];
     // its gradient backward in time, from Q and dO, held without the factor c, which its outputs have
-    DecayPass r = common(dtype, a, true);
+    DecayPass r = common(dtype, a);
     r.reverse = true;
     r.da = a.dk, r.dv = a.dv;
     r.B = a.Q, r.ldb = a.ld_q, r.V = g.dO, r.ldv = a.ld_o;
@@ -300,7 +312,7 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
         p.last = g.dstate_in;
         sw.pass[sw.count++] = p;
     }
-    // one launch for sweeps of the same widths
+    // one launch for sweeps of the same tiles
     for (int i = 0; i < sw.count;) {
         DecaySweeps some{};
         do some.pass[some.count++] = sw.pass[i++];
@@ -309,9 +321,8 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
         e = sweep(dtype, some, true, s);
         if (e != hipSuccess) return e;
     }
-    if (share > 1 && g.dK) e = share_out(dtype, a, r, part_k, g.dK, a.ld_k, a.dk, s);
-    if (share > 1 && g.dV && e == hipSuccess) e = share_out(dtype, a, r, part_v, g.dV, a.ld_v, a.dv, s);
-    return e;
+    if (share == 1 || (!g.dK && !g.dV)) return e;
+    return share_out(dtype, a, r, Shared{{part_k, part_v}, {g.dK, g.dV}, {a.ld_k, a.ld_v}, {a.dk, a.dv}}, s);
 }
 
 }  // namespace seq
