@@ -321,7 +321,7 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
         e = sweep(dtype, some, true, s);
         if (e != hipSuccess) return e;
     }
-    if (share == 1 || (!g.dK && !g.dV)) return e;
+    if (share == 1 || a.length == 0 || (!g.dK && !g.dV)) return e;
     return share_out(dtype, a, r, Shared{{part_k, part_v}, {g.dK, g.dV}, {a.ld_k, a.ld_v}, {a.dk, a.dv}}, s);
 }
 

@@ -155,6 +155,17 @@ def test_decay(driver, sequences, length, heads, kv, dk, dv, t):
     decay_check(got, s, at, t, 0.7, length, ("dQ", "dK", "dV", "dstate"))
 
 
+@pytest.mark.parametrize("t,length,token_step", [("f32", 257, 1), ("bf16", 515, 1), ("bf16", 513, 3)])
+def test_decay_in_segments(driver, t, length, token_step):
+    """Long enough for several segments of a sequence, whose states are joined; whole pieces and others."""
+    for dk, dv in ((16, 24), (9, 17)):
+        s = decay_case(length * token_step, 1, 2, 1, dk, dv, t, seed=length + dk)
+        at = [list(range(0, length * token_step, token_step))]
+        for grads, names in ((False, ("O", "state")), (True, ("dQ", "dK", "dV", "dstate"))):
+            got = run_decay(driver, s, t, grads, length * token_step, 1, length, 2, 1, dk, dv, 1, token_step)
+            decay_check(got, s, at, t, 0.7, length, names)
+
+
 def test_decay_by_position_and_packed(driver):
     for t in ("bf16", "f32"):
         s = decay_case(120, 4, 2, 2, 24, 40, t, seed=5)

@@ -71,6 +71,13 @@ def test_embed_rows_and_vocabularies(rows, vocab, tokens, t):
     check_embed(rows, 24, vocab, t, tokens, seed=rows)
 
 
+def test_embed_runs_of_many_segments():
+    """One id's rows over more segments than a wavefront looks ahead, wide rows and narrow ones."""
+    check_embed(30000, 40, 7, "bf16", "one")
+    check_embed(5000, 700, 3, "f32", "even")
+    check_embed(33000, 2050, 11, "bf16", "zipf")
+
+
 def test_embed_more_elements_than_32_bits_count():
     vocab, d, rows = 1100000, 2048, 40
     if torch.cuda.mem_get_info()[0] < 40 << 30:
@@ -170,6 +177,12 @@ def test_head_sizes(d, rot, t):
 def test_head_rows(rows, heads, kv):
     check_heads(rows, heads, kv, 64, 64, "bf16", seed=rows)
     check_heads(rows, heads, kv, 32, 16, "f32", adjacent=True, seed=rows)
+
+
+@pytest.mark.parametrize("rows,heads,kv,d,rot", [(16500, 12, 12, 64, 32), (16500, 3, 1, 32, 32), (8300, 5, 1, 96, 96), (40000, 1, 1, 16, 16)])
+def test_head_turns_of_many_rows(rows, heads, kv, d, rot):
+    """More rows than workgroups take at once, heads that leave lanes idle."""
+    check_heads(rows, heads, kv, d, rot, "bf16", adjacent=rot < d, seed=rows)
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
@@ -425,6 +438,36 @@ def test_decay_without_tokens():
         assert torch.equal(after, state)
     stl.stl_decay_attention_forward(prob, None, None, None, None, None, None, None, after, None, 0)
     assert not after.any()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_decay_without_tokens_and_with_shared_heads(t):
+    """Empty sequences: gradients of keys and values have no rows to write, states pass through."""
+    prob = stl.DecayAttentionProblem(6, 2, 6, 4, 2, 16, scale=0.5, dtype=STL_DT[t])
+    n = stl.stl_decay_attention_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    Q, dO = (torch.randn(6, 4, 16, device="cuda").to(TORCH_DT[t]) for _ in range(2))
+    K, V = (torch.randn(6, 2, 16, device="cuda").to(TORCH_DT[t]) for _ in range(2))
+    state, after = torch.randn(2, 4, 16, 16, device="cuda"), torch.empty(2, 4, 16, 16, device="cuda")
+    outs = [torch.full_like(x, 3.0) for x in (Q, K, V)]
+    offset = torch.tensor([2, 2, 2], device="cuda")
+    stl.stl_decay_attention_backward(prob, Q, K, V, None, offset, None, dO, state, *outs, after, ws, n)
+    assert torch.equal(after, state) and all(bool((o == 3).all()) for o in outs)
+    none = stl.DecayAttentionProblem(0, 2, 0, 4, 2, 16, scale=0.5, dtype=STL_DT[t])
+    after.zero_()
+    stl.stl_decay_attention_backward(none, Q, K, V, None, None, None, dO, state, *outs, after, ws, n)
+    assert torch.equal(after, state) and all(bool((o == 3).all()) for o in outs)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("share", [1, 2])
+def test_decay_in_segments(t, share):
+    """Few heads and long sequences, which come in segments: rows one after the other, far apart, packed, and not of whole pieces."""
+    for length, dk, dv in ((1024, 64, 48), (777, 33, 70), (2049, 128, 128)):
+        check_decay(2, length, 2 * share, 2, dk, dv, t, seed=length)
+    check_decay(3, 600, 2 * share, 2, 48, 64, t, at=dict(sequences=3, length=600, seq_step=1, token_step=3), seed=1, in_place=True)
+    offset = np.array([5, 5, 1200, 1201, 1900, 2500], np.int64)
+    check_decay(5, 1195, 2 * share, 2, 64, 64, t, at=dict(sequences=5, length=1195, offset=offset), rows=2600, seed=2)
 
 
 def test_decay_gradients_are_differences():
