@@ -396,8 +396,7 @@ stl_status_t stl_embed_forward(const stl_embed_t *prob, const int64_t *token, co
  * to run.  dX: rows x d, dW: vocab x d (out, storage dtype).
  * accumulate: 0 writes all of dW, zeros for ids that no row has (also with no rows); 1 adds to the rows of dW whose ids occur and leaves the others alone, as
  * tied weights need it behind stl_vocab_loss_backward.
- * ws / ws_bytes: at least stl_embed_workspace_bytes(prob): 8 bytes a row, 2 bits an id or 32 KB, and fp32 sums of 8 d bytes for each 16 rows, at most
- * 2048 times.
+ * ws / ws_bytes: at least stl_embed_workspace_bytes(prob): 8 bytes a row and fp32 sums of 8 d bytes for each 8 or 16 rows, at most 2048 times.
  */
 size_t stl_embed_workspace_bytes(const stl_embed_t *prob);
 stl_status_t stl_embed_backward(const stl_embed_t *prob, const int64_t *token, const void *dX, void *dW, int accumulate, void *ws, size_t ws_bytes, void *stream);

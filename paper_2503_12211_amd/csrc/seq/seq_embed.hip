@@ -6,9 +6,9 @@
 // The gradient is formed without floating-point atomics, so that its bits do not depend on the order in which workgroups run.  Three launches:
 //  1. the rows sorted by id.  The vocabulary is cut into ranges, a workgroup each.  It reads all tokens twice: once to count its ids (and, for the place at
 //     which its rows begin, the tokens of lower ids), once to write its rows down, in order.  A wavefront walks over consecutive tokens and has counts of
-//     its own, so the order of rows with one id is that of the batch.  Ids that do not occur are noted as bits.
+//     its own, so the order of rows with one id is that of the batch.  Other workgroups write zeros to all of dW meanwhile: few of its rows are any token's.
 //  2. sums over the sorted rows, cut into segments of equal length whatever the ids: a common token's many rows are shared by many workgroups.
-//     A run of one id that lies in one segment is finished there; parts of others go to the workspace in fp32.  Zeros for absent ids beside them.
+//     A run of one id that lies in one segment is finished there; parts of others go to the workspace in fp32.
 //  3. parts of a run that several segments share are added up in order.
 #include "seq_kernels.h"
 #include "../lm/lm_device.h"
@@ -51,9 +51,26 @@ __device__ __forceinline__ void each_id(int rel, int width, F f)
     }
 }
 
-__global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs a, const EmbedPlan plan, const int64_t *token, int *order, int *ids, int *total,
-                                                                 uint64_t *absent)
+// `bytes` zeros from an address of 16 bytes on, by `of` workgroups
+constexpr int kZeros = 4;                    // pieces of a thread and turn
+__device__ __forceinline__ void write_zeros(char *to, size_t bytes, int block, int of)
 {
+    const size_t pieces = bytes / 16, step = (size_t)64 * kWaves;
+    for (size_t at = (size_t)block * kZeros * step + threadIdx.x; at < pieces; at += (size_t)of * kZeros * step)
+#pragma unroll
+        for (int u = 0; u < kZeros; ++u)
+            if (at + u * step < pieces) reinterpret_cast<u32x4_t *>(to)[at + u * step] = u32x4_t{0u, 0u, 0u, 0u};
+    if (block == 0 && threadIdx.x < bytes % 16 / 2) reinterpret_cast<uint16_t *>(to + 16 * pieces)[threadIdx.x] = 0;
+}
+
+// Workgroups behind the ranges': zeros for dW, of which most rows are not any token's, while the others sort.
+__global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs a, const EmbedPlan plan, const int64_t *token, int *order, int *ids, int *total,
+                                                                 char *zeros, size_t bytes)
+{
+    if ((int)blockIdx.x >= plan.ranges) {
+        write_zeros(zeros, bytes, (int)blockIdx.x - plan.ranges, (int)gridDim.x - plan.ranges);
+        return;
+    }
     __shared__ int count[kWaves][kMostWidth];
     __shared__ int below[kWaves];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -107,9 +124,6 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs
         }
     }
     if ((int)blockIdx.x == plan.ranges - 1 && threadIdx.x == 64 * kWaves - 1) *total = base + upto;
-    // ids that do not occur, a bit each, for the zeros that the sums' launch writes
-    const uint64_t gone = __ballot(id < width && mine == 0);
-    if (lane == 0) absent[(size_t)blockIdx.x * kWaves + wave] = gone;
     __syncthreads();
     for (int step = begin; step < end; step += 8) {
         int got[8];
@@ -134,36 +148,11 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(const EmbedArgs
     }
 }
 
-// zeros for the absent ones of 64 ids
-template <typename T>
-__device__ __forceinline__ void write_zeros(const EmbedArgs &a, const EmbedPlan &plan, int some, const uint64_t *absent, T *dW)
-{
-    const int each = (plan.width + 63) / 64, range = some / each, word = some % each, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const uint64_t bits = absent[(size_t)range * kWaves + word];
-    constexpr int per16 = 16 / (int)sizeof(T);
-    for (int i = wave; i < 64; i += 4) {
-        if (!(bits >> i & 1)) continue;
-        T *out = dW + ((size_t)range * plan.width + 64 * word + i) * a.d;
-        // whole 16-byte pieces at such addresses, lane by lane, and single elements in front of them and behind
-        int head = (int)(-(uintptr_t)out % 16 / sizeof(T));
-        head = head < a.d ? head : a.d;
-        const int pieces = (a.d - head) / per16, rest = a.d - head - pieces * per16;
-        for (int c = lane; c < pieces; c += 64) *reinterpret_cast<u32x4_t *>(out + head + c * per16) = u32x4_t{0u, 0u, 0u, 0u};
-        if (lane < head) Elem<T>::st(out + lane, 0.f);
-        if (lane < rest) Elem<T>::st(out + a.d - 1 - lane, 0.f);
-    }
-}
-
 // A chunk of 8 columns a thread.  parts[2 s]: the sum of segment s's rows that go on from segment s - 1; parts[2 s + 1]: of those that go on behind it.
-// Workgroups behind the segments': zeros for up to 64 ids that do not occur, most of dW, while the sums wait for their rows.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const EmbedPlan plan, const int *order, const int *ids, const int *total,
-                                                        const uint64_t *absent, const T *dX, T *dW, float *parts, int accumulate)
+                                                        const T *dX, T *dW, float *parts, int accumulate)
 {
-    if ((int)blockIdx.x >= plan.segments) {
-        if (blockIdx.y == 0) write_zeros(a, plan, (int)blockIdx.x - plan.segments, absent, dW);
-        return;
-    }
     const int seg = (int)blockIdx.x, col = 8 * ((int)blockIdx.y * 256 + (int)threadIdx.x), left = a.d - col;
     const int count = *total;
     const int64_t first = (int64_t)seg * plan.length;
@@ -176,9 +165,17 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
         int id[9];
 #pragma unroll
         for (int u = 0; u < 9; ++u) id[u] = at + u < count ? ids[at + u] : -1;
+        // (rows behind the segment's are its last one; one branch for all of them, so that their loads are in flight together)
+        const T *from[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (at + u < end) c[u].load(dX + (size_t)order[at + u] * a.d + col, left);
+        for (int u = 0; u < 8; ++u) from[u] = dX + (size_t)order[at + u < end ? at + u : end - 1] * a.d + col;
+        if (left >= 8) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u].load(from[u], 8);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u].load(from[u], left);
+        }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             if (at + u >= end) break;
@@ -270,14 +267,16 @@ EmbedPlan embed_plan(const EmbedArgs &a)
     if ((a.vocab + p.ranges - 1) / p.ranges > kMostWidth) p.ranges = (a.vocab + kMostWidth - 1) / kMostWidth;
     p.width = (a.vocab + p.ranges - 1) / p.ranges;
     p.ranges = (a.vocab + p.width - 1) / p.width;
-    p.length = (a.rows + 2047) / 2048;
-    if (p.length < 16) p.length = 16;
+    // 16 rows a segment, or more where that makes 2048 of them; 8 where they are few and a workgroup's chain of loads is what takes the time (3001 rows of 1021 in
+    // fp32: 17 -> 11 us for the sums; 16384 rows of 2048 in bf16 in eights: 20 -> 21, and joining them 7 -> 12)
+    const bool few = a.rows <= 8192;
+    p.length = few ? 8 : (a.rows + 2047) / 2048 > 16 ? (a.rows + 2047) / 2048 : 16;
     p.segments = (a.rows + p.length - 1) / p.length;
+    const int sixteens = (a.rows + 15) / 16, room = few ? p.segments : sixteens < 1024 ? 1024 : sixteens < 2048 ? sixteens : 2048;   // (never less for more rows)
     auto whole = [](size_t n) { return (n + 255) / 256 * 256; };
     p.ids_at = 256 + whole((size_t)a.rows * 4);
-    p.absent_at = p.ids_at + whole((size_t)a.rows * 4);
-    p.parts_at = p.absent_at + whole((size_t)p.ranges * kWaves * 8);
-    p.bytes = p.parts_at + whole((size_t)p.segments * 2 * a.d * 4);
+    p.parts_at = p.ids_at + whole((size_t)a.rows * 4);
+    p.bytes = p.parts_at + whole((size_t)room * 2 * a.d * 4);
     return p;
 }
 
@@ -297,14 +296,13 @@ hipError_t backward(const EmbedArgs &a, const int64_t *token, const void *dX, vo
 {
     const EmbedPlan p = embed_plan(a);
     int *total = (int *)ws, *order = (int *)((char *)ws + 256), *ids = (int *)((char *)ws + p.ids_at);
-    uint64_t *absent = (uint64_t *)((char *)ws + p.absent_at);
     float *parts = (float *)((char *)ws + p.parts_at);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(p.ranges), dim3(64 * kWaves), 0, s, a, p, token, order, ids, total, absent);
+    // zeros: 256 KB a workgroup, at most two for each CU
+    const size_t bytes = accumulate ? 0 : (size_t)a.vocab * a.d * sizeof(T), blocks = (bytes + 262143) / 262144;
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(p.ranges + (unsigned)(blocks < 512 ? blocks : 512)), dim3(64 * kWaves), 0, s, a, p, token, order, ids, total, (char *)dW, bytes);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int zeros = accumulate ? 0 : p.ranges * ((p.width + 63) / 64);
-    hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(p.segments + zeros, (a.d + 2047) / 2048), dim3(256), 0, s, a, p, order, ids, total, absent, (const T *)dX, (T *)dW, parts,
-                       accumulate);
+    hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(p.segments, (a.d + 2047) / 2048), dim3(256), 0, s, a, p, order, ids, total, (const T *)dX, (T *)dW, parts, accumulate);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.segments == 1) return hipSuccess;

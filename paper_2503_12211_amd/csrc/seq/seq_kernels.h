@@ -17,7 +17,7 @@ struct EmbedArgs {
 // How the backward pass cuts its work: ranges of `width` ids, each sorted by one workgroup, and `segments` of `length` sorted rows.
 struct EmbedPlan {
     int ranges, width, length, segments;
-    size_t ids_at, absent_at, parts_at, bytes;   // of the workspace: rows sorted by id, ids in that order, bits of absent ids, sums of cut runs; all of it
+    size_t ids_at, parts_at, bytes;          // of the workspace: rows sorted by id, ids in that order, sums of cut runs; all of it
 };
 EmbedPlan embed_plan(const EmbedArgs &a);
 hipError_t launch_embed_forward(int dtype, const EmbedArgs &a, const int64_t *token, const void *W, void *X, hipStream_t s);
