@@ -9,12 +9,14 @@
 //
 // A workgroup takes a segment of a sequence, a head and 128 columns of v at most, chunk after chunk.  Where there are too few heads to fill the chip, a sequence has
 // several segments: a sweep without outputs first forms what each adds to the state, a small kernel joins these in order to the state in front of each
-// segment (decay_join_kernel), and all segments run at once.  That reads K and V twice (from the last-level cache, if they fit there).  A wavefront owns 32 columns of v: its part of S
-// stays in accumulators (dk x 32, fp32) all along.  Products are formed so that accumulators are the next product's operand as they lie:
+// segment (decay_join_kernel), and all segments run at once.  That reads K and V twice (largely from the last-level cache: 108 of 201 MB come from memory the second
+// time in the sizes below).
+// A wavefront owns 16 columns of v: its part of S stays in accumulators (dk x 16, fp32) all along, in 128 registers with all else, so that two workgroups share a
+// CU.  Products are formed so that accumulators are the next product's operand as they lie:
 //   P^T = K Q^T (tokens j x i)   ->   O^T += V^T P^T,      S (dk x columns) as S^T in   O^T = S^T Q^T
-// An accumulator's lane holds rows 8 (e / 4) + 4 h + e % 4 of its column (h = lane / 32), an operand's lane eight elements of the contraction, whose
-// order is free as long as both operands have it.  Contractions over tokens go in the accumulators' order; those over columns in the order of memory, as
-// columns are dealt to lanes such that the accumulators have it too (dealt).
+// An accumulator's lane holds rows 4 g + e of its column (g = lane / 16), an operand's lane eight elements of the contraction, whose order is free as long as
+// both operands have it: along the rows it is the order that two tiles of accumulators have (state_row), over tokens 8 g + e.  P is the same for all columns:
+// the wavefronts form a quarter of its tile each and share them through LDS, which is one more barrier a chunk and saves each wavefront three quarters of it.
 //
 // Chunks of 32 tokens come through a ring of LDS stages, loaded without a register between (rows of whole 16-byte pieces at such addresses; others go through
 // registers and one stage).
@@ -25,6 +27,12 @@
 // bf16 storage: operands that come from fp32 (P, S, V scaled by the decay up to the chunk's end) are given to the matrix cores as sums of bf16 numbers, two of
 // them (a relative error of 2^-16) for what goes into outputs that are rounded to bf16, three (2^-24) for what goes into the fp32 state.  With one, P's
 // and S's roundings would each be as large as the output's own.  fp32 storage: fp32 matrix instructions.
+//
+// What bounds it, 8192 tokens x 32 heads of 128 in bf16, 8 segments: states 43 us, join 8, outputs 82 (matrix cores busy for 30 % of it, vector unit, which splits S, V and P,
+// for half, wavefronts waiting for 40 %).  With the loads and stores alone the last takes 61, with the products alone 67: both at once are near what there is.
+// Tried without gain: matrix and vector instructions in turn by scheduling groups (equal), the products of P behind the state's update (3 % slower), the remainders of
+// a split by two-element dot products in the place of shifts and subtractions (6 % slower), 32 columns a wavefront and two of them on a SIMD (3 to 7 % slower but for
+// gradients of bf16, 3 % faster; fp32 a third slower).
 #pragma once
 #include "seq_kernels.h"
 #include "../lm/lm_device.h"
