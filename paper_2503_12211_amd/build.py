@@ -21,12 +21,12 @@ FLAGS = [
 
 
 def sources():
-    return sorted(CSRC.glob("*.hip")) + sorted((CSRC / "lm").glob("*.hip")) + sorted((CSRC / "seq").glob("*.hip"))
+    return sorted(CSRC.glob("*.hip")) + sorted((CSRC / "lm").glob("*.hip")) + sorted((HERE / "csrc_seq").glob("*.hip"))
 
 
 def build(force: bool = True, verbose: bool = False) -> Path:
     OBJ_DIR.mkdir(exist_ok=True)
-    headers = list(CSRC.glob("**/*.h")) + [HERE.parent / "include" / "stl.h"]
+    headers = list(CSRC.glob("**/*.h")) + list((HERE / "csrc_seq").glob("*.h")) + [HERE.parent / "include" / "stl.h"]
     newest_hdr = max(h.stat().st_mtime for h in headers)
 
     def compile_one(src: Path):

@@ -1,7 +1,7 @@
 // C ABI of the embedding, the norms and rotation of queries and keys, and attention with decay: argument validation and launch sequencing.
-#include "../../../include/stl.h"
+#include "../../include/stl.h"
 #include "seq_kernels.h"
-#include "../lm/lm_kernels.h"
+#include "../csrc/lm/lm_kernels.h"
 
 #include <cmath>
 #include <cstdarg>

@@ -31,12 +31,12 @@
 // What bounds it, 8192 tokens x 32 heads of 128 in bf16, 8 segments: states 43 us, join 8, outputs 82 (matrix cores busy for 30 % of it, vector unit, which splits S, V and P,
 // for half, wavefronts waiting for 40 %).  With the loads and stores alone the last takes 61, with the products alone 67: both at once are near what there is.
 // Tried without gain: matrix and vector instructions in turn by scheduling groups (equal), the products of P behind the state's update (3 % slower), the remainders of
-// a split by two-element dot products in the place of shifts and subtractions (6 % slower), 32 columns a wavefront and two of them on a SIMD (3 to 7 % slower but for
-// gradients of bf16, 3 % faster; fp32 a third slower).
+// a split by two-element dot products in the place of shifts and subtractions (6 % slower), 32 columns a wavefront and two of them on a SIMD (5 to 7 % slower but for
+// gradients of bf16, 3 % faster; fp32 a fifth slower).
 #pragma once
 #include "seq_kernels.h"
-#include "../lm/lm_device.h"
-#include "../stl_gemm_pipe.h"
+#include "../csrc/lm/lm_device.h"
+#include "../csrc/stl_gemm_pipe.h"
 
 #include <atomic>
 

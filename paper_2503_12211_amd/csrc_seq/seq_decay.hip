@@ -4,8 +4,9 @@
 namespace stl {
 namespace seq {
 
-// Up to so many tokens a sequence go one by one, with the state in registers (decay_few_kernel): a sweep's chunk is 32 tokens whatever it holds.
-constexpr int kFewTokens = 8;
+// Up to so many tokens a sequence go one by one, with the state in registers (decay_few_kernel): a sweep's chunk is 32 tokens whatever it holds.  6 tokens, in
+// brackets as a sweep, us: 64 sequences x 32 heads of 128: 68 (75); 8 x 32 of 128: 12 (12); 1 x 32 of 128: 7.5 (10); 8 tokens: 77 (76), 15 (12), 9 (10).
+constexpr int kFewTokens = 6;
 
 // A few tokens: memory bound by the state, which is read once and written once (64 tokens x 32 heads of 128: 268 MB in 53 us, 5.1 TB/s, the rate of a copy; one token of
 // 8 heads of 64: 4 us, a launch).  A thread has four columns of every RG-th row (RG: groups of COLS / 4 threads), RPT
@@ -144,7 +145,7 @@ size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 
 // Segments of a sequence.  They cost a sweep more, so only where a head has four of them at least for a workgroup a CU (and sweep), and of 128 tokens (fp32, whose
 // products take three times as long: 64).  More of them, of 8192 tokens x 32 heads: 132 us in 8, 138 in 16, 145 in 12; 4 x 2048 tokens x 16 heads, gradients: 156 us in
-// four, 168 in two, 182 in eight; 13 sequences of up to 777 tokens x 16 heads: 46 us in one piece, 76 in two.
+// four, 168 in two, 182 in eight; 13 sequences of up to 777 tokens x 16 heads: 54 us in one piece, 76 in two.
 int most_segments(int dtype, const DecayArgs &a)
 {
     const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns), most = 256 / groups, fit = a.length / (dtype ? 128 : 64);
@@ -228,8 +229,9 @@ size_t decay_workspace_bytes(int dtype, const DecayArgs &a, bool grads)
 hipError_t launch_decay_forward(int dtype, const DecayArgs &a, void *O, float *state_out, void *ws, hipStream_t s)
 {
     if (a.length <= kFewTokens) {
-        // 32 columns a workgroup where 128 would leave CUs without one (rows of 128 bytes in the place of 512)
-        const bool narrow = (int64_t)a.sequences * a.heads * ((a.dv + 127) / 128) < 1024;
+        // 32 columns a workgroup where 128 would leave lanes idle (256 x 8 heads of 64: 15 us for 28) or CUs without one; rows of 512 bytes elsewhere (64 tokens x 32 heads
+        // of 128: 54 us for 57)
+        const bool narrow = a.dv <= 96 || (int64_t)a.sequences * a.heads < 1024;
         if (dtype) return narrow ? few_tokens<bf16_t, 32>(a, O, state_out, s) : few_tokens<bf16_t, 128>(a, O, state_out, s);
         return narrow ? few_tokens<float, 32>(a, O, state_out, s) : few_tokens<float, 128>(a, O, state_out, s);
     }

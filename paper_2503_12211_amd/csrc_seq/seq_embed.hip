@@ -13,7 +13,7 @@
 // 16384 rows of 2048 in bf16, 32000 ids: 33 us (131 MB of zeros; the sort alone takes 17), 20 (96 MB, 4.7 TB/s) and 7 (a chain of loads: the commonest id has 102
 // segments); a forward call of 8192 rows of 4096: 21 us, 5.4 TB/s.
 #include "seq_kernels.h"
-#include "../lm/lm_device.h"
+#include "../csrc/lm/lm_device.h"
 
 namespace stl {
 namespace seq {

@@ -11,7 +11,7 @@
 // 8192 rows of 32 + 8 heads of 128 in bf16: 35 us, 4.7 TB/s (kernel 29).  Backward, 64 x 197 rows of 2 x 12 heads of 64: 35 us (3.3 TB/s; wavefronts wait for two thirds of
 // it, one turn of rows a workgroup whose angles come before its first load) and 5.
 #include "seq_kernels.h"
-#include "../lm/lm_device.h"
+#include "../csrc/lm/lm_device.h"
 
 namespace stl {
 namespace seq {

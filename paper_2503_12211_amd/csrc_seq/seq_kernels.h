@@ -1,7 +1,7 @@
 // Internal launcher interface between the C ABI (seq_api.hip) and the kernels of the embedding, the norms and rotation of queries and keys, and
 // attention with decay.
 #pragma once
-#include "../stl_kernels.h"
+#include "../csrc/stl_kernels.h"
 
 #include <stddef.h>
 #include <type_traits>

@@ -1,4 +1,4 @@
-// Runs one call of the library's C ABI on host buffers (tests/test_cpu_seq.py): as tests/cpu_emu/driver.cpp does, for the entry points of csrc/seq.
+// Runs one call of the library's C ABI on host buffers (tests/test_cpu_seq.py): as tests/cpu_emu/driver.cpp does, for the entry points of csrc_seq.
 //   driver CALL DIR key=value ... name:bytes ...   inputs DIR/<name>.in (absent: NULL), outputs DIR/<name>.out
 // An output starts as DIR/<name>.was where there is one, as ones bits otherwise.  The workspace is of exactly its size, filled with ones bits.
 #include "stl.h"

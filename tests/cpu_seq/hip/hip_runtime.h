@@ -1,4 +1,4 @@
-// The stand-in for the HIP runtime that runs kernels as they are meant to run (tests/cpu_emu/), with what the kernels of csrc/seq use beside.
+// The stand-in for the HIP runtime that runs kernels as they are meant to run (tests/cpu_emu/), with what the kernels of csrc_seq use beside.
 #pragma once
 #include "../../cpu_emu/hip/hip_runtime.h"
 inline unsigned long long __ballot(int v)

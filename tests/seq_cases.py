@@ -1,4 +1,4 @@
-"""Inputs, oracle results and error bounds that the CPU and GPU tests of csrc/seq share.
+"""Inputs, oracle results and error bounds that the CPU and GPU tests of csrc_seq share.
 
 Bounds.  An output is rounded to its type once, at most 2^-8 |O| for bf16 (2^-24 |O| for fp32).  Before it, sums are fp32: a chain of n additions, and the few
 products in front of and behind it, is off by at most (n + 32) 2^-24 times the same expression on absolute values.  A two-part bf16 operand is off by

@@ -16,22 +16,22 @@ from test_cpu_address_check import CLANG, CSRC, ROOT, _host_source, pytestmark  
 @pytest.fixture(scope="module")
 def driver(tmp_path_factory):
     work = tmp_path_factory.mktemp("cpu_seq")
-    (work / "csrc").mkdir()
     (work / "include").mkdir()
     shutil.copy(ROOT / "include" / "stl.h", work / "include" / "stl.h")
     meet = {'asm volatile("s_barrier" ::: "memory");': "emu_barrier();", 'asm volatile("" ::: "memory");': "emu_wave();",
             'asm volatile("" : "+s"(out_kind));': ";", '__device__ float fmul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");': "",
             r'asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");': "cpu_touch16(base + off, l);"}
     srcs = []
-    for f in sorted(CSRC.glob("**/*.hip")) + sorted(CSRC.glob("**/*.h")):
-        to = work / "csrc" / f.relative_to(CSRC)
-        to.parent.mkdir(exist_ok=True)
+    package = CSRC.parent
+    for f in sorted(package.glob("csrc*/**/*.hip")) + sorted(package.glob("csrc*/**/*.h")):
+        to = work / f.relative_to(package)
+        to.parent.mkdir(parents=True, exist_ok=True)
         to = to.with_suffix(".cpp") if f.suffix == ".hip" else to
-        text = f.read_text().replace("../../../include/stl.h", "stl.h")
+        text = f.read_text().replace("../../../include/stl.h", "stl.h").replace("../../include/stl.h", "stl.h")
         for device, host in meet.items():
             text = text.replace(device, host)
         to.write_text(_host_source(text))
-        if f.suffix == ".hip" and (f.parent.name == "seq" or f.stem in ("lm_residual", "lm_residual_f32")):
+        if f.suffix == ".hip" and (f.parent.name == "csrc_seq" or f.stem in ("lm_residual", "lm_residual_f32")):
             srcs.append(to)
     shutil.copy(ROOT / "tests" / "cpu_seq" / "driver.cpp", work / "driver.cpp")
     srcs.append(work / "driver.cpp")

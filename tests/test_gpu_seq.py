@@ -460,6 +460,14 @@ def test_decay_without_tokens_and_with_shared_heads(t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [3, 6, 7, 9])
+def test_decay_few_tokens(t, length):
+    """Around the number of tokens up to which they go one by one; heads enough for wide workgroups, and fewer; widths that end inside one."""
+    for sequences, heads, kv, dk, dv in ((3, 4, 2, 64, 64), (70, 16, 8, 40, 128), (129, 8, 8, 24, 97), (2, 2, 1, 256, 130), (40, 30, 30, 16, 96)):
+        check_decay(sequences, length, heads, kv, dk, dv, t, seed=length + dv, in_place=True)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
 @pytest.mark.parametrize("share", [1, 2])
 def test_decay_in_segments(t, share):
     """Few heads and long sequences, which come in segments: rows one after the other, far apart, packed, and not of whole pieces."""
