@@ -353,14 +353,17 @@ __device__ __forceinline__ void put8(char *rows, int r, int u, const Chunk<float
     *reinterpret_cast<f32x4_t *>(rows + piece_at(r, 2 * u + 1)) = c.b;
 }
 
-// One operand's share of a stage that a wavefront loads by LDS-DMA.  Instruction i brings 64 pieces, one a lane: four of each of 16 rows.  Where the row
-// ends before the groups do, or instructions are no multiple of the wavefronts, some of them bring the same again: all wavefronts issue as many.
+// 16 bytes a lane, from `base` + `off`, to LDS: lane l's to lds_wave_base + 16 l.
 __device__ __forceinline__ void dma16_at(const char *base, uint32_t off, uint32_t lds_wave_base)
 {
     const uint32_t l = __builtin_amdgcn_readfirstlane(lds_wave_base);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");
+    // M0 has to be written one wait state ahead of the load, a scalar register that a vector instruction writes (the base, where the compiler brings it from
+    // one) five; the compiler, which sees to that elsewhere, does not look into the statement
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");
 }
 
+// One operand's share of a stage that a wavefront loads by LDS-DMA.  Instruction i brings 64 pieces, one a lane: four of each of 16 rows.  Where the row
+// ends before the groups do, or instructions are no multiple of the wavefronts, some of them bring the same again: all wavefronts issue as many.
 template <typename T, int GROUPS, int NW>
 struct RingSource {
     static constexpr int kAll = 2 * GROUPS, kPer = (kAll + NW - 1) / NW, kInGroup = 64 / (int)sizeof(T);

@@ -20,7 +20,7 @@ def driver(tmp_path_factory):
     shutil.copy(ROOT / "include" / "stl.h", work / "include" / "stl.h")
     meet = {'asm volatile("s_barrier" ::: "memory");': "emu_barrier();", 'asm volatile("" ::: "memory");': "emu_wave();",
             'asm volatile("" : "+s"(out_kind));': ";", '__device__ float fmul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");': "",
-            r'asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");': "cpu_touch16(base + off, l);"}
+            r'asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l) : "memory", "m0");': "cpu_touch16(base + off, l);"}
     srcs = []
     package = CSRC.parent
     for f in sorted(package.glob("csrc*/**/*.hip")) + sorted(package.glob("csrc*/**/*.h")):
