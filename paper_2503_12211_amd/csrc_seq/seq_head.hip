@@ -236,6 +236,7 @@ __global__ __launch_bounds__(256, VEC && sizeof(T) == 2 ? 4 : 2) void head_back_
         if (heads == 0 || (!out && !g.dw[side])) continue;
         const size_t ld_in = a.ld_in[side], ld_up = a.ld_out[side];
         float dw[16] = {};
+        if (side > 0) __syncthreads();                           // everybody is done with the queries' weights and sums
         if ((int)threadIdx.x < plan.units) {
             float w[16];
 #pragma unroll
@@ -312,7 +313,6 @@ __global__ __launch_bounds__(256, VEC && sizeof(T) == 2 ? 4 : 2) void head_back_
             }
             if (at < a.d) parts[((size_t)blockIdx.x * 2 + side) * a.d + at] = v;
         }
-        __syncthreads();
     }
 }
 

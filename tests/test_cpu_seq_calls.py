@@ -1,0 +1,27 @@
+"""Calls of the embedding, the norms and rotation of queries and keys, and attention with decay that ask for a part of the outputs, come in many steps or lie at the
+ends of what is allowed, without a GPU (as tests/test_cpu_seq.py)."""
+import itertools
+
+import numpy as np
+import pytest
+
+from seq_cases import head_case
+from test_cpu_seq import driver, pytestmark  # noqa: F401
+
+HEAD_GRADS = ("dQ", "dK", "dw_q", "dw_k")
+
+
+@pytest.mark.parametrize("t,d,rot,adjacent", [("bf16", 64, 64, 0), ("f32", 50, 20, 1)])
+def test_any_set_of_head_gradients(driver, t, d, rot, adjacent):  # noqa: F811
+    """Every set of outputs has the bits of the call that asks for all of them: 70 heads, so that all wavefronts of a workgroup have some, weights of queries unlike
+    those of keys."""
+    rows, heads = 3, 70
+    c = head_case(rows, heads, heads, d, t, seed=1)
+    numbers = dict(rows=rows, heads=heads, kv_heads=heads, d=d, rot=rot, ld_q=heads * d, ld_k=heads * d, ld_qout=heads * d, ld_kout=heads * d, base=10000.0,
+                   dtype=int(t == "bf16"), flags=0x800 | 0x2000 * adjacent)
+    shapes = {"dQ": ((rows, heads, d), t), "dK": ((rows, heads, d), t), "dw_q": ((d,), "f32"), "dw_k": ((d,), "f32")}
+    full = driver("head_backward", numbers, c, shapes)
+    for n in range(1, 4):
+        for some in itertools.combinations(HEAD_GRADS, n):
+            got = driver("head_backward", numbers, c, {k: shapes[k] for k in some})
+            assert all(np.array_equal(got[k], full[k]) for k in some), some

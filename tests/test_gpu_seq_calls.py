@@ -1,0 +1,37 @@
+"""Calls of the embedding, the norms and rotation of queries and keys, and attention with decay that ask for a part of the outputs, come in many steps or lie at the
+ends of what is allowed, on the GPU."""
+import itertools
+
+import pytest
+import torch
+
+import paper_2503_12211_amd as stl
+from gpu_util import STL_DT
+from seq_cases import head_case
+from test_gpu_seq import ADJ, PRE, up
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("t,d,rot,adjacent", [("bf16", 64, 64, False), ("bf16", 128, 64, True), ("f32", 64, 64, False), ("f32", 50, 20, True), ("bf16", 256, 256, False)])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_any_set_of_head_gradients(rows, t, d, rot, adjacent):
+    """Every set of outputs has the bits of the call that asks for all of them: 70 heads, so that all wavefronts of a workgroup have some, weights of queries unlike
+    those of keys."""
+    heads, flags = 70, PRE | (ADJ if adjacent else 0)
+    c = {k: up(v) for k, v in head_case(rows, heads, heads, d, t, seed=1).items()}
+    prob = stl.HeadNormProblem(rows, heads, heads, d, rot, dtype=STL_DT[t])
+    n = stl.stl_head_norm_workspace_bytes(prob, flags)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    every = ("dQ", "dK", "dw_q", "dw_k")
+
+    def run(some):
+        out = {k: torch.full_like(c[k[1:]], 3.0) if k in ("dQ", "dK") else torch.full((d,), 3.0, device="cuda") for k in some}
+        stl.stl_head_norm_backward(prob, *(c[k] for k in ("Q", "K", "w_q", "w_k", "position", "dQout", "dKout")), *(out.get(k) for k in every), 0, ws, n, flags)
+        return out
+
+    full = run(every)
+    for size in range(1, 4):
+        for some in itertools.combinations(every, size):
+            for k, v in run(some).items():
+                assert torch.equal(v, full[k]), (some, k)
