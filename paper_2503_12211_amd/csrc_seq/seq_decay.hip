@@ -32,7 +32,8 @@ __global__ __launch_bounds__(256) void decay_few_kernel(const DecayArgs a, T *O,
     }
     double fall = a.log_decay ? (double)a.log_decay[head] : 0.0;
     fall = power(fall < -1e5 ? -1e5 : fall, 1);
-    const float by = (float)fall;
+    // lambda in two numbers: its rounding to fp32 has the same sign at every token, and thousands of calls would add it up (3000 tokens: a state off by 7e-5)
+    const float by = (float)fall, rest = (float)(fall - (double)by);
     const int share = a.heads / a.kv_heads;
     for (int t = 0; t < tokens.count; ++t) {
         const size_t row = (size_t)(tokens.first + (int64_t)t * (a.offset ? 1 : a.token_step));
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void decay_few_kernel(const DecayArgs a, T *O,
             const float k = lk[i], q = lq[i];                    // (there is LDS behind the last row too, and any value does)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                state[r][e] = fmaf(state[r][e], by, k * v[e]);
+                state[r][e] = fmaf(state[r][e], by, fmaf(state[r][e], rest, k * v[e]));
                 sum[e] = i < a.dk ? fmaf(q, state[r][e], sum[e]) : sum[e];
             }
         }

@@ -106,7 +106,22 @@ int main(int argc, char **argv)
         if (!back) {
             float *after = (float *)out("state_out");
             if (num["in_place"] && after) memcpy(after, state, outs["state_out"].second);
-            st = stl_decay_attention_forward(&p, in("Q"), in("K"), in("V"), decay, offset, num["in_place"] ? after : state, out("O"), after, block(n), n, nullptr);
+            if (num["step"]) {                                  // one sequence, so many tokens a call, whose state goes on in its place
+                stl_decay_attention_t some = p;
+                char *q = (char *)in("Q"), *k = (char *)in("K"), *v = (char *)in("V"), *o = (char *)out("O");
+                const int64_t size = dtype ? 2 : 4;
+                void *ws = block(n);
+                some.rows = some.length = whole("step");
+                for (st = 0; st == 0 && some.rows <= p.rows; some.rows += some.length) {
+                    stl_decay_attention_t one = some;
+                    const int64_t row = some.rows - some.length;
+                    one.rows = some.length;
+                    st = stl_decay_attention_forward(&one, q + row * p.ld_q * size, k + row * p.ld_k * size, v + row * p.ld_v * size, decay, nullptr, after,
+                                                     o + row * p.ld_o * size, after, ws, n, nullptr);
+                }
+            } else {
+                st = stl_decay_attention_forward(&p, in("Q"), in("K"), in("V"), decay, offset, num["in_place"] ? after : state, out("O"), after, block(n), n, nullptr);
+            }
         } else {
             st = stl_decay_attention_backward(&p, in("Q"), in("K"), in("V"), decay, offset, state, in("dO"), (const float *)in("dstate_out"), out("dQ"), out("dK"), out("dV"),
                                               (float *)out("dstate_in"), block(n), n, nullptr);

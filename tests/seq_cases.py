@@ -105,3 +105,27 @@ def decay_check(got, s, rows_of, t, scale, length, names):
             g, w, z = g[covered], w[covered], z[covered]
         close(g, w, z, kind, decay_chain(length, dk, dv) + 32 + share, n, operand)
     return want, covered
+
+
+def walk_case(length, dk, dv):
+    """One sequence of fp32 tokens, three heads whose decays last longer than it does and whose lambda is off in fp32 by about as much as it can be, and the state behind
+    the last token in 64 bits."""
+    rng = np.random.default_rng(5)
+    s = {"Q": rng.standard_normal((length, 3, dk)), "K": rng.standard_normal((length, 3, dk)), "V": rng.standard_normal((length, 3, dv)),
+         "state": rng.standard_normal((1, 3, dk, dv)) * np.sqrt(length)}
+    s = {k: v.astype(np.float32) for k, v in s.items()}
+    near = -np.linspace(1e-5, 1e-4, 30000).astype(np.float32)
+    off = np.exp(near.astype(np.float64))
+    off = np.abs(off.astype(np.float32).astype(np.float64) - off)
+    s["log_decay"] = np.array([near[at][off[at].argmax()] for at in np.array_split(np.arange(near.size), 3)])
+    lam, state = np.exp(s["log_decay"].astype(np.float64))[:, None, None], s["state"][0].astype(np.float64)
+    for k, v in zip(s["K"].astype(np.float64), s["V"].astype(np.float64)):
+        state = lam * state + k[:, :, None] * v[:, None, :]
+    return s, state
+
+
+def walk_bound(calls, roundings):
+    """Error of a state that is rounded to fp32 so many times in each of so many calls, relative to its norm.  A rounding is off by half a step at most, which is 2^-24 of the
+    value at most and by 2^-24 0.42 in the root mean square (evenly spread significands and remainders); roundings of different calls are independent, so that
+    n of them are off by 2^-24 0.42 sqrt(n) of a state that does not grow smaller on its way.  2^-24 sqrt(n) is more than twice that, of a norm over 64 entries or more."""
+    return 2.0 ** -24 * np.sqrt(calls * roundings)

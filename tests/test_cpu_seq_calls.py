@@ -5,7 +5,7 @@ import itertools
 import numpy as np
 import pytest
 
-from seq_cases import head_case
+from seq_cases import head_case, walk_bound, walk_case
 from test_cpu_seq import driver, pytestmark  # noqa: F401
 
 HEAD_GRADS = ("dQ", "dK", "dw_q", "dw_k")
@@ -25,3 +25,14 @@ def test_any_set_of_head_gradients(driver, t, d, rot, adjacent):  # noqa: F811
         for some in itertools.combinations(HEAD_GRADS, n):
             got = driver("head_backward", numbers, c, {k: shapes[k] for k in some})
             assert all(np.array_equal(got[k], full[k]) for k in some), some
+
+
+@pytest.mark.parametrize("step,length", [(1, 3000), (6, 6000)])
+def test_decay_token_by_token_for_long(driver, step, length):  # noqa: F811
+    """States after thousands of tokens, a few a call: lambda's own rounding, which has the same sign at each token, is not in them."""
+    s, want = walk_case(length, 8, 8)
+    numbers = dict(rows=length, sequences=1, length=length, heads=3, kv_heads=3, dk=8, dv=8, seq_step=step, token_step=1, ld_q=24, ld_k=24, ld_v=24, ld_o=24, scale=1.0,
+                   dtype=0, in_place=1, step=step)
+    got = driver("decay_forward", numbers, s, {"O": ((length, 3, 8), "f32"), "state_out": ((1, 3, 8, 8), "f32")})["state_out"][0]
+    off = np.linalg.norm(got - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
+    assert (off <= walk_bound(length, 2)).all(), off

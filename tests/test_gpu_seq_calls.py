@@ -2,13 +2,14 @@
 ends of what is allowed, on the GPU."""
 import itertools
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2503_12211_amd as stl
 from gpu_util import STL_DT
-from seq_cases import head_case
-from test_gpu_seq import ADJ, PRE, up
+from seq_cases import head_case, walk_bound, walk_case
+from test_gpu_seq import ADJ, PRE, down, up
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,17 @@ def test_any_set_of_head_gradients(rows, t, d, rot, adjacent):
         for some in itertools.combinations(every, size):
             for k, v in run(some).items():
                 assert torch.equal(v, full[k]), (some, k)
+
+
+@pytest.mark.parametrize("step", [1, 5])
+def test_decay_token_by_token_for_long(step):
+    """States after thousands of tokens, a few a call and in place: lambda's own rounding, which has the same sign at each token, is not in them."""
+    length = 6000
+    s, want = walk_case(length, 32, 32)
+    g = {k: up(v) for k, v in s.items()}
+    prob, O, state = stl.DecayAttentionProblem(step, 1, step, 3, dk=32, dtype=stl.STL_F32), torch.empty((step, 3, 32), device="cuda"), g["state"]
+    assert stl.stl_decay_attention_workspace_bytes(prob) == 0
+    for at in range(0, length, step):
+        stl.stl_decay_attention_forward(prob, *(g[n][at:at + step] for n in "QKV"), g["log_decay"], None, state, O, state)
+    off = np.linalg.norm(down(state)[0] - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
+    assert (off <= walk_bound(length, 2)).all(), off
