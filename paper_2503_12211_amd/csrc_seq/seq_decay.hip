@@ -104,9 +104,10 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecaySweeps s)
     for (int k = 0; k < full; ++k) {
         const f32x4_t add = next;
         if (k + 1 < full) next = load4(starts + (size_t)(k + 1) * each, left);
-        const float fall = (float)power(a, steps);
+        const double exact = power(a, steps);
+        const float fall = (float)exact, rest = (float)(exact - (double)fall);       // (as for single tokens: the rounding is in every call's)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], fall, add[e]);
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], fall, fmaf(v[e], rest, add[e]));
         put4(starts + (size_t)k * each, left, v);
         steps = p.seg_tokens;
     }

@@ -127,5 +127,6 @@ def walk_case(length, dk, dv):
 def walk_bound(calls, roundings):
     """Error of a state that is rounded to fp32 so many times in each of so many calls, relative to its norm.  A rounding is off by half a step at most, which is 2^-24 of the
     value at most and by 2^-24 0.42 in the root mean square (evenly spread significands and remainders); roundings of different calls are independent, so that
-    n of them are off by 2^-24 0.42 sqrt(n) of a state that does not grow smaller on its way.  2^-24 sqrt(n) is more than twice that, of a norm over 64 entries or more."""
+    n of them are off by 2^-24 0.42 sqrt(n), where what is rounded fades no faster than its error does, as here.  2^-24 sqrt(n) is more than twice that, of a norm over 64
+    entries or more."""
     return 2.0 ** -24 * np.sqrt(calls * roundings)

@@ -36,3 +36,14 @@ def test_decay_token_by_token_for_long(driver, step, length):  # noqa: F811
     got = driver("decay_forward", numbers, s, {"O": ((length, 3, 8), "f32"), "state_out": ((1, 3, 8, 8), "f32")})["state_out"][0]
     off = np.linalg.norm(got - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
     assert (off <= walk_bound(length, 2)).all(), off
+
+
+def test_decay_in_short_calls_for_long(driver):  # noqa: F811
+    """The same where a call has one chunk: 2500 calls of 8 tokens, sums of 32 products (24 of them zeros) and a product by lambda^8 a call."""
+    step, calls = 8, 2500
+    s, want = walk_case(step * calls, 8, 8)
+    numbers = dict(rows=step * calls, sequences=1, length=step * calls, heads=3, kv_heads=3, dk=8, dv=8, seq_step=step, token_step=1, ld_q=24, ld_k=24, ld_v=24, ld_o=24, scale=1.0,
+                   dtype=0, in_place=1, step=step)
+    got = driver("decay_forward", numbers, s, {"O": ((step * calls, 3, 8), "f32"), "state_out": ((1, 3, 8, 8), "f32")})["state_out"][0]
+    off = np.linalg.norm(got - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
+    assert (off <= walk_bound(calls, 9)).all(), (off, walk_bound(calls, 9))

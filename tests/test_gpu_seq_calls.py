@@ -50,3 +50,19 @@ def test_decay_token_by_token_for_long(step):
         stl.stl_decay_attention_forward(prob, *(g[n][at:at + step] for n in "QKV"), g["log_decay"], None, state, O, state)
     off = np.linalg.norm(down(state)[0] - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
     assert (off <= walk_bound(length, 2)).all(), off
+
+
+@pytest.mark.parametrize("length,step,roundings", [(40000, 8, 9), (40000, 32, 33), (200000, 512, 16 * 33)])
+def test_decay_in_short_calls_for_long(length, step, roundings):
+    """The same where a call has one chunk of up to 32 products and a product by a power of lambda, or several chunks in segments."""
+    s, want = walk_case(length, 32, 32)
+    g = {k: up(v) for k, v in s.items()}
+    probs = {n: stl.DecayAttentionProblem(n, 1, n, 3, dk=32, dtype=stl.STL_F32) for n in (step, length % step) if n}
+    n, O, state = stl.stl_decay_attention_workspace_bytes(probs[step]), torch.empty((step, 3, 32), device="cuda"), g["state"]
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    calls = -(-length // step)
+    for at in range(0, length, step):                            # (the last call takes what is left)
+        prob = probs[min(step, length - at)]
+        stl.stl_decay_attention_forward(prob, *(g[k][at:at + step] for k in "QKV"), g["log_decay"], None, state, O, state, ws, n)
+    off = np.linalg.norm(down(state)[0] - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
+    assert (off <= walk_bound(calls, roundings)).all(), (off, walk_bound(calls, roundings))
