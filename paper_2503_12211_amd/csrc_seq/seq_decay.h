@@ -594,12 +594,12 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
         out_advance = (reverse ? -kChunk : kChunk) * token_step * (int64_t)p.ldo * size, out_half = out_advance / 2;
     }
     // What the roundings of a chunk's lambda to fp32 have left out: made good by the next ones.  What the last one leaves out would have the same sign in call after call of
-    // few tokens (8 a call, 20000 of them: a state off by 3e-5), so it begins anywhere within half a step, by the state's own bits, and is nothing in the mean.  (Formed with
-    // two numbers, in the last chunk or where the state comes in, the product costs 1 to 8 % of a sweep or 4 to 12 registers that are not there.)
+    // few tokens (8 a call, 20000 of them: a state off by 3e-5), so it begins anywhere within half a step of the first product, by the state's own bits, and is nothing in
+    // the mean.  (Formed with two numbers, in the last chunk or where the state comes in, the product costs 1 to 8 % of a sweep or 4 to 12 registers that are not there.)
     uint32_t mixed = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) mixed ^= __float_as_uint(state[0][e >> 2][e & 3]);
-    float owed = OUT ? (float)(int32_t)(mixed * 0x9e3779b1u) * 0x1p-56f : 0.f;
+    float owed = OUT ? (float)(int32_t)(mixed * 0x9e3779b1u) * 0x1p-56f * through_first.high : 0.f;
 
     int stage = 0;
     for (int c = 0; c < chunks; ++c) {

@@ -5,8 +5,8 @@ import itertools
 import numpy as np
 import pytest
 
-from seq_cases import head_case, walk_bound, walk_case
-from test_cpu_seq import driver, pytestmark  # noqa: F401
+from seq_cases import decay_case, head_case, walk_bound, walk_case
+from test_cpu_seq import driver, pytestmark, run_decay  # noqa: F401
 
 HEAD_GRADS = ("dQ", "dK", "dw_q", "dw_k")
 
@@ -47,3 +47,17 @@ def test_decay_in_short_calls_for_long(driver):  # noqa: F811
     got = driver("decay_forward", numbers, s, {"O": ((step * calls, 3, 8), "f32"), "state_out": ((1, 3, 8, 8), "f32")})["state_out"][0]
     off = np.linalg.norm(got - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
     assert (off <= walk_bound(calls, 9)).all(), (off, walk_bound(calls, 9))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [5, 20, 40, 70])
+def test_decay_of_a_state_alone(driver, length, t):  # noqa: F811
+    """Keys and queries of zeros: states and their gradients fade by lambda^length, however little of them is left (half a step for each chunk's product, each rounding of
+    lambda^n, and what these begin with)."""
+    s = decay_case(length, 1, 9, 9, 20, 36, t, seed=2)
+    s["K"][:], s["Q"][:] = 0, 0
+    s["log_decay"][-1] = -1.0
+    left = np.exp(length * s["log_decay"].astype(np.float64))[:, None, None]
+    for grads, n, was in ((False, "state", "state"), (True, "dstate", "dstate_out")):
+        got = run_decay(driver, s, t, grads, length, 1, length, 9, 9, 20, 36, length, 1)[n]
+        assert (np.abs(got - left * s[was]) <= (length // 32 * 3 + 6) * 2.0 ** -24 * left * np.abs(s[was])).all()

@@ -8,8 +8,8 @@ import torch
 
 import paper_2503_12211_amd as stl
 from gpu_util import STL_DT
-from seq_cases import head_case, walk_bound, walk_case
-from test_gpu_seq import ADJ, PRE, down, up
+from seq_cases import decay_case, head_case, walk_bound, walk_case
+from test_gpu_seq import ADJ, PRE, decay_run, down, up
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,17 @@ def test_decay_in_short_calls_for_long(length, step, roundings):
         stl.stl_decay_attention_forward(prob, *(g[k][at:at + step] for k in "QKV"), g["log_decay"], None, state, O, state, ws, n)
     off = np.linalg.norm(down(state)[0] - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))
     assert (off <= walk_bound(calls, roundings)).all(), (off, walk_bound(calls, roundings))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [5, 20, 40, 70])
+def test_decay_of_a_state_alone(length, t):
+    """Keys and queries of zeros: states and their gradients fade by lambda^length, however little of them is left (half a step for each chunk's product, each rounding of
+    lambda^n, and what these begin with)."""
+    s = decay_case(length, 1, 9, 9, 20, 36, t, seed=2)
+    s["K"][:], s["Q"][:] = 0, 0
+    s["log_decay"][-1] = -1.0
+    left = np.exp(length * s["log_decay"].astype(np.float64))[:, None, None]
+    got = decay_run(s, t, dict(sequences=1, length=length))
+    for n, was in (("state", "state"), ("dstate", "dstate_out")):
+        assert (np.abs(down(got[n]) - left * s[was]) <= (length // 32 * 3 + 6) * 2.0 ** -24 * left * np.abs(s[was])).all(), n
