@@ -56,15 +56,16 @@ struct DecayPass {
     int share_a, share_b, share_v;
     void *O;                                 // storage type, or fp32 (out32); NULL: the state alone
     bool out32, reverse;
-    float out_scale;
+    // factors of probabilities, of what outputs take from the state, and of what goes into it: c, c and 1 forward in time; backward, where the state is the gradient as the
+    // formula has it (what is handed in belongs to it as it is), c, 1 and c
+    float out_scale, state_scale, value_scale;
     const float *log_decay;
     const int64_t *offset;
-    // states lie [sequence][head][da][dv], or [dv][da] (turned).  The first is multiplied by init_scale and, for the first token, lambda^init_power (1 forward in
-    // time, 0 backward, where what is given belongs to the last token itself); the last by last_scale lambda^last_power.
+    // states lie [sequence][head][da][dv], or [dv][da] (turned).  The first is multiplied, for the first token, by lambda^init_power (1 forward in time, 0 backward,
+    // where what is given belongs to the last token itself); the last by lambda^last_power.
     const float *init;
     float *last;
     bool turned;
-    float init_scale, last_scale;
     int init_power, last_power;
     // segments of seg_tokens (a multiple of 32).  starts [sequence][head][segments][da dv]: number s holds what segment s adds to the state, and behind decay_join_kernel
     // the state in front of segment s + 1; the last one `init` as it was, where the last state may be written over it.
@@ -432,7 +433,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     using O = Ops<T>;
     using Frag = typename O::Frag;
     constexpr int threads = S::threads;
-    // lambda^n, n = 0 .. 32; lambda^(31 - n), n = 0 .. 31; the same for the last chunk's tokens, and zeros behind them
+    // lambda^n, n = 0 .. 32; value_scale lambda^(31 - n), n = 0 .. 31; the same for the last chunk's tokens, and zeros behind them
     float *fade = reinterpret_cast<float *>(smem + S::stages * S::stage), *rising = fade + kChunk + 4, *ending = rising + kChunk;
     char *probs = smem + S::stages * S::stage + S::tables;       // the tile of probabilities of a chunk
 
@@ -509,9 +510,10 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     double a = p.log_decay ? (double)p.log_decay[head] : 0.0;
     a = a < -1e5 ? -1e5 : a;
     for (int i = (int)threadIdx.x; i <= kChunk; i += threads) {
-        const float f = (float)power(a, i);
-        fade[i] = f;
+        const double exact = power(a, i);
+        fade[i] = (float)exact;
         if (i < kChunk) {
+            const float f = (float)(p.value_scale * exact);
             const int last = (end - begin - 1) % kChunk - i;      // (no chunk: nobody reads it)
             rising[kChunk - 1 - i] = f;
             if (last >= 0) ending[last] = f;
@@ -523,13 +525,12 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     f32x4_t state[KT][2];
     const size_t each = (size_t)p.da * p.dv, state_at = ((size_t)b * p.heads + head) * each;
     const float *init = OUT ? p.init : nullptr;
-    float init_scale = p.init_scale;
     size_t init_at = state_at;
     int power_of_first = p.init_power;                           // of lambda, from the state to the next token
     if (OUT && p.segments > 1 && (seg > 0 || (init && p.last))) {
         init = p.starts;
         init_at = (((size_t)b * p.heads + head) * p.segments + (seg > 0 ? seg - 1 : p.segments - 1)) * each;
-        if (seg > 0) init_scale = 1.f, power_of_first = 1;
+        if (seg > 0) power_of_first = 1;
     }
     // (loads of elements that there are not go to the last ones and are dropped: without a branch all of them are in flight at once)
     const int j = z * kDecayColumns + col + n, j_in = j < p.dv ? j : p.dv - 1;
@@ -553,7 +554,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) state[k][t][e] = 32 * k + state_row(g, t, e) < p.da && j < p.dv ? init_scale * state[k][t][e] : 0.f;
+                for (int e = 0; e < 4; ++e) state[k][t][e] = 32 * k + state_row(g, t, e) < p.da && j < p.dv ? state[k][t][e] : 0.f;
     } else {
 #pragma unroll
         for (int k = 0; k < KT; ++k) state[k][0] = state[k][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -579,8 +580,8 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
             near[e] = ago >= 0 ? p.out_scale * fade[ago >= 0 ? ago : 0] : 0.f;
         }
     }
-    float since[2] = {};                                         // c lambda^(tokens from the state to n and n + 16)
-    if (OUT) since[0] = p.out_scale * fade[n + power_of_first], since[1] = p.out_scale * fade[n + 16 + power_of_first];
+    float since[2] = {};                                         // state_scale lambda^(tokens from the state to n and n + 16)
+    if (OUT) since[0] = p.state_scale * fade[n + power_of_first], since[1] = p.state_scale * fade[n + 16 + power_of_first];
     // where this lane's outputs of the next chunk go (and those of 16 tokens on), and how many of its columns there are (none: no outputs); bit 0: in fp32,
     // bit 1: not all columns of the wavefront
     char *out_at = nullptr;
@@ -713,13 +714,13 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
                 else put4((float *)to, out_left, out[half]);
             }
         if (OUT) out_at += out_advance;
-        if (OUT && !power_of_first) since[0] = p.out_scale * fade[n + 1], since[1] = p.out_scale * fade[n + 17];
+        if (OUT && !power_of_first) since[0] = p.state_scale * fade[n + 1], since[1] = p.state_scale * fade[n + 17];
         power_of_first = 1;
         if (RING) stage = stage + 1 < S::stages ? stage + 1 : 0;
     }
     if (OUT ? final && p.last : true) {
         float *to = OUT ? p.last + state_at : p.starts + (((size_t)b * p.heads + head) * p.segments + seg) * each;
-        const float by = OUT ? (float)(p.last_scale * (tokens.count > 0 ? power(a, p.last_power) : 1.0)) : 1.f;
+        const float by = OUT ? (float)(tokens.count > 0 ? power(a, p.last_power) : 1.0) : 1.f;
         float *column = to + j * (p.turned ? p.da : 1);
         const size_t step_i = p.turned ? 1 : p.dv;
         if (j < p.dv)

@@ -96,7 +96,6 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecaySweeps s)
     if (p.init) {
         v = load4(p.init + (size_t)bh * each + at, left);
         put4(starts + (size_t)(p.segments - 1) * each, left, v);
-        v *= p.init_scale;
     }
     int steps = p.seg_tokens - 1 + p.init_power;
     const int full = (tokens.count - 1) / p.seg_tokens;          // segments with another behind them
@@ -165,7 +164,7 @@ DecayPass common(int dtype, const DecayArgs &a)
     p.rows = a.rows, p.sequences = a.sequences, p.length = a.length, p.heads = a.heads, p.seq_step = a.seq_step, p.token_step = a.token_step;
     p.log_decay = a.log_decay, p.offset = a.offset;
     p.share_a = p.share_b = p.share_v = 1;
-    p.out_scale = a.scale, p.init_scale = p.last_scale = 1.f;
+    p.out_scale = p.state_scale = a.scale, p.value_scale = 1.f;
     cut(a, most_segments(dtype, a), &p.segments, &p.seg_tokens);
     return p;
 }
@@ -274,13 +273,13 @@ hipError_t launch_decay_backward(int dtype, const DecayArgs &a, const DecayGrads
     f.share_b = f.share_v = share;
     f.init = a.state, f.init_power = 1;
     f.starts = starts[0];
-    // its gradient backward in time, from Q and dO, held without the factor c, which its outputs have
+    // its gradient backward in time, from Q and dO
     DecayPass r = common(dtype, a);
     r.reverse = true;
     r.da = a.dk, r.dv = a.dv;
     r.B = a.Q, r.ldb = a.ld_q, r.V = g.dO, r.ldv = a.ld_o;
-    r.init = g.dstate_out, r.init_scale = 1.f / a.scale;
-    r.last_scale = a.scale, r.last_power = 1;
+    r.init = g.dstate_out, r.state_scale = 1.f, r.value_scale = a.scale;
+    r.last_power = 1;
     r.starts = starts[1];
     const bool back = g.dK || g.dV || g.dstate_in;
     hipError_t e = hipSuccess;

@@ -5,7 +5,7 @@ import itertools
 import numpy as np
 import pytest
 
-from seq_cases import decay_case, head_case, walk_bound, walk_case
+from seq_cases import decay_case, decay_check, head_case, narrow, walk_bound, walk_case, wide
 from test_cpu_seq import driver, pytestmark, run_decay  # noqa: F401
 
 HEAD_GRADS = ("dQ", "dK", "dw_q", "dw_k")
@@ -61,3 +61,25 @@ def test_decay_of_a_state_alone(driver, length, t):  # noqa: F811
     for grads, n, was in ((False, "state", "state"), (True, "dstate", "dstate_out")):
         got = run_decay(driver, s, t, grads, length, 1, length, 9, 9, 20, 36, length, 1)[n]
         assert (np.abs(got - left * s[was]) <= (length // 32 * 3 + 6) * 2.0 ** -24 * left * np.abs(s[was])).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("scale,up,after", [(2.0 ** -100, 2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** -60, 2.0 ** -60), (1e-30, 1.0, 1e9), (1e30, 1e-30, 1e-12)])
+def test_decay_gradients_of_scales_far_from_one(driver, scale, up, after, t):  # noqa: F811
+    """The state's gradient is held as the formula has it: neither it nor what is handed in is divided by the scale."""
+    s = decay_case(70, 1, 2, 1, 20, 36, t, seed=3)
+    s["dO"], s["dstate_out"] = narrow(wide(s["dO"], t) * up, t), (s["dstate_out"].astype(np.float64) * after).astype(np.float32)
+    at = [list(range(70))]
+    got = run_decay(driver, s, t, True, 70, 1, 70, 2, 1, 20, 36, 70, 1, scale=scale)
+    decay_check(got, s, at, t, float(np.float32(scale)), 70, ("dQ", "dK", "dV", "dstate"))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_decay_gradients_of_states_without_tokens_pass_through(driver, t):  # noqa: F811
+    """Sequences without tokens: the same bits, whatever the scale; states alike."""
+    s = decay_case(40, 3, 2, 1, 20, 36, t, seed=4)
+    offset = np.array([0, 0, 40, 40], np.int64)
+    got = run_decay(driver, s, t, True, 40, 3, 40, 2, 1, 20, 36, 0, 0, offset, scale=0.7)
+    assert all(np.array_equal(got["dstate"][b], s["dstate_out"][b]) for b in (0, 2))
+    got = run_decay(driver, s, t, False, 40, 3, 40, 2, 1, 20, 36, 0, 0, offset, scale=0.7)
+    assert all(np.array_equal(got["state"][b], s["state"][b]) for b in (0, 2))

@@ -8,10 +8,11 @@ import torch
 
 import paper_2503_12211_amd as stl
 from gpu_util import STL_DT
-from seq_cases import decay_case, head_case, walk_bound, walk_case
+from seq_cases import decay_case, decay_check, head_case, narrow, walk_bound, walk_case, wide
 from test_gpu_seq import ADJ, PRE, decay_run, down, up
 
 pytestmark = pytest.mark.gpu
+GRADS = ("dQ", "dK", "dV", "dstate")
 
 
 @pytest.mark.parametrize("t,d,rot,adjacent", [("bf16", 64, 64, False), ("bf16", 128, 64, True), ("f32", 64, 64, False), ("f32", 50, 20, True), ("bf16", 256, 256, False)])
@@ -80,3 +81,24 @@ def test_decay_of_a_state_alone(length, t):
     got = decay_run(s, t, dict(sequences=1, length=length))
     for n, was in (("state", "state"), ("dstate", "dstate_out")):
         assert (np.abs(down(got[n]) - left * s[was]) <= (length // 32 * 3 + 6) * 2.0 ** -24 * left * np.abs(s[was])).all(), n
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [70, 700])
+@pytest.mark.parametrize("scale,more,after", [(2.0 ** -100, 2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** -60, 2.0 ** -60), (1e-30, 1.0, 1e9), (1e30, 1e-30, 1e-12)])
+def test_decay_gradients_of_scales_far_from_one(length, scale, more, after, t):
+    """The state's gradient is held as the formula has it: neither it nor what is handed in is divided by the scale.  In one piece and in segments."""
+    s = decay_case(length, 1, 2, 1, 20, 36, t, seed=3)
+    s["dO"], s["dstate_out"] = narrow(wide(s["dO"], t) * more, t), (s["dstate_out"].astype(np.float64) * after).astype(np.float32)
+    got = decay_run(s, t, dict(sequences=1, length=length), scale)
+    decay_check({k: down(got[k]) for k in GRADS}, s, [list(range(length))], t, float(np.float32(scale)), length, GRADS)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_decay_gradients_of_states_without_tokens_pass_through(t):
+    """Sequences without tokens: the same bits, whatever the scale; states alike."""
+    for length in (40, 700):
+        s = decay_case(length, 3, 2, 1, 20, 36, t, seed=4)
+        got = decay_run(s, t, dict(sequences=3, length=length, offset=np.array([0, 0, length, length], np.int64)), 0.7)
+        for b in (0, 2):
+            assert torch.equal(got["dstate"][b], up(s["dstate_out"][b])) and torch.equal(got["state"][b], up(s["state"][b]))
