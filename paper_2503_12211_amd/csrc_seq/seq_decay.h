@@ -426,7 +426,7 @@ struct Two {
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
 
 template <typename T, int KT, int NW, bool OUT, bool RING>
-__device__ __forceinline__ void decay_body(const DecayPass &p)
+__device__ __forceinline__ void decay_body(const DecayPass &p, int first)
 {
     extern __shared__ __align__(16) char smem[];
     using S = DecayShape<T, KT, NW, OUT, RING>;
@@ -438,7 +438,7 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
     char *probs = smem + S::stages * S::stage + S::tables;       // the tile of probabilities of a chunk
 
     const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
-    int at = (int)blockIdx.x;
+    int at = first + (int)blockIdx.x;
     const int z = at % blocks;
     at /= blocks;
     const int seg = at % p.segments;
@@ -738,12 +738,12 @@ __device__ __forceinline__ void decay_body(const DecayPass &p)
 constexpr int kMostSweeps = 3;
 struct DecaySweeps {
     DecayPass pass[kMostSweeps];
-    int count;
+    int count, first;                        // (first: the number of a launch's first workgroup)
 };
 template <typename T, int KT, int NW, bool OUT, bool RING>
 __global__ __launch_bounds__(64 * NW, decay_waves(sizeof(T), KT)) void decay_kernel(const DecaySweeps s)
 {
-    decay_body<T, KT, NW, OUT, RING>(s.pass[blockIdx.y]);
+    decay_body<T, KT, NW, OUT, RING>(s.pass[blockIdx.y], s.first);
 }
 
 template <typename T, int KT, int NW, bool OUT, bool RING>
@@ -755,9 +755,16 @@ hipError_t launch_shape(const DecaySweeps &sw, hipStream_t s)
     const int blocks = (p.dv + kDecayColumns - 1) / kDecayColumns;
     const hipError_t e = allow_lds((const void *)decay_kernel<T, KT, NW, OUT, RING>, S::lds, S::lds, granted);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)((size_t)p.sequences * p.heads * p.segments * blocks), sw.count);
-    hipLaunchKernelGGL((decay_kernel<T, KT, NW, OUT, RING>), grid, dim3(S::threads), S::lds, s, sw);
-    return hipGetLastError();
+    // (a dimension's threads have to fit into 32 bits: at most half as many a launch)
+    constexpr int kMost = (int)((1u << 31) / S::threads);
+    DecaySweeps part = sw;
+    for (int all = p.sequences * p.heads * p.segments * blocks, at = 0; at < all; at += kMost) {
+        part.first = at;
+        hipLaunchKernelGGL((decay_kernel<T, KT, NW, OUT, RING>), dim3(all - at < kMost ? all - at : kMost, sw.count), dim3(S::threads), S::lds, s, part);
+        const hipError_t launched = hipGetLastError();
+        if (launched != hipSuccess) return launched;
+    }
+    return hipSuccess;
 }
 
 inline int key_tiles(int da) { return da <= 128 ? (da + 31) / 32 : 8; }

@@ -83,3 +83,28 @@ def test_decay_gradients_of_states_without_tokens_pass_through(driver, t):  # no
     assert all(np.array_equal(got["dstate"][b], s["dstate_out"][b]) for b in (0, 2))
     got = run_decay(driver, s, t, False, 40, 3, 40, 2, 1, 20, 36, 0, 0, offset, scale=0.7)
     assert all(np.array_equal(got["state"][b], s["state"][b]) for b in (0, 2))
+
+
+@pytest.mark.parametrize("dk,dv", [(1, 256), (256, 1), (129, 129), (128, 128), (33, 97)])
+@pytest.mark.parametrize("length", [1, 7])
+def test_decay_launches_of_the_most_heads(driver, monkeypatch, tmp_path, length, dk, dv):  # noqa: F811
+    """As many heads of all sequences as are allowed: no launch has more threads than 32 bits count in a dimension, and together they have every workgroup."""
+    most, t = 4194304, "bf16"
+    s = {k: np.zeros((length, w), np.uint16) for k, w in (("Q", dk), ("K", dk), ("V", dv), ("dO", dv))}
+    s.update(log_decay=None, state=None, dstate_out=None)
+    offset = np.full(most + 1, length, np.int64)
+    offset[0] = 0
+    numbers = dict(rows=length, sequences=most, length=length, heads=1, kv_heads=1, dk=dk, dv=dv, seq_step=0, token_step=0, ld_q=dk, ld_k=dk, ld_v=dv, ld_o=dv, scale=1.0, dtype=1)
+    inputs = {"offset": offset, **{k: s[k] for k in ("Q", "K", "V", "dO")}}
+    for call, outs in (("decay_forward", {"O": dv}), ("decay_backward", {"dQ": dk, "dK": dk, "dV": dv})):
+        to = tmp_path / call
+        monkeypatch.setenv("STL_LAUNCHES", str(to))
+        driver(call, numbers, inputs, {k: ((length, w), t) for k, w in outs.items()})
+        launches = [ln.split(maxsplit=4) for ln in to.read_text().splitlines()]
+        assert all(int(x) * int(threads) < 1 << 32 and int(y) < 1 << 16 and int(z) < 1 << 16 for x, y, z, threads, _ in launches), launches
+        groups = sum(int(x) * int(y) for x, y, z, threads, _ in launches)
+        if call == "decay_backward":
+            blocks = sum(-(-w // 128) for w in (dk, dk, dv))
+        else:
+            blocks = -(-dv // (32 if length == 1 and dv <= 96 else 128))
+        assert groups == most * blocks, launches

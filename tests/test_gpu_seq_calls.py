@@ -7,9 +7,9 @@ import pytest
 import torch
 
 import paper_2503_12211_amd as stl
-from gpu_util import STL_DT
+from gpu_util import STL_DT, TORCH_DT
 from seq_cases import decay_case, decay_check, head_case, narrow, walk_bound, walk_case, wide
-from test_gpu_seq import ADJ, PRE, decay_run, down, up
+from test_gpu_seq import ADJ, PRE, decay_problem, decay_run, down, up
 
 pytestmark = pytest.mark.gpu
 GRADS = ("dQ", "dK", "dV", "dstate")
@@ -102,3 +102,22 @@ def test_decay_gradients_of_states_without_tokens_pass_through(t):
         got = decay_run(s, t, dict(sequences=3, length=length, offset=np.array([0, 0, length, length], np.int64)), 0.7)
         for b in (0, 2):
             assert torch.equal(got["dstate"][b], up(s["dstate_out"][b])) and torch.equal(got["state"][b], up(s["state"][b]))
+
+
+@pytest.mark.parametrize("t,dk,dv", [("bf16", 16, 136), ("f32", 130, 8)])
+def test_decay_of_the_most_heads(t, dk, dv):
+    """As many heads of all sequences as are allowed, in more workgroups than one launch has room for: all but the first and the last few sequences are empty."""
+    most, length, rows = 4194304, 9, 40
+    s = decay_case(rows, 1, 1, 1, dk, dv, t, seed=1, states=False)
+    offset = np.full(most + 1, 16, np.int64)
+    offset[:3], offset[-3:] = [0, 9, 16], [16, 25, 32]
+    at = dict(sequences=most, length=length, offset=offset)
+    prob, g = decay_problem(s, t, at, 0.7), {k: up(v) for k, v in s.items()}
+    out = {n: torch.full(s[like].shape, float("nan"), dtype=TORCH_DT[t], device="cuda") for n, like in (("O", "dO"), ("dQ", "Q"), ("dK", "K"), ("dV", "V"))}
+    where, n = up(offset), stl.stl_decay_attention_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    stl.stl_decay_attention_forward(prob, g["Q"], g["K"], g["V"], g["log_decay"], where, None, out["O"], None, ws, n)
+    stl.stl_decay_attention_backward(prob, g["Q"], g["K"], g["V"], g["log_decay"], where, None, g["dO"], None, out["dQ"], out["dK"], out["dV"], None, ws, n)
+    rows_of = [list(range(9)), list(range(9, 16)), list(range(16, 25)), list(range(25, 32))]
+    _, covered = decay_check({k: down(v) for k, v in out.items()}, s, rows_of, t, 0.7, length, ("O", "dQ", "dK", "dV"))
+    assert all(bool(torch.isnan(v[32:]).all()) for v in out.values()) and covered[:32].all()
