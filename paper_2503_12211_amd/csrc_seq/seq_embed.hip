@@ -31,10 +31,12 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a, int per, 
     const int64_t id = token[row];
     Chunk<T> c;
     c.fill(0.f);
-    if (id >= 0 && id < a.vocab) c.load(W + (size_t)id * a.d + at, left);
+    const bool there = id >= 0 && id < a.vocab;
+    if (there) c.load(W + (size_t)id * a.d + at, left);
+    const float scale = there ? a.scale : 0.f;                   // (zeros also where the scale is no finite number)
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = a.scale * c.get(e);
+    for (int e = 0; e < 8; ++e) v[e] = scale * c.get(e);
     Chunk<T>::store(X + row * a.d + at, left, v);
 }
 

@@ -5,7 +5,7 @@ import itertools
 import numpy as np
 import pytest
 
-from seq_cases import decay_case, decay_check, head_case, narrow, walk_bound, walk_case, wide
+from seq_cases import decay_case, decay_check, embed_case, head_case, narrow, walk_bound, walk_case, wide
 from test_cpu_seq import driver, pytestmark, run_decay  # noqa: F401
 
 HEAD_GRADS = ("dQ", "dK", "dw_q", "dw_k")
@@ -108,3 +108,17 @@ def test_decay_launches_of_the_most_heads(driver, monkeypatch, tmp_path, length,
         else:
             blocks = -(-dv // (32 if length == 1 and dv <= 96 else 128))
         assert groups == most * blocks, launches
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [np.inf, np.nan])
+def test_embed_rows_without_a_token_are_zeros_whatever_the_scale(driver, scale, t):  # noqa: F811
+    rows, d, vocab = 40, 21, 30
+    c = embed_case(rows, d, vocab, t, seed=1, tokens="even")
+    there = (c["token"] >= 0) & (c["token"] < vocab)
+    numbers = dict(rows=rows, d=d, vocab=vocab, scale=scale, dtype=int(t == "bf16"), accumulate=0)
+    got = driver("embed_forward", numbers, {k: c[k] for k in ("token", "W")}, {"X": ((rows, d), t)})["X"]
+    assert not there.all() and not got[~there].any() and not np.isfinite(got[there]).any()
+    got = driver("embed_backward", numbers, {k: c[k] for k in ("token", "dX")}, {"dW": ((vocab, d), t)})["dW"]
+    absent = np.setdiff1d(np.arange(vocab), c["token"])
+    assert len(absent) and not got[absent].any() and not np.isfinite(np.delete(got, absent, 0)).any()

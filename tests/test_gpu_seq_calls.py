@@ -121,3 +121,12 @@ def test_decay_of_the_most_heads(t, dk, dv):
     rows_of = [list(range(9)), list(range(9, 16)), list(range(16, 25)), list(range(25, 32))]
     _, covered = decay_check({k: down(v) for k, v in out.items()}, s, rows_of, t, 0.7, length, ("O", "dQ", "dK", "dV"))
     assert all(bool(torch.isnan(v[32:]).all()) for v in out.values()) and covered[:32].all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan")])
+def test_embed_rows_without_a_token_are_zeros_whatever_the_scale(scale, t):
+    token, W = torch.tensor([3, -100, 0, 30, 2 ** 40, 29], device="cuda"), torch.randn(30, 21, device="cuda").to(TORCH_DT[t])
+    X = torch.empty((6, 21), dtype=W.dtype, device="cuda")
+    stl.stl_embed_forward(stl.EmbedProblem(6, 21, 30, scale, STL_DT[t]), token, W, X)
+    assert not X[[1, 3, 4]].any() and not torch.isfinite(X[[0, 2, 5]]).any()
