@@ -443,7 +443,8 @@ stl_status_t stl_head_norm_backward(const stl_head_norm_t *prob, const void *Q, 
  * dv, O: heads of dv.  They may be parts of the rows of one matrix; these pointers are aligned to an element, the others to 16 bytes.  Storage dtype; states fp32,
  * sequences x heads x dk x dv, decays fp32, -infinity (the present token alone) to 0; NULL: zeros.
  * Which rows: offset NULL: token t of sequence b is row b seq_step + t token_step, all sequences have `length` tokens.  seq_step >= length with token_step 1 has one
- * sequence after the other, token_step >= sequences with seq_step 1 one position after the other; rows that two tokens share are refused.
+ * sequence after the other, token_step >= sequences with seq_step 1 one position after the other; rows that two tokens share are refused.  A distance that no two
+ * tokens have (one sequence, one token) is not looked at.
  * offset (sequences + 1 int64, ascending): sequence b has the rows offset[b] .. offset[b + 1] - 1, the first `length` of them if there are more; it may have
  * none.  Offsets are on the device: what lies outside 0 .. rows is cut off.  Rows that no sequence has are not read and left as they are.
  * state_in: NULL (zeros) or the states in front of the first tokens; state_out: NULL or the states behind the last (state_in's where there is no token).

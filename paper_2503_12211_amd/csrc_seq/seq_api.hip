@@ -132,14 +132,16 @@ stl_status_t decay_rows(const char *fn, const stl_decay_attention_t *p, const in
         return STL_OK;
     }
     if (p->length == 0) return STL_OK;
-    if (p->seq_step < 0 || p->token_step < 0 || p->seq_step > p->rows || p->token_step > p->rows)
+    // (distances that no two tokens have are not looked at)
+    const int64_t seq_step = p->sequences > 1 ? p->seq_step : 0, token_step = p->length > 1 ? p->token_step : 0;
+    if (seq_step < 0 || token_step < 0 || seq_step > p->rows || token_step > p->rows)
         return fail(STL_ERR_INVALID_ARG, "%s: seq_step=%lld token_step=%lld with %lld rows", fn, (long long)p->seq_step, (long long)p->token_step, (long long)p->rows);
-    const int64_t tokens = (p->length - 1) * p->token_step, seqs = (p->sequences - 1) * p->seq_step;
+    const int64_t tokens = (p->length - 1) * token_step, seqs = (p->sequences - 1) * seq_step;
     if (tokens + seqs >= p->rows) return fail(STL_ERR_INVALID_ARG, "%s: the last token lies in row %lld of %lld", fn, (long long)(tokens + seqs), (long long)p->rows);
-    const bool one_by_one = (p->sequences == 1 || p->seq_step > tokens) && (p->length == 1 || p->token_step > 0);
-    const bool side_by_side = (p->length == 1 || p->token_step > seqs) && (p->sequences == 1 || p->seq_step > 0);
+    const bool one_by_one = (p->sequences == 1 || seq_step > tokens) && (p->length == 1 || token_step > 0);
+    const bool side_by_side = (p->length == 1 || token_step > seqs) && (p->sequences == 1 || seq_step > 0);
     if (!one_by_one && !side_by_side) return fail(STL_ERR_INVALID_ARG, "%s: two tokens share a row", fn);
-    a->seq_step = (int)p->seq_step, a->token_step = (int)p->token_step;
+    a->seq_step = (int)seq_step, a->token_step = (int)token_step;
     return STL_OK;
 }
 

@@ -5,6 +5,7 @@ import itertools
 import numpy as np
 import pytest
 
+from oracle import seq
 from seq_cases import decay_case, decay_check, embed_case, head_case, narrow, walk_bound, walk_case, wide
 from test_cpu_seq import driver, pytestmark, run_decay  # noqa: F401
 
@@ -122,3 +123,13 @@ def test_embed_rows_without_a_token_are_zeros_whatever_the_scale(driver, scale, 
     got = driver("embed_backward", numbers, {k: c[k] for k in ("token", "dX")}, {"dW": ((vocab, d), t)})["dW"]
     absent = np.setdiff1d(np.arange(vocab), c["token"])
     assert len(absent) and not got[absent].any() and not np.isfinite(np.delete(got, absent, 0)).any()
+
+
+@pytest.mark.parametrize("sequences,length,seq_step,token_step,rows", [(1, 5, 10, 2, 9), (1, 20, 1 << 40, 3, 58), (3, 1, 2, 100, 5), (2, 1, 1, 1 << 50, 2), (1, 1, -7, -7, 1)])
+def test_decay_distances_that_no_token_has_are_not_checked(driver, sequences, length, seq_step, token_step, rows):  # noqa: F811
+    """From sequence to sequence where there is one, from token to token where a sequence has one."""
+    s = decay_case(rows, sequences, 2, 1, 8, 12, "f32", seed=length)
+    at = seq.decay_rows(sequences, length, seq_step, token_step)
+    for grads, names in ((False, ("O", "state")), (True, ("dQ", "dK", "dV", "dstate"))):
+        got = run_decay(driver, s, "f32", grads, rows, sequences, length, 2, 1, 8, 12, seq_step, token_step)
+        decay_check(got, s, at, "f32", 0.7, length, names)
