@@ -392,8 +392,8 @@ typedef struct {
 } stl_embed_t;
 stl_status_t stl_embed_forward(const stl_embed_t *prob, const int64_t *token, const void *W, void *X, void *stream);
 /*
- * Backward: dW[v] = scale * sum of dX[i] over the rows i with token[i] = v, in fp32 and in the order of the rows, rounded once.  The same bits from run
- * to run.  dX: rows x d, dW: vocab x d (out, storage dtype).
+ * Backward: dW[v] = scale * sum of dX[i] over the rows i with token[i] = v, in fp32, rounded once.  Its order depends on tokens and sizes alone (the rows of a token in
+ * segments of 8, 16 or more, in their order; segments in four sums in turn), so the bits are the same from run to run.  dX: rows x d, dW: vocab x d (out, storage dtype).
  * accumulate: 0 writes all of dW, zeros for ids that no row has (also with no rows); 1 adds to the rows of dW whose ids occur and leaves the others alone, as
  * tied weights need it behind stl_vocab_loss_backward.
  * ws / ws_bytes: at least stl_embed_workspace_bytes(prob): 8 bytes a row and fp32 sums of 8 d bytes for each 8 or 16 rows, at most 2048 times.
