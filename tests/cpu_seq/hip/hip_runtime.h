@@ -13,25 +13,8 @@ inline int __shfl(int v, int from) { return emu::from_lane(v, [&](int) { return 
 inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
 inline int atomicAdd(int *p, int v) { const int old = *p; *p += v; return old; }
 inline void sincospif(float x, float *s, float *c) { *s = (float)sin(M_PI * (double)x), *c = (float)cos(M_PI * (double)x); }
-// D[i][j] += sum_k A[i][k] B[k][j]: a lane holds row (column) lane % 32, k = 8 (lane / 32) ..., and of D column lane % 32, rows 8 (e / 4) + 4 (lane / 32) + e % 4
-inline emu_f32x16 emu_mfma32(emu_bf16x8 a, emu_bf16x8 b, emu_f32x16 c)
-{
-    struct Both { EmuBits8 a, b; } mine;
-    memcpy(&mine.a, &a, 16);
-    memcpy(&mine.b, &b, 16);
-    Both *s = emu::Exchange<Both>::all(mine);
-    const int l = emu::lane();
-    for (int e = 0; e < 16; ++e) {
-        const int i = 8 * (e >> 2) + 4 * (l / 32) + (e & 3), j = l % 32;
-        float t = c[e];
-        for (int k = 0; k < 16; ++k) t += emu_bf16(s[i + 32 * (k / 8)].a.v[k % 8]) * emu_bf16(s[j + 32 * (k / 8)].b.v[k % 8]);
-        c[e] = t;
-    }
-    emu::Exchange<Both>::release();
-    return c;
-}
 inline float fmul_legacy(float a, float b) { return a == 0.0f || b == 0.0f ? 0.0f : a * b; }
-// the same of 16 x 16 by 4 contractions: a lane holds row (column) lane % 16, k = lane / 16, and of D column lane % 16, rows 4 (lane / 16) + e
+// D[i][j] += sum_k A[i][k] B[k][j] of 16 x 16 by 4 contractions: a lane holds row (column) lane % 16, k = lane / 16, and of D column lane % 16, rows 4 (lane / 16) + e
 inline emu_f32x4 emu_mfma16f(float a, float b, emu_f32x4 c)
 {
     struct Two { float a, b; };
@@ -44,8 +27,6 @@ inline emu_f32x4 emu_mfma16f(float a, float b, emu_f32x4 c)
 }
 #undef __builtin_amdgcn_mfma_f32_16x16x4f32
 #define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) emu_mfma16f(a, b, c)
-#undef __builtin_amdgcn_mfma_f32_32x32x16_bf16
-#define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) emu_mfma32(a, b, c)
 // STL_LAUNCHES: a file that takes the sizes of launches, whose kernels do not run
 template <class F>
 inline void seq_launch(const char *name, const void *kern, dim3 grid, dim3 block, size_t smem, F f)
