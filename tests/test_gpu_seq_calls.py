@@ -130,3 +130,66 @@ def test_embed_rows_without_a_token_are_zeros_whatever_the_scale(scale, t):
     X = torch.empty((6, 21), dtype=W.dtype, device="cuda")
     stl.stl_embed_forward(stl.EmbedProblem(6, 21, 30, scale, STL_DT[t]), token, W, X)
     assert not X[[1, 3, 4]].any() and not torch.isfinite(X[[0, 2, 5]]).any()
+
+
+def far(x, ld, fill=None):
+    """The same rows, ld elements from row to row, in memory that holds nothing else"""
+    rows, wide_ = x.shape[0], x[0].numel()
+    v = torch.empty((rows - 1) * ld + wide_, dtype=x.dtype, device="cuda").as_strided((rows, wide_), (ld, 1))
+    return v.fill_(fill) if fill is not None else v.copy_(x.reshape(rows, -1))
+
+
+def test_heads_more_elements_apart_than_32_bits_count():
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("not enough free memory")
+    rows, heads, d, ld = 4, 3, 64, (1 << 30) + 17
+    c = {k: up(v) for k, v in head_case(rows, heads, heads, d, "bf16", seed=1).items()}
+    want, prob = {}, stl.HeadNormProblem(rows, heads, heads, d)
+    apart = stl.HeadNormProblem(rows, heads, heads, d, None, ld, ld, ld, ld)
+    n = stl.stl_head_norm_workspace_bytes(prob)
+    ws, dw = torch.empty(n, dtype=torch.uint8, device="cuda"), [torch.empty(d, device="cuda") for _ in range(4)]
+    want = {k: torch.empty_like(c["Q"]) for k in ("Qout", "Kout", "dQ", "dK")}
+    stl.stl_head_norm_forward(prob, c["Q"], c["K"], c["w_q"], c["w_k"], c["position"], want["Qout"], want["Kout"])
+    stl.stl_head_norm_backward(prob, c["Q"], c["K"], c["w_q"], c["w_k"], c["position"], c["dQout"], c["dKout"], want["dQ"], want["dK"], dw[0], dw[1], 0, ws, n)
+    x = {k: far(c[k], ld) for k in ("Q", "K", "dQout", "dKout")}
+    stl.stl_head_norm_backward(apart, x["Q"], x["K"], c["w_q"], c["w_k"], c["position"], x["dQout"], x["dKout"], x["dQout"], x["dKout"], dw[2], dw[3], 0, ws, n)
+    stl.stl_head_norm_forward(apart, x["Q"], x["K"], c["w_q"], c["w_k"], c["position"], x["Q"], x["K"])
+    for k, v in (("Qout", "Q"), ("Kout", "K"), ("dQ", "dQout"), ("dK", "dKout")):
+        assert torch.equal(x[v].reshape(rows, heads, d), want[k]), k
+    assert torch.equal(dw[0], dw[2]) and torch.equal(dw[1], dw[3])
+    del x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("t,rows,ld,kv", [("bf16", 300, 1 << 23, 2), ("bf16", 70, 1 << 25, 1), ("bf16", 5, 1 << 29, 2), ("f32", 300, 1 << 23, 1)])
+def test_decay_more_elements_apart_than_32_bits_count(t, rows, ld, kv):
+    """Rows as far apart as the ring of loads takes them, and further."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("not enough free memory")
+    assert rows * ld > 1 << 31
+    s = decay_case(rows, 1, 2, kv, 32, 48, t, seed=2)
+    g = {k: up(v) for k, v in s.items()}
+    x = {k: far(g[k], ld) for k in ("Q", "K", "V", "dO")}
+    out = {k: far(x[like], ld, float("nan")) for k, like in (("O", "dO"), ("dQ", "Q"), ("dK", "K"), ("dV", "V"))}
+    prob = stl.DecayAttentionProblem(rows, 1, rows, 2, kv, 32, 48, None, 1, ld, ld, ld, ld, scale=0.7, dtype=STL_DT[t])
+    state, dstate = torch.empty_like(g["state"]), torch.empty_like(g["state"])
+    n = stl.stl_decay_attention_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    stl.stl_decay_attention_forward(prob, x["Q"], x["K"], x["V"], g["log_decay"], None, g["state"], out["O"], state, ws, n)
+    stl.stl_decay_attention_backward(prob, x["Q"], x["K"], x["V"], g["log_decay"], None, g["state"], x["dO"], g["dstate_out"], out["dQ"], out["dK"], out["dV"], dstate, ws, n)
+    got = {k: down(v).reshape(rows, -1, 48 if k in ("O", "dV") else 32) for k, v in out.items()}
+    decay_check(dict(got, state=down(state), dstate=down(dstate)), s, [list(range(rows))], t, 0.7, rows, ("O", "state", *GRADS))
+    del x, out
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_heads_of_zeros_with_the_smallest_eps(t):
+    x, out = torch.zeros((3, 2, 64), dtype=TORCH_DT[t], device="cuda"), [torch.full((3, 2, 64), 3.0, dtype=TORCH_DT[t], device="cuda") for _ in range(2)]
+    for eps in (1e-30, 1.2e-38, 1e-40):
+        prob = stl.HeadNormProblem(3, 2, 0, 64, eps=eps, dtype=STL_DT[t])
+        n = stl.stl_head_norm_workspace_bytes(prob)
+        ws, dw = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(64, device="cuda")
+        stl.stl_head_norm_forward(prob, x, None, None, None, None, out[0], None)
+        stl.stl_head_norm_backward(prob, x, None, None, None, None, x, None, out[1], None, dw, None, 0, ws, n)
+        assert not out[0].any() and not out[1].any() and not dw.any(), eps
