@@ -11,8 +11,8 @@
 // several segments: a sweep without outputs first forms what each adds to the state, a small kernel joins these in order to the state in front of each
 // segment (decay_join_kernel), and all segments run at once.  That reads K and V twice (largely from the last-level cache: 108 of 201 MB come from memory the second
 // time in the sizes below).
-// A wavefront owns 16 columns of v: its part of S stays in accumulators (dk x 16, fp32) all along, in 128 registers with all else, so that two workgroups share a
-// CU.  Products are formed so that accumulators are the next product's operand as they lie:
+// A wavefront owns 16 columns of v: its part of S stays in accumulators (dk x 16, fp32) all along, in 128 registers with all else (4 to 8 of a thread's in scratch memory
+// for rows of 97 to 128 in bf16), so that two workgroups share a CU.  Products are formed so that accumulators are the next product's operand as they lie:
 //   P^T = K Q^T (tokens j x i)   ->   O^T += V^T P^T,      S (dk x columns) as S^T in   O^T = S^T Q^T
 // An accumulator's lane holds rows 4 g + e of its column (g = lane / 16), an operand's lane eight elements of the contraction, whose order is free as long as
 // both operands have it: along the rows it is the order that two tiles of accumulators have (state_row), over tokens 8 g + e.  P is the same for all columns:

@@ -5,7 +5,8 @@ namespace stl {
 namespace seq {
 
 // Up to so many tokens a sequence go one by one, with the state in registers (decay_few_kernel): a sweep's chunk is 32 tokens whatever it holds.  6 tokens, in
-// brackets as a sweep, us: 64 sequences x 32 heads of 128: 68 (75); 8 x 32 of 128: 12 (12); 1 x 32 of 128: 7.5 (10); 8 tokens: 77 (76), 15 (12), 9 (10).
+// brackets as a sweep, us of a call among others: 64 sequences x 32 heads of 128: 76 (75); 8 x 32 of 128: 14 (12.5); 1 x 32 of 128: 8 (10); 8 tokens: 86 (75.5), 17 (12.5),
+// 9 (10); 4 tokens one by one: 67, 11.6, 8.
 constexpr int kFewTokens = 6;
 
 // A few tokens: memory bound by the state, which is read once and written once (64 tokens x 32 heads of 128: 268 MB in 53 us, 5.1 TB/s, the rate of a copy; one token of
@@ -145,8 +146,10 @@ namespace {
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 
 // Segments of a sequence.  They cost a sweep more, so only where a head has four of them at least for a workgroup a CU (and sweep), and of 128 tokens (fp32, whose
-// products take three times as long: 64).  More of them, of 8192 tokens x 32 heads: 132 us in 8, 138 in 16, 145 in 12; 4 x 2048 tokens x 16 heads, gradients: 156 us in
-// four, 168 in two, 182 in eight; 13 sequences of up to 777 tokens x 16 heads: 54 us in one piece, 76 in two.
+// products take three times as long: 64).  us of a call: 8192 tokens x 32 heads of 128 in bf16: 493 in one piece, 376 in 2, 200 in 4, 120 in 8, 135 in 12, 131 in 16; 13 sequences of
+// up to 777 tokens x 16 heads: 52 in one piece, 70 in 2, 82 in 4; fp32, 4096 tokens x 16 heads: 724 in one piece, 152 in 8, 95 in 16; gradients in fp32, 8 x 333 tokens x 4 heads: 99
+// in one piece, 81 in 2, 56 in 4 and 8.  In gradients the three sweeps of a launch are not counted: 4 x 2048 tokens x 16 heads of 128 in bf16 take 147 in 4, 154 in 2, 172 in 8, but
+// 130 in one piece (192 workgroups).
 int most_segments(int dtype, const DecayArgs &a)
 {
     const int64_t groups = (int64_t)a.sequences * a.heads * ((a.dv + kDecayColumns - 1) / kDecayColumns), most = 256 / groups, fit = a.length / (dtype ? 128 : 64);

@@ -9,7 +9,9 @@
 // Backward: with dy the gradient turned back, x^ = x / sqrt(...): dw = sum dy x^ over rows and heads, dx = r (dy w - x^ mean(dy w x^)).  A workgroup keeps
 // its sums for the weights in registers over all of its rows; a second launch adds up the workgroups'.
 // 8192 rows of 32 + 8 heads of 128 in bf16: 35 us, 4.7 TB/s (kernel 29).  Backward, 64 x 197 rows of 2 x 12 heads of 64: 35 us (3.3 TB/s; wavefronts wait for two thirds of
-// it, one turn of rows a workgroup whose angles come before its first load) and 5.
+// it, one turn of rows a workgroup whose angles come before its first load) and 5.  fp32, 8192 rows of 32 + 8 heads of 128: 70 us (4.8 TB/s), backward 115 (4.4).
+// Where 16 divides d and rot a unit is two chunks of 8; elsewhere each element is loaded and stored by itself: 8192 rows of 32 + 8 heads in bf16, d 80 and rot 20: 120 us (0.9 TB/s),
+// backward 163; d 96 and rot 24: 135 and 175.
 #include "seq_kernels.h"
 #include "../csrc/lm/lm_device.h"
 
