@@ -8,7 +8,8 @@ import torch
 
 import paper_2503_12211_amd as stl
 from gpu_util import STL_DT, TORCH_DT
-from seq_cases import decay_case, decay_check, head_case, narrow, walk_bound, walk_case, wide
+from oracle import seq
+from seq_cases import close, decay_bounds, decay_case, decay_chain, decay_check, head_case, narrow, walk_bound, walk_case, wide
 from test_gpu_seq import ADJ, PRE, decay_problem, decay_run, down, up
 
 pytestmark = pytest.mark.gpu
@@ -193,3 +194,109 @@ def test_heads_of_zeros_with_the_smallest_eps(t):
         stl.stl_head_norm_forward(prob, x, None, None, None, None, out[0], None)
         stl.stl_head_norm_backward(prob, x, None, None, None, None, x, None, out[1], None, dw, None, 0, ws, n)
         assert not out[0].any() and not out[1].any() and not dw.any(), eps
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("packed", [False, True])
+def test_decay_gradients_of_more_sequences_than_a_grid_is_high(packed, t):
+    """Shared key heads of 70000 sequences: the bits of two calls with half of them each."""
+    n, length, heads, d = 70000, 3, 2, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda k: torch.randn((n * length, k, d), generator=g, device="cuda").to(TORCH_DT[t])  # noqa: E731
+    Q, K, V, dO = r(heads), r(1), r(1), r(heads)
+    # packed: 0 to 3 tokens each, and rows of no sequence at the end
+    ends = torch.randint(0, length + 1, (n,), generator=g, device="cuda").cumsum(0) if packed else None
+    offset = torch.cat([ends.new_zeros(1), ends]) if packed else None
+    decay = torch.tensor([-0.1, -0.5], device="cuda")
+
+    def grads(first, last):
+        count, at = last - first, slice(first * length, last * length)
+        some = [x if packed else x[at] for x in (Q, K, V, dO)]
+        prob = stl.DecayAttentionProblem(some[0].shape[0], count, length, heads, 1, d, scale=0.5, dtype=STL_DT[t])
+        size = stl.stl_decay_attention_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        outs = [torch.full_like(x, 3.0) for x in some[:3]]
+        stl.stl_decay_attention_backward(prob, *some[:3], decay, offset[first:last + 1].clone() if packed else None, None, some[3], None, *outs, None, ws, size)
+        return outs
+
+    whole, low, high = grads(0, n), grads(0, n // 2), grads(n // 2, n)
+    for w, a, b in zip(whole, low, high):
+        if packed:
+            cut, end = int(offset[n // 2]), int(offset[-1])
+            assert torch.equal(w[:cut], a[:cut]) and torch.equal(w[cut:], b[cut:]) and bool((a[cut:] == 3).all()) and bool((w[end:] == 3).all())
+        else:
+            assert torch.equal(w, torch.cat([a, b]))
+
+
+def test_embed_of_the_most_rows():
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("not enough free memory")
+    rows, vocab = stl.STL_MAX_DIM, 1000
+    token = torch.randint(-1, vocab, (rows,), device="cuda")
+    at = torch.cat([torch.arange(5000, device="cuda"), torch.arange(rows - 5000, rows, device="cuda"), torch.randint(0, rows, (5000,), device="cuda")])
+    W = torch.randn(vocab, 2048, device="cuda").to(torch.bfloat16)
+    X = torch.empty((rows, 2048), dtype=W.dtype, device="cuda")
+    stl.stl_embed_forward(stl.EmbedProblem(rows, 2048, vocab), token, W, X)
+    assert torch.equal(X[at], torch.where((token[at] >= 0)[:, None], W[token[at].clamp_min(0)], 0.0).to(W.dtype))
+    del X
+    torch.cuda.empty_cache()
+    # gradients that are small whole numbers: their sums are too
+    dX, dW = torch.randint(-2, 3, (rows, 8), device="cuda").float(), torch.empty((vocab, 8), device="cuda")
+    prob = stl.EmbedProblem(rows, 8, vocab, dtype=stl.STL_F32)
+    n = stl.stl_embed_workspace_bytes(prob)
+    stl.stl_embed_backward(prob, token, dX, dW, 0, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    want = torch.zeros((vocab + 1, 8), dtype=torch.float64, device="cuda").index_add_(0, torch.where(token < 0, vocab, token), dX.double())
+    assert torch.equal(dW.double(), want[:vocab])
+
+
+def test_heads_of_the_most_rows():
+    rows, d = stl.STL_MAX_DIM, 16
+    Q, up_ = (torch.randn((rows, 1, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    position, w = torch.arange(rows, device="cuda"), torch.randn(d, device="cuda").to(torch.bfloat16)
+    out, dQ, dw = torch.empty_like(Q), torch.empty_like(Q), torch.empty(d, device="cuda")
+    prob = stl.HeadNormProblem(rows, 1, 0, d)
+    n = stl.stl_head_norm_workspace_bytes(prob)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    stl.stl_head_norm_forward(prob, Q, None, w, None, position, out, None)
+    stl.stl_head_norm_backward(prob, Q, None, w, None, position, up_, None, dQ, None, dw, None, 0, ws, n)
+    for lo in (0, rows // 2 - 50, rows - 100):
+        some = slice(lo, lo + 100)
+        part, b, c = stl.HeadNormProblem(100, 1, 0, d), torch.empty_like(Q[some]), torch.empty_like(Q[some])
+        stl.stl_head_norm_forward(part, Q[some].clone(), None, w, None, position[some].clone(), b, None)
+        stl.stl_head_norm_backward(part, Q[some].clone(), None, w, None, position[some].clone(), up_[some].clone(), None, c, None, None, None, 0, ws, n)
+        assert torch.equal(out[some], b) and torch.equal(dQ[some], c)
+    angle = position.double()[:, None] * 10000.0 ** (-torch.arange(0, d, 2, device="cuda", dtype=torch.float64) / d)
+    x, u = Q[:, 0].double(), up_[:, 0].double()
+    a, b = u[:, :d // 2], u[:, d // 2:]
+    back = torch.cat([a * angle.cos() + b * angle.sin(), b * angle.cos() - a * angle.sin()], 1)
+    hat = x / (x.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    # a workgroup's sums are chains of rows / 1024, its lanes' and the workgroups' come behind them
+    assert bool(((dw.double() - (back * hat).sum(0)).abs() <= (rows // 1024 + 64) * 2.0 ** -24 * (back * hat).abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_decay_of_the_longest_sequence(t):
+    """16.8 million tokens in segments; a token sees some thousand before it."""
+    rows, d = stl.STL_MAX_DIM, 8
+    g = torch.Generator(device="cuda").manual_seed(2)
+    Q, K, V, dO = (torch.randn((rows, 1, d), generator=g, device="cuda").to(TORCH_DT[t]) for _ in range(4))
+    decay = torch.tensor([-0.02], device="cuda")
+    prob = stl.DecayAttentionProblem(rows, 1, rows, 1, dk=d, scale=0.5, dtype=STL_DT[t])
+    n = stl.stl_decay_attention_workspace_bytes(prob, stl.STL_OP_BACKWARD)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    O, dQ, dK, dV = (torch.empty_like(Q) for _ in range(4))
+    state = torch.empty((1, 1, d, d), device="cuda")
+    stl.stl_decay_attention_forward(prob, Q, K, V, decay, None, None, O, state, ws, n)
+    stl.stl_decay_attention_backward(prob, Q, K, V, decay, None, None, dO, None, dQ, dK, dV, None, ws, n)
+    window, inner = 2400, 1000                                   # what is behind 1000 tokens has faded to 2e-9
+    for lo in (0, rows // 256 * 100 - window // 2, rows - window):
+        some = slice(lo, lo + window)
+        cut = slice(0 if lo == 0 else inner, window if lo == rows - window else window - inner)
+        s = {"Q": Q, "K": K, "V": V, "dO": dO}
+        s = {k: v[some].cpu() for k, v in s.items()}
+        want = seq.decay(*(s[k].double().numpy() for k in "QKV"), [list(range(window))], decay.cpu().numpy(), 0.5, None, s["dO"].double().numpy())
+        for name, got in (("O", O), ("dQ", dQ), ("dK", dK), ("dV", dV)):
+            kind, operand = decay_bounds(name, t)
+            close(down(got[some])[cut], want[name][cut], want["size"][name][cut], kind, decay_chain(window, d, d) + 33, name, operand + 2e-8)
+    kind, operand = decay_bounds("state", t)
+    close(down(state), want["state"], want["size"]["state"], kind, decay_chain(window, d, d) + 33, "state", operand + 2e-8)
