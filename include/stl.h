@@ -452,7 +452,7 @@ stl_status_t stl_head_norm_backward(const stl_head_norm_t *prob, const void *Q, 
  * what is added to a state.  A value that is no finite number reaches its own and later tokens alone, whose results may then be NaN where the formula gives
  * an infinity.
  * 0 <= rows <= STL_MAX_DIM, 1 <= sequences, 0 <= length (0: states are copied), sequences * heads <= 4194304, 1 <= kv_heads dividing heads,
- * 1 <= dk, dv <= STL_DECAY_WIDEST (UNSUPPORTED above), ld at least the row's elements, scale finite and not 0, and so its reciprocal.
+ * 1 <= dk, dv <= STL_DECAY_WIDEST (UNSUPPORTED above), ld at least the row's elements, scale and 1 / scale finite and not 0.
  * ws / ws_bytes: at least stl_decay_attention_workspace_bytes(prob, STL_OP_FORWARD or STL_OP_BACKWARD).
  */
 typedef struct {
